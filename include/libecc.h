@@ -636,6 +636,72 @@ ecc_status_t ecc_mf_iterate(ecc_mf_t h, ecc_plan_t plan, double eta, double lam,
 ecc_status_t ecc_mf_error(ecc_mf_t h, const double *d_W, double *d_rmse, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * Operators of language models: the work at the two ends of a model and
+ * between its blocks that is bound by memory, with gradients of parameters
+ * laid out per worker as the collectives above take contributions.
+ *
+ * Conventions of this section:
+ *   - Arrays are row-major; a matrix has a leading dimension (elements from
+ *     one row to the next, at least the row length).  Element types are
+ *     ECC_F64, ECC_F32 and ECC_BF16, at the alignment of one element.
+ *   - Sums, norms and softmax statistics are held in fp32, in fp64 where the
+ *     operands or the result are fp64; every result is rounded once, to the
+ *     nearest, when it is stored.
+ *   - P workers hold n rows each: row t of P * n belongs to worker t / n.
+ *     Worker p's gradient of a parameter starts p * worker_stride elements
+ *     after the first one's.  accumulate = 0 writes a gradient (every
+ *     element), 1 adds to what it holds.
+ *   - Work buffers are the caller's, in bytes as the size calls give, 16-byte
+ *     aligned; they carry nothing from call to call but what is stated.
+ *   - Results are bitwise reproducible.  Calls are enqueued on hip_stream.
+ *     Outputs must not overlap inputs, other outputs or the work buffer
+ *     unless stated.  ECC_ERR_ARG for a bad size, type, leading dimension,
+ *     NULL, alignment or overlap; ECC_ERR_RANGE for a size beyond the
+ *     stated limits.
+ * --------------------------------------------------------------------------- */
+#define ECC_F64 0
+#define ECC_F32 1
+#define ECC_BF16 2
+#define ECC_I32 3
+#define ECC_I64 4
+
+/* Token embedding: d_out[t] = scale * table[ids[t] - row0] for 0 <= t < n,
+ * rows of D elements; zeros where ids[t] - row0 lies outside [0, V) (padding,
+ * or a token of another part of a table that is split by rows).  The product
+ * is formed in fp32 (fp64 when table or out is fp64).  id_type: ECC_I32 or
+ * ECC_I64.  V, D >= 1, n >= 0. */
+ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, const void *d_ids,
+                              int32_t id_type, const void *d_table, int32_t table_type,
+                              int64_t ld_table, double scale, void *d_out, int32_t out_type,
+                              int64_t ld_out, void *hip_stream);
+
+/* The tokens of P workers (n each, worker after worker in d_ids) sorted by
+ * worker and token, tokens that are alike in their order in d_ids: what
+ * ecc_embed_grad sums by.  d_index: ecc_embed_index_size(P, n, V) bytes,
+ * kept until the gradients that use it are done; one index serves any number
+ * of gradients.  P >= 1, n >= 0, V >= 1; ECC_ERR_RANGE when P * n or P * (V
+ * + 1) reaches 2^31 - 1 (the size call then returns -1). */
+int64_t ecc_embed_index_size(int32_t P, int64_t n, int64_t V);
+ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, const void *d_ids,
+                             int32_t id_type, void *d_index, void *hip_stream);
+
+/* The table's gradient, one per worker, V rows of D elements each:
+ *   G_p[v] = (accumulate ? G_p[v] : 0) + scale * sum of d_dy[t] over the
+ *            tokens t of worker p with ids[t] - row0 = v
+ * from the P * n rows d_dy and the tokens' index (made with the same P, n and
+ * V).  Rows of d_dy whose token lies outside the table are not read.
+ * Tokens are added in order within pieces of up to 64 sorted tokens, and the
+ * pieces of a token in order.  worker_stride >= (V - 1) * ld_grad + D when
+ * P > 1.  D up to 2^22, P * V below 2^29 (else ECC_ERR_RANGE).  d_work:
+ * ecc_embed_work_size(...) bytes (-1 for arguments that the call refuses). */
+int64_t ecc_embed_work_size(int32_t P, int64_t n, int64_t D, int32_t dy_type, int32_t grad_type);
+ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const void *d_index,
+                            const void *d_dy, int32_t dy_type, int64_t ld_dy, double scale,
+                            void *d_grad, int32_t grad_type, int64_t ld_grad,
+                            int64_t worker_stride, int32_t accumulate, void *d_work,
+                            void *hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Plain streaming copy d_dst[i] = d_src[i], 0 <= i < n, enqueued on
  * hip_stream.  Both buffers 8-byte aligned and not overlapping
  * (ECC_ERR_ARG otherwise); 16-byte accesses when both are 16-byte aligned.

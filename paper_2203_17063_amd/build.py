@@ -17,7 +17,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 # -ffp-contract=off: sums that run sequentially on one lane perform the same
 # rounded operations as the written definition (no fused multiply-add).
-# packed-fp32-ops is disabled as a precaution; nothing here is fp32 anyway.
+# packed-fp32-ops is disabled: some forms of those instructions have given wrong results.
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=" + ARCH, "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-result", "-I", INCLUDE, "-I", CSRC]

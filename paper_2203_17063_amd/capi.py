@@ -31,6 +31,7 @@ ECC_FORM_GENERAL, ECC_FORM_COLUMN_VALUES, ECC_FORM_DIAGONALS = 0, 1, 2
 ECC_MAX_DIAGONALS = 8
 ECC_SCRATCH_DOUBLES = 1 << 20
 ECC_GATHER_CHUNK = 2048
+ECC_F64, ECC_F32, ECC_BF16, ECC_I32, ECC_I64 = 0, 1, 2, 3, 4
 
 STATUS_NAMES = {0: "ECC_OK", 1: "ECC_ERR_ARG", 2: "ECC_ERR_OVERLAP", 3: "ECC_ERR_RANGE",
                 4: "ECC_ERR_ALLOC", 5: "ECC_ERR_DEVICE", 6: "ECC_ERR_STATE"}
@@ -106,6 +107,13 @@ _SIGS = [
     ("ecc_mf_iterate", ctypes.c_int, [_VP, _VP, _D, _D, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
                                       _VP]),
     ("ecc_mf_error", ctypes.c_int, [_VP, _VP, _VP, _VP]),
+    ("ecc_embed_lookup", ctypes.c_int, [_I64, _I64, _I64, _I64, _VP, _I32, _VP, _I32, _I64, _D,
+                                        _VP, _I32, _I64, _VP]),
+    ("ecc_embed_index_size", _I64, [_I32, _I64, _I64]),
+    ("ecc_embed_index", ctypes.c_int, [_I32, _I64, _I64, _I64, _VP, _I32, _VP, _VP]),
+    ("ecc_embed_work_size", _I64, [_I32, _I64, _I64, _I32, _I32]),
+    ("ecc_embed_grad", ctypes.c_int, [_I32, _I64, _I64, _I64, _VP, _VP, _I32, _I64, _D, _VP, _I32,
+                                      _I64, _I64, _I32, _VP, _VP]),
     ("ecc_solve", ctypes.c_int, [_VP, _VP, _VP, _D, _D, _VP, _VP, _VP, _VP, _I32, _D, _VP, _VP,
                                  _VP, _VP]),
 ]
@@ -423,3 +431,28 @@ def ecc_mf_iterate(h, plan, eta, lam, d_W, d_grads, d_slots, d_G, d_arrived, d_b
 
 def ecc_mf_error(h, d_W, d_rmse, hip_stream=None):
     _check(lib().ecc_mf_error(h, _ptr(d_W), _ptr(d_rmse), hip_stream))
+
+
+def ecc_embed_lookup(n, V, D, row0, d_ids, id_type, d_table, table_type, ld_table, scale, d_out,
+                     out_type, ld_out, hip_stream=None):
+    _check(lib().ecc_embed_lookup(n, V, D, row0, _ptr(d_ids), id_type, _ptr(d_table), table_type,
+                                  ld_table, scale, _ptr(d_out), out_type, ld_out, hip_stream))
+
+
+def ecc_embed_index_size(P, n, V) -> int:
+    return int(lib().ecc_embed_index_size(P, n, V))
+
+
+def ecc_embed_index(P, n, V, row0, d_ids, id_type, d_index, hip_stream=None):
+    _check(lib().ecc_embed_index(P, n, V, row0, _ptr(d_ids), id_type, _ptr(d_index), hip_stream))
+
+
+def ecc_embed_work_size(P, n, D, dy_type, grad_type) -> int:
+    return int(lib().ecc_embed_work_size(P, n, D, dy_type, grad_type))
+
+
+def ecc_embed_grad(P, n, V, D, d_index, d_dy, dy_type, ld_dy, scale, d_grad, grad_type, ld_grad,
+                   worker_stride, accumulate, d_work, hip_stream=None):
+    _check(lib().ecc_embed_grad(P, n, V, D, _ptr(d_index), _ptr(d_dy), dy_type, ld_dy, scale,
+                                _ptr(d_grad), grad_type, ld_grad, worker_stride, accumulate,
+                                _ptr(d_work), hip_stream))

@@ -1,0 +1,823 @@
+// Token embedding: scaled rows of a table, and the table's gradient summed
+// over tokens sorted by row.
+//
+// The lookup reads one row per token and writes one: bound by memory.
+//
+// The gradient G_p[v] = scale * sum of dY[t] over worker p's tokens t of row
+// v has to read every token's row of dY and to write every row of G.  The
+// rows of dY that belong together lie anywhere, and a few tokens of a
+// language make up much of a text, so neither a workgroup per row of G (the
+// commonest token's would run alone) nor atomic additions (their order, and
+// so the result, would change) will do.  Instead the tokens are sorted by
+// (worker, row), stably, and the sorted order is cut into tiles of equal
+// length:
+//  - a tile adds its tokens' rows run by run of equal tokens; a run that lies
+//    within the tile is finished and written at once, one that was begun or
+//    is continued in another tile leaves its sum in the work buffer (at most
+//    two a tile);
+//  - a second launch adds the pieces of every run that crosses tiles, in tile
+//    order;
+//  - rows of G without tokens are zeroed by further workgroups of the first
+//    launch, which find them by bisection of the sorted tokens.
+// Every element of G is written once, by one thread, in a fixed order.
+//
+// The sort is by counting, digit by digit from the lowest: up to
+// kSmallSort tokens per worker in one launch, a workgroup per worker with
+// tokens and positions in LDS; beyond, three launches per digit of up to 9
+// bits (counts of each tile, their running sums, the moves).
+#include <algorithm>
+
+#include "lm_common.h"
+
+namespace ecc {
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int64_t kSmallSort = 16 * kSortThreads;  // tokens of a worker that one workgroup sorts
+constexpr int kSmallBins = 256;
+constexpr int kTileThreads = 256;                  // the launches of a longer sort
+constexpr int kTileItems = 8;
+constexpr int kSortTile = kTileThreads * kTileItems;
+constexpr int kBigBits = 9;
+constexpr int kBigBins = 1 << kBigBits;
+
+__device__ __forceinline__ int64_t load_id(const void *ids, int id64, int64_t t) {
+    return id64 ? reinterpret_cast<const int64_t *>(ids)[t]
+                : (int64_t) reinterpret_cast<const int32_t *>(ids)[t];
+}
+
+// The row of a token within the table, V for one outside it.
+__device__ __forceinline__ uint32_t local_row(int64_t id, int64_t row0, int64_t V) {
+    // (the difference of two int64 may pass int64: compared as unsigned)
+    const uint64_t r = (uint64_t)id - (uint64_t)row0;
+    return id >= row0 && r < (uint64_t)V ? (uint32_t)r : (uint32_t)V;
+}
+
+// Lanes of the wave whose digit (rb bits) is this lane's.
+__device__ __forceinline__ uint64_t digit_peers(uint32_t d, int rb) {
+    uint64_t peers = ~0ull;
+    for (int b = 0; b < rb; ++b) {
+        const bool bit = (d >> b) & 1u;
+        const uint64_t set = __ballot(bit);
+        peers &= bit ? set : ~set;
+    }
+    return peers;
+}
+
+// One digit of this lane's element: its place among the wave's elements of
+// that digit so far, counted in hist (a row of bins for the wave).
+__device__ __forceinline__ uint32_t count_digit(uint32_t d, int rb, uint32_t *hist, int lane) {
+    const uint64_t peers = digit_peers(d, rb);
+    const int leader = __ffsll((unsigned long long)peers) - 1;
+    uint32_t old = 0;
+    if (lane == leader) old = atomicAdd(&hist[d], (uint32_t)__popcll(peers));
+    old = __shfl(old, leader, 64);
+    return old + (uint32_t)__popcll(peers & ((1ull << lane) - 1ull));
+}
+
+// Exclusive running sums over `bins` (<= NT) values, one per thread; `sums`
+// holds NT / 64 + 1 words of LDS.
+template <int NT>
+__device__ __forceinline__ uint32_t bins_scan(uint32_t v, uint32_t *sums) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t run = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(run, o, 64);
+        if (lane >= o) run += up;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    uint32_t base = 0;
+    for (int w = 0; w < wave; ++w) base += sums[w];
+    return base + run - v;
+}
+
+// A worker's n <= 1024 * ITEMS tokens sorted in LDS.
+template <int ITEMS>
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t V, int64_t row0,
+                                                             const void *ids, int id64,
+                                                             int passes, int rb,
+                                                             uint32_t *__restrict__ keys_out,
+                                                             int32_t *__restrict__ order_out) {
+    __shared__ uint32_t s_hist[kSortWaves][kSmallBins];
+    __shared__ uint32_t s_key[kSortThreads * ITEMS];
+    __shared__ uint16_t s_pos[kSortThreads * ITEMS];
+    __shared__ uint32_t s_sums[kSortWaves + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = (int64_t)blockIdx.x * n;
+    const uint32_t mask = (1u << rb) - 1u;
+    const int bins = 1 << rb;
+    uint32_t key[ITEMS], pos[ITEMS], place[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int at = wave * 64 * ITEMS + i * 64 + lane;
+        pos[i] = (uint32_t)at;
+        // past the end: the highest value of the digits sorted, which stays
+        // behind the tokens that were ahead of it
+        key[i] = at < n ? local_row(load_id(ids, id64, first + at), row0, V) : ~0u;
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * rb;
+        for (int i = tid; i < kSortWaves * kSmallBins; i += kSortThreads)
+            (&s_hist[0][0])[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            place[i] = count_digit((key[i] >> shift) & mask, rb, s_hist[wave], lane);
+        __syncthreads();
+        uint32_t total = 0;
+        if (tid < bins)
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = s_hist[w][tid];
+                s_hist[w][tid] = total;
+                total += c;
+            }
+        const uint32_t base = bins_scan<kSortThreads>(total, s_sums);
+        if (tid < bins)
+            for (int w = 0; w < kSortWaves; ++w) s_hist[w][tid] += base;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t to = place[i] + s_hist[wave][(key[i] >> shift) & mask];
+            s_key[to] = key[i];
+            s_pos[to] = (uint16_t)pos[i];
+        }
+        __syncthreads();
+        if (pass + 1 < passes) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int at = wave * 64 * ITEMS + i * 64 + lane;
+                key[i] = s_key[at];
+                pos[i] = s_pos[at];
+            }
+        }
+    }
+    const uint32_t key0 = blockIdx.x * (uint32_t)(V + 1);
+    for (int i = tid; i < n; i += kSortThreads) {
+        const int32_t t = (int32_t)(first + s_pos[i]);
+        keys_out[first + i] = key0 + s_key[i];
+        order_out[first + i] = s_key[i] < (uint32_t)V ? t : ~t;
+    }
+}
+
+// The elements of one digit pass of a longer sort: (worker, row) and position
+// from the tokens (keys == NULL), or as the pass before left them.
+struct SortIn {
+    const uint32_t *keys;
+    const int32_t *order;
+    const void *ids;
+    int64_t N, n, V, row0;
+    int id64;
+};
+__device__ __forceinline__ uint32_t sort_key(const SortIn &in, int64_t t) {
+    if (in.keys) return in.keys[t];
+    const uint32_t worker = (uint32_t)(t / in.n);
+    return worker * (uint32_t)(in.V + 1) + local_row(load_id(in.ids, in.id64, t), in.row0, in.V);
+}
+
+// counts[d][tile]: elements of digit d in each tile.
+__global__ __launch_bounds__(kTileThreads) void k_sort_count(SortIn in, int shift, int rb,
+                                                             uint32_t *__restrict__ counts) {
+    __shared__ uint32_t s_hist[kBigBins];
+    const uint32_t mask = (1u << rb) - 1u;
+    for (int i = threadIdx.x; i < kBigBins; i += kTileThreads) s_hist[i] = 0;
+    __syncthreads();
+    const int64_t base = (int64_t)blockIdx.x * kSortTile + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i) {
+        const int64_t t = base + i * kTileThreads;
+        if (t < in.N) atomicAdd(&s_hist[(sort_key(in, t) >> shift) & mask], 1u);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < (1 << rb); d += kTileThreads)
+        counts[(int64_t)d * gridDim.x + blockIdx.x] = s_hist[d];
+}
+
+// Running sums of digit d's counts over the tiles (workgroup d); totals[d].
+__global__ __launch_bounds__(kTileThreads) void k_sort_scan(int64_t tiles,
+                                                            uint32_t *__restrict__ counts,
+                                                            uint32_t *__restrict__ totals) {
+    __shared__ uint32_t s_sums[kTileThreads / 64 + 1];
+    __shared__ uint32_t s_total;
+    uint32_t *row = counts + (int64_t)blockIdx.x * tiles;
+    uint32_t run = 0;
+    for (int64_t at = 0; at < tiles; at += kTileThreads) {
+        const int64_t i = at + threadIdx.x;
+        const uint32_t v = i < tiles ? row[i] : 0u;
+        const uint32_t before = bins_scan<kTileThreads>(v, s_sums);
+        if (i < tiles) row[i] = run + before;
+        if (threadIdx.x == kTileThreads - 1) s_total = before + v;
+        __syncthreads();
+        run += s_total;
+    }
+    if (threadIdx.x == 0) totals[blockIdx.x] = run;
+}
+
+__global__ __launch_bounds__(kTileThreads) void k_sort_move(SortIn in, int shift, int rb,
+                                                            const uint32_t *__restrict__ counts,
+                                                            const uint32_t *__restrict__ totals,
+                                                            uint32_t *__restrict__ keys_out,
+                                                            int32_t *__restrict__ order_out,
+                                                            int last) {
+    constexpr int kWaves = kTileThreads / 64;
+    __shared__ uint32_t s_hist[kWaves][kBigBins];
+    __shared__ uint32_t s_base[kBigBins];
+    __shared__ uint32_t s_sums[kWaves + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t mask = (1u << rb) - 1u;
+    const int bins = 1 << rb;
+    for (int i = tid; i < kWaves * kBigBins; i += kTileThreads) (&s_hist[0][0])[i] = 0;
+    // the first place of each digit: those of the lower digits, then those of
+    // this digit in the tiles before
+    uint32_t low = 0;
+    for (int d0 = 0; d0 < bins; d0 += kTileThreads) {
+        const int d = d0 + tid;
+        const uint32_t v = d < bins ? totals[d] : 0u;
+        const uint32_t before = bins_scan<kTileThreads>(v, s_sums);
+        if (d < bins) s_base[d] = low + before + counts[(int64_t)d * gridDim.x + blockIdx.x];
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) low += s_sums[w];
+    }
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * kSortTile + wave * 64 * kTileItems + lane;
+    uint32_t key[kTileItems], place[kTileItems];
+    int32_t pos[kTileItems];
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i) {
+        const int64_t t = first + i * 64;
+        const bool live = t < in.N;
+        key[i] = live ? sort_key(in, t) : ~0u;
+        pos[i] = !live ? 0 : in.keys ? in.order[t] : (int32_t)t;
+    }
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i)
+        place[i] = count_digit((key[i] >> shift) & mask, rb, s_hist[wave], lane);
+    __syncthreads();
+    for (int d = tid; d < bins; d += kTileThreads) {
+        uint32_t run = s_base[d];
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t c = s_hist[w][d];
+            s_hist[w][d] = run;
+            run += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i) {
+        // (elements past the end come last in their digit: their places are
+        // not used)
+        if (first + i * 64 < in.N) {
+            const uint32_t to = place[i] + s_hist[wave][(key[i] >> shift) & mask];
+            keys_out[to] = key[i];
+            const bool held = !last || key[i] % (uint32_t)(in.V + 1) < (uint32_t)in.V;
+            order_out[to] = held ? pos[i] : ~pos[i];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// lookup
+// ---------------------------------------------------------------------------
+constexpr int kEmbedThreads = 256;
+
+template <typename T, typename O, typename A, int VEC>
+__global__ __launch_bounds__(kEmbedThreads) void k_embed_lookup(
+    int64_t n, int64_t V, int64_t D, int64_t row0, const void *ids, int id64,
+    const T *__restrict__ table, int64_t ld_table, A scale, O *__restrict__ out, int64_t ld_out,
+    int log2_lanes, int64_t chunks) {
+    const int lanes = 1 << log2_lanes;
+    const int64_t unit =
+        ((int64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> log2_lanes;
+    const int64_t t = unit / chunks;
+    if (t >= n) return;
+    const int64_t col = ((unit % chunks) * lanes + (threadIdx.x & (lanes - 1))) * VEC;
+    const uint32_t row = local_row(load_id(ids, id64, t), row0, V);
+    if (col >= D) return;
+    A v[VEC];
+    if (row < V) {
+        Raw<T, VEC> in;
+        in.load_upto(table + (int64_t)row * ld_table + col, D - col);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = in.template get<A>(i) * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (A)0;
+    }
+    Raw<O, VEC> r;
+    r.set_all(v);
+    r.store_upto(out + t * ld_out + col, D - col);
+}
+
+// ---------------------------------------------------------------------------
+// gradient
+// ---------------------------------------------------------------------------
+template <typename Y, typename G, typename A>
+struct EmbedGradArgs {
+    int64_t N, V, D;              // tokens of all workers, rows and columns of the table
+    int64_t rows;                 // P * V
+    const uint32_t *keys;         // [N] worker * (V + 1) + row, sorted
+    const int32_t *order;         // [N] the token t, whose row of dy it is; ~t outside the table
+    const Y *dy;
+    int64_t ld_dy;
+    A scale;
+    G *grad;
+    int64_t ld_grad, stride;      // a row's and a worker's distance
+    A *pieces;                    // [tiles][2][D]: sums of a tile's first and last run
+    int64_t tiles;
+    int32_t tile;                 // tokens of a tile
+    int32_t accumulate;
+    int32_t log2_lanes;           // lanes that hold a chunk of a row
+    int64_t chunks;               // chunks of a row
+    int64_t sum_blocks;           // workgroups that add; the others zero
+    int32_t zero_rows;            // rows a zeroing workgroup looks after
+};
+
+template <typename Y, typename G, typename A, int VEC>
+__device__ __forceinline__ void embed_write(const EmbedGradArgs<Y, G, A> &a, uint32_t key,
+                                            int64_t col, const A (&sum)[VEC]) {
+    const int64_t worker = key / (uint32_t)(a.V + 1), row = key % (uint32_t)(a.V + 1);
+    G *g = a.grad + worker * a.stride + row * a.ld_grad + col;
+    A v[VEC];
+    if (a.accumulate) {
+        Raw<G, VEC> old;
+        old.load_upto(g, a.D - col);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = old.template get<A>(i) + a.scale * sum[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = a.scale * sum[i];
+    }
+    Raw<G, VEC> r;
+    r.set_all(v);
+    r.store_upto(g, a.D - col);
+}
+
+// Zeros in the rows of workgroup `block`'s share that no token names.
+template <typename Y, typename G, typename A>
+__device__ __forceinline__ void embed_zero(const EmbedGradArgs<Y, G, A> &a, int64_t block) {
+    __shared__ uint8_t s_empty[64];
+    const int64_t r0 = block * a.zero_rows;
+    const int count = (int)min((int64_t)a.zero_rows, a.rows - r0);
+    if ((int)threadIdx.x < count) {
+        const int64_t r = r0 + threadIdx.x;
+        const uint32_t key = (uint32_t)(r / a.V * (a.V + 1) + r % a.V);
+        int64_t lo = 0, hi = a.N;  // the first token whose key is not below
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (a.keys[mid] < key) lo = mid + 1;
+            else hi = mid;
+        }
+        s_empty[threadIdx.x] = lo >= a.N || a.keys[lo] != key;
+    }
+    __syncthreads();
+    constexpr int W = kVec<G>;
+    Raw<G, W> zero;
+#pragma unroll
+    for (int i = 0; i < Raw<G, W>::kWords; ++i) zero.w[i] = 0;
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; i < count; i += kEmbedThreads / 64) {
+        if (!s_empty[i]) continue;
+        const int64_t r = r0 + i;
+        G *g = a.grad + r / a.V * a.stride + r % a.V * a.ld_grad;
+        for (int64_t col = lane * W; col < a.D; col += 64 * W)
+            zero.template store_upto<true>(g + col, a.D - col);
+    }
+}
+
+template <typename Y, typename G, typename A, bool WHOLE_WAVE>
+__global__ __launch_bounds__(kEmbedThreads) void k_embed_sum(EmbedGradArgs<Y, G, A> a) {
+    constexpr int VEC = kVec<Y>, U = 8;
+    if ((int64_t)blockIdx.x >= a.sum_blocks) {
+        embed_zero(a, (int64_t)blockIdx.x - a.sum_blocks);
+        return;
+    }
+    int64_t unit = ((int64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.log2_lanes;
+    if constexpr (WHOLE_WAVE) unit = (int64_t)wave_uniform((uint64_t)unit);
+    const int64_t tile = unit / a.chunks;
+    if (tile >= a.tiles) return;
+    const int lanes = 1 << a.log2_lanes;
+    const int64_t col = ((unit % a.chunks) * lanes + (threadIdx.x & (lanes - 1))) * VEC;
+    const bool live = col < a.D;
+    const int64_t t0 = tile * a.tile, t1 = min(t0 + a.tile, a.N);
+    const uint32_t none = ~0u;
+    const uint32_t before = t0 > 0 ? a.keys[t0 - 1] : none;
+    const uint32_t after = t1 < a.N ? a.keys[t1] : none;
+    A acc[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] = (A)0;
+    uint32_t run = a.keys[t0];
+    bool held = a.order[t0] >= 0;  // the run's tokens lie in the table
+    bool first = run == before;    // the run was begun in an earlier tile
+    for (int64_t j = t0; j < t1; j += U) {
+        uint32_t key[U];
+        int32_t order[U];
+        Raw<Y, VEC> y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = j + u < t1 ? j + u : t1 - 1;
+            key[u] = a.keys[at];
+            order[u] = a.order[at];
+            if (live && order[u] >= 0)
+                y[u].template load_upto<true>(a.dy + order[u] * a.ld_dy + col, a.D - col);
+            else
+#pragma unroll
+                for (int i = 0; i < Raw<Y, VEC>::kWords; ++i) y[u].w[i] = 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (j + u < t1) {
+                if (key[u] != run) {
+                    // a run ends within the tile
+                    if (live && held) {
+                        if (first) {
+                            Raw<A, VEC> r;
+                            r.set_all(acc);
+                            r.store_upto(a.pieces + 2 * tile * a.D + col, a.D - col);
+                        } else {
+                            embed_write<Y, G, A, VEC>(a, run, col, acc);
+                        }
+                    }
+                    run = key[u];
+                    held = order[u] >= 0;
+                    first = false;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[i] = (A)0;
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[i] += y[u].template get<A>(i);
+            }
+        }
+    }
+    if (!live || !held) return;
+    const bool last = run == after;  // the run goes on in the next tile
+    if (first || last) {
+        Raw<A, VEC> r;
+        r.set_all(acc);
+        r.store_upto(a.pieces + (2 * tile + (first ? 0 : 1)) * a.D + col, a.D - col);
+    } else {
+        embed_write<Y, G, A, VEC>(a, run, col, acc);
+    }
+}
+
+// Runs that cross tiles: the piece that the run's first tile left, then those
+// of the tiles it goes on in, in order.  The waves of a workgroup take
+// sections of a run's tiles, whose sums are added in order.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinTiles = 8;  // tiles a workgroup looks through
+
+template <typename Y, typename G, typename A>
+__global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G, A> a) {
+    constexpr int W = kVec<A>, NW = kJoinThreads / 64, U = 8;
+    __shared__ A s_part[NW][64 * W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col = ((int64_t)blockIdx.y * 64 + lane) * W;
+    const bool live = col < a.D;
+    for (int q = 0; q < kJoinTiles; ++q) {
+        const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + q;
+        const int64_t t1 = (tile + 1) * a.tile;
+        if (tile >= a.tiles || t1 >= a.N) return;
+        const uint32_t key = a.keys[t1];
+        if (a.keys[t1 - 1] != key || a.order[t1] < 0) continue;  // no run crosses here
+        // is it begun in this tile?
+        const int64_t t0 = tile * a.tile;
+        if (t0 > 0 && a.keys[t0 - 1] == key) continue;
+        // tiles after this one that it goes on in
+        int64_t more = 0;
+        for (;;) {
+            const int64_t at = (tile + 1 + more + lane) * a.tile;
+            const uint64_t same = __ballot(at < a.N && a.keys[at < a.N ? at : a.N - 1] == key);
+            const int run = ~same ? __ffsll((unsigned long long)~same) - 1 : 64;
+            more += run;
+            if (run < 64) break;
+        }
+        // pieces 0 .. more: the last run's of this tile, then the first runs'
+        const int64_t lo = (more + 1) * wave / NW, hi = (more + 1) * (wave + 1) / NW;
+        A acc[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) acc[i] = (A)0;
+        for (int64_t s = lo; s < hi; s += U) {
+            Raw<A, W> r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t piece = s + u == 0 ? 2 * tile + 1 : 2 * (tile + s + u);
+                if (live && s + u < hi) r[u].load_upto(a.pieces + piece * a.D + col, a.D - col);
+                else
+#pragma unroll
+                    for (int i = 0; i < Raw<A, W>::kWords; ++i) r[u].w[i] = 0;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < W; ++i) acc[i] += r[u].template get<A>(i);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) s_part[wave][lane * W + i] = acc[i];
+        __syncthreads();
+        if (wave == 0 && live) {
+            for (int w = 1; w < NW; ++w)
+#pragma unroll
+                for (int i = 0; i < W; ++i) acc[i] += s_part[w][lane * W + i];
+            embed_write<Y, G, A, W>(a, key, col, acc);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+constexpr int64_t kMaxDim = int64_t(1) << 22;  // columns of a gradient
+
+inline int64_t round16(int64_t bytes) { return (bytes + 15) & ~int64_t(15); }
+
+inline int key_bits(int64_t values) {
+    int bits = 1;
+    while ((int64_t(1) << bits) < values) ++bits;
+    return bits;
+}
+
+// Where an index keeps what: the sorted keys and their tokens first, then,
+// for a longer sort, a second copy of both, the counts and the totals.
+struct IndexLayout {
+    int64_t N = 0, tiles = 0, order = 0, keys2 = 0, order2 = 0, counts = 0, totals = 0, bytes = 0;
+};
+inline bool index_layout(int64_t P, int64_t n, int64_t V, IndexLayout *l) {
+    const int64_t lim = (int64_t(1) << 31) - 1;
+    if (P < 1 || n < 0 || V < 1 || V >= lim || (n > 0 && P > lim / n) || P * n >= lim ||
+        P > lim / (V + 1) || P * (V + 1) >= lim)
+        return false;
+    l->N = P * n;
+    const int64_t part = round16(4 * l->N);
+    l->order = part;
+    l->bytes = 2 * part;
+    if (n > kSmallSort) {
+        l->tiles = (l->N + kSortTile - 1) / kSortTile;
+        l->keys2 = 2 * part;
+        l->order2 = 3 * part;
+        l->counts = 4 * part;
+        l->totals = l->counts + round16(4 * kBigBins * l->tiles);
+        l->bytes = l->totals + 4 * kBigBins;
+    }
+    l->bytes = std::max<int64_t>(l->bytes, 16);
+    return true;
+}
+
+// The tiles of a gradient's sum: as many units of work (a tile's chunk of
+// columns) as fill the device, but no fewer tokens than keep the pieces'
+// traffic low and no more than are summed in one order.
+struct GradShape {
+    int log2_lanes;
+    int64_t chunks;
+    int32_t tile;
+    int64_t tiles;
+};
+inline GradShape grad_shape(int64_t N, int64_t D, int vec) {
+    GradShape s;
+    const int64_t vecs = (D + vec - 1) / vec;
+    s.log2_lanes = 0;
+    while ((1 << s.log2_lanes) < vecs && s.log2_lanes < 6) ++s.log2_lanes;
+    s.chunks = (vecs + (1 << s.log2_lanes) - 1) >> s.log2_lanes;
+    s.tile = 8;
+    while (s.tile < 64 && (N / (2 * s.tile)) * (s.chunks << s.log2_lanes) >= 64 * 8192) s.tile *= 2;
+    s.tiles = (N + s.tile - 1) / s.tile;
+    return s;
+}
+
+inline bool known_type(int32_t t) { return t == ECC_F64 || t == ECC_F32 || t == ECC_BF16; }
+
+}  // namespace ecc
+
+using namespace ecc;
+
+extern "C" {
+
+ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, const void *d_ids,
+                              int32_t id_type, const void *d_table, int32_t table_type,
+                              int64_t ld_table, double scale, void *d_out, int32_t out_type,
+                              int64_t ld_out, void *hip_stream) {
+    clear_error();
+    ECC_ARG(n >= 0 && V >= 1 && D >= 1, "n must be >= 0, V and D >= 1");
+    ECC_ARG(id_type == ECC_I32 || id_type == ECC_I64, "id_type must be ECC_I32 or ECC_I64");
+    ECC_ARG(known_type(table_type) && known_type(out_type), "unknown element type");
+    ECC_ARG(ld_table >= D && ld_out >= D, "a leading dimension is below D");
+    if (n == 0) return ECC_OK;
+    ECC_ARG(d_ids && d_table && d_out, "NULL pointer");
+    const int64_t ib = id_type == ECC_I64 ? 8 : 4, tb = type_size(table_type),
+                  ob = type_size(out_type);
+    ECC_ARG((uintptr_t)d_ids % ib == 0 && (uintptr_t)d_table % tb == 0 &&
+                (uintptr_t)d_out % ob == 0,
+            "an array is not aligned to its elements");
+    if (V >= (int64_t(1) << 32) - 1 || D >= (int64_t(1) << 40) || n >= (int64_t(1) << 40) ||
+        ld_table >= (int64_t(1) << 40) || ld_out >= (int64_t(1) << 40)) {
+        set_error("a size is too large");
+        return ECC_ERR_RANGE;
+    }
+    const int vec = (int)(16 / std::min(tb, ob));
+    const int64_t vecs = (D + vec - 1) / vec;
+    int log2_lanes = 0;
+    while ((1 << log2_lanes) < vecs && log2_lanes < 6) ++log2_lanes;
+    const int64_t chunks = (vecs + (1 << log2_lanes) - 1) >> log2_lanes;
+    const int64_t per_block = kEmbedThreads >> log2_lanes;
+    if (n > (int64_t(1) << 44) / chunks ||
+        (n * chunks + per_block - 1) / per_block > 0x7fffff) {
+        set_error("n * D is too large for one launch");
+        return ECC_ERR_RANGE;
+    }
+    const int64_t out_bytes = row_extent(n, ld_out, D) * ob;
+    ECC_ARG(!ranges_meet(d_out, out_bytes, d_table, row_extent(V, ld_table, D) * tb) &&
+                !ranges_meet(d_out, out_bytes, d_ids, n * ib),
+            "the output overlaps an input");
+    const dim3 grid((unsigned)((n * chunks + per_block - 1) / per_block));
+    with_type(table_type, [&](auto t) {
+        with_type(out_type, [&](auto o) {
+            using T = decltype(t);
+            using O = decltype(o);
+            using A = Wider<T, O>;
+            constexpr int VEC = kVec<T> > kVec<O> ? kVec<T> : kVec<O>;
+            hipLaunchKernelGGL((k_embed_lookup<T, O, A, VEC>), grid, dim3(kEmbedThreads), 0,
+                               (hipStream_t)hip_stream, n, V, D, row0, d_ids,
+                               id_type == ECC_I64, (const T *)d_table, ld_table, (A)scale,
+                               (O *)d_out, ld_out, log2_lanes, chunks);
+        });
+    });
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+int64_t ecc_embed_index_size(int32_t P, int64_t n, int64_t V) {
+    IndexLayout l;
+    return index_layout(P, n, V, &l) ? l.bytes : -1;
+}
+
+ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, const void *d_ids,
+                             int32_t id_type, void *d_index, void *hip_stream) {
+    clear_error();
+    ECC_ARG(P >= 1 && n >= 0 && V >= 1, "P and V must be >= 1, n >= 0");
+    ECC_ARG(id_type == ECC_I32 || id_type == ECC_I64, "id_type must be ECC_I32 or ECC_I64");
+    IndexLayout l;
+    if (!index_layout(P, n, V, &l)) {
+        set_error("P * n and P * (V + 1) must be below 2^31 - 1");
+        return ECC_ERR_RANGE;
+    }
+    if (n == 0) return ECC_OK;
+    ECC_ARG(d_ids && d_index, "NULL pointer");
+    ECC_ARG((uintptr_t)d_index % 16 == 0, "d_index must be 16-byte aligned");
+    const int64_t ib = id_type == ECC_I64 ? 8 : 4;
+    ECC_ARG((uintptr_t)d_ids % ib == 0, "d_ids is not aligned to its elements");
+    ECC_ARG(!ranges_meet(d_ids, l.N * ib, d_index, l.bytes), "d_ids and d_index overlap");
+    hipStream_t s = (hipStream_t)hip_stream;
+    char *base = (char *)d_index;
+    uint32_t *keys = (uint32_t *)base;
+    int32_t *order = (int32_t *)(base + l.order);
+    const int id64 = id_type == ECC_I64;
+    if (n <= kSmallSort) {
+        const int bits = key_bits(V + 1), passes = (bits + 7) / 8,
+                  rb = (bits + passes - 1) / passes;
+        const dim3 grid((unsigned)P), block(kSortThreads);
+#define ECC_SORT(ITEMS)                                                                      \
+    hipLaunchKernelGGL(k_embed_sort<ITEMS>, grid, block, 0, s, n, V, row0, d_ids, id64, passes, \
+                       rb, keys, order)
+        if (n <= kSortThreads) ECC_SORT(1);
+        else if (n <= 2 * kSortThreads) ECC_SORT(2);
+        else if (n <= 4 * kSortThreads) ECC_SORT(4);
+        else if (n <= 8 * kSortThreads) ECC_SORT(8);
+        else ECC_SORT(16);
+#undef ECC_SORT
+        ECC_LAUNCH_CHECK();
+        return ECC_OK;
+    }
+    const int bits = key_bits((int64_t)P * (V + 1)), passes = (bits + kBigBits - 1) / kBigBits,
+              rb = (bits + passes - 1) / passes;
+    uint32_t *keys2 = (uint32_t *)(base + l.keys2);
+    int32_t *order2 = (int32_t *)(base + l.order2);
+    uint32_t *counts = (uint32_t *)(base + l.counts), *totals = (uint32_t *)(base + l.totals);
+    SortIn in{nullptr, nullptr, d_ids, l.N, n, V, row0, id64};
+    for (int pass = 0; pass < passes; ++pass) {
+        const bool to_first = (passes - 1 - pass) % 2 == 0;  // the last pass: the index itself
+        uint32_t *k_out = to_first ? keys : keys2;
+        int32_t *o_out = to_first ? order : order2;
+        hipLaunchKernelGGL(k_sort_count, dim3((unsigned)l.tiles), dim3(kTileThreads), 0, s, in,
+                           pass * rb, rb, counts);
+        ECC_LAUNCH_CHECK();
+        hipLaunchKernelGGL(k_sort_scan, dim3(1u << rb), dim3(kTileThreads), 0, s, l.tiles, counts,
+                           totals);
+        ECC_LAUNCH_CHECK();
+        hipLaunchKernelGGL(k_sort_move, dim3((unsigned)l.tiles), dim3(kTileThreads), 0, s, in,
+                           pass * rb, rb, counts, totals, k_out, o_out,
+                           (int)(pass + 1 == passes));
+        ECC_LAUNCH_CHECK();
+        in.keys = k_out;
+        in.order = o_out;
+    }
+    return ECC_OK;
+}
+
+int64_t ecc_embed_work_size(int32_t P, int64_t n, int64_t D, int32_t dy_type, int32_t grad_type) {
+    if (P < 1 || n < 0 || D < 1 || D > kMaxDim || !known_type(dy_type) ||
+        !known_type(grad_type) || (n > 0 && P >= (int64_t(1) << 31) / n))
+        return -1;
+    const GradShape g = grad_shape(P * n, D, (int)(16 / type_size(dy_type)));
+    const int64_t acc = dy_type == ECC_F64 || grad_type == ECC_F64 ? 8 : 4;
+    return std::max<int64_t>(16, round16(2 * g.tiles * D * acc));
+}
+
+ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const void *d_index,
+                            const void *d_dy, int32_t dy_type, int64_t ld_dy, double scale,
+                            void *d_grad, int32_t grad_type, int64_t ld_grad,
+                            int64_t worker_stride, int32_t accumulate, void *d_work,
+                            void *hip_stream) {
+    clear_error();
+    ECC_ARG(P >= 1 && n >= 0 && V >= 1 && D >= 1, "P, V and D must be >= 1, n >= 0");
+    ECC_ARG(known_type(dy_type) && known_type(grad_type), "unknown element type");
+    ECC_ARG(accumulate == 0 || accumulate == 1, "accumulate must be 0 or 1");
+    IndexLayout l;
+    if (!index_layout(P, n, V, &l) || D > kMaxDim || ld_dy >= (int64_t(1) << 40) ||
+        ld_grad >= (int64_t(1) << 40) || worker_stride >= (int64_t(1) << 50) ||
+        worker_stride < 0) {
+        set_error("P * n and P * (V + 1) must be below 2^31 - 1, D at most 2^22");
+        return ECC_ERR_RANGE;
+    }
+    ECC_ARG(ld_dy >= D && ld_grad >= D, "a leading dimension is below D");
+    const int64_t per_worker = row_extent(V, ld_grad, D);
+    ECC_ARG(P == 1 || worker_stride >= per_worker, "workers' gradients overlap");
+    ECC_ARG(d_grad, "NULL pointer");
+    ECC_ARG(n == 0 || (d_index && d_dy && d_work), "NULL pointer");
+    const int64_t yb = type_size(dy_type), gb = type_size(grad_type);
+    ECC_ARG((uintptr_t)d_grad % gb == 0 && (n == 0 || (uintptr_t)d_dy % yb == 0),
+            "an array is not aligned to its elements");
+    const int64_t work = ecc_embed_work_size(P, n, D, dy_type, grad_type);
+    const int64_t grad_bytes = ((P - 1) * worker_stride + per_worker) * gb;
+    if (n > 0) {
+        ECC_ARG((uintptr_t)d_work % 16 == 0 && (uintptr_t)d_index % 16 == 0,
+                "d_work and d_index must be 16-byte aligned");
+        const int64_t dy_bytes = row_extent(l.N, ld_dy, D) * yb;
+        ECC_ARG(!ranges_meet(d_grad, grad_bytes, d_dy, dy_bytes) &&
+                    !ranges_meet(d_grad, grad_bytes, d_index, l.bytes) &&
+                    !ranges_meet(d_grad, grad_bytes, d_work, work) &&
+                    !ranges_meet(d_work, work, d_dy, dy_bytes) &&
+                    !ranges_meet(d_work, work, d_index, l.bytes),
+                "the gradient, the work buffer and the inputs must not overlap");
+    }
+    if (n == 0 && accumulate) return ECC_OK;
+    const GradShape g = grad_shape(l.N, D, (int)(16 / yb));
+    const int64_t per_block = kEmbedThreads >> g.log2_lanes;
+    const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
+    const int64_t rows = (int64_t)P * V;
+    // a zeroing workgroup looks after up to 64 rows, fewer where the device
+    // would not be filled
+    const int64_t zero_rows = std::max<int64_t>(4, std::min<int64_t>(64, rows / 2048));
+    const int64_t zero_blocks = accumulate ? 0 : (rows + zero_rows - 1) / zero_rows;
+    if (sum_blocks + zero_blocks > 0x7fffff) {
+        set_error("P * n * D or P * V is too large for one launch");
+        return ECC_ERR_RANGE;
+    }
+    hipStream_t s = (hipStream_t)hip_stream;
+    with_type(dy_type, [&](auto y) {
+        with_type(grad_type, [&](auto gr) {
+            using Y = decltype(y);
+            using G = decltype(gr);
+            using A = Wider<Y, G>;
+            EmbedGradArgs<Y, G, A> a{};
+            a.N = l.N;
+            a.V = V;
+            a.D = D;
+            a.rows = rows;
+            a.keys = (const uint32_t *)d_index;
+            a.order = (const int32_t *)((const char *)d_index + l.order);
+            a.dy = (const Y *)d_dy;
+            a.ld_dy = ld_dy;
+            a.scale = (A)scale;
+            a.grad = (G *)d_grad;
+            a.ld_grad = ld_grad;
+            a.stride = worker_stride;
+            a.pieces = (A *)d_work;
+            a.tiles = g.tiles;
+            a.tile = g.tile;
+            a.accumulate = accumulate;
+            a.log2_lanes = g.log2_lanes;
+            a.chunks = g.chunks;
+            a.sum_blocks = sum_blocks;
+            a.zero_rows = (int32_t)zero_rows;
+            const dim3 grid((unsigned)(sum_blocks + zero_blocks));
+            if (g.log2_lanes == 6)
+                hipLaunchKernelGGL((k_embed_sum<Y, G, A, true>), grid, dim3(kEmbedThreads), 0, s,
+                                   a);
+            else
+                hipLaunchKernelGGL((k_embed_sum<Y, G, A, false>), grid, dim3(kEmbedThreads), 0, s,
+                                   a);
+            if (g.tiles > 1) {
+                constexpr int W = kVec<A>;
+                hipLaunchKernelGGL((k_embed_join<Y, G, A>),
+                                   dim3((unsigned)((g.tiles + kJoinTiles - 1) / kJoinTiles),
+                                        (unsigned)((D + 64 * W - 1) / (64 * W))),
+                                   dim3(kJoinThreads), 0, s, a);
+            }
+        });
+    });
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+}  // extern "C"

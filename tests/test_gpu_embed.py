@@ -1,0 +1,416 @@
+"""Token embedding through the library's calls: the scaled lookup and the
+table's gradient by sorted tokens, against their definitions in 64 bits.
+
+Tolerances.  u = 2^-24 for fp32 sums, 2^-53 for fp64; a bf16 result (8
+significant bits) adds 2^-8 relative.  A lookup is one rounded product.  A
+gradient of m tokens adds m numbers in some order and scales once: its error
+is at most (m + 3) u * scale * sum |dy|, whatever the order."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from gpu_common import announce                           # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+F64, F32, BF16 = torch.float64, torch.float32, torch.bfloat16
+HALF_ULP = {F64: 2.0 ** -53, F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+    yield
+    torch.cuda.synchronize()
+
+
+def _lm():
+    from paper_2203_17063_amd import lm
+    return lm
+
+
+def _unit(*types):
+    return 2.0 ** -53 if F64 in types else 2.0 ** -24
+
+
+def _random(shape, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(shape, generator=g, dtype=F64).to(dtype)
+
+
+def _tokens(n, lo, hi, seed, common=0.0):
+    """n tokens in [lo, hi); a share `common` of them one token."""
+    rng = np.random.default_rng(seed)
+    t = rng.integers(lo, hi, n)
+    t[rng.random(n) < common] = (lo + hi) // 2
+    return torch.from_numpy(t)
+
+
+# ---------------------------------------------------------------------------
+# lookup
+# ---------------------------------------------------------------------------
+
+def _lookup_ref(table, ids, scale, row0):
+    r = ids.reshape(-1).long() - row0
+    held = (r >= 0) & (r < table.shape[0])
+    y = table.double()[r.clamp(0, table.shape[0] - 1)] * scale
+    return torch.where(held[:, None], y, torch.zeros((), dtype=F64)).view(*ids.shape, -1)
+
+
+@pytest.mark.parametrize("tt", [F64, F32, BF16])
+@pytest.mark.parametrize("ot", [F64, F32, BF16])
+@pytest.mark.parametrize("n,V,D", [(1, 1, 1), (3, 7, 5), (64, 50, 64), (257, 129, 250),
+                                   (33, 1000, 1023), (5, 11, 4104)])
+def test_lookup(tt, ot, n, V, D):
+    announce("lookup", tt, ot, n, V, D)
+    table, ids = _random((V, D), tt, 1), _tokens(n, -2, V + 2, 2)
+    got = _lm().embed_lookup(table.cuda(), ids.cuda(), scale=3.7, dtype=ot).cpu().double()
+    ref = _lookup_ref(table, ids, 3.7, 0)
+    assert torch.all((got - ref).abs() <= (2 * _unit(tt, ot) + HALF_ULP[ot]) * ref.abs())
+
+
+def test_lookup_no_tokens_and_shapes():
+    lm = _lm()
+    announce("lookup, empty")
+    table = _random((9, 6), F32, 3).cuda()
+    assert lm.embed_lookup(table, torch.empty((0,), dtype=torch.int64, device="cuda")).shape == \
+        (0, 6)
+    ids = _tokens(24, 0, 9, 4).view(2, 3, 4).cuda()
+    got = lm.embed_lookup(table, ids)
+    assert got.shape == (2, 3, 4, 6) and torch.equal(got, table[ids])
+
+
+@pytest.mark.parametrize("id_type", [torch.int32, torch.int64])
+def test_lookup_part_of_a_table(id_type):
+    """Tables split by rows: the parts' lookups add up to the whole's; tokens
+    far outside any 32-bit range are outside."""
+    lm = _lm()
+    announce("lookup, parts", id_type)
+    table = _random((100, 40), F32, 5).cuda()
+    ids = _tokens(300, 0, 100, 6).to(id_type)
+    whole = lm.embed_lookup(table, ids.cuda(), scale=2.0)
+    parts = sum(lm.embed_lookup(table[lo:hi], ids.cuda(), scale=2.0, row0=lo)
+                for lo, hi in ((0, 37), (37, 38), (38, 100)))
+    assert torch.equal(whole, parts)
+    far = torch.tensor([-1, -100, 2 ** 31 - 1, -2 ** 31], dtype=id_type)
+    if id_type == torch.int64:
+        far = torch.cat([far, torch.tensor([2 ** 32, 2 ** 63 - 1, -2 ** 63, 2 ** 32 + 5])])
+    for row0 in (0, 3):
+        assert not lm.embed_lookup(table, far.cuda(), row0=row0).any()
+
+
+def test_lookup_strided_and_unaligned():
+    """Rows inside wider buffers, starting at any element."""
+    lm = _lm()
+    for dt, D, off in [(BF16, 61, 1), (BF16, 64, 3), (F32, 33, 1), (F64, 17, 1)]:
+        announce("lookup, strided", dt, D, off)
+        wide = _random((50, D + 9), dt, 7).cuda()
+        table = wide[:, off:off + D]
+        out = torch.full((40, D + 5), 8.0, dtype=dt, device="cuda")
+        ids = _tokens(40, 0, 50, 8).cuda()
+        lm.embed_lookup(table, ids, out=out[:, 2:2 + D])
+        assert torch.equal(out[:, 2:2 + D], table[ids])
+        assert (out[:, :2] == 8).all() and (out[:, 2 + D:] == 8).all()
+
+
+def test_lookup_special_values():
+    """Infinities and NaN of a row arrive; those of other rows do not, and a
+    token outside the table gives zeros whatever the table holds."""
+    lm = _lm()
+    announce("lookup, special values")
+    table = torch.full((4, 19), float("nan"), dtype=BF16)
+    table[1] = 2.0
+    table[2] = float("inf")
+    got = lm.embed_lookup(table.cuda(), torch.tensor([1, 2, -1, 0, 4]).cuda(), scale=0.5).cpu()
+    assert (got[0] == 1).all() and torch.isinf(got[1]).all()
+    assert (got[2] == 0).all() and torch.isnan(got[3]).all() and (got[4] == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# index and gradient
+# ---------------------------------------------------------------------------
+
+def _index_ref(ids, V, P, row0):
+    n = ids.numel() // P
+    r = ids.reshape(-1).long() - row0
+    held = (r >= 0) & (r < V)
+    key = torch.arange(P * n) // max(n, 1) * (V + 1) + torch.where(held, r, V)
+    key, order = torch.sort(key, stable=True)
+    return key, torch.where(held[order], order, ~order)
+
+
+@pytest.mark.parametrize("P,n,V", [(1, 1, 1), (1, 63, 5), (1, 1024, 300), (1, 1025, 70000),
+                                   (1, 2049, 7), (1, 4097, 128000), (1, 8193, 255),
+                                   (1, 16384, 65535), (1, 16385, 1000), (1, 70001, 128000),
+                                   (3, 5000, 40), (33, 77, 511), (2, 20011, 300000),
+                                   (5, 17000, 65536)])
+def test_index(P, n, V):
+    """Both sorts: one workgroup per worker, and digits over tiles."""
+    announce("index", P, n, V)
+    ids = _tokens(P * n, -3, V + 3, P + n, common=0.3)
+    index = _lm().embed_index(ids.cuda(), V, P=P)
+    N = P * n
+    at = (4 * N + 15) // 16 * 16
+    data = index.data.cpu()
+    key, order = _index_ref(ids, V, P, 0)
+    assert torch.equal(data[:4 * N].view(torch.int32).long(), key)
+    assert torch.equal(data[at:at + 4 * N].view(torch.int32).long(), order)
+
+
+def _grad_ref(ids, dy, V, P, scale, row0=0):
+    """(gradient, its error scale, tokens of each row)."""
+    n = ids.numel() // P
+    r = ids.reshape(-1).long() - row0
+    held = (r >= 0) & (r < V)
+    rows = torch.arange(P * n) // max(n, 1) * V + r
+    rows, dy = rows[held], dy.reshape(P * n, -1)[held].double()
+    shape = (P * V, dy.shape[1])
+    g = torch.zeros(shape, dtype=F64).index_add_(0, rows, dy)
+    s = torch.zeros(shape, dtype=F64).index_add_(0, rows, dy.abs())
+    m = torch.bincount(rows, minlength=P * V)
+    return ((g * scale).view(P, V, -1), (s * abs(scale)).view(P, V, -1),
+            m.view(P, V, 1).double())
+
+
+def _check_grad(got, ref, mass, count, u, ulp, before=None):
+    got = got.cpu().double()
+    tol = (count + 3) * u * mass
+    want = ref if before is None else before.double() + ref
+    if before is not None:
+        tol = tol + 2 * u * (before.double().abs() + mass)
+    assert torch.all((got - want).abs() <= tol + ulp * want.abs()), (got - want).abs().max()
+
+
+@pytest.mark.parametrize("yt,gt", [(BF16, F32), (BF16, F64), (BF16, BF16), (F32, F32),
+                                   (F32, F64), (F32, BF16), (F64, F64), (F64, F32), (F64, BF16)])
+@pytest.mark.parametrize("P,n,V,D,common", [
+    (1, 1, 1, 1, 0.0), (1, 1, 5, 300, 0.0), (1, 7, 3, 17, 0.0), (2, 100, 40, 8, 0.5),
+    (1, 1500, 30, 65, 0.9), (3, 333, 700, 250, 0.2), (1, 3000, 5000, 1030, 0.1)])
+def test_grad(yt, gt, P, n, V, D, common):
+    announce("grad", yt, gt, P, n, V, D, common)
+    lm = _lm()
+    ids, dy = _tokens(P * n, -1, V + 1, 3, common), _random((P * n, D), yt, 4)
+    index = lm.embed_index(ids.cuda(), V, P=P)
+    ref, mass, count = _grad_ref(ids, dy, V, P, 1.3)
+    got = lm.embed_grad(index, dy.cuda(), scale=1.3, dtype=gt)
+    assert got.shape == (P, V, D)
+    _check_grad(got, ref, mass, count, _unit(yt, gt), HALF_ULP[gt])
+    # the same bits again, and added to what is there
+    before = _random((P, V, D), gt, 5)
+    more = before.cuda()
+    lm.embed_grad(index, dy.cuda(), scale=1.3, grad=more, accumulate=True)
+    _check_grad(more, ref, mass, count, _unit(yt, gt), HALF_ULP[gt], before)
+    assert torch.equal(got, lm.embed_grad(index, dy.cuda(), scale=1.3, dtype=gt))
+    untouched = (count == 0).expand(P, V, D)
+    assert torch.equal(more.cpu()[untouched], before[untouched])
+    assert not got.cpu()[untouched].any()
+
+
+@pytest.mark.parametrize("n,D", [(40000, 64), (40000, 520)])
+def test_grad_long_runs(n, D):
+    """One token makes up the whole text, or nearly: its pieces cover
+    thousands of tiles."""
+    lm = _lm()
+    for common, V in ((1.0, 1), (0.97, 50)):
+        announce("grad, long runs", n, D, common)
+        ids, dy = _tokens(n, 0, V, 6, common), _random((n, D), BF16, 7)
+        ref, mass, count = _grad_ref(ids, dy, V, 1, 1.0)
+        got = lm.embed_grad(lm.embed_index(ids.cuda(), V), dy.cuda())
+        _check_grad(got, ref, mass, count, 2.0 ** -24, 2.0 ** -24)
+
+
+def test_grad_no_tokens():
+    lm = _lm()
+    announce("grad, no tokens")
+    empty = torch.empty((0,), dtype=torch.int32, device="cuda")
+    dy = torch.empty((0, 33), dtype=F32, device="cuda")
+    got = torch.full((2, 10, 33), 5.0, device="cuda")
+    index = lm.embed_index(empty, 10, P=2)
+    lm.embed_grad(index, dy, grad=got, accumulate=True)
+    assert (got == 5).all()
+    lm.embed_grad(index, dy, grad=got)
+    assert not got.any()
+    # tokens, but none in the table: their rows are not read
+    ids = torch.full((50,), -1, dtype=torch.int64, device="cuda")
+    dy = torch.full((50, 33), float("nan"), device="cuda")
+    assert not lm.embed_grad(lm.embed_index(ids, 10), dy).any()
+
+
+def test_grad_nan_of_padding_stays_out():
+    """NaN and infinities in rows of tokens outside the table, next to every
+    other row."""
+    lm = _lm()
+    announce("grad, NaN in padding")
+    n, V, D = 999, 20, 70
+    ids, dy = _tokens(n, 0, V, 8), _random((n, D), F32, 9)
+    ids[::3] = -1
+    dy[::3] = float("nan")
+    dy[::6] = float("inf")
+    ref, mass, count = _grad_ref(ids, dy, V, 1, 1.0)
+    got = lm.embed_grad(lm.embed_index(ids.cuda(), V), dy.cuda())
+    _check_grad(got, ref, mass, count, 2.0 ** -24, 2.0 ** -24)
+
+
+def test_grad_in_rank_contributions():
+    """Workers' gradients inside the contributions of a stale allreduce: rows
+    at their own stride, the elements around them left alone."""
+    lm = _lm()
+    announce("grad in contributions")
+    P, n, V, D = 4, 120, 33, 31
+    contrib = torch.full((P, 5 + V * (D + 2) + 3), 9.0, dtype=F64, device="cuda")
+    view = contrib[:, 5:5 + V * (D + 2)].view(P, V, D + 2)[:, :, :D]
+    ids, dy = _tokens(P * n, -1, V, 10), _random((P * n, D + 3), BF16, 11)
+    ref, mass, count = _grad_ref(ids, dy[:, 1:1 + D], V, P, 0.25)
+    lm.embed_grad(lm.embed_index(ids.cuda(), V, P=P), dy.cuda()[:, 1:1 + D], scale=0.25,
+                  grad=view)
+    _check_grad(view, ref, mass, count, 2.0 ** -53, 2.0 ** -53)
+    rest = contrib.clone()
+    rest[:, 5:5 + V * (D + 2)].view(P, V, D + 2)[:, :, :D] = 9.0
+    assert (rest == 9).all()
+
+
+def test_grad_of_part_of_a_table():
+    lm = _lm()
+    announce("grad of a table's part")
+    n, V, D = 700, 90, 24
+    ids, dy = _tokens(n, 0, V, 12), _random((n, D), F32, 13)
+    ref, mass, count = _grad_ref(ids, dy, 40, 1, 1.0, row0=30)
+    got = lm.embed_grad(lm.embed_index(ids.cuda(), 40, row0=30), dy.cuda())
+    _check_grad(got, ref, mass, count, 2.0 ** -24, 2.0 ** -24)
+
+
+def test_grad_against_differences():
+    """The gradient of sum(lookup * c) in the table, against differences of
+    the lookup in 64 bits (linear: exact but for rounding)."""
+    lm = _lm()
+    announce("grad against differences")
+    n, V, D = 30, 6, 5
+    ids, c = _tokens(n, -1, V, 14).cuda(), _random((n, D), F64, 15).cuda()
+    table = _random((V, D), F64, 16).cuda()
+
+    def value(t):
+        return float((lm.embed_lookup(t, ids, scale=1.7) * c).sum())
+
+    got = lm.embed_grad(lm.embed_index(ids, V), c, scale=1.7, dtype=F64)[0]
+    for v in range(V):
+        for d in range(D):
+            up, down = table.clone(), table.clone()
+            up[v, d] += 0.5
+            down[v, d] -= 0.5
+            assert abs(value(up) - value(down) - float(got[v, d])) <= 1e-12 * n * D
+
+
+def test_on_another_stream():
+    """Index and gradient on a stream of their own, joined by events."""
+    lm = _lm()
+    announce("another stream")
+    n, V, D = 5000, 400, 96
+    ids, dy = _tokens(n, 0, V, 17), _random((n, D), BF16, 18)
+    d_ids, d_dy = ids.cuda(), dy.cuda()
+    want = lm.embed_grad(lm.embed_index(d_ids, V), d_dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = lm.embed_grad(lm.embed_index(d_ids, V), d_dy)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+
+
+def test_in_a_graph():
+    """Index, lookup and gradient captured once and replayed on new tokens."""
+    lm = _lm()
+    announce("graph")
+    n, V, D = 3000, 500, 130
+    ids, table = _tokens(n, -1, V, 19).cuda(), _random((V, D), F32, 20).cuda()
+    dy = _random((n, D), F32, 21).cuda()
+    lm.embed_grad(lm.embed_index(ids, V), lm.embed_lookup(table, ids))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = lm.embed_lookup(table, ids, scale=2.0)
+        g = lm.embed_grad(lm.embed_index(ids, V), dy)
+    for k in range(4):
+        ids.copy_(_tokens(n, -1, V, 30 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, lm.embed_lookup(table, ids, scale=2.0))
+        assert torch.equal(g, lm.embed_grad(lm.embed_index(ids, V), dy))
+
+
+def test_refusals():
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("embed refusals")
+    table = torch.zeros((10, 8), device="cuda")
+    ids = torch.zeros(6, dtype=torch.int64, device="cuda")
+    out = torch.zeros((6, 8), device="cuda")
+
+    def lookup(**kw):
+        a = dict(n=6, V=10, D=8, row0=0, d_ids=ids, id_type=E.ECC_I64, d_table=table,
+                 table_type=E.ECC_F32, ld_table=8, scale=1.0, d_out=out, out_type=E.ECC_F32,
+                 ld_out=8)
+        a.update(kw)
+        with pytest.raises(E.EccError) as e:
+            E.ecc_embed_lookup(**a)
+        return e.value.status
+
+    for bad in (dict(n=-1), dict(V=0), dict(D=0), dict(id_type=E.ECC_F32), dict(table_type=7),
+                dict(out_type=E.ECC_I32), dict(ld_table=7), dict(ld_out=7), dict(d_ids=None),
+                dict(d_table=None), dict(d_out=None), dict(d_out=table),
+                dict(d_out=out.data_ptr() + 2), dict(d_ids=ids.data_ptr() + 4),
+                dict(d_out=ids)):
+        assert lookup(**bad) == E.ECC_ERR_ARG, bad
+    assert lookup(V=1 << 33) == E.ECC_ERR_RANGE
+    assert lookup(n=1 << 36) == E.ECC_ERR_RANGE
+
+    index = lm.embed_index(ids, 10, P=2)
+    work = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    grad = torch.zeros((2, 10, 8), device="cuda")
+
+    def embed_grad(**kw):
+        a = dict(P=2, n=3, V=10, D=8, d_index=index.data, d_dy=out, dy_type=E.ECC_F32, ld_dy=8,
+                 scale=1.0, d_grad=grad, grad_type=E.ECC_F32, ld_grad=8, worker_stride=80,
+                 accumulate=0, d_work=work)
+        a.update(kw)
+        with pytest.raises(E.EccError) as e:
+            E.ecc_embed_grad(**a)
+        return e.value.status
+
+    for bad in (dict(P=0), dict(n=-1), dict(V=0), dict(D=0), dict(dy_type=E.ECC_I64),
+                dict(grad_type=9), dict(ld_dy=7), dict(ld_grad=7), dict(worker_stride=79),
+                dict(accumulate=2), dict(d_index=None), dict(d_dy=None), dict(d_grad=None),
+                dict(d_work=None), dict(d_work=work.data_ptr() + 8),
+                dict(d_index=index.data.data_ptr() + 4), dict(d_work=grad), dict(d_dy=grad),
+                dict(d_grad=grad.data_ptr() + 1)):
+        assert embed_grad(**bad) == E.ECC_ERR_ARG, bad
+    assert embed_grad(n=1 << 31) == E.ECC_ERR_RANGE
+    assert embed_grad(D=(1 << 22) + 1, ld_dy=1 << 23, ld_grad=1 << 23, worker_stride=1 << 27) == \
+        E.ECC_ERR_RANGE
+    with pytest.raises(E.EccError):
+        E.ecc_embed_index(2, 3, 10, 0, ids, E.ECC_I64, index.data.data_ptr() + 4)
+    with pytest.raises(E.EccError):
+        E.ecc_embed_index(2, 3, 10, 0, None, E.ECC_I64, index.data)
+    # what the tensors say
+    with pytest.raises(TypeError):
+        lm.embed_lookup(table, ids.float())
+    with pytest.raises(TypeError):
+        lm.embed_lookup(table.half(), ids)
+    with pytest.raises(ValueError):
+        lm.embed_lookup(table.t(), ids)
+    with pytest.raises(ValueError):
+        lm.embed_lookup(table, ids[::2])
+    with pytest.raises(ValueError):
+        lm.embed_lookup(table.cpu(), ids)
+    with pytest.raises(ValueError):
+        lm.embed_lookup(table, ids, out=out[:5])
+    with pytest.raises(ValueError):
+        lm.embed_index(ids, 10, P=4)
+    with pytest.raises(ValueError):
+        lm.embed_grad(index, out[:5])
+    with pytest.raises(ValueError):
+        lm.embed_grad(index, out, accumulate=True)
+    with pytest.raises(ValueError):
+        lm.embed_grad(index, out, grad=grad[:, :9])
