@@ -701,6 +701,75 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
                             int64_t worker_stride, int32_t accumulate, void *d_work,
                             void *hip_stream);
 
+/* The joint between two blocks of a residual network, for rows t of P * n
+ * (D elements each; rms(v) = v / sqrt(mean(v^2) + eps)):
+ *   u  = rms(f) * (w_offset + w_post)          (u = f when d_w_post is NULL)
+ *   x' = res_scale * x + branch_scale * g * u  (the second term is absent
+ *                                               when d_f is NULL)
+ *   h  = rms(x') * (w_offset + w_pre)          (absent when d_w_pre is NULL)
+ * so that one call is the norm before a block, the norm after it, or both
+ * with the next block's.  The gate g is
+ *   absent (1)                                  d_gate NULL;
+ *   a row of d_gate of element type `type`      gate_rows >= 1: row t uses
+ *     gate row t / gate_rows (a multiple of gate_rows rows per worker when
+ *     P > 1);
+ *   a parameter of D elements of type w_type    gate_rows = 0.
+ * x, f and gate rows are of element type `type`, w_post, w_pre and a
+ * parameter gate of w_type.  h is formed from x' before x' is rounded.
+ * P, D >= 1, n >= 0, eps > 0; D up to ECC_NORM_MAX_DIM (half of that for
+ * ECC_F64), else ECC_ERR_RANGE. */
+#define ECC_NORM_MAX_DIM 16384
+typedef struct {
+    int64_t n, D;
+    int32_t P;
+    int32_t type, w_type;
+    const void *d_x;
+    int64_t ld_x;
+    const void *d_f;
+    int64_t ld_f;
+    const void *d_gate;
+    int64_t ld_gate, gate_rows;
+    const void *d_w_post, *d_w_pre;
+    double w_offset, res_scale, branch_scale, eps;
+} ecc_norm_t;
+
+/* d_x_out may be NULL (not written) or d_x, d_h may be d_f or d_x (with the same
+ * leading dimension); d_h is NULL exactly when d_w_pre is. */
+ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_out, void *d_h,
+                              int64_t ld_h, void *hip_stream);
+
+/* The gradients at a->d_x = x' (what the forward call wrote to d_x_out):
+ *   dX      = d_dx_out + (the gradient of h in x', for the given d_dh)
+ *   d_dx    = res_scale * dX,   d_df = the gradient in f, for the given dX
+ *   d_dw_post, d_dw_pre, d_dgate: sums over a worker's rows (over the rows
+ *     that share it for a row gate: ceil(P n / gate_rows) rows of D elements
+ *     of `type` at ld_dgate, always written), D elements of grad_type per
+ *     worker for parameters.
+ * d_dx_out NULL: zero.  d_dh is NULL exactly when d_w_pre is; NULL outputs
+ * are not computed; d_df, d_dw_post and d_dgate need d_f (d_dw_post also
+ * d_w_post, d_dgate d_gate, d_dw_pre d_w_pre).  d_dx may be d_dx_out or
+ * d_dh, and d_df may be d_f or d_dh (with the same leading dimension).
+ * d_work: ecc_norm_work_size(a) bytes. */
+typedef struct {
+    const void *d_dh;
+    int64_t ld_dh;
+    const void *d_dx_out;
+    int64_t ld_dx_out;
+    void *d_dx;
+    int64_t ld_dx;
+    void *d_df;
+    int64_t ld_df;
+    void *d_dgate;
+    int64_t ld_dgate;
+    void *d_dw_post, *d_dw_pre;
+    int32_t grad_type;
+    int32_t accumulate;
+    int64_t worker_stride;
+} ecc_norm_grad_t;
+int64_t ecc_norm_work_size(const ecc_norm_t *a);
+ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *d_work,
+                           void *hip_stream);
+
 /* ---------------------------------------------------------------------------
  * Plain streaming copy d_dst[i] = d_src[i], 0 <= i < n, enqueued on
  * hip_stream.  Both buffers 8-byte aligned and not overlapping

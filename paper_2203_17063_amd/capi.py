@@ -31,6 +31,7 @@ ECC_FORM_GENERAL, ECC_FORM_COLUMN_VALUES, ECC_FORM_DIAGONALS = 0, 1, 2
 ECC_MAX_DIAGONALS = 8
 ECC_SCRATCH_DOUBLES = 1 << 20
 ECC_GATHER_CHUNK = 2048
+ECC_NORM_MAX_DIM = 16384
 ECC_F64, ECC_F32, ECC_BF16, ECC_I32, ECC_I64 = 0, 1, 2, 3, 4
 
 STATUS_NAMES = {0: "ECC_OK", 1: "ECC_ERR_ARG", 2: "ECC_ERR_OVERLAP", 3: "ECC_ERR_RANGE",
@@ -52,6 +53,28 @@ class ecc_csr_t(ctypes.Structure):
 class ecc_matrix_opts_t(ctypes.Structure):
     _fields_ = [("range_bytes", ctypes.c_int64), ("tile_rows", ctypes.c_int64),
                 ("schedule", ctypes.c_int32), ("compact", ctypes.c_int32)]
+
+
+class ecc_norm_t(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("D", ctypes.c_int64), ("P", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("w_type", ctypes.c_int32), ("d_x", ctypes.c_void_p),
+                ("ld_x", ctypes.c_int64), ("d_f", ctypes.c_void_p), ("ld_f", ctypes.c_int64),
+                ("d_gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
+                ("gate_rows", ctypes.c_int64), ("d_w_post", ctypes.c_void_p),
+                ("d_w_pre", ctypes.c_void_p), ("w_offset", ctypes.c_double),
+                ("res_scale", ctypes.c_double), ("branch_scale", ctypes.c_double),
+                ("eps", ctypes.c_double)]
+
+
+class ecc_norm_grad_t(ctypes.Structure):
+    _fields_ = [("d_dh", ctypes.c_void_p), ("ld_dh", ctypes.c_int64),
+                ("d_dx_out", ctypes.c_void_p), ("ld_dx_out", ctypes.c_int64),
+                ("d_dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64),
+                ("d_df", ctypes.c_void_p), ("ld_df", ctypes.c_int64),
+                ("d_dgate", ctypes.c_void_p), ("ld_dgate", ctypes.c_int64),
+                ("d_dw_post", ctypes.c_void_p), ("d_dw_pre", ctypes.c_void_p),
+                ("grad_type", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+                ("worker_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -114,6 +137,10 @@ _SIGS = [
     ("ecc_embed_work_size", _I64, [_I32, _I64, _I64, _I32, _I32]),
     ("ecc_embed_grad", ctypes.c_int, [_I32, _I64, _I64, _I64, _VP, _VP, _I32, _I64, _D, _VP, _I32,
                                       _I64, _I64, _I32, _VP, _VP]),
+    ("ecc_norm_forward", ctypes.c_int, [ctypes.POINTER(ecc_norm_t), _VP, _I64, _VP, _I64, _VP]),
+    ("ecc_norm_work_size", _I64, [ctypes.POINTER(ecc_norm_t)]),
+    ("ecc_norm_grad", ctypes.c_int, [ctypes.POINTER(ecc_norm_t),
+                                     ctypes.POINTER(ecc_norm_grad_t), _VP, _VP]),
     ("ecc_solve", ctypes.c_int, [_VP, _VP, _VP, _D, _D, _VP, _VP, _VP, _VP, _I32, _D, _VP, _VP,
                                  _VP, _VP]),
 ]
@@ -456,3 +483,15 @@ def ecc_embed_grad(P, n, V, D, d_index, d_dy, dy_type, ld_dy, scale, d_grad, gra
     _check(lib().ecc_embed_grad(P, n, V, D, _ptr(d_index), _ptr(d_dy), dy_type, ld_dy, scale,
                                 _ptr(d_grad), grad_type, ld_grad, worker_stride, accumulate,
                                 _ptr(d_work), hip_stream))
+
+
+def ecc_norm_forward(a: ecc_norm_t, d_x_out, ld_x_out, d_h, ld_h, hip_stream=None):
+    _check(lib().ecc_norm_forward(a, _ptr(d_x_out), ld_x_out, _ptr(d_h), ld_h, hip_stream))
+
+
+def ecc_norm_work_size(a: ecc_norm_t) -> int:
+    return int(lib().ecc_norm_work_size(a))
+
+
+def ecc_norm_grad(a: ecc_norm_t, g: ecc_norm_grad_t, d_work, hip_stream=None):
+    _check(lib().ecc_norm_grad(a, g, _ptr(d_work), hip_stream))

@@ -585,8 +585,6 @@ inline GradShape grad_shape(int64_t N, int64_t D, int vec) {
     return s;
 }
 
-inline bool known_type(int32_t t) { return t == ECC_F64 || t == ECC_F32 || t == ECC_BF16; }
-
 }  // namespace ecc
 
 using namespace ecc;

@@ -23,6 +23,8 @@ template <typename A, typename B>
 using Wider = std::conditional_t<std::is_same_v<A, double> || std::is_same_v<B, double>, double,
                                  float>;
 
+inline bool known_type(int32_t t) { return t == ECC_F64 || t == ECC_F32 || t == ECC_BF16; }
+
 inline int64_t type_size(int32_t type) {
     switch (type) {
         case ECC_F64: return 8;

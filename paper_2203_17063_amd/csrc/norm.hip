@@ -1,0 +1,716 @@
+// The joint between two blocks of a residual network, forward and backward:
+//   u = rms(f) (o + w_post),  x' = a x + b g u,  h = rms(x') (o + w_pre)
+// (see libecc.h for what may be absent).  Bound by memory: forward reads x, f
+// and the gate and writes x' and h; backward reads x', f, the gate and the
+// gradients of x' and h and writes those of x, f and the gate.
+//
+// A workgroup holds a row in registers: it reads every operand of the row
+// once and writes every result once, and the weights are read once per
+// workgroup, which walks several rows.  The workgroup is as wide as makes a
+// thread hold 16 elements of the row (backward 8, for its registers).
+//
+// Forward has two sums per row, that of f^2 and then that of x'^2 (formed
+// from the squares themselves: as a combination of sums over x and f they
+// could cancel).  Backward takes one round for all of its sums.  With
+//   q = 1/sqrt(mean x'^2 + eps),  k = 1/sqrt(mean f^2 + eps),
+//   A = dh (o + w_pre),  C = b g (o + w_post) f:
+//   dX = dx' + q A - c x',                 c = q^3 mean(A x')
+//   df = k (C/f dX - f k^2 mean(C dX)),    sum C dX = sum C dx' + q sum C A - c sum C x'
+// so sum x'^2, f^2, A x', C dx', C A and C x' are formed together, and no
+// statistics are kept from the forward call.
+//
+// The sums over rows (gradients of the weights and of a shared gate) stay in
+// registers while a workgroup walks its unit of consecutive rows; the units'
+// sums go to the work buffer and a second launch adds them in order.
+#include <algorithm>
+
+#include "lm_common.h"
+
+namespace ecc {
+
+constexpr int kNormCus = 256;
+
+struct NormArgs {
+    int64_t N, D;
+    const void *x, *f, *gate, *w_post, *w_pre;
+    int64_t ld_x, ld_f, ld_gate;
+    int64_t gate_rows;  // rows that share a gate row; 0: a parameter
+    int32_t w_type;
+    double offset, res, branch, eps;
+};
+
+// A parameter's element as the accumulator's type; 1 where there is none.
+template <typename A>
+__device__ __forceinline__ A load_param(const void *p, int32_t type, int64_t i) {
+    if (type == ECC_F64) return (A) reinterpret_cast<const double *>(p)[i];
+    if (type == ECC_F32) return (A) reinterpret_cast<const float *>(p)[i];
+    return load_elem<A>(reinterpret_cast<const bf16_t *>(p) + i);
+}
+template <typename A>
+__device__ __forceinline__ void store_param(void *p, int32_t type, int64_t i, A v, int accumulate) {
+    if (type == ECC_F64) {
+        double *q = reinterpret_cast<double *>(p) + i;
+        *q = accumulate ? *q + (double)v : (double)v;
+    } else if (type == ECC_F32) {
+        float *q = reinterpret_cast<float *>(p) + i;
+        *q = accumulate ? (float)((A)*q + v) : (float)v;
+    } else {
+        bf16_t *q = reinterpret_cast<bf16_t *>(p) + i;
+        store_elem<A>(q, accumulate ? load_elem<A>(q) + v : v);
+    }
+}
+
+__device__ __forceinline__ float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
+__device__ __forceinline__ float rsqrt_(float v) { return 1.0f / __builtin_sqrtf(v); }
+__device__ __forceinline__ double rsqrt_(double v) { return 1.0 / __builtin_sqrt(v); }
+
+// K sums over the workgroup's NT threads, in every thread.  s holds [2][NT /
+// 64][K]; the two halves are used in turn, so that one barrier is enough:
+// a half is written again only after every wave has passed the barrier of
+// the other, and so has read this one.
+template <int NT, int K, typename A>
+__device__ __forceinline__ void row_sums(A (&v)[K], A *s, int &half) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = wave_all(v[k], OpSum{});
+    if constexpr (NT > 64) {
+        constexpr int NW = NT / 64;
+        A *b = s + half * NW * K;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) b[(threadIdx.x >> 6) * K + k] = v[k];
+        }
+        lds_barrier();
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = b[k];
+#pragma unroll
+        for (int w = 1; w < NW; ++w)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] += b[w * K + k];
+        half ^= 1;
+    }
+}
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, int64_t ld_x_out,
+                                                     void *h_out, int64_t ld_h) {
+    using A = Acc<T>;
+    constexpr int VEC = kVec<T>, E = NV * VEC;
+    __shared__ A s_red[2 * (NT / 64)];
+    int half = 0;
+    const A res = (A)a.res, branch = (A)a.branch, eps = (A)a.eps, inv_d = (A)1 / (A)a.D;
+    A wq[E], wp[E];  // branch scale, parameter gate and post-norm weight; pre-norm weight
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC + i;
+            A q = branch, p = (A)0;
+            if (c < a.D) {
+                if (a.w_post) q *= (A)a.offset + load_param<A>(a.w_post, a.w_type, c);
+                if (a.gate && a.gate_rows == 0) q *= load_param<A>(a.gate, a.w_type, c);
+                if (a.w_pre) p = (A)a.offset + load_param<A>(a.w_pre, a.w_type, c);
+            }
+            wq[v * VEC + i] = q;
+            wp[v * VEC + i] = p;
+        }
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        const T *x = reinterpret_cast<const T *>(a.x) + row * a.ld_x;
+        const T *f = reinterpret_cast<const T *>(a.f) + row * a.ld_f;
+        const bool row_gate = a.gate && a.gate_rows > 0;
+        const T *g = reinterpret_cast<const T *>(a.gate) +
+                     (row_gate ? row / a.gate_rows * a.ld_gate : 0);
+        Raw<T, VEC> rx[NV], rf[NV], rg[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
+            rx[v].load_upto(x + c, a.D - c);
+            if (a.f) rf[v].load_upto(f + c, a.D - c);
+            if (row_gate) rg[v].load_upto(g + c, a.D - c);
+        }
+        A y[E];
+        A k = (A)1;
+        if (a.f && a.w_post) {
+            A sum[1] = {(A)0};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const A t = rf[e / VEC].template get<A>(e % VEC);
+                sum[0] = fma_(t, t, sum[0]);
+            }
+            row_sums<NT>(sum, s_red, half);
+            k = rsqrt_(fma_(sum[0], inv_d, eps));
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            y[e] = res * rx[e / VEC].template get<A>(e % VEC);
+            if (a.f) {
+                A u = k * rf[e / VEC].template get<A>(e % VEC) * wq[e];
+                if (row_gate) u *= rg[e / VEC].template get<A>(e % VEC);
+                y[e] += u;
+            }
+        }
+        if (x_out) {
+            T *o = reinterpret_cast<T *>(x_out) + row * ld_x_out;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
+                A t[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i];
+                Raw<T, VEC> r;
+                r.set_all(t);
+                r.store_upto(o + c, a.D - c);
+            }
+        }
+        if (h_out) {
+            A sum[1] = {(A)0};
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[0] = fma_(y[e], y[e], sum[0]);
+            row_sums<NT>(sum, s_red, half);
+            const A q = rsqrt_(fma_(sum[0], inv_d, eps));
+            T *o = reinterpret_cast<T *>(h_out) + row * ld_h;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
+                A t[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i] * q * wp[v * VEC + i];
+                Raw<T, VEC> r;
+                r.set_all(t);
+                r.store_upto(o + c, a.D - c);
+            }
+        }
+    }
+}
+
+// How the rows are shared out in backward.  A group is the rows of a worker
+// that share a gate row (all of a worker's rows where the gate is no row
+// gate).  Units are `rows` consecutive rows: several whole groups where a
+// group is shorter (split = 0), a part of one otherwise.
+struct NormUnits {
+    int64_t n, group, rows, per_worker, per_group, total;
+    int32_t split;
+};
+inline NormUnits norm_units(int64_t P, int64_t n, int64_t group, int64_t target) {
+    NormUnits u{};
+    u.n = n;
+    u.group = std::max<int64_t>(1, std::min(group, n));
+    const int64_t want = std::max<int64_t>(4, (P * n + target - 1) / target);
+    if (want >= u.group) {
+        u.rows = want / u.group * u.group;
+        u.per_group = 1;
+        u.per_worker = (n + u.rows - 1) / u.rows;
+        u.split = 0;
+    } else {
+        u.per_group = (u.group + want - 1) / want;
+        u.rows = (u.group + u.per_group - 1) / u.per_group;
+        u.per_group = (u.group + u.rows - 1) / u.rows;
+        u.per_worker = (n + u.group - 1) / u.group * u.per_group;
+        u.split = 1;
+    }
+    u.total = P * u.per_worker;
+    return u;
+}
+
+struct NormGradArgs {
+    const void *dh, *dxo;
+    int64_t ld_dh, ld_dxo;
+    void *dx, *df, *dgate;
+    int64_t ld_dx, ld_df, ld_dgate;
+    void *pre, *post, *share;  // [units][D] sums of a unit: dw_pre, dw_post, dgate (or NULL)
+    NormUnits u;
+};
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void k_norm_grad(NormArgs a, NormGradArgs g) {
+    using A = Acc<T>;
+    constexpr int VEC = kVec<T>, E = NV * VEC;
+    __shared__ A s_red[2 * (NT / 64) * 6];
+    int half = 0;
+    const A res = (A)a.res, branch = (A)a.branch, eps = (A)a.eps, inv_d = (A)1 / (A)a.D;
+    const bool post = a.f && a.w_post, pre = a.w_pre != nullptr;
+    const bool row_gate = a.f && a.gate && a.gate_rows > 0;
+    const bool param_gate = a.f && a.gate && a.gate_rows == 0;
+    // the unit's rows
+    const NormUnits &u = g.u;
+    const int64_t worker = blockIdx.x / u.per_worker, part = blockIdx.x % u.per_worker;
+    int64_t r0, r1;
+    if (u.split) {
+        const int64_t group = part / u.per_group;
+        r0 = group * u.group + part % u.per_group * u.rows;
+        r1 = min(min(r0 + u.rows, (group + 1) * u.group), u.n);
+    } else {
+        r0 = part * u.rows;
+        r1 = min(r0 + u.rows, u.n);
+    }
+    r0 += worker * u.n;
+    r1 += worker * u.n;
+    A wq[E], wp[E], wg[E];  // post-norm weight, pre-norm weight, b times a parameter gate
+    A s_pre[E], s_post[E], s_gate[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int64_t c = ((int64_t)(e / VEC) * NT + threadIdx.x) * VEC + e % VEC;
+        wq[e] = (A)1;
+        wp[e] = (A)0;
+        wg[e] = branch;
+        if (c < a.D) {
+            if (post) wq[e] = (A)a.offset + load_param<A>(a.w_post, a.w_type, c);
+            if (pre) wp[e] = (A)a.offset + load_param<A>(a.w_pre, a.w_type, c);
+            if (param_gate) wg[e] *= load_param<A>(a.gate, a.w_type, c);
+        }
+        s_pre[e] = s_post[e] = s_gate[e] = (A)0;
+    }
+    for (int64_t row = r0; row < r1; ++row) {
+        Raw<T, VEC> rx[NV], rf[NV], rg[NV], rh[NV], ro[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - c;
+#pragma unroll
+            for (int i = 0; i < Raw<T, VEC>::kWords; ++i)
+                rx[v].w[i] = rf[v].w[i] = rg[v].w[i] = rh[v].w[i] = ro[v].w[i] = 0;
+            if (pre) {
+                rx[v].load_upto(reinterpret_cast<const T *>(a.x) + row * a.ld_x + c, left);
+                rh[v].load_upto(reinterpret_cast<const T *>(g.dh) + row * g.ld_dh + c, left);
+            }
+            if (g.dxo)
+                ro[v].load_upto(reinterpret_cast<const T *>(g.dxo) + row * g.ld_dxo + c, left);
+            if (a.f) rf[v].load_upto(reinterpret_cast<const T *>(a.f) + row * a.ld_f + c, left);
+            if (row_gate)
+                rg[v].load_upto(reinterpret_cast<const T *>(a.gate) +
+                                    row / a.gate_rows * a.ld_gate + c,
+                                left);
+        }
+        // sums of x^2, f^2, A x, C dx', C A, C x
+        A s[6] = {(A)0, (A)0, (A)0, (A)0, (A)0, (A)0};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int v = e / VEC, i = e % VEC;
+            const A x = rx[v].template get<A>(i), f = rf[v].template get<A>(i);
+            const A d = ro[v].template get<A>(i);
+            const A ah = rh[v].template get<A>(i) * wp[e];
+            A b = wg[e] * wq[e] * f;
+            if (row_gate) b *= rg[v].template get<A>(i);
+            s[0] = fma_(x, x, s[0]);
+            s[1] = fma_(f, f, s[1]);
+            s[2] = fma_(ah, x, s[2]);
+            s[3] = fma_(b, d, s[3]);
+            s[4] = fma_(b, ah, s[4]);
+            s[5] = fma_(b, x, s[5]);
+        }
+        row_sums<NT>(s, s_red, half);
+        const A q = pre ? rsqrt_(fma_(s[0], inv_d, eps)) : (A)0;
+        const A k = post ? rsqrt_(fma_(s[1], inv_d, eps)) : (A)1;
+        const A c = q * q * q * s[2] * inv_d;
+        const A m = post ? k * k * inv_d * (s[3] + q * s[4] - c * s[5]) : (A)0;
+        const bool group_end = row_gate && !u.split &&
+                               ((row + 1) % a.gate_rows == 0 || row + 1 == r1);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - col;
+            A dx[VEC], df[VEC], dg[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int e = v * VEC + i;
+                const A x = rx[v].template get<A>(i), f = rf[v].template get<A>(i);
+                const A h = rh[v].template get<A>(i);
+                const A d = ro[v].template get<A>(i) + q * (h * wp[e]) - c * x;
+                A gb = wg[e];  // b g
+                if (row_gate) gb *= rg[v].template get<A>(i);
+                const A du = gb * d;
+                dx[i] = res * d;
+                df[i] = k * (du * wq[e] - f * m);
+                s_pre[e] = fma_(h, x * q, s_pre[e]);
+                s_post[e] = fma_(du, f * k, s_post[e]);
+                s_gate[e] = fma_(branch * d, f * k * wq[e], s_gate[e]);
+                dg[i] = s_gate[e];
+                if (group_end) s_gate[e] = (A)0;
+            }
+            Raw<T, VEC> r;
+            if (g.dx) {
+                r.set_all(dx);
+                r.store_upto(reinterpret_cast<T *>(g.dx) + row * g.ld_dx + col, left);
+            }
+            if (g.df) {
+                r.set_all(df);
+                r.store_upto(reinterpret_cast<T *>(g.df) + row * g.ld_df + col, left);
+            }
+            if (g.dgate && group_end) {
+                r.set_all(dg);
+                r.store_upto(reinterpret_cast<T *>(g.dgate) + row / a.gate_rows * g.ld_dgate + col,
+                             left);
+            }
+        }
+    }
+    const int64_t at = (int64_t)blockIdx.x * a.D;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - col;
+        auto put = [&](void *to, const A (&sum)[E]) {
+            if (!to) return;
+            A t[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t[i] = sum[v * VEC + i];
+            Raw<A, VEC> r;
+            r.set_all(t);
+            r.store_upto(reinterpret_cast<A *>(to) + at + col, left);
+        };
+        put(g.pre, s_pre);
+        put(g.post, s_post);
+        put(g.share, s_gate);
+    }
+}
+
+// Sums of consecutive units: result j (of `count`) adds units [j per, (j + 1)
+// per) of up to three arrays of [units][D] sums.  A workgroup takes 64
+// columns of a result; its waves take every 16th unit each, and their sums
+// are added in order.
+struct NormJoin {
+    const void *from[3];
+    void *to[3];
+    int64_t ld[3];        // elements from one result to the next
+    int32_t type[3];
+    int32_t accumulate;
+    int64_t per, count, D;
+};
+constexpr int kNormJoinThreads = 1024;
+
+template <typename A>
+__global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
+    constexpr int NW = kNormJoinThreads / 64, U = 8;
+    __shared__ A s_part[NW][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t cols = (a.D + 63) / 64;
+    const int64_t j = blockIdx.x / cols, c = blockIdx.x % cols * 64 + lane;
+    const int z = blockIdx.y;
+    const A *from = reinterpret_cast<const A *>(z == 0 ? a.from[0] : z == 1 ? a.from[1]
+                                                                           : a.from[2]);
+    void *to = z == 0 ? a.to[0] : z == 1 ? a.to[1] : a.to[2];
+    const int64_t ld = z == 0 ? a.ld[0] : z == 1 ? a.ld[1] : a.ld[2];
+    const int32_t type = z == 0 ? a.type[0] : z == 1 ? a.type[1] : a.type[2];
+    if (!to) return;
+    A sum = (A)0;
+    for (int64_t i = wave; i < a.per; i += NW * U) {
+        A t[U];
+#pragma unroll
+        for (int s = 0; s < U; ++s) {
+            const int64_t at = i + s * NW;
+            t[s] = at < a.per && c < a.D ? from[(j * a.per + at) * a.D + c] : (A)0;
+        }
+#pragma unroll
+        for (int s = 0; s < U; ++s) sum += t[s];
+    }
+    s_part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < a.D) {
+        for (int w = 1; w < NW; ++w) sum += s_part[w][lane];
+        store_param<A>(to, type, j * ld + c, sum, a.accumulate);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+// Calls f with the thread count and vectors per thread that hold a row: the
+// narrowest workgroup whose threads hold up to FULL vectors each, beyond 1,024
+// threads (WIDER) twice as many.
+template <int NT, int NV>
+struct RowShape {
+    static constexpr int nt = NT, nv = NV;
+};
+template <int FULL, bool WIDER, typename F>
+void with_row_shape(int64_t vecs, F &&f) {
+    if (FULL > 1 && vecs <= 64 * (FULL / 2)) f(RowShape<64, (FULL > 1 ? FULL / 2 : 1)>{});
+    else if (vecs <= 64 * FULL) f(RowShape<64, FULL>{});
+    else if (vecs <= 128 * FULL) f(RowShape<128, FULL>{});
+    else if (vecs <= 256 * FULL) f(RowShape<256, FULL>{});
+    else if (vecs <= 512 * FULL) f(RowShape<512, FULL>{});
+    else if (!WIDER || vecs <= 1024 * FULL) f(RowShape<1024, FULL>{});
+    else f(RowShape<1024, (WIDER ? 2 : 1) * FULL>{});
+}
+// Vectors (16 bytes) a thread holds of an operand's row.
+template <typename T>
+constexpr int kForwardVecs = std::is_same_v<T, bf16_t> ? 2 : 4;
+static_assert(1024 * kForwardVecs<bf16_t> * kVec<bf16_t> == ECC_NORM_MAX_DIM &&
+                  1024 * kForwardVecs<float> * kVec<float> == ECC_NORM_MAX_DIM &&
+                  1024 * kForwardVecs<double> * kVec<double> == ECC_NORM_MAX_DIM / 2,
+              "the widest workgroup holds the longest row");
+template <typename T>
+constexpr int kBackwardVecs = std::is_same_v<T, bf16_t> ? 1 : 2;
+
+inline int64_t backward_threads(int32_t type, int64_t D) {
+    const int64_t vec = 16 / type_size(type), full = type == ECC_BF16 ? 1 : 2;
+    const int64_t vecs = (D + vec - 1) / vec;
+    int64_t nt = 64;
+    while (nt < 1024 && vecs > nt * full) nt *= 2;
+    return nt;
+}
+// The device holds 2,048 threads a CU; twice the units it holds at once.
+inline NormUnits units_of(const ecc_norm_t *a) {
+    const int64_t target = kNormCus * 2048 / backward_threads(a->type, a->D);
+    const int64_t group = a->d_f && a->d_gate && a->gate_rows > 0 ? a->gate_rows : a->n;
+    return norm_units(a->P, a->n, group, target);
+}
+
+static ecc_status_t check_norm(const ecc_norm_t *a) {
+    ECC_ARG(a != nullptr, "the description is NULL");
+    ECC_ARG(a->P >= 1 && a->n >= 0 && a->D >= 1, "P and D must be >= 1, n >= 0");
+    ECC_ARG(known_type(a->type) && known_type(a->w_type), "unknown element type");
+    ECC_ARG(a->eps > 0.0, "eps must be positive");
+    ECC_ARG(a->gate_rows >= 0, "gate_rows must be >= 0");
+    const int64_t most = a->type == ECC_F64 ? ECC_NORM_MAX_DIM / 2 : ECC_NORM_MAX_DIM;
+    const int64_t lim = int64_t(1) << 40;
+    if (a->D > most || a->n >= lim || (a->n > 0 && a->P >= lim / a->n) || a->ld_x >= lim ||
+        a->ld_f >= lim || a->ld_gate >= lim) {
+        set_error("D = %lld exceeds %lld, or another size is too large", (long long)a->D,
+                  (long long)most);
+        return ECC_ERR_RANGE;
+    }
+    ECC_ARG(a->w_type != ECC_F64 || a->type == ECC_F64,
+            "fp64 weights go with fp64 rows only");
+    // (the arrays of no rows may be NULL)
+    ECC_ARG(a->n == 0 || a->d_f || (!a->d_gate && !a->d_w_post), "a gate or a post-norm weight without f");
+    ECC_ARG(a->ld_x >= a->D && (!a->d_f || a->ld_f >= a->D), "a leading dimension is below D");
+    const int64_t tb = type_size(a->type), wb = type_size(a->w_type);
+    ECC_ARG(((uintptr_t)a->d_x | (uintptr_t)a->d_f) % tb == 0 &&
+                ((uintptr_t)a->d_w_post | (uintptr_t)a->d_w_pre) % wb == 0,
+            "an array is not aligned to its elements");
+    if (a->d_gate) {
+        ECC_ARG((uintptr_t)a->d_gate % (a->gate_rows ? tb : wb) == 0,
+                "an array is not aligned to its elements");
+        if (a->gate_rows) {
+            ECC_ARG(a->ld_gate >= a->D, "a leading dimension is below D");
+            ECC_ARG(a->P == 1 || a->n % a->gate_rows == 0,
+                    "a gate row would be shared by two workers");
+        }
+    }
+    return ECC_OK;
+}
+
+// An output: NULL, or rows x D elements of `type` that meet none of the
+// inputs but one that it may stand in for (the same address and ld).
+struct Span {
+    const void *p;
+    int64_t bytes;
+};
+static bool meets_input(const ecc_norm_t *a, const Span &o) {
+    const int64_t rows = a->P * a->n, tb = type_size(a->type), wb = type_size(a->w_type);
+    const int64_t grows = a->gate_rows ? (rows + a->gate_rows - 1) / a->gate_rows : 1;
+    return (a->d_gate &&
+            ranges_meet(o.p, o.bytes, a->d_gate,
+                        a->gate_rows ? row_extent(grows, a->ld_gate, a->D) * tb : a->D * wb)) ||
+           (a->d_w_post && ranges_meet(o.p, o.bytes, a->d_w_post, a->D * wb)) ||
+           (a->d_w_pre && ranges_meet(o.p, o.bytes, a->d_w_pre, a->D * wb));
+}
+
+}  // namespace ecc
+
+using namespace ecc;
+
+extern "C" {
+
+ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_out, void *d_h,
+                              int64_t ld_h, void *hip_stream) {
+    clear_error();
+    const ecc_status_t st = check_norm(a);
+    if (st != ECC_OK) return st;
+    ECC_ARG(a->n == 0 || (d_h != nullptr) == (a->d_w_pre != nullptr), "d_h goes with d_w_pre");
+    ECC_ARG(a->n == 0 || d_x_out || d_h, "no output");
+    const int64_t lim = int64_t(1) << 40, tb = type_size(a->type), N = a->P * a->n;
+    ECC_ARG((!d_x_out || ld_x_out >= a->D) && (!d_h || ld_h >= a->D),
+            "a leading dimension is below D");
+    if (ld_x_out >= lim || ld_h >= lim) {
+        set_error("a leading dimension is too large");
+        return ECC_ERR_RANGE;
+    }
+    if (N == 0) return ECC_OK;
+    ECC_ARG(a->d_x, "NULL pointer");
+    ECC_ARG(((uintptr_t)d_x_out | (uintptr_t)d_h) % tb == 0,
+            "an array is not aligned to its elements");
+    const Span x{a->d_x, row_extent(N, a->ld_x, a->D) * tb},
+        f{a->d_f, a->d_f ? row_extent(N, a->ld_f, a->D) * tb : 0},
+        xo{d_x_out, d_x_out ? row_extent(N, ld_x_out, a->D) * tb : 0},
+        h{d_h, d_h ? row_extent(N, ld_h, a->D) * tb : 0};
+    auto clash = [](const Span &p, const Span &q) {
+        return ranges_meet(p.p, p.bytes, q.p, q.bytes);
+    };
+    const bool xo_is_x = d_x_out == a->d_x && ld_x_out == a->ld_x;
+    const bool h_is_f = d_h == a->d_f && ld_h == a->ld_f;
+    const bool h_is_x = d_h == a->d_x && ld_h == a->ld_x;
+    ECC_ARG((!clash(xo, x) || xo_is_x) && !clash(xo, f) && (!clash(h, f) || h_is_f) &&
+                (!clash(h, x) || h_is_x) && !clash(xo, h) && !meets_input(a, xo) &&
+                !meets_input(a, h),
+            "an output overlaps an input or the other output");
+    NormArgs n{N,          a->D,      a->d_x,    a->d_f,       a->d_gate, a->d_w_post,
+               a->d_w_pre, a->ld_x,   a->ld_f,   a->ld_gate,   a->gate_rows, a->w_type,
+               a->w_offset, a->res_scale, a->branch_scale, a->eps};
+    with_type(a->type, [&](auto t) {
+        using T = decltype(t);
+        with_row_shape<kForwardVecs<T>, false>((a->D + kVec<T> - 1) / kVec<T>, [&](auto shape) {
+            constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
+            const int64_t grid = std::min<int64_t>(N, kNormCus * (2048 / NT));
+            hipLaunchKernelGGL((k_norm_forward<T, NT, NV>), dim3((unsigned)grid), dim3(NT), 0,
+                               (hipStream_t)hip_stream, n, d_x_out, ld_x_out, d_h, ld_h);
+        });
+    });
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+int64_t ecc_norm_work_size(const ecc_norm_t *a) {
+    if (check_norm(a) != ECC_OK) return -1;
+    const int64_t acc = a->type == ECC_F64 ? 8 : 4;
+    return std::max<int64_t>(16, (3 * units_of(a).total * a->D * acc + 15) & ~int64_t(15));
+}
+
+ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *d_work,
+                           void *hip_stream) {
+    clear_error();
+    const ecc_status_t st = check_norm(a);
+    if (st != ECC_OK) return st;
+    ECC_ARG(g != nullptr, "the gradients' description is NULL");
+    ECC_ARG(a->n == 0 || (g->d_dh != nullptr) == (a->d_w_pre != nullptr),
+            "d_dh goes with d_w_pre");
+    ECC_ARG(known_type(g->grad_type), "unknown element type");
+    ECC_ARG(g->accumulate == 0 || g->accumulate == 1, "accumulate must be 0 or 1");
+    ECC_ARG(a->n == 0 || g->d_dx || g->d_df || g->d_dgate || g->d_dw_post || g->d_dw_pre,
+            "no output");
+    ECC_ARG(a->n == 0 || (!g->d_df && !g->d_dgate && !g->d_dw_post) || a->d_f,
+            "gradients of f without f");
+    ECC_ARG(a->n == 0 || ((!g->d_dw_post || a->d_w_post) && (!g->d_dw_pre || a->d_w_pre) &&
+                    (!g->d_dgate || a->d_gate)),
+            "a gradient of an operand that is absent");
+    const int64_t lim = int64_t(1) << 40, tb = type_size(a->type), N = a->P * a->n, D = a->D;
+    const int64_t gb = type_size(g->grad_type);
+    const bool row_gate = g->d_dgate && a->gate_rows > 0;
+    ECC_ARG((!g->d_dh || g->ld_dh >= D) && (!g->d_dx_out || g->ld_dx_out >= D) &&
+                (!g->d_dx || g->ld_dx >= D) && (!g->d_df || g->ld_df >= D) &&
+                (!row_gate || g->ld_dgate >= D),
+            "a leading dimension is below D");
+    if (g->ld_dh >= lim || g->ld_dx_out >= lim || g->ld_dx >= lim || g->ld_df >= lim ||
+        g->ld_dgate >= lim || g->worker_stride >= lim) {
+        set_error("a leading dimension or the stride is too large");
+        return ECC_ERR_RANGE;
+    }
+    const bool params = g->d_dw_post || g->d_dw_pre || (g->d_dgate && !row_gate);
+    ECC_ARG(a->P == 1 || !params || g->worker_stride >= D, "workers' gradients overlap");
+    ECC_ARG(N == 0 || d_work, "NULL pointer");
+    ECC_ARG(N == 0 || (a->d_x || !a->d_w_pre), "NULL pointer");
+    ECC_ARG((uintptr_t)d_work % 16 == 0, "d_work must be 16-byte aligned");
+    ECC_ARG(((uintptr_t)g->d_dh | (uintptr_t)g->d_dx_out | (uintptr_t)g->d_dx |
+             (uintptr_t)g->d_df | (row_gate ? (uintptr_t)g->d_dgate : 0)) % tb == 0 &&
+                ((uintptr_t)g->d_dw_post | (uintptr_t)g->d_dw_pre |
+                 (row_gate ? 0 : (uintptr_t)g->d_dgate)) % gb == 0,
+            "an array is not aligned to its elements");
+    // inputs and outputs, and which output may stand in for which input
+    const int64_t gate_n = a->gate_rows ? (N + a->gate_rows - 1) / a->gate_rows : 0;
+    const int64_t param_bytes = ((a->P - 1) * (a->P > 1 ? g->worker_stride : 0) + D) * gb;
+    auto rows = [&](const void *p, int64_t ld) {
+        return Span{p, p ? row_extent(N, ld, D) * tb : 0};
+    };
+    const Span in[4] = {rows(a->d_x, a->ld_x), rows(a->d_f, a->ld_f), rows(g->d_dh, g->ld_dh),
+                        rows(g->d_dx_out, g->ld_dx_out)};
+    const Span out[6] = {
+        rows(g->d_dx, g->ld_dx), rows(g->d_df, g->ld_df),
+        Span{g->d_dgate, !g->d_dgate ? 0
+                         : row_gate  ? row_extent(gate_n, g->ld_dgate, D) * tb
+                                     : param_bytes},
+        Span{g->d_dw_post, g->d_dw_post ? param_bytes : 0},
+        Span{g->d_dw_pre, g->d_dw_pre ? param_bytes : 0},
+        Span{d_work, N ? ecc_norm_work_size(a) : 0}};
+    const int64_t in_ld[4] = {a->ld_x, a->ld_f, g->ld_dh, g->ld_dx_out};
+    const int64_t out_ld[2] = {g->ld_dx, g->ld_df};
+    for (int o = 0; o < 6; ++o) {
+        for (int i = 0; i < 4; ++i) {
+            const bool stands_in = o < 2 && out[o].p == in[i].p && out_ld[o] == in_ld[i] &&
+                                   (o == 0 ? i >= 2 : i == 1 || i == 2);
+            ECC_ARG(stands_in || !ranges_meet(out[o].p, out[o].bytes, in[i].p, in[i].bytes),
+                    "an output overlaps an input");
+        }
+        ECC_ARG(!meets_input(a, out[o]), "an output overlaps an input");
+        // (parameters of several workers lie side by side in one
+        // contribution: of them only the first worker's can be compared)
+        for (int q = 0; q < o; ++q) {
+            const bool both_params = a->P > 1 && o >= 2 && o < 5 && q >= 2 && q < 5 &&
+                                     (o != 2 || !row_gate) && (q != 2 || !row_gate);
+            const int64_t bo = both_params ? D * gb : out[o].bytes;
+            const int64_t bq = both_params ? D * gb : out[q].bytes;
+            ECC_ARG(!ranges_meet(out[o].p, out[o].bytes ? bo : 0, out[q].p,
+                                 out[q].bytes ? bq : 0),
+                    "two outputs, or an output and the work buffer, overlap");
+        }
+    }
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (N == 0 && (!params || g->accumulate)) return ECC_OK;
+    NormArgs n{N,          D,          a->d_x,    a->d_f,       a->d_gate, a->d_w_post,
+               a->d_w_pre, a->ld_x,   a->ld_f,   a->ld_gate,   a->gate_rows, a->w_type,
+               a->w_offset, a->res_scale, a->branch_scale, a->eps};
+    NormGradArgs ga{};
+    ga.dh = g->d_dh;
+    ga.dxo = g->d_dx_out;
+    ga.ld_dh = g->ld_dh;
+    ga.ld_dxo = g->ld_dx_out;
+    ga.dx = g->d_dx;
+    ga.df = g->d_df;
+    ga.ld_dx = g->ld_dx;
+    ga.ld_df = g->ld_df;
+    ga.ld_dgate = g->ld_dgate;
+    ga.u = units_of(a);
+    if (ga.u.total > 0x7fffff) {
+        set_error("P * n is too large for one launch");
+        return ECC_ERR_RANGE;
+    }
+    with_type(a->type, [&](auto t) {
+        using T = decltype(t);
+        using A = Acc<T>;
+        A *work = (A *)d_work;
+        const int64_t sums = ga.u.total * D;
+        ga.pre = g->d_dw_pre ? work : nullptr;
+        ga.post = g->d_dw_post ? work + sums : nullptr;
+        const bool gate_sums = g->d_dgate && (!row_gate || ga.u.split);
+        ga.share = gate_sums ? work + 2 * sums : nullptr;
+        ga.dgate = row_gate && !ga.u.split ? g->d_dgate : nullptr;
+        if (N > 0)
+            with_row_shape<kBackwardVecs<T>, true>((D + kVec<T> - 1) / kVec<T>, [&](auto shape) {
+                constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
+                hipLaunchKernelGGL((k_norm_grad<T, NT, NV>), dim3((unsigned)ga.u.total), dim3(NT),
+                                   0, s, n, ga);
+            });
+        const int64_t cols = (D + 63) / 64;
+        if (params) {
+            NormJoin j{};
+            j.from[0] = ga.pre;
+            j.from[1] = ga.post;
+            j.from[2] = ga.share;
+            j.to[0] = g->d_dw_pre;
+            j.to[1] = g->d_dw_post;
+            j.to[2] = row_gate ? nullptr : g->d_dgate;
+            for (int z = 0; z < 3; ++z) {
+                j.ld[z] = g->worker_stride;
+                j.type[z] = g->grad_type;
+            }
+            j.accumulate = g->accumulate;
+            j.per = ga.u.per_worker;
+            j.count = a->P;
+            j.D = D;
+            hipLaunchKernelGGL(k_norm_join<A>, dim3((unsigned)(a->P * cols), 3),
+                               dim3(kNormJoinThreads), 0, s, j);
+        }
+        if (row_gate && ga.u.split && N > 0) {
+            NormJoin j{};
+            j.from[0] = ga.share;
+            j.to[0] = g->d_dgate;
+            j.ld[0] = g->ld_dgate;
+            j.type[0] = a->type;
+            j.per = ga.u.per_group;
+            j.count = gate_n;
+            j.D = D;
+            hipLaunchKernelGGL(k_norm_join<A>, dim3((unsigned)(gate_n * cols), 1),
+                               dim3(kNormJoinThreads), 0, s, j);
+        }
+    });
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+}  // extern "C"

@@ -159,3 +159,148 @@ def embed_grad(index, dy, scale=1.0, grad=None, dtype=torch.float32, accumulate=
                      grad.stride(1) if V > 1 else D, grad.stride(0) if P > 1 else V * D,
                      1 if accumulate else 0, work, _stream())
     return grad
+
+
+# ----------------------------------------------------------------------------
+# norms, gate and residual around a block
+# ----------------------------------------------------------------------------
+
+def _vector(t, D, dtype, what):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != D or t.dtype != dtype:
+        raise ValueError("%s must be %d elements of %s, not %s of %s" %
+                         (what, D, dtype, tuple(t.shape), t.dtype))
+    _contiguous(t, what)
+    return t.data_ptr()
+
+
+def _norm(x, f, w_post, w_pre, gate, gate_rows, res_scale, branch_scale, eps, offset, P):
+    """The ecc_norm_t of tensors; rows and width."""
+    D = x.shape[-1] if x.dim() else 0
+    N, ld_x = _rows(x, "x")
+    t = _type(x, "x")
+    ld_f = 0
+    if f is not None:
+        rows, ld_f = _rows(f, "f", D)
+        if rows != N or f.dtype != x.dtype:
+            raise ValueError("f must be like x, not %s of shape %s" % (f.dtype, tuple(f.shape)))
+    if P < 1 or N % P:
+        raise ValueError("%d rows cannot be shared equally by %d workers" % (N, P))
+    weights = [w for w in (w_post, w_pre, gate if gate is not None and gate_rows == 0 else None)
+               if w is not None]
+    w_dtype = weights[0].dtype if weights else x.dtype
+    if gate_rows < 0:
+        raise ValueError("gate_rows must be >= 0")
+    ld_gate, d_gate = 0, None
+    if gate is None:
+        gate_rows = 0
+    elif gate_rows == 0:
+        d_gate = _vector(gate, D, w_dtype, "gate")
+    else:
+        rows, ld_gate = _rows(gate, "gate", D)
+        if rows != -(-N // gate_rows) or gate.dtype != x.dtype:
+            raise ValueError("gate must have %d rows of %s, not %s of %s" %
+                             (-(-N // gate_rows), x.dtype, tuple(gate.shape), gate.dtype))
+        d_gate = gate.data_ptr()
+    a = E.ecc_norm_t(N // P, D, P, t, _type(w_dtype, "the weights"), x.data_ptr(), ld_x,
+                     None if f is None else f.data_ptr(), ld_f, d_gate, ld_gate, gate_rows,
+                     _vector(w_post, D, w_dtype, "w_post"), _vector(w_pre, D, w_dtype, "w_pre"),
+                     offset, res_scale, branch_scale, eps)
+    return a, N, D, w_dtype
+
+
+def norm_forward(x, f=None, *, w_post=None, w_pre=None, gate=None, gate_rows=1, res_scale=1.0,
+                 branch_scale=1.0, eps=1e-6, offset=0.0, x_out=None, h=None):
+    """(x', h):  x' = res_scale x + branch_scale gate rms(f) (offset + w_post),
+    h = rms(x') (offset + w_pre).
+
+    Without w_post the branch is f itself, without f there is no branch and x'
+    is None unless x_out is given or res_scale differs from 1; without w_pre h
+    is None.  gate: rows like x's, each shared by gate_rows rows, or with
+    gate_rows = 0 a parameter of x.shape[-1] elements.  x_out may be x, and h
+    may be f."""
+    a, N, D, _ = _norm(x, f, w_post, w_pre, gate, gate_rows, res_scale, branch_scale, eps, offset,
+                       1)
+    ld_xo = ld_h = 0
+    if x_out is not None or f is not None or res_scale != 1.0 or w_pre is None:
+        x_out = _out(x_out, x.shape, x.dtype, x.device, "x_out")
+        _, ld_xo = _rows(x_out, "x_out")
+    if w_pre is not None:
+        h = _out(h, x.shape, x.dtype, x.device, "h")
+        _, ld_h = _rows(h, "h")
+    elif h is not None:
+        raise ValueError("h needs w_pre")
+    E.ecc_norm_forward(a, x_out, ld_xo, h, ld_h, _stream())
+    return x_out, h
+
+
+def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=None, gate_rows=1,
+              res_scale=1.0, branch_scale=1.0, eps=1e-6, offset=0.0, P=1, dtype=None, dx=None,
+              df=None, dgate=None, dw_post=None, dw_pre=None, accumulate=False, work=None):
+    """The gradients at x = x' of norm_forward, given those of h (dh) and of x'
+    (dx_out, None for zero): a dict of dx, df, dgate, dw_post and dw_pre (None
+    where the operand is absent).
+
+    Parameters' gradients are per worker, (P, D) of dtype (the weights' type by
+    default); given ones may be views of contributions whose rows lie one
+    common stride apart, and accumulate adds to them.  dx may be dx_out or dh,
+    df may be f or dh."""
+    a, N, D, w_dtype = _norm(x, f, w_post, w_pre, gate, gate_rows, res_scale, branch_scale, eps,
+                             offset, P)
+    given = [t for t in (dw_post, dw_pre, dgate if gate is not None and gate_rows == 0 else None)
+             if t is not None]
+    dtype = given[0].dtype if given else dtype or w_dtype
+    stride = given[0].stride(0) if given and P > 1 else D
+    g = E.ecc_norm_grad_t(grad_type=_type(dtype, "the gradients"),
+                          accumulate=1 if accumulate else 0, worker_stride=stride)
+
+    def rows_in(t, what):
+        if t is None:
+            return None, 0
+        rows, ld = _rows(t, what, D)
+        if rows != N or t.dtype != x.dtype:
+            raise ValueError("%s must be like x, not %s of shape %s" %
+                             (what, t.dtype, tuple(t.shape)))
+        return t.data_ptr(), ld
+
+    def rows_out(t, like, what):
+        t = _out(t, like.shape, like.dtype, like.device, what)
+        _, ld = _rows(t, what)
+        return t, t.data_ptr(), ld
+
+    def param(t, what):
+        if t is None:
+            if accumulate:
+                raise ValueError("accumulate needs %s" % what)
+            t = torch.empty((P, stride), dtype=dtype, device=x.device)[:, :D]
+        elif tuple(t.shape) != (P, D) or t.dtype != dtype or (D > 1 and t.stride(1) != 1) or \
+                (P > 1 and t.stride(0) != stride):
+            raise ValueError("%s must be %s of shape %s, one stride for all" %
+                             (what, dtype, (P, D)))
+        _on_gpu(t, what)
+        return t
+
+    g.d_dh, g.ld_dh = rows_in(dh, "dh")
+    g.d_dx_out, g.ld_dx_out = rows_in(dx_out, "dx_out")
+    dx, g.d_dx, g.ld_dx = rows_out(dx, x, "dx")
+    if f is not None:
+        df, g.d_df, g.ld_df = rows_out(df, f, "df")
+    if gate is not None:
+        if gate_rows:
+            dgate, g.d_dgate, g.ld_dgate = rows_out(dgate, gate, "dgate")
+        else:
+            dgate = param(dgate, "dgate")
+            g.d_dgate = dgate.data_ptr()
+    if w_post is not None:
+        dw_post = param(dw_post, "dw_post")
+        g.d_dw_post = dw_post.data_ptr()
+    if w_pre is not None:
+        dw_pre = param(dw_pre, "dw_pre")
+        g.d_dw_pre = dw_pre.data_ptr()
+    if work is None:
+        work = _work(E.ecc_norm_work_size(a), x.device)
+    elif work.numel() * work.element_size() < E.ecc_norm_work_size(a):
+        raise ValueError("the work buffer is too small")
+    E.ecc_norm_grad(a, g, work, _stream())
+    return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
