@@ -770,6 +770,47 @@ int64_t ecc_norm_work_size(const ecc_norm_t *a);
 ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *d_work,
                            void *hip_stream);
 
+/* Distillation from a teacher's top logits, loss and gradient, for N rows
+ * (positions) of V student logits z and K teacher logits s with their
+ * entries' numbers i_k:
+ *   p = softmax over k of s_k / tau, over the entries with 0 <= i_k < V
+ *   Q = softmax(z / tau),  q = softmax(z)
+ *   loss[r]  = w_r (kd_weight * tau^2 * sum_k p_k (log p_k - log Q[i_k])
+ *                   + ce_weight * (-log q[y_r]))
+ *   dz[r, j] = w_r (kd_weight * tau * (Q_j - sum of p_k with i_k = j)
+ *                   + ce_weight * (q_j - [j = y_r]))
+ * A row without entries (or whose entries all have a logit of -infinity)
+ * has no first term, one whose label y_r lies outside [0, V), or all with
+ * d_labels NULL, no second.  A row of weight 0 is not read: its loss and
+ * gradient are 0 (d_weight NULL: all 1).  An entry named twice counts with
+ * the sum of its p_k.  Logits of -infinity have probability 0.
+ *   d_z      N x V of `type`; d_dz the same, may be d_z (with the same
+ *            leading dimension) or NULL (loss only).
+ *   d_top    N x K of top_type; d_idx N x K int32, contiguous both, K in [0,
+ *            ECC_DISTILL_MAX_TOP]; a teacher's logits are not NaN or +infinity.
+ *   d_labels int32 [N] or NULL; d_weight fp32 [N] or NULL.
+ *   d_loss   [N] of fp32, fp64 when type is ECC_F64.
+ * A weight of 0 leaves its term out.  V in [1, 2^31 - 1), N in [0, 2^31 -
+ * 1), tau > 0.  d_work: ecc_distill_work_size(a) bytes (-1 for a
+ * description that the call refuses). */
+#define ECC_DISTILL_MAX_TOP 1024
+typedef struct {
+    int64_t N, V;
+    int32_t K;
+    int32_t type, top_type;
+    int32_t pad;
+    const void *d_z;
+    int64_t ld_z;
+    const void *d_top;
+    const int32_t *d_idx;
+    const int32_t *d_labels;
+    const float *d_weight;
+    double tau, kd_weight, ce_weight;
+} ecc_distill_t;
+int64_t ecc_distill_work_size(const ecc_distill_t *a);
+ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64_t ld_dz,
+                         void *d_work, void *hip_stream);
+
 /* ---------------------------------------------------------------------------
  * Plain streaming copy d_dst[i] = d_src[i], 0 <= i < n, enqueued on
  * hip_stream.  Both buffers 8-byte aligned and not overlapping

@@ -32,6 +32,7 @@ ECC_MAX_DIAGONALS = 8
 ECC_SCRATCH_DOUBLES = 1 << 20
 ECC_GATHER_CHUNK = 2048
 ECC_NORM_MAX_DIM = 16384
+ECC_DISTILL_MAX_TOP = 1024
 ECC_F64, ECC_F32, ECC_BF16, ECC_I32, ECC_I64 = 0, 1, 2, 3, 4
 
 STATUS_NAMES = {0: "ECC_OK", 1: "ECC_ERR_ARG", 2: "ECC_ERR_OVERLAP", 3: "ECC_ERR_RANGE",
@@ -75,6 +76,15 @@ class ecc_norm_grad_t(ctypes.Structure):
                 ("d_dw_post", ctypes.c_void_p), ("d_dw_pre", ctypes.c_void_p),
                 ("grad_type", ctypes.c_int32), ("accumulate", ctypes.c_int32),
                 ("worker_stride", ctypes.c_int64)]
+
+
+class ecc_distill_t(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int64), ("K", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("top_type", ctypes.c_int32), ("pad", ctypes.c_int32),
+                ("d_z", ctypes.c_void_p), ("ld_z", ctypes.c_int64), ("d_top", ctypes.c_void_p),
+                ("d_idx", ctypes.c_void_p), ("d_labels", ctypes.c_void_p),
+                ("d_weight", ctypes.c_void_p), ("tau", ctypes.c_double),
+                ("kd_weight", ctypes.c_double), ("ce_weight", ctypes.c_double)]
 
 
 _lib = None
@@ -141,6 +151,8 @@ _SIGS = [
     ("ecc_norm_work_size", _I64, [ctypes.POINTER(ecc_norm_t)]),
     ("ecc_norm_grad", ctypes.c_int, [ctypes.POINTER(ecc_norm_t),
                                      ctypes.POINTER(ecc_norm_grad_t), _VP, _VP]),
+    ("ecc_distill_work_size", _I64, [ctypes.POINTER(ecc_distill_t)]),
+    ("ecc_distill", ctypes.c_int, [ctypes.POINTER(ecc_distill_t), _VP, _VP, _I64, _VP, _VP]),
     ("ecc_solve", ctypes.c_int, [_VP, _VP, _VP, _D, _D, _VP, _VP, _VP, _VP, _I32, _D, _VP, _VP,
                                  _VP, _VP]),
 ]
@@ -495,3 +507,11 @@ def ecc_norm_work_size(a: ecc_norm_t) -> int:
 
 def ecc_norm_grad(a: ecc_norm_t, g: ecc_norm_grad_t, d_work, hip_stream=None):
     _check(lib().ecc_norm_grad(a, g, _ptr(d_work), hip_stream))
+
+
+def ecc_distill_work_size(a: ecc_distill_t) -> int:
+    return int(lib().ecc_distill_work_size(a))
+
+
+def ecc_distill(a: ecc_distill_t, d_loss, d_dz, ld_dz, d_work, hip_stream=None):
+    _check(lib().ecc_distill(a, _ptr(d_loss), _ptr(d_dz), ld_dz, _ptr(d_work), hip_stream))

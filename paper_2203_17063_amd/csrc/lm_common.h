@@ -75,6 +75,14 @@ __device__ __forceinline__ void store_elem(T *p, A v) {
     else *p = (T)v;
 }
 
+// Element i of an array whose type is known at run time only.
+template <typename A>
+__device__ __forceinline__ A load_typed(const void *p, int32_t type, int64_t i) {
+    if (type == ECC_F64) return (A) reinterpret_cast<const double *>(p)[i];
+    if (type == ECC_F32) return (A) reinterpret_cast<const float *>(p)[i];
+    return load_elem<A>(reinterpret_cast<const bf16_t *>(p) + i);
+}
+
 // W 32-bit words as memory holds them, at the alignment of one element
 // (gfx950 takes 4-, 8- and 16-byte global accesses at any alignment).
 template <int W, int ALIGN>

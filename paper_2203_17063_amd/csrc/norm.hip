@@ -39,13 +39,6 @@ struct NormArgs {
     double offset, res, branch, eps;
 };
 
-// A parameter's element as the accumulator's type; 1 where there is none.
-template <typename A>
-__device__ __forceinline__ A load_param(const void *p, int32_t type, int64_t i) {
-    if (type == ECC_F64) return (A) reinterpret_cast<const double *>(p)[i];
-    if (type == ECC_F32) return (A) reinterpret_cast<const float *>(p)[i];
-    return load_elem<A>(reinterpret_cast<const bf16_t *>(p) + i);
-}
 template <typename A>
 __device__ __forceinline__ void store_param(void *p, int32_t type, int64_t i, A v, int accumulate) {
     if (type == ECC_F64) {
@@ -107,9 +100,9 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
             const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC + i;
             A q = branch, p = (A)0;
             if (c < a.D) {
-                if (a.w_post) q *= (A)a.offset + load_param<A>(a.w_post, a.w_type, c);
-                if (a.gate && a.gate_rows == 0) q *= load_param<A>(a.gate, a.w_type, c);
-                if (a.w_pre) p = (A)a.offset + load_param<A>(a.w_pre, a.w_type, c);
+                if (a.w_post) q *= (A)a.offset + load_typed<A>(a.w_post, a.w_type, c);
+                if (a.gate && a.gate_rows == 0) q *= load_typed<A>(a.gate, a.w_type, c);
+                if (a.w_pre) p = (A)a.offset + load_typed<A>(a.w_pre, a.w_type, c);
             }
             wq[v * VEC + i] = q;
             wp[v * VEC + i] = p;
@@ -254,9 +247,9 @@ __global__ __launch_bounds__(NT) void k_norm_grad(NormArgs a, NormGradArgs g) {
         wp[e] = (A)0;
         wg[e] = branch;
         if (c < a.D) {
-            if (post) wq[e] = (A)a.offset + load_param<A>(a.w_post, a.w_type, c);
-            if (pre) wp[e] = (A)a.offset + load_param<A>(a.w_pre, a.w_type, c);
-            if (param_gate) wg[e] *= load_param<A>(a.gate, a.w_type, c);
+            if (post) wq[e] = (A)a.offset + load_typed<A>(a.w_post, a.w_type, c);
+            if (pre) wp[e] = (A)a.offset + load_typed<A>(a.w_pre, a.w_type, c);
+            if (param_gate) wg[e] *= load_typed<A>(a.gate, a.w_type, c);
         }
         s_pre[e] = s_post[e] = s_gate[e] = (A)0;
     }

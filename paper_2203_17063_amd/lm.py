@@ -304,3 +304,51 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         raise ValueError("the work buffer is too small")
     E.ecc_norm_grad(a, g, work, _stream())
     return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
+
+
+# ----------------------------------------------------------------------------
+# distillation
+# ----------------------------------------------------------------------------
+
+def distill(z, top, idx, tau=1.0, kd_weight=1.0, ce_weight=0.0, labels=None, weight=None,
+            loss=None, grad=True, work=None):
+    """(loss, gradient) of student logits z (..., V) against a teacher's top
+    logits top (..., K) of the entries idx (..., K, int32; outside [0, V):
+    absent): per position
+    weight (kd_weight tau^2 KL + ce_weight * cross entropy of labels), and its
+    gradient in z.  labels: int32, outside [0, V) for none; weight: fp32.
+    grad: True (a new tensor), a tensor to write (z itself for in place), or
+    None (loss only)."""
+    t = _type(z, "z")
+    N, ld_z = _rows(z, "z")
+    V, shape = z.shape[-1], z.shape[:-1]
+    if top.dim() < 1 or top.shape != idx.shape or top.shape[:-1] != shape:
+        raise ValueError("top and idx must have K entries for every row of z, not shapes %s and "
+                         "%s" % (tuple(top.shape), tuple(idx.shape)))
+    if idx.dtype != torch.int32:
+        raise TypeError("idx must be int32, not %s" % idx.dtype)
+    for v, dtype, what in ((labels, torch.int32, "labels"), (weight, torch.float32, "weight")):
+        if v is not None and (v.shape != shape or v.dtype != dtype):
+            raise ValueError("%s must be %s of shape %s, not %s of %s" %
+                             (what, dtype, tuple(shape), tuple(v.shape), v.dtype))
+    a = E.ecc_distill_t(N, V, top.shape[-1], t, _type(top, "top"), 0, z.data_ptr(), ld_z,
+                        _contiguous(top, "top").data_ptr(), _contiguous(idx, "idx").data_ptr(),
+                        None if labels is None else _contiguous(labels, "labels").data_ptr(),
+                        None if weight is None else _contiguous(weight, "weight").data_ptr(),
+                        tau, kd_weight, ce_weight)
+    loss = _out(loss, shape, torch.float64 if t == E.ECC_F64 else torch.float32, z.device, "loss")
+    _contiguous(loss, "loss")
+    ld_dz = 0
+    if grad is True:
+        grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    if grad is not None:
+        _out(grad, z.shape, z.dtype, z.device, "grad")
+        _, ld_dz = _rows(grad, "grad")
+    size = E.ecc_distill_work_size(a)
+    if work is None:
+        # (a refused description has no size: the call says what is wrong)
+        work = _work(max(size, 16), z.device)
+    elif work.numel() * work.element_size() < size:
+        raise ValueError("the work buffer is too small")
+    E.ecc_distill(a, loss, grad, ld_dz, work, _stream())
+    return loss, grad
