@@ -11,14 +11,18 @@
 // so the result, would change) will do.  Instead the tokens are sorted by
 // (worker, row), stably, and the sorted order is cut into tiles of equal
 // length:
-//  - a tile adds its tokens' rows run by run of equal tokens; a run that lies
-//    within the tile is finished and written at once, one that was begun or
-//    is continued in another tile leaves its sum in the work buffer (at most
-//    two a tile);
-//  - a second launch adds the pieces of every run that crosses tiles, in tile
-//    order;
-//  - rows of G without tokens are zeroed by further workgroups of the first
-//    launch, which find them by bisection of the sorted tokens.
+//  - a run of equal tokens no longer than a tile is added by the tile that it
+//    begins in, to its end, and written at once; a longer one is added in
+//    every tile that it touches, and each leaves its sum in the work buffer
+//    (at most two a tile);
+//  - a second launch adds the pieces of every longer run, in tile order (few:
+//    a run of a text's 131,072 tokens is longer than 64 only for its
+//    commonest hundred or two);
+//  - rows of G without tokens, by flags that the sort has left, are zeroed by
+//    further workgroups of the first launch, behind those that add (128,000
+//    rows of 4,096: 0.62 ms against 0.68 ms dealt out among them), past the
+//    caches where G exceeds the last of them (0.58 ms against 0.60 ms; 32,003
+//    rows of 2,048, which it holds: 50 us through them, 60 us past them).
 // Every element of G is written once, by one thread, in a fixed order.
 //
 // The sort is by counting, digit by digit from the lowest: up to
@@ -34,9 +38,13 @@ namespace ecc {
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int64_t kSmallSort = 16 * kSortThreads;  // tokens of a worker that one workgroup sorts
-constexpr int kSmallBins = 256;
-constexpr int kTileThreads = 256;                  // the launches of a longer sort
-constexpr int kTileItems = 8;
+constexpr int kPosBits = 14;                       // bits of such a token's position
+static_assert(kSmallSort == int64_t(1) << kPosBits, "positions of a sort in LDS");
+constexpr int kSmallBits = 5;
+constexpr int kSmallBins = 1 << kSmallBits;
+constexpr int kTileThreads = 1024;                 // the launches of a longer sort
+constexpr int kTileItems = 2;
+constexpr int kScanThreads = 256;
 constexpr int kSortTile = kTileThreads * kTileItems;
 constexpr int kBigBits = 9;
 constexpr int kBigBins = 1 << kBigBits;
@@ -90,75 +98,129 @@ __device__ __forceinline__ uint32_t bins_scan(uint32_t v, uint32_t *sums) {
     if (lane == 63) sums[wave] = run;
     __syncthreads();
     uint32_t base = 0;
-    for (int w = 0; w < wave; ++w) base += sums[w];
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) base += w < wave ? sums[w] : 0u;
     return base + run - v;
 }
 
-// A worker's n <= 1024 * ITEMS tokens sorted in LDS.
-template <int ITEMS>
+// A worker's n <= 1024 * ITEMS tokens sorted in LDS, ITEMS consecutive ones per
+// thread, by digits of 5 bits: every thread counts its digits in counters
+// of its own, whose running sums in the order (digit, thread) are the places
+// of its tokens.  The one CU's LDS bounds it: rows and positions travel in one
+// word where that holds them (PACK: tables below 2^18 rows).
+template <int ITEMS, bool PACK>
 __global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t V, int64_t row0,
                                                              const void *ids, int id64,
-                                                             int passes, int rb,
+                                                             int passes,
                                                              uint32_t *__restrict__ keys_out,
-                                                             int32_t *__restrict__ order_out) {
-    __shared__ uint32_t s_hist[kSortWaves][kSmallBins];
-    __shared__ uint32_t s_key[kSortThreads * ITEMS];
-    __shared__ uint16_t s_pos[kSortThreads * ITEMS];
+                                                             int32_t *__restrict__ order_out,
+                                                             uint8_t *touched) {
+    // the counters, and in turn the tokens on their way to their places
+    constexpr int kTokens = kSortThreads * ITEMS;
+    // (four words more after every thread's share of the counters, one after
+    // that of the tokens, against bank conflicts)
+    constexpr int kCountBytes = kSmallBins * kSortThreads * 2 + kSortThreads * 16;
+    constexpr int kTokenBytes = kTokens * 6 + kSortThreads * 8;
+    __shared__ uint4 s_mem[(kCountBytes > kTokenBytes ? kCountBytes : kTokenBytes) / 16];
     __shared__ uint32_t s_sums[kSortWaves + 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint16_t *s_count = reinterpret_cast<uint16_t *>(s_mem);
+    uint32_t *s_key = reinterpret_cast<uint32_t *>(s_mem);
+    uint16_t *s_pos = reinterpret_cast<uint16_t *>(s_key + kTokens + kSortThreads);
+    auto key_at = [](uint32_t i) { return i + i / ITEMS; };
+    auto pos_at = [](uint32_t i) { return i + i / ITEMS * 2; };
+    const int tid = threadIdx.x;
     const int64_t first = (int64_t)blockIdx.x * n;
-    const uint32_t mask = (1u << rb) - 1u;
-    const int bins = 1 << rb;
-    uint32_t key[ITEMS], pos[ITEMS], place[ITEMS];
+    constexpr int rb = kSmallBits, bins = kSmallBins;
+    constexpr uint32_t mask = bins - 1;
+    auto count_at = [&](uint32_t digit) {
+        const uint32_t i = digit * kSortThreads + tid;
+        return s_count + i + 8 * (i >> rb);
+    };
+    // (cleared by stores that the first of the barriers below waits for)
+    uint8_t *const flags = touched + blockIdx.x * V;
+    const int64_t whole = min((int64_t)(-(uintptr_t)flags & 15), V);  // before 16-byte accesses
+    const int64_t quads16 = (V - whole) / 16, behind = whole + 16 * quads16;
+    if (tid < whole) flags[tid] = 0;
+    for (int64_t i = tid; i < quads16; i += kSortThreads)
+        reinterpret_cast<uint4 *>(flags + whole)[i] = make_uint4(0, 0, 0, 0);
+    if (tid < V - behind) flags[behind + tid] = 0;
+    constexpr int LOW = PACK ? kPosBits : 0;
+    uint32_t key[ITEMS], place[ITEMS];
+    uint16_t pos[PACK ? 1 : ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int at = wave * 64 * ITEMS + i * 64 + lane;
-        pos[i] = (uint32_t)at;
+        const int at = tid * ITEMS + i;
         // past the end: the highest value of the digits sorted, which stays
         // behind the tokens that were ahead of it
         key[i] = at < n ? local_row(load_id(ids, id64, first + at), row0, V) : ~0u;
+        if constexpr (PACK) key[i] = key[i] << kPosBits | (uint32_t)at;
+        else pos[i] = (uint16_t)at;
     }
     for (int pass = 0; pass < passes; ++pass) {
-        const int shift = pass * rb;
-        for (int i = tid; i < kSortWaves * kSmallBins; i += kSortThreads)
-            (&s_hist[0][0])[i] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            place[i] = count_digit((key[i] >> shift) & mask, rb, s_hist[wave], lane);
-        __syncthreads();
-        uint32_t total = 0;
-        if (tid < bins)
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = s_hist[w][tid];
-                s_hist[w][tid] = total;
-                total += c;
-            }
-        const uint32_t base = bins_scan<kSortThreads>(total, s_sums);
-        if (tid < bins)
-            for (int w = 0; w < kSortWaves; ++w) s_hist[w][tid] += base;
+        const int shift = LOW + pass * rb;
+        for (int i = tid; i < (bins + 8) * kSortThreads / 8; i += kSortThreads)
+            s_mem[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const uint32_t to = place[i] + s_hist[wave][(key[i] >> shift) & mask];
-            s_key[to] = key[i];
-            s_pos[to] = (uint16_t)pos[i];
+            uint16_t *c = count_at((key[i] >> shift) & mask);
+            place[i] = *c;
+            *c = (uint16_t)(place[i] + 1);
+        }
+        __syncthreads();
+        // this thread's `bins` consecutive counters to running sums (a total
+        // of at most 16,384)
+        uint4 *quads = s_mem + tid * (bins / 8 + 1);
+        auto pair = [](uint32_t c) { return (c & 0xffffu) + (c >> 16); };
+        uint32_t total = 0;
+#pragma unroll
+        for (int i = 0; i < bins / 8; ++i) {
+            const uint4 c = quads[i];
+            total += pair(c.x) + pair(c.y) + pair(c.z) + pair(c.w);
+        }
+        uint32_t run = bins_scan<kSortThreads>(total, s_sums);
+        auto sums = [&](uint32_t c) {
+            const uint32_t low = c & 0xffffu, both = run | (run + low) << 16;
+            run += low + (c >> 16);
+            return both;
+        };
+#pragma unroll
+        for (int i = 0; i < bins / 8; ++i) {
+            uint4 c = quads[i];
+            c.x = sums(c.x);
+            c.y = sums(c.y);
+            c.z = sums(c.z);
+            c.w = sums(c.w);
+            quads[i] = c;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            place[i] += *count_at((key[i] >> shift) & mask);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            s_key[key_at(place[i])] = key[i];
+            if constexpr (!PACK) s_pos[pos_at(place[i])] = pos[i];
         }
         __syncthreads();
         if (pass + 1 < passes) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
-                const int at = wave * 64 * ITEMS + i * 64 + lane;
-                key[i] = s_key[at];
-                pos[i] = s_pos[at];
+                key[i] = s_key[key_at(tid * ITEMS + i)];
+                if constexpr (!PACK) pos[i] = s_pos[pos_at(tid * ITEMS + i)];
             }
+            __syncthreads();
         }
     }
     const uint32_t key0 = blockIdx.x * (uint32_t)(V + 1);
     for (int i = tid; i < n; i += kSortThreads) {
-        const int32_t t = (int32_t)(first + s_pos[i]);
-        keys_out[first + i] = key0 + s_key[i];
-        order_out[first + i] = s_key[i] < (uint32_t)V ? t : ~t;
+        const uint32_t row = s_key[key_at(i)] >> LOW;
+        const int32_t t = (int32_t)(first + (PACK ? s_key[key_at(i)] & ((1u << kPosBits) - 1)
+                                                  : s_pos[pos_at(i)]));
+        keys_out[first + i] = key0 + row;
+        order_out[first + i] = row < (uint32_t)V ? t : ~t;
+        if (row < (uint32_t)V) flags[row] = 1;
     }
 }
 
@@ -178,9 +240,15 @@ __device__ __forceinline__ uint32_t sort_key(const SortIn &in, int64_t t) {
 }
 
 // counts[d][tile]: elements of digit d in each tile.
+// The first pass also clears the `rows` flags of rows with tokens.
 __global__ __launch_bounds__(kTileThreads) void k_sort_count(SortIn in, int shift, int rb,
-                                                             uint32_t *__restrict__ counts) {
+                                                             uint32_t *__restrict__ counts,
+                                                             uint8_t *touched, int64_t rows) {
     __shared__ uint32_t s_hist[kBigBins];
+    if (touched)
+        for (int64_t i = (int64_t)blockIdx.x * kTileThreads + threadIdx.x; i < rows;
+             i += (int64_t)gridDim.x * kTileThreads)
+            touched[i] = 0;
     const uint32_t mask = (1u << rb) - 1u;
     for (int i = threadIdx.x; i < kBigBins; i += kTileThreads) s_hist[i] = 0;
     __syncthreads();
@@ -196,19 +264,19 @@ __global__ __launch_bounds__(kTileThreads) void k_sort_count(SortIn in, int shif
 }
 
 // Running sums of digit d's counts over the tiles (workgroup d); totals[d].
-__global__ __launch_bounds__(kTileThreads) void k_sort_scan(int64_t tiles,
+__global__ __launch_bounds__(kScanThreads) void k_sort_scan(int64_t tiles,
                                                             uint32_t *__restrict__ counts,
                                                             uint32_t *__restrict__ totals) {
-    __shared__ uint32_t s_sums[kTileThreads / 64 + 1];
+    __shared__ uint32_t s_sums[kScanThreads / 64 + 1];
     __shared__ uint32_t s_total;
     uint32_t *row = counts + (int64_t)blockIdx.x * tiles;
     uint32_t run = 0;
-    for (int64_t at = 0; at < tiles; at += kTileThreads) {
+    for (int64_t at = 0; at < tiles; at += kScanThreads) {
         const int64_t i = at + threadIdx.x;
         const uint32_t v = i < tiles ? row[i] : 0u;
-        const uint32_t before = bins_scan<kTileThreads>(v, s_sums);
+        const uint32_t before = bins_scan<kScanThreads>(v, s_sums);
         if (i < tiles) row[i] = run + before;
-        if (threadIdx.x == kTileThreads - 1) s_total = before + v;
+        if (threadIdx.x == kScanThreads - 1) s_total = before + v;
         __syncthreads();
         run += s_total;
     }
@@ -220,7 +288,7 @@ __global__ __launch_bounds__(kTileThreads) void k_sort_move(SortIn in, int shift
                                                             const uint32_t *__restrict__ totals,
                                                             uint32_t *__restrict__ keys_out,
                                                             int32_t *__restrict__ order_out,
-                                                            int last) {
+                                                            uint8_t *touched) {
     constexpr int kWaves = kTileThreads / 64;
     __shared__ uint32_t s_hist[kWaves][kBigBins];
     __shared__ uint32_t s_base[kBigBins];
@@ -271,7 +339,13 @@ __global__ __launch_bounds__(kTileThreads) void k_sort_move(SortIn in, int shift
         if (first + i * 64 < in.N) {
             const uint32_t to = place[i] + s_hist[wave][(key[i] >> shift) & mask];
             keys_out[to] = key[i];
-            const bool held = !last || key[i] % (uint32_t)(in.V + 1) < (uint32_t)in.V;
+            bool held = true;
+            if (touched) {  // the last pass
+                const uint32_t per = (uint32_t)(in.V + 1), worker = key[i] / per,
+                               row = key[i] % per;
+                held = row < (uint32_t)in.V;
+                if (held) touched[(int64_t)worker * in.V + row] = 1;
+            }
             order_out[to] = held ? pos[i] : ~pos[i];
         }
     }
@@ -307,7 +381,7 @@ __global__ __launch_bounds__(kEmbedThreads) void k_embed_lookup(
     }
     Raw<O, VEC> r;
     r.set_all(v);
-    r.store_upto(out + t * ld_out + col, D - col);
+    r.template store_upto<true>(out + t * ld_out + col, D - col);
 }
 
 // ---------------------------------------------------------------------------
@@ -330,8 +404,10 @@ struct EmbedGradArgs {
     int32_t accumulate;
     int32_t log2_lanes;           // lanes that hold a chunk of a row
     int64_t chunks;               // chunks of a row
+    const uint8_t *touched;       // [rows] rows with tokens; NULL: none has any
     int64_t sum_blocks;           // workgroups that add; the others zero
     int32_t zero_rows;            // rows a zeroing workgroup looks after
+    int32_t stream;               // zeros pass the caches by
 };
 
 template <typename Y, typename G, typename A, int VEC>
@@ -354,147 +430,195 @@ __device__ __forceinline__ void embed_write(const EmbedGradArgs<Y, G, A> &a, uin
     r.store_upto(g, a.D - col);
 }
 
-// Zeros in the rows of workgroup `block`'s share that no token names.
-template <typename Y, typename G, typename A>
+// Zeros in the rows of workgroup `block`'s share that no token names: about
+// 16 KiB of consecutive rows, which its threads write side by side.
+template <bool STREAM, typename Y, typename G, typename A>
 __device__ __forceinline__ void embed_zero(const EmbedGradArgs<Y, G, A> &a, int64_t block) {
-    __shared__ uint8_t s_empty[64];
-    const int64_t r0 = block * a.zero_rows;
-    const int count = (int)min((int64_t)a.zero_rows, a.rows - r0);
-    if ((int)threadIdx.x < count) {
-        const int64_t r = r0 + threadIdx.x;
-        const uint32_t key = (uint32_t)(r / a.V * (a.V + 1) + r % a.V);
-        int64_t lo = 0, hi = a.N;  // the first token whose key is not below
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (a.keys[mid] < key) lo = mid + 1;
-            else hi = mid;
-        }
-        s_empty[threadIdx.x] = lo >= a.N || a.keys[lo] != key;
-    }
-    __syncthreads();
     constexpr int W = kVec<G>;
     Raw<G, W> zero;
 #pragma unroll
     for (int i = 0; i < Raw<G, W>::kWords; ++i) zero.w[i] = 0;
-    const int lane = threadIdx.x & 63;
-    for (int i = threadIdx.x >> 6; i < count; i += kEmbedThreads / 64) {
-        if (!s_empty[i]) continue;
-        const int64_t r = r0 + i;
-        G *g = a.grad + r / a.V * a.stride + r % a.V * a.ld_grad;
-        for (int64_t col = lane * W; col < a.D; col += 64 * W)
-            zero.template store_upto<true>(g + col, a.D - col);
+    // as many neighbouring threads to a row as it has accesses, or all
+    int lg = 0;
+    while (lg < 8 && ((int64_t)W << lg) < a.D) ++lg;
+    static_assert(kEmbedThreads == 256, "up to all threads to a row");
+    const int64_t r1 = min((block + 1) * a.zero_rows, a.rows);
+    for (int64_t r = block * a.zero_rows + (threadIdx.x >> lg); r < r1; r += kEmbedThreads >> lg) {
+        if (a.touched && a.touched[r]) continue;
+        const int64_t worker = a.rows == a.V ? 0 : (int64_t)((uint32_t)r / (uint32_t)a.V);
+        G *g = a.grad + worker * a.stride + (r - worker * a.V) * a.ld_grad;
+        for (int64_t col = (threadIdx.x & ((1 << lg) - 1)) * W; col < a.D; col += (int64_t)W << lg)
+            zero.template store_upto<STREAM>(g + col, a.D - col);
     }
 }
+
+// The run of equal keys around a position, counted up to a limit (lanes of a
+// group alike): how many positions just below `at` (down to lo), or from `at`
+// on (below hi), hold `key`.
+__device__ __forceinline__ int run_below(const uint32_t *keys, int64_t at, int64_t lo,
+                                         uint32_t key) {
+    int64_t l = lo, h = at;
+    while (l < h) {
+        const int64_t mid = (l + h) >> 1;
+        if (keys[mid] < key) l = mid + 1;
+        else h = mid;
+    }
+    return (int)(at - l);
+}
+__device__ __forceinline__ int run_from(const uint32_t *keys, int64_t at, int64_t hi,
+                                        uint32_t key) {
+    int64_t l = at, h = hi;
+    while (l < h) {
+        const int64_t mid = (l + h) >> 1;
+        if (keys[mid] > key) h = mid;
+        else l = mid + 1;
+    }
+    return (int)(l - at);
+}
+__device__ __forceinline__ int leading(uint64_t mask) {  // ones from bit 0 on
+    return ~mask ? __ffsll((unsigned long long)~mask) - 1 : 64;
+}
+
+// A tile's share of the work: tokens t0 + i for begin <= i < end, of which the
+// first run is a piece of a longer one (head), or the last (rest).
+struct TileWork {
+    int64_t t0;
+    int begin, end, count;
+    bool head, rest;
+};
 
 template <typename Y, typename G, typename A, bool WHOLE_WAVE>
 __global__ __launch_bounds__(kEmbedThreads) void k_embed_sum(EmbedGradArgs<Y, G, A> a) {
     constexpr int VEC = kVec<Y>, U = 8;
     if ((int64_t)blockIdx.x >= a.sum_blocks) {
-        embed_zero(a, (int64_t)blockIdx.x - a.sum_blocks);
+        if (a.stream) embed_zero<true>(a, (int64_t)blockIdx.x - a.sum_blocks);
+        else embed_zero<false>(a, (int64_t)blockIdx.x - a.sum_blocks);
         return;
     }
     int64_t unit = ((int64_t)blockIdx.x * kEmbedThreads + threadIdx.x) >> a.log2_lanes;
     if constexpr (WHOLE_WAVE) unit = (int64_t)wave_uniform((uint64_t)unit);
     const int64_t tile = unit / a.chunks;
     if (tile >= a.tiles) return;
-    const int lanes = 1 << a.log2_lanes;
+    const int lanes = 1 << a.log2_lanes, lane = threadIdx.x & 63;
     const int64_t col = ((unit % a.chunks) * lanes + (threadIdx.x & (lanes - 1))) * VEC;
     const bool live = col < a.D;
-    const int64_t t0 = tile * a.tile, t1 = min(t0 + a.tile, a.N);
-    const uint32_t none = ~0u;
-    const uint32_t before = t0 > 0 ? a.keys[t0 - 1] : none;
-    const uint32_t after = t1 < a.N ? a.keys[t1] : none;
+    TileWork w;
+    w.t0 = tile * a.tile;
+    w.count = (int)min((int64_t)a.tile, a.N - w.t0);
+    const int64_t t1 = w.t0 + w.count;
+    // the tokens of the tile and of the one after it, a lane each (WHOLE_WAVE)
+    uint32_t key = 0, key2 = 0;
+    int32_t order = 0, order2 = 0;
+    uint64_t ends = 0;
+    {
+        int below, head, tail, beyond;  // of the first run: before, within; of the last: within, after
+        if constexpr (WHOLE_WAVE) {
+            const bool in = lane < w.count, in2 = lane < a.tile && t1 + lane < a.N;
+            const bool in0 = lane < a.tile && w.t0 - 1 - lane >= 0;
+            const uint32_t key0 = in0 ? a.keys[w.t0 - 1 - lane] : ~0u;
+            key = in ? a.keys[w.t0 + lane] : ~0u;
+            key2 = in2 ? a.keys[t1 + lane] : ~0u;
+            order = in ? a.order[w.t0 + lane] : -1;
+            order2 = in2 ? a.order[t1 + lane] : -1;
+            const uint32_t first = __builtin_amdgcn_readlane(key, 0);
+            const uint32_t last = __builtin_amdgcn_readlane(key, w.count - 1);
+            const uint32_t next = __shfl(key, (lane + 1) & 63, 64);
+            below = leading(__ballot(in0 && key0 == first));
+            head = leading(__ballot(in && key == first));
+            tail = w.count - leading(__ballot(in && key != last));
+            beyond = leading(__ballot(in2 && key2 == last));
+            ends = __ballot(in && (lane == w.count - 1 || next != key));
+        } else {
+            const uint32_t first = a.keys[w.t0], last = a.keys[t1 - 1];
+            below = run_below(a.keys, w.t0, max(w.t0 - a.tile, (int64_t)0), first);
+            head = run_from(a.keys, w.t0, t1, first);
+            tail = run_below(a.keys, t1, w.t0, last);
+            beyond = run_from(a.keys, t1, min(t1 + a.tile, a.N), last);
+        }
+        const bool one_run = head == w.count;
+        const bool began = below > 0;
+        const bool head_long = began && below + head + (one_run ? beyond : 0) > a.tile;
+        // a run that began in an earlier tile: its piece, or that tile's alone
+        w.head = head_long;
+        w.begin = began && !head_long ? head : 0;
+        w.rest = beyond > 0 && (one_run && began ? head_long : tail + beyond > a.tile);
+        w.end = w.count + (w.rest ? 0 : beyond);
+        if (one_run && began && !head_long) return;
+    }
+    auto order_of = [&](int i) -> int32_t {
+        if constexpr (WHOLE_WAVE) {
+            const int32_t x = __builtin_amdgcn_readlane(order, i < w.count ? i : 0);
+            const int32_t y = __builtin_amdgcn_readlane(order2, i < w.count ? 0 : i - w.count);
+            return i < w.count ? x : y;
+        } else {
+            return a.order[w.t0 + i];
+        }
+    };
+    auto ends_at = [&](int i) -> bool {
+        if (i == w.end - 1) return true;
+        if constexpr (WHOLE_WAVE) return i < w.count - 1 && (ends >> i & 1);
+        else return a.keys[w.t0 + i] != a.keys[w.t0 + i + 1];
+    };
     A acc[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) acc[i] = (A)0;
-    uint32_t run = a.keys[t0];
-    bool held = a.order[t0] >= 0;  // the run's tokens lie in the table
-    bool first = run == before;    // the run was begun in an earlier tile
-    for (int64_t j = t0; j < t1; j += U) {
-        uint32_t key[U];
-        int32_t order[U];
+    bool head = w.head;
+    for (int j = w.begin; j < w.end; j += U) {
+        int32_t row[U];
         Raw<Y, VEC> y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = j + u < t1 ? j + u : t1 - 1;
-            key[u] = a.keys[at];
-            order[u] = a.order[at];
-            if (live && order[u] >= 0)
-                y[u].template load_upto<true>(a.dy + order[u] * a.ld_dy + col, a.D - col);
-            else
-#pragma unroll
-                for (int i = 0; i < Raw<Y, VEC>::kWords; ++i) y[u].w[i] = 0;
+            row[u] = j + u < w.end ? order_of(j + u) : -1;
+            if (live && row[u] >= 0)
+                y[u].template load_upto<true>(a.dy + row[u] * a.ld_dy + col, a.D - col);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (j + u < t1) {
-                if (key[u] != run) {
-                    // a run ends within the tile
-                    if (live && held) {
-                        if (first) {
+            if (j + u < w.end && row[u] >= 0) {
+                if (live)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[i] += y[u].template get<A>(i);
+                if (ends_at(j + u)) {
+                    if (live) {
+                        const bool rest = w.rest && j + u == w.end - 1;
+                        if (head || rest) {
                             Raw<A, VEC> r;
                             r.set_all(acc);
-                            r.store_upto(a.pieces + 2 * tile * a.D + col, a.D - col);
+                            r.store_upto(a.pieces + (2 * tile + (head ? 0 : 1)) * a.D + col,
+                                         a.D - col);
                         } else {
-                            embed_write<Y, G, A, VEC>(a, run, col, acc);
+                            embed_write<Y, G, A, VEC>(a, a.keys[w.t0 + j + u], col, acc);
                         }
                     }
-                    run = key[u];
-                    held = order[u] >= 0;
-                    first = false;
+                    head = false;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) acc[i] = (A)0;
                 }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] += y[u].template get<A>(i);
+            } else if (j + u < w.end && ends_at(j + u)) {
+                head = false;  // a run of tokens outside the table
             }
         }
     }
-    if (!live || !held) return;
-    const bool last = run == after;  // the run goes on in the next tile
-    if (first || last) {
-        Raw<A, VEC> r;
-        r.set_all(acc);
-        r.store_upto(a.pieces + (2 * tile + (first ? 0 : 1)) * a.D + col, a.D - col);
-    } else {
-        embed_write<Y, G, A, VEC>(a, run, col, acc);
-    }
 }
 
-// Runs that cross tiles: the piece that the run's first tile left, then those
-// of the tiles it goes on in, in order.  The waves of a workgroup take
-// sections of a run's tiles, whose sums are added in order.
+// Runs longer than a tile: the piece that the run's first tile left, then
+// those of the tiles it goes on in, in order.  The waves of a workgroup look
+// for such runs in a tile each; a wave adds a short one's pieces by itself, and
+// all take sections of a long one's, whose sums are added in order.
 constexpr int kJoinThreads = 512;
-constexpr int kJoinTiles = 8;  // tiles a workgroup looks through
+constexpr int kJoinTiles = kJoinThreads / 64;
 
 template <typename Y, typename G, typename A>
 __global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G, A> a) {
     constexpr int W = kVec<A>, NW = kJoinThreads / 64, U = 8;
     __shared__ A s_part[NW][64 * W];
+    __shared__ int64_t s_more[kJoinTiles];  // tiles that the run goes on in, 0: no such run
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = ((int64_t)blockIdx.y * 64 + lane) * W;
     const bool live = col < a.D;
-    for (int q = 0; q < kJoinTiles; ++q) {
-        const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + q;
-        const int64_t t1 = (tile + 1) * a.tile;
-        if (tile >= a.tiles || t1 >= a.N) return;
-        const uint32_t key = a.keys[t1];
-        if (a.keys[t1 - 1] != key || a.order[t1] < 0) continue;  // no run crosses here
-        // is it begun in this tile?
-        const int64_t t0 = tile * a.tile;
-        if (t0 > 0 && a.keys[t0 - 1] == key) continue;
-        // tiles after this one that it goes on in
-        int64_t more = 0;
-        for (;;) {
-            const int64_t at = (tile + 1 + more + lane) * a.tile;
-            const uint64_t same = __ballot(at < a.N && a.keys[at < a.N ? at : a.N - 1] == key);
-            const int run = ~same ? __ffsll((unsigned long long)~same) - 1 : 64;
-            more += run;
-            if (run < 64) break;
-        }
-        // pieces 0 .. more: the last run's of this tile, then the first runs'
-        const int64_t lo = (more + 1) * wave / NW, hi = (more + 1) * (wave + 1) / NW;
-        A acc[W];
+    // pieces lo .. hi - 1 of the run that begins in `tile`: its last run's,
+    // then the first runs' of the tiles after it
+    auto add_pieces = [&](int64_t tile, int64_t lo, int64_t hi, A(&acc)[W]) {
 #pragma unroll
         for (int i = 0; i < W; ++i) acc[i] = (A)0;
         for (int64_t s = lo; s < hi; s += U) {
@@ -512,6 +636,46 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G,
 #pragma unroll
                 for (int i = 0; i < W; ++i) acc[i] += r[u].template get<A>(i);
         }
+    };
+    {
+        const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + wave;
+        const int64_t t0 = tile * a.tile, t1 = t0 + a.tile;
+        int64_t more = 0;
+        if (tile < a.tiles && t1 < a.N) {
+            const uint32_t last = a.keys[t1 - 1];
+            const bool in = lane < a.tile;
+            const uint32_t key = in ? a.keys[t0 + lane] : ~0u;
+            const bool in2 = in && t1 + lane < a.N;
+            const uint32_t key2 = in2 ? a.keys[t1 + lane] : ~0u;
+            const bool began = t0 > 0 && a.keys[t0 - 1] == last;
+            const int tail = a.tile - leading(__ballot(in && key != last));
+            const int beyond = leading(__ballot(in2 && key2 == last));
+            if (!began && beyond > 0 && tail + beyond > a.tile && a.order[t1] >= 0) {
+                for (;;) {
+                    const int64_t at = (tile + 1 + more + lane) * a.tile;
+                    const int run = leading(__ballot(at < a.N &&
+                                                     a.keys[at < a.N ? at : a.N - 1] == last));
+                    more += run;
+                    if (run < 64) break;
+                }
+            }
+        }
+        // a wave alone adds a few pieces, all together a longer run's
+        const bool alone = more > 0 && more < U;
+        if (lane == 0) s_more[wave] = alone ? 0 : more;
+        if (alone) {
+            A acc[W];
+            add_pieces(tile, 0, more + 1, acc);
+            if (live) embed_write<Y, G, A, W>(a, a.keys[t1], col, acc);
+        }
+    }
+    __syncthreads();
+    for (int q = 0; q < kJoinTiles; ++q) {
+        const int64_t more = s_more[q];
+        if (more == 0) continue;
+        const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + q;
+        A acc[W];
+        add_pieces(tile, (more + 1) * wave / NW, (more + 1) * (wave + 1) / NW, acc);
 #pragma unroll
         for (int i = 0; i < W; ++i) s_part[wave][lane * W + i] = acc[i];
         __syncthreads();
@@ -519,7 +683,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G,
             for (int w = 1; w < NW; ++w)
 #pragma unroll
                 for (int i = 0; i < W; ++i) acc[i] += s_part[w][lane * W + i];
-            embed_write<Y, G, A, W>(a, key, col, acc);
+            embed_write<Y, G, A, W>(a, a.keys[(tile + 1) * a.tile], col, acc);
         }
         __syncthreads();
     }
@@ -528,6 +692,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G,
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+constexpr int64_t kCacheBytes = 256 << 20;       // the device's last cache
 constexpr int64_t kMaxDim = int64_t(1) << 22;  // columns of a gradient
 
 inline int64_t round16(int64_t bytes) { return (bytes + 15) & ~int64_t(15); }
@@ -538,10 +703,12 @@ inline int key_bits(int64_t values) {
     return bits;
 }
 
-// Where an index keeps what: the sorted keys and their tokens first, then,
-// for a longer sort, a second copy of both, the counts and the totals.
+// Where an index keeps what: the sorted keys, their tokens, a flag for every
+// row of every worker that has tokens; then, for a longer sort, a second copy
+// of keys and tokens, the counts and the totals.
 struct IndexLayout {
-    int64_t N = 0, tiles = 0, order = 0, keys2 = 0, order2 = 0, counts = 0, totals = 0, bytes = 0;
+    int64_t N = 0, tiles = 0, order = 0, touched = 0, keys2 = 0, order2 = 0, counts = 0,
+            totals = 0, bytes = 0;
 };
 inline bool index_layout(int64_t P, int64_t n, int64_t V, IndexLayout *l) {
     const int64_t lim = (int64_t(1) << 31) - 1;
@@ -551,12 +718,13 @@ inline bool index_layout(int64_t P, int64_t n, int64_t V, IndexLayout *l) {
     l->N = P * n;
     const int64_t part = round16(4 * l->N);
     l->order = part;
-    l->bytes = 2 * part;
+    l->touched = 2 * part;
+    l->bytes = l->touched + round16(P * V);
     if (n > kSmallSort) {
         l->tiles = (l->N + kSortTile - 1) / kSortTile;
-        l->keys2 = 2 * part;
-        l->order2 = 3 * part;
-        l->counts = 4 * part;
+        l->keys2 = l->bytes;
+        l->order2 = l->keys2 + part;
+        l->counts = l->order2 + part;
         l->totals = l->counts + round16(4 * kBigBins * l->tiles);
         l->bytes = l->totals + 4 * kBigBins;
     }
@@ -580,7 +748,7 @@ inline GradShape grad_shape(int64_t N, int64_t D, int vec) {
     while ((1 << s.log2_lanes) < vecs && s.log2_lanes < 6) ++s.log2_lanes;
     s.chunks = (vecs + (1 << s.log2_lanes) - 1) >> s.log2_lanes;
     s.tile = 8;
-    while (s.tile < 64 && (N / (2 * s.tile)) * (s.chunks << s.log2_lanes) >= 64 * 8192) s.tile *= 2;
+    while (s.tile < 64 && (N / (2 * s.tile)) * (s.chunks << s.log2_lanes) >= 64 * 32768) s.tile *= 2;
     s.tiles = (N + s.tile - 1) / s.tile;
     return s;
 }
@@ -669,19 +837,30 @@ ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, cons
     char *base = (char *)d_index;
     uint32_t *keys = (uint32_t *)base;
     int32_t *order = (int32_t *)(base + l.order);
+    uint8_t *touched = (uint8_t *)(base + l.touched);
     const int id64 = id_type == ECC_I64;
     if (n <= kSmallSort) {
-        const int bits = key_bits(V + 1), passes = (bits + 7) / 8,
-                  rb = (bits + passes - 1) / passes;
+        const int passes = (key_bits(V + 1) + kSmallBits - 1) / kSmallBits;
         const dim3 grid((unsigned)P), block(kSortThreads);
-#define ECC_SORT(ITEMS)                                                                      \
-    hipLaunchKernelGGL(k_embed_sort<ITEMS>, grid, block, 0, s, n, V, row0, d_ids, id64, passes, \
-                       rb, keys, order)
-        if (n <= kSortThreads) ECC_SORT(1);
-        else if (n <= 2 * kSortThreads) ECC_SORT(2);
-        else if (n <= 4 * kSortThreads) ECC_SORT(4);
-        else if (n <= 8 * kSortThreads) ECC_SORT(8);
-        else ECC_SORT(16);
+        const bool pack = key_bits(V + 1) + kPosBits <= 32;
+#define ECC_SORT(ITEMS)                                                                         \
+    if (pack)                                                                                   \
+        hipLaunchKernelGGL((k_embed_sort<ITEMS, true>), grid, block, 0, s, n, V, row0, d_ids,    \
+                           id64, passes, keys, order, touched);                                 \
+    else                                                                                        \
+        hipLaunchKernelGGL((k_embed_sort<ITEMS, false>), grid, block, 0, s, n, V, row0, d_ids,   \
+                           id64, passes, keys, order, touched)
+        if (n <= kSortThreads) {
+            ECC_SORT(1);
+        } else if (n <= 2 * kSortThreads) {
+            ECC_SORT(2);
+        } else if (n <= 4 * kSortThreads) {
+            ECC_SORT(4);
+        } else if (n <= 8 * kSortThreads) {
+            ECC_SORT(8);
+        } else {
+            ECC_SORT(16);
+        }
 #undef ECC_SORT
         ECC_LAUNCH_CHECK();
         return ECC_OK;
@@ -697,14 +876,14 @@ ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, cons
         uint32_t *k_out = to_first ? keys : keys2;
         int32_t *o_out = to_first ? order : order2;
         hipLaunchKernelGGL(k_sort_count, dim3((unsigned)l.tiles), dim3(kTileThreads), 0, s, in,
-                           pass * rb, rb, counts);
+                           pass * rb, rb, counts, pass == 0 ? touched : nullptr, (int64_t)P * V);
         ECC_LAUNCH_CHECK();
-        hipLaunchKernelGGL(k_sort_scan, dim3(1u << rb), dim3(kTileThreads), 0, s, l.tiles, counts,
+        hipLaunchKernelGGL(k_sort_scan, dim3(1u << rb), dim3(kScanThreads), 0, s, l.tiles, counts,
                            totals);
         ECC_LAUNCH_CHECK();
         hipLaunchKernelGGL(k_sort_move, dim3((unsigned)l.tiles), dim3(kTileThreads), 0, s, in,
                            pass * rb, rb, counts, totals, k_out, o_out,
-                           (int)(pass + 1 == passes));
+                           pass + 1 == passes ? touched : nullptr);
         ECC_LAUNCH_CHECK();
         in.keys = k_out;
         in.order = o_out;
@@ -763,9 +942,7 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t per_block = kEmbedThreads >> g.log2_lanes;
     const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
     const int64_t rows = (int64_t)P * V;
-    // a zeroing workgroup looks after up to 64 rows, fewer where the device
-    // would not be filled
-    const int64_t zero_rows = std::max<int64_t>(4, std::min<int64_t>(64, rows / 2048));
+    const int64_t zero_rows = std::max<int64_t>(1, 16384 / (D * gb));
     const int64_t zero_blocks = accumulate ? 0 : (rows + zero_rows - 1) / zero_rows;
     if (sum_blocks + zero_blocks > 0x7fffff) {
         set_error("P * n * D or P * V is too large for one launch");
@@ -797,7 +974,9 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
             a.log2_lanes = g.log2_lanes;
             a.chunks = g.chunks;
             a.sum_blocks = sum_blocks;
+            a.touched = n > 0 ? (const uint8_t *)d_index + l.touched : nullptr;
             a.zero_rows = (int32_t)zero_rows;
+            a.stream = rows * D * gb > kCacheBytes;
             const dim3 grid((unsigned)(sum_blocks + zero_blocks));
             if (g.log2_lanes == 6)
                 hipLaunchKernelGGL((k_embed_sum<Y, G, A, true>), grid, dim3(kEmbedThreads), 0, s,
