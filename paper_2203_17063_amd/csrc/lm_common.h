@@ -159,17 +159,23 @@ struct Raw {
     }
     template <typename A>
     __device__ __forceinline__ void set_all(const A (&v)[N]) {
+        set_some<N>(0, v);
+    }
+    // elements first .. first + M - 1
+    template <int M, typename A>
+    __device__ __forceinline__ void set_some(int first, const A (&v)[M]) {
         if constexpr (std::is_same_v<T, bf16_t>) {
 #pragma unroll
-            for (int i = 0; i < N; i += 2) w[i / 2] = bf16_pair((float)v[i], (float)v[i + 1]);
+            for (int i = 0; i < M; i += 2)
+                w[(first + i) / 2] = bf16_pair((float)v[i], (float)v[i + 1]);
         } else if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = __float_as_uint((float)v[i]);
+            for (int i = 0; i < M; ++i) w[first + i] = __float_as_uint((float)v[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                w[2 * i] = (uint32_t)__double2loint((double)v[i]);
-                w[2 * i + 1] = (uint32_t)__double2hiint((double)v[i]);
+            for (int i = 0; i < M; ++i) {
+                w[2 * (first + i)] = (uint32_t)__double2loint((double)v[i]);
+                w[2 * (first + i) + 1] = (uint32_t)__double2hiint((double)v[i]);
             }
         }
     }

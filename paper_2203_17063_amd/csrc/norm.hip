@@ -58,6 +58,22 @@ __device__ __forceinline__ double fma_(double a, double b, double c) { return __
 __device__ __forceinline__ float rsqrt_(float v) { return 1.0f / __builtin_sqrtf(v); }
 __device__ __forceinline__ double rsqrt_(double v) { return 1.0 / __builtin_sqrt(v); }
 
+// The sum over the 16 lanes of a DPP row, and a lane's value in all lanes.
+__device__ __forceinline__ float row_add(float v) {
+    v += dpp_f32<kDppQuadXor1>(v);
+    v += dpp_f32<kDppQuadXor2>(v);
+    v += dpp_f32<kDppRowHalfMirror>(v);
+    return v + dpp_f32<kDppRowMirror>(v);
+}
+__device__ __forceinline__ double row_add(double v) { return group_sum<16>(v); }
+__device__ __forceinline__ float read_lane(float v, int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ __forceinline__ double read_lane(double v, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                            __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+
 // K sums over the workgroup's NT threads, in every thread.  s holds [2][NT /
 // 64][K]; the two halves are used in turn, so that one barrier is enough:
 // a half is written again only after every wave has passed the barrier of
@@ -74,13 +90,26 @@ __device__ __forceinline__ void row_sums(A (&v)[K], A *s, int &half) {
             for (int k = 0; k < K; ++k) b[(threadIdx.x >> 6) * K + k] = v[k];
         }
         lds_barrier();
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] = b[k];
-#pragma unroll
-        for (int w = 1; w < NW; ++w)
-#pragma unroll
-            for (int k = 0; k < K; ++k) v[k] += b[w * K + k];
         half ^= 1;
+        if constexpr (K * NW <= 16) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k] = b[k];
+#pragma unroll
+            for (int w = 1; w < NW; ++w)
+#pragma unroll
+                for (int k = 0; k < K; ++k) v[k] += b[w * K + k];
+            return;
+        }
+        // every wave joins the waves' sums for itself: lane 16 r + w takes wave
+        // w's sums r and r + 4, a row of 16 lanes adds them up
+        const int lane = threadIdx.x & 63, w = lane & 15, r = lane >> 4;
+        static_assert(NW <= 16 && K <= 8, "a lane for every wave, two sums in a lane");
+        A lo = w < NW && r < K ? b[w * K + r] : (A)0, hi = (A)0;
+        if constexpr (K > 4) hi = w < NW && r + 4 < K ? b[w * K + r + 4] : (A)0;
+        lo = row_add(lo);
+        if constexpr (K > 4) hi = row_add(hi);
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = read_lane(k < 4 ? lo : hi, 16 * (k & 3));
     }
 }
 
@@ -116,10 +145,10 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
         Raw<T, VEC> rx[NV], rf[NV], rg[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
-            rx[v].load_upto(x + c, a.D - c);
-            if (a.f) rf[v].load_upto(f + c, a.D - c);
-            if (row_gate) rg[v].load_upto(g + c, a.D - c);
+            const uint32_t c = (v * NT + threadIdx.x) * VEC;
+            rx[v].load_upto(x + c, (int32_t)a.D - (int32_t)c);
+            if (a.f) rf[v].load_upto(f + c, (int32_t)a.D - (int32_t)c);
+            if (row_gate) rg[v].load_upto(g + c, (int32_t)a.D - (int32_t)c);
         }
         A y[E];
         A k = (A)1;
@@ -146,13 +175,13 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
             T *o = reinterpret_cast<T *>(x_out) + row * ld_x_out;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
+                const uint32_t c = (v * NT + threadIdx.x) * VEC;
                 A t[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i];
                 Raw<T, VEC> r;
                 r.set_all(t);
-                r.store_upto(o + c, a.D - c);
+                r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
             }
         }
         if (h_out) {
@@ -164,13 +193,13 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
             T *o = reinterpret_cast<T *>(h_out) + row * ld_h;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC;
+                const uint32_t c = (v * NT + threadIdx.x) * VEC;
                 A t[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i] * q * wp[v * VEC + i];
                 Raw<T, VEC> r;
                 r.set_all(t);
-                r.store_upto(o + c, a.D - c);
+                r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
             }
         }
     }
@@ -214,10 +243,18 @@ struct NormGradArgs {
     NormUnits u;
 };
 
-template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void k_norm_grad(NormArgs a, NormGradArgs g) {
+// HOLD: the row's operands stay in registers between the sums and the results,
+// and the weights lie in LDS, each where the thread that needs it has put it
+// (in registers, 173 of them for a row of 4,096 bf16, one workgroup filled a
+// CU: 129 us for 8,192 such rows, 95 us with two).  Otherwise (the longest
+// rows) both are read again, and the sums over rows stay in the work buffer.
+template <typename T, int NT, int NV, bool HOLD>
+__global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) void k_norm_grad(NormArgs a, NormGradArgs g) {
     using A = Acc<T>;
-    constexpr int VEC = kVec<T>, E = NV * VEC;
+    constexpr int VEC = kVec<T>, KEEP = HOLD ? NV : 1;
+    constexpr int Q = 16 / (int)sizeof(A), CH = VEC / Q;  // accumulators of 16 bytes
+    typedef A quad __attribute__((ext_vector_type(Q)));
+    extern __shared__ double s_weights[];  // [3][NV * CH][NT] quads
     __shared__ A s_red[2 * (NT / 64) * 6];
     int half = 0;
     const A res = (A)a.res, branch = (A)a.branch, eps = (A)a.eps, inv_d = (A)1 / (A)a.D;
@@ -238,57 +275,122 @@ __global__ __launch_bounds__(NT) void k_norm_grad(NormArgs a, NormGradArgs g) {
     }
     r0 += worker * u.n;
     r1 += worker * u.n;
-    A wq[E], wp[E], wg[E];  // post-norm weight, pre-norm weight, b times a parameter gate
-    A s_pre[E], s_post[E], s_gate[E];
+    // quad c of vector v's columns of the post-norm weight (0), the pre-norm
+    // weight (1) and b times a parameter gate (2)
+    auto read_weights = [&](int which, int v, int c, A(&w)[Q]) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int64_t c = ((int64_t)(e / VEC) * NT + threadIdx.x) * VEC + e % VEC;
-        wq[e] = (A)1;
-        wp[e] = (A)0;
-        wg[e] = branch;
-        if (c < a.D) {
-            if (post) wq[e] = (A)a.offset + load_typed<A>(a.w_post, a.w_type, c);
-            if (pre) wp[e] = (A)a.offset + load_typed<A>(a.w_pre, a.w_type, c);
-            if (param_gate) wg[e] *= load_typed<A>(a.gate, a.w_type, c);
-        }
-        s_pre[e] = s_post[e] = s_gate[e] = (A)0;
-    }
-    for (int64_t row = r0; row < r1; ++row) {
-        Raw<T, VEC> rx[NV], rf[NV], rg[NV], rh[NV], ro[NV];
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - c;
-#pragma unroll
-            for (int i = 0; i < Raw<T, VEC>::kWords; ++i)
-                rx[v].w[i] = rf[v].w[i] = rg[v].w[i] = rh[v].w[i] = ro[v].w[i] = 0;
-            if (pre) {
-                rx[v].load_upto(reinterpret_cast<const T *>(a.x) + row * a.ld_x + c, left);
-                rh[v].load_upto(reinterpret_cast<const T *>(g.dh) + row * g.ld_dh + c, left);
+        for (int i = 0; i < Q; ++i) {
+            const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC + c * Q + i;
+            w[i] = which == 0 ? (A)1 : which == 1 ? (A)0 : branch;
+            if (col < a.D) {
+                if (which == 0 && post)
+                    w[i] = (A)a.offset + load_typed<A>(a.w_post, a.w_type, col);
+                if (which == 1 && pre) w[i] = (A)a.offset + load_typed<A>(a.w_pre, a.w_type, col);
+                if (which == 2 && param_gate) w[i] *= load_typed<A>(a.gate, a.w_type, col);
             }
-            if (g.dxo)
-                ro[v].load_upto(reinterpret_cast<const T *>(g.dxo) + row * g.ld_dxo + c, left);
-            if (a.f) rf[v].load_upto(reinterpret_cast<const T *>(a.f) + row * a.ld_f + c, left);
-            if (row_gate)
-                rg[v].load_upto(reinterpret_cast<const T *>(a.gate) +
-                                    row / a.gate_rows * a.ld_gate + c,
-                                left);
         }
+    };
+    quad *const lds = reinterpret_cast<quad *>(s_weights) + threadIdx.x;
+    auto weights = [&](int which, int v, int c, A(&w)[Q]) {
+        if constexpr (HOLD) {
+            const quad t = lds[((which * NV + v) * CH + c) * NT];
+#pragma unroll
+            for (int i = 0; i < Q; ++i) w[i] = t[i];
+        } else {
+            read_weights(which, v, c, w);
+        }
+    };
+    if constexpr (HOLD) {
+#pragma unroll
+        for (int which = 0; which < 3; ++which)
+#pragma unroll
+            for (int vc = 0; vc < NV * CH; ++vc) {
+                A w[Q];
+                read_weights(which, vc / CH, vc % CH, w);
+                quad t;
+#pragma unroll
+                for (int i = 0; i < Q; ++i) t[i] = w[i];
+                lds[(which * NV * CH + vc) * NT] = t;
+            }
+    }
+    struct Operands {
+        Raw<T, VEC> x, f, gate, dh, dxo;
+    };
+    auto fetch = [&](int64_t row, int v, Operands &o) {
+        const uint32_t c = (v * NT + threadIdx.x) * VEC;
+        const int32_t left = (int32_t)a.D - (int32_t)c;
+#pragma unroll
+        for (int i = 0; i < Raw<T, VEC>::kWords; ++i)
+            o.x.w[i] = o.f.w[i] = o.gate.w[i] = o.dh.w[i] = o.dxo.w[i] = 0;
+        if (pre) {
+            o.x.load_upto(reinterpret_cast<const T *>(a.x) + row * a.ld_x + c, left);
+            o.dh.load_upto(reinterpret_cast<const T *>(g.dh) + row * g.ld_dh + c, left);
+        }
+        if (g.dxo)
+            o.dxo.load_upto(reinterpret_cast<const T *>(g.dxo) + row * g.ld_dxo + c, left);
+        if (a.f) o.f.load_upto(reinterpret_cast<const T *>(a.f) + row * a.ld_f + c, left);
+        if (row_gate)
+            o.gate.load_upto(reinterpret_cast<const T *>(a.gate) + row / a.gate_rows * a.ld_gate + c,
+                             left);
+    };
+    // the sums over rows of vector v's columns, in registers or (unless this is
+    // the unit's or the gate's first row) in the work buffer
+    const int64_t at = (int64_t)blockIdx.x * a.D;
+    A s_pre[KEEP * VEC], s_post[KEEP * VEC], s_gate[KEEP * VEC];
+#pragma unroll
+    for (int e = 0; e < KEEP * VEC; ++e) s_pre[e] = s_post[e] = s_gate[e] = (A)0;
+    auto get = [&](const void *from, int v, bool first, A *sum) {
+        const uint32_t c = (v * NT + threadIdx.x) * VEC;
+        Raw<A, VEC> r;
+        if (from && !first) r.load_upto(reinterpret_cast<const A *>(from) + at + c, (int32_t)a.D - (int32_t)c);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] = from && !first ? r.template get<A>(i) : (A)0;
+    };
+    auto put = [&](void *to, int v, const A *sum) {
+        const uint32_t c = (v * NT + threadIdx.x) * VEC;
+        if (!to) return;
+        A t[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) t[i] = sum[i];
+        Raw<A, VEC> r;
+        r.set_all(t);
+        r.store_upto(reinterpret_cast<A *>(to) + at + c, (int32_t)a.D - (int32_t)c);
+    };
+    constexpr int UNROLL = HOLD ? NV : 1;
+    Operands op[KEEP];
+    for (int64_t row = r0; row < r1; ++row) {
+        if constexpr (HOLD)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) fetch(row, v, op[v]);
         // sums of x^2, f^2, A x, C dx', C A, C x
         A s[6] = {(A)0, (A)0, (A)0, (A)0, (A)0, (A)0};
+#pragma unroll UNROLL
+        for (int v = 0; v < NV; ++v) {
+            if constexpr (!HOLD) fetch(row, v, op[0]);
+            const Operands &o = op[HOLD ? v : 0];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int v = e / VEC, i = e % VEC;
-            const A x = rx[v].template get<A>(i), f = rf[v].template get<A>(i);
-            const A d = ro[v].template get<A>(i);
-            const A ah = rh[v].template get<A>(i) * wp[e];
-            A b = wg[e] * wq[e] * f;
-            if (row_gate) b *= rg[v].template get<A>(i);
-            s[0] = fma_(x, x, s[0]);
-            s[1] = fma_(f, f, s[1]);
-            s[2] = fma_(ah, x, s[2]);
-            s[3] = fma_(b, d, s[3]);
-            s[4] = fma_(b, ah, s[4]);
-            s[5] = fma_(b, x, s[5]);
+            for (int c = 0; c < CH; ++c) {
+                A wq[Q], wp[Q], wg[Q];
+                weights(0, v, c, wq);
+                weights(1, v, c, wp);
+                weights(2, v, c, wg);
+#pragma unroll
+                for (int j = 0; j < Q; ++j) {
+                    const int i = c * Q + j;
+                    const A x = o.x.template get<A>(i), f = o.f.template get<A>(i);
+                    const A d = o.dxo.template get<A>(i);
+                    const A ah = o.dh.template get<A>(i) * wp[j];
+                    A b = wg[j] * wq[j] * f;
+                    if (row_gate) b *= o.gate.template get<A>(i);
+                    s[0] = fma_(x, x, s[0]);
+                    s[1] = fma_(f, f, s[1]);
+                    s[2] = fma_(ah, x, s[2]);
+                    s[3] = fma_(b, d, s[3]);
+                    s[4] = fma_(b, ah, s[4]);
+                    s[5] = fma_(b, x, s[5]);
+                }
+                __builtin_amdgcn_sched_barrier(0);  // a quad's weights at a time
+            }
         }
         row_sums<NT>(s, s_red, half);
         const A q = pre ? rsqrt_(fma_(s[0], inv_d, eps)) : (A)0;
@@ -297,59 +399,68 @@ __global__ __launch_bounds__(NT) void k_norm_grad(NormArgs a, NormGradArgs g) {
         const A m = post ? k * k * inv_d * (s[3] + q * s[4] - c * s[5]) : (A)0;
         const bool group_end = row_gate && !u.split &&
                                ((row + 1) % a.gate_rows == 0 || row + 1 == r1);
-#pragma unroll
+        const bool group_begin = row == r0 || (row_gate && !u.split && row % a.gate_rows == 0);
+#pragma unroll UNROLL
         for (int v = 0; v < NV; ++v) {
-            const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - col;
-            A dx[VEC], df[VEC], dg[VEC];
+            const uint32_t col = (v * NT + threadIdx.x) * VEC;
+            const int32_t left = (int32_t)a.D - (int32_t)col;
+            if constexpr (!HOLD) {
+                fetch(row, v, op[0]);
+                get(g.pre, v, row == r0, s_pre);
+                get(g.post, v, row == r0, s_post);
+                get(g.share, v, group_begin, s_gate);
+            }
+            const Operands &o = op[HOLD ? v : 0];
+            Raw<T, VEC> rdx, rdf, rdg;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int e = v * VEC + i;
-                const A x = rx[v].template get<A>(i), f = rf[v].template get<A>(i);
-                const A h = rh[v].template get<A>(i);
-                const A d = ro[v].template get<A>(i) + q * (h * wp[e]) - c * x;
-                A gb = wg[e];  // b g
-                if (row_gate) gb *= rg[v].template get<A>(i);
-                const A du = gb * d;
-                dx[i] = res * d;
-                df[i] = k * (du * wq[e] - f * m);
-                s_pre[e] = fma_(h, x * q, s_pre[e]);
-                s_post[e] = fma_(du, f * k, s_post[e]);
-                s_gate[e] = fma_(branch * d, f * k * wq[e], s_gate[e]);
-                dg[i] = s_gate[e];
-                if (group_end) s_gate[e] = (A)0;
+            for (int cq = 0; cq < CH; ++cq) {
+                A wq[Q], wp[Q], wg[Q], dx[Q], df[Q], dg[Q];
+                weights(0, v, cq, wq);
+                weights(1, v, cq, wp);
+                weights(2, v, cq, wg);
+#pragma unroll
+                for (int j = 0; j < Q; ++j) {
+                    const int i = cq * Q + j, e = HOLD ? v * VEC + i : i;
+                    const A x = o.x.template get<A>(i), f = o.f.template get<A>(i);
+                    const A h = o.dh.template get<A>(i);
+                    const A d = o.dxo.template get<A>(i) + q * (h * wp[j]) - c * x;
+                    A gb = wg[j];  // b g
+                    if (row_gate) gb *= o.gate.template get<A>(i);
+                    const A du = gb * d;
+                    dx[j] = res * d;
+                    df[j] = k * (du * wq[j] - f * m);
+                    s_pre[e] = fma_(h, x * q, s_pre[e]);
+                    s_post[e] = fma_(du, f * k, s_post[e]);
+                    s_gate[e] = fma_(branch * d, f * k * wq[j], s_gate[e]);
+                    dg[j] = s_gate[e];
+                    if (group_end) s_gate[e] = (A)0;
+                }
+                rdx.template set_some<Q>(cq * Q, dx);
+                rdf.template set_some<Q>(cq * Q, df);
+                rdg.template set_some<Q>(cq * Q, dg);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            Raw<T, VEC> r;
-            if (g.dx) {
-                r.set_all(dx);
-                r.store_upto(reinterpret_cast<T *>(g.dx) + row * g.ld_dx + col, left);
-            }
-            if (g.df) {
-                r.set_all(df);
-                r.store_upto(reinterpret_cast<T *>(g.df) + row * g.ld_df + col, left);
-            }
-            if (g.dgate && group_end) {
-                r.set_all(dg);
-                r.store_upto(reinterpret_cast<T *>(g.dgate) + row / a.gate_rows * g.ld_dgate + col,
-                             left);
+            if (g.dx)
+                rdx.store_upto(reinterpret_cast<T *>(g.dx) + row * g.ld_dx + col, left);
+            if (g.df)
+                rdf.store_upto(reinterpret_cast<T *>(g.df) + row * g.ld_df + col, left);
+            if (g.dgate && group_end)
+                rdg.store_upto(
+                    reinterpret_cast<T *>(g.dgate) + row / a.gate_rows * g.ld_dgate + col, left);
+            if constexpr (!HOLD) {
+                put(g.pre, v, s_pre);
+                put(g.post, v, s_post);
+                put(g.share, v, s_gate);
             }
         }
     }
-    const int64_t at = (int64_t)blockIdx.x * a.D;
+    if constexpr (HOLD) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC, left = a.D - col;
-        auto put = [&](void *to, const A (&sum)[E]) {
-            if (!to) return;
-            A t[VEC];
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) t[i] = sum[v * VEC + i];
-            Raw<A, VEC> r;
-            r.set_all(t);
-            r.store_upto(reinterpret_cast<A *>(to) + at + col, left);
-        };
-        put(g.pre, s_pre);
-        put(g.post, s_post);
-        put(g.share, s_gate);
+        for (int v = 0; v < NV; ++v) {
+            put(g.pre, v, s_pre + v * VEC);
+            put(g.post, v, s_post + v * VEC);
+            put(g.share, v, s_gate + v * VEC);
+        }
     }
 }
 
@@ -438,9 +549,9 @@ inline int64_t backward_threads(int32_t type, int64_t D) {
     while (nt < 1024 && vecs > nt * full) nt *= 2;
     return nt;
 }
-// The device holds 2,048 threads a CU; twice the units it holds at once.
+// A CU holds 1,024 threads of the backward kernel: one unit for each workgroup.
 inline NormUnits units_of(const ecc_norm_t *a) {
-    const int64_t target = kNormCus * 2048 / backward_threads(a->type, a->D);
+    const int64_t target = kNormCus * 1024 / backward_threads(a->type, a->D);
     const int64_t group = a->d_f && a->d_gate && a->gate_rows > 0 ? a->gate_rows : a->n;
     return norm_units(a->P, a->n, group, target);
 }
@@ -666,8 +777,21 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
         if (N > 0)
             with_row_shape<kBackwardVecs<T>, true>((D + kVec<T> - 1) / kVec<T>, [&](auto shape) {
                 constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
-                hipLaunchKernelGGL((k_norm_grad<T, NT, NV>), dim3((unsigned)ga.u.total), dim3(NT),
-                                   0, s, n, ga);
+                constexpr bool HOLD = NV <= kBackwardVecs<T> &&
+                                      !(std::is_same_v<T, double> && NT == 1024);
+                constexpr size_t lds = HOLD ? 3 * sizeof(A) * NV * kVec<T> * NT : 0;
+                static_assert(lds <= 128 << 10, "the weights of a row in LDS");
+                NormGradArgs args = ga;
+                // (the longest rows' sums lie there even where a group ends
+                // within its unit)
+                if (!HOLD && g->d_dgate) args.share = work + 2 * sums;
+                auto kernel = k_norm_grad<T, NT, NV, HOLD>;
+                if constexpr (lds > (64 << 10))
+                    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)lds);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)ga.u.total), dim3(NT), lds, s, n,
+                                   args);
             });
         const int64_t cols = (D + 63) / 64;
         if (params) {

@@ -17,8 +17,16 @@ _TYPES = {torch.float64: E.ECC_F64, torch.float32: E.ECC_F32, torch.bfloat16: E.
 _ID_TYPES = {torch.int32: E.ECC_I32, torch.int64: E.ECC_I64}
 
 
-def _stream():
-    return torch.cuda.current_stream().cuda_stream
+# The current stream's handle without the object around it (2.5 us of a call of
+# 10), where torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(t):
+    """The current stream of t's device."""
+    if _raw_stream is not None:
+        return _raw_stream(t.get_device())
+    return torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _type(t, what):
@@ -59,20 +67,20 @@ def _contiguous(t, what):
     return t
 
 
-def _out(t, shape, dtype, device, what):
-    """The caller's output, checked, or a new one."""
+def _out(t, shape, dtype, like, what):
+    """The caller's output, checked, or a new one where `like` is."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
         raise ValueError("%s must be %s of shape %s, not %s of %s" %
                          (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
     return t
 
 
-def _work(size, device):
+def _work(size, like):
     if size < 0:
         raise E.EccError(E.ECC_ERR_RANGE, "the sizes are beyond what the library supports")
-    return torch.empty(size, dtype=torch.uint8, device=device)
+    return like.new_empty(size, dtype=torch.uint8)
 
 
 # ----------------------------------------------------------------------------
@@ -96,10 +104,10 @@ def embed_lookup(table, ids, scale=1.0, dtype=None, out=None, row0=0):
     ids, id_type = _ids(ids)
     dtype = out.dtype if out is not None else dtype or table.dtype
     ot = _type(dtype, "the result")
-    out = _out(out, tuple(ids.shape) + (D,), dtype, ids.device, "out")
+    out = _out(out, tuple(ids.shape) + (D,), dtype, table, "out")
     _, ld_out = _rows(out, "out")
     E.ecc_embed_lookup(ids.numel(), V, D, row0, ids, id_type, table, tt, ld, scale, out, ot,
-                       ld_out, _stream())
+                       ld_out, _stream(table))
     return out
 
 
@@ -122,10 +130,10 @@ def embed_index(ids, V, P=1, row0=0, index=None):
         raise ValueError("%d tokens cannot be shared equally by %d workers" % (N, P))
     n = N // P
     if index is None:
-        index = EmbedIndex(P, n, V, _work(E.ecc_embed_index_size(P, n, V), ids.device))
+        index = EmbedIndex(P, n, V, _work(E.ecc_embed_index_size(P, n, V), ids))
     elif (index.P, index.n, index.V) != (P, n, V):
         raise ValueError("the index was made for other sizes")
-    E.ecc_embed_index(P, n, V, row0, ids, id_type, index.data, _stream())
+    E.ecc_embed_index(P, n, V, row0, ids, id_type, index.data, _stream(ids))
     return index
 
 
@@ -144,7 +152,7 @@ def embed_grad(index, dy, scale=1.0, grad=None, dtype=torch.float32, accumulate=
     if grad is None:
         if accumulate:
             raise ValueError("accumulate needs grad")
-        grad = torch.empty((P, V, D), dtype=dtype, device=index.data.device)
+        grad = index.data.new_empty((P, V, D), dtype=dtype)
     elif tuple(grad.shape) != (P, V, D):
         raise ValueError("grad must have shape %s, not %s" % ((P, V, D), tuple(grad.shape)))
     _on_gpu(grad, "grad")
@@ -152,12 +160,12 @@ def embed_grad(index, dy, scale=1.0, grad=None, dtype=torch.float32, accumulate=
         raise ValueError("grad must be contiguous in its last dimension")
     yt, gt = _type(dy, "dy"), _type(grad, "grad")
     if work is None:
-        work = _work(E.ecc_embed_work_size(P, n, D, yt, gt), grad.device)
+        work = _work(E.ecc_embed_work_size(P, n, D, yt, gt), grad)
     elif work.numel() * work.element_size() < E.ecc_embed_work_size(P, n, D, yt, gt):
         raise ValueError("the work buffer is too small")
     E.ecc_embed_grad(P, n, V, D, index.data, dy, yt, ld_dy, scale, grad, gt,
                      grad.stride(1) if V > 1 else D, grad.stride(0) if P > 1 else V * D,
-                     1 if accumulate else 0, work, _stream())
+                     1 if accumulate else 0, work, _stream(grad))
     return grad
 
 
@@ -224,14 +232,14 @@ def norm_forward(x, f=None, *, w_post=None, w_pre=None, gate=None, gate_rows=1, 
                        1)
     ld_xo = ld_h = 0
     if x_out is not None or f is not None or res_scale != 1.0 or w_pre is None:
-        x_out = _out(x_out, x.shape, x.dtype, x.device, "x_out")
+        x_out = _out(x_out, x.shape, x.dtype, x, "x_out")
         _, ld_xo = _rows(x_out, "x_out")
     if w_pre is not None:
-        h = _out(h, x.shape, x.dtype, x.device, "h")
+        h = _out(h, x.shape, x.dtype, x, "h")
         _, ld_h = _rows(h, "h")
     elif h is not None:
         raise ValueError("h needs w_pre")
-    E.ecc_norm_forward(a, x_out, ld_xo, h, ld_h, _stream())
+    E.ecc_norm_forward(a, x_out, ld_xo, h, ld_h, _stream(x))
     return x_out, h
 
 
@@ -265,7 +273,7 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         return t.data_ptr(), ld
 
     def rows_out(t, like, what):
-        t = _out(t, like.shape, like.dtype, like.device, what)
+        t = _out(t, like.shape, like.dtype, like, what)
         _, ld = _rows(t, what)
         return t, t.data_ptr(), ld
 
@@ -273,7 +281,7 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         if t is None:
             if accumulate:
                 raise ValueError("accumulate needs %s" % what)
-            t = torch.empty((P, stride), dtype=dtype, device=x.device)[:, :D]
+            t = x.new_empty((P, stride), dtype=dtype)[:, :D]
         elif tuple(t.shape) != (P, D) or t.dtype != dtype or (D > 1 and t.stride(1) != 1) or \
                 (P > 1 and t.stride(0) != stride):
             raise ValueError("%s must be %s of shape %s, one stride for all" %
@@ -299,10 +307,10 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         dw_pre = param(dw_pre, "dw_pre")
         g.d_dw_pre = dw_pre.data_ptr()
     if work is None:
-        work = _work(E.ecc_norm_work_size(a), x.device)
+        work = _work(E.ecc_norm_work_size(a), x)
     elif work.numel() * work.element_size() < E.ecc_norm_work_size(a):
         raise ValueError("the work buffer is too small")
-    E.ecc_norm_grad(a, g, work, _stream())
+    E.ecc_norm_grad(a, g, work, _stream(x))
     return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
 
 
@@ -336,19 +344,19 @@ def distill(z, top, idx, tau=1.0, kd_weight=1.0, ce_weight=0.0, labels=None, wei
                         None if labels is None else _contiguous(labels, "labels").data_ptr(),
                         None if weight is None else _contiguous(weight, "weight").data_ptr(),
                         tau, kd_weight, ce_weight)
-    loss = _out(loss, shape, torch.float64 if t == E.ECC_F64 else torch.float32, z.device, "loss")
+    loss = _out(loss, shape, torch.float64 if t == E.ECC_F64 else torch.float32, z, "loss")
     _contiguous(loss, "loss")
     ld_dz = 0
     if grad is True:
-        grad = torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        grad = z.new_empty(z.shape)
     if grad is not None:
-        _out(grad, z.shape, z.dtype, z.device, "grad")
+        _out(grad, z.shape, z.dtype, z, "grad")
         _, ld_dz = _rows(grad, "grad")
     size = E.ecc_distill_work_size(a)
     if work is None:
         # (a refused description has no size: the call says what is wrong)
-        work = _work(max(size, 16), z.device)
+        work = _work(max(size, 16), z)
     elif work.numel() * work.element_size() < size:
         raise ValueError("the work buffer is too small")
-    E.ecc_distill(a, loss, grad, ld_dz, work, _stream())
+    E.ecc_distill(a, loss, grad, ld_dz, work, _stream(z))
     return loss, grad
