@@ -20,9 +20,10 @@
 //    commonest hundred or two);
 //  - rows of G without tokens, by flags that the sort has left, are zeroed by
 //    further workgroups of the first launch, behind those that add (128,000
-//    rows of 4,096: 0.62 ms against 0.68 ms dealt out among them), past the
-//    caches where G exceeds the last of them (0.58 ms against 0.60 ms; 32,003
-//    rows of 2,048, which it holds: 50 us through them, 60 us past them).
+//    rows of 4,096: 0.62 ms, 0.68 ms dealt out among them), past the caches
+//    where G exceeds the last of them (112,882 rows of 2,378 fp32: 125 us,
+//    through them 175 us; 32,003 rows of 2,048, which it holds: 47 us past
+//    them, 33 us through them).
 // Every element of G is written once, by one thread, in a fixed order.
 //
 // The sort is by counting, digit by digit from the lowest: up to
@@ -411,6 +412,7 @@ struct EmbedGradArgs {
     int64_t sum_blocks;           // workgroups that add; the others zero
     int32_t zero_rows;            // rows a zeroing workgroup looks after
     int32_t stream;               // zeros pass the caches by
+    int32_t flat;                 // the rows of all workers follow each other
 };
 
 template <typename Y, typename G, typename A, int VEC>
@@ -433,14 +435,47 @@ __device__ __forceinline__ void embed_write(const EmbedGradArgs<Y, G, A> &a, uin
     r.store_upto(g, a.D - col);
 }
 
-// Zeros in the rows of workgroup `block`'s share that no token names: about
-// 16 KiB of consecutive rows, which its threads write side by side.
+// Zeros in the rows that no token names, workgroup `block`'s share of them.
+// Where all rows follow each other (a.flat), that is kZeroBytes of memory in
+// 16-byte accesses at 16-byte boundaries wherever the rows begin, or element by
+// element where some of the rows there have tokens; otherwise zero_rows rows,
+// which the threads write side by side.
+constexpr int kZeroBytes = 16384;
+
 template <bool STREAM, typename Y, typename G, typename A>
 __device__ __forceinline__ void embed_zero(const EmbedGradArgs<Y, G, A> &a, int64_t block) {
     constexpr int W = kVec<G>;
     Raw<G, W> zero;
 #pragma unroll
     for (int i = 0; i < Raw<G, W>::kWords; ++i) zero.w[i] = 0;
+    if (a.flat) {
+        constexpr int U = kZeroBytes / 16 / kEmbedThreads;
+        const int64_t e0 = block * (kZeroBytes / (int)sizeof(G));
+        const uint32_t count =
+            (uint32_t)min((int64_t)(kZeroBytes / (int)sizeof(G)), a.rows * a.D - e0);
+        const int64_t row0 = e0 / a.D;
+        const uint32_t D = (uint32_t)a.D, in0 = (uint32_t)(e0 - row0 * a.D);
+        G *const g = a.grad + e0;
+        // the rows of the workgroup's share: none with tokens, or all?
+        const uint32_t n = (in0 + count - 1) / D + 1, lane = threadIdx.x & 63;
+        bool none = a.touched == nullptr;
+        if (!none && n <= 64) {
+            const uint64_t with = __ballot(lane < n && a.touched[row0 + (lane < n ? lane : 0)]);
+            if ((uint32_t)__popcll(with) == n) return;
+            none = with == 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t at = (u * kEmbedThreads + threadIdx.x) * W;  // from e0 on
+            if (none && at + W <= count) {
+                zero.template store<STREAM>(g + at);
+                continue;
+            }
+            for (uint32_t i = at; i < at + W && i < count; ++i)
+                if (none || !a.touched[row0 + (in0 + i) / D]) store_elem<A>(g + i, (A)0);
+        }
+        return;
+    }
     // as many neighbouring threads to a row as it has accesses, or all
     int lg = 0;
     while (lg < 8 && ((int64_t)W << lg) < a.D) ++lg;
@@ -945,8 +980,12 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t per_block = kEmbedThreads >> g.log2_lanes;
     const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
     const int64_t rows = (int64_t)P * V;
-    const int64_t zero_rows = std::max<int64_t>({1, 16384 / (D * gb), rows >> 22});
-    const int64_t zero_blocks = accumulate ? 0 : (rows + zero_rows - 1) / zero_rows;
+    const int64_t zero_rows = std::max<int64_t>({1, kZeroBytes / (D * gb), rows >> 22});
+    const bool flat = ld_grad == D && (P == 1 || worker_stride == V * D) &&
+                      (uintptr_t)d_grad % 16 == 0;
+    const int64_t zero_blocks = accumulate ? 0
+                                : flat     ? (rows * D * gb + kZeroBytes - 1) / kZeroBytes
+                                           : (rows + zero_rows - 1) / zero_rows;
     if (sum_blocks + zero_blocks > 0x7fffff) {
         set_error("P * n * D or P * V is too large for one launch");
         return ECC_ERR_RANGE;
@@ -980,6 +1019,7 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
             a.touched = n > 0 ? (const uint8_t *)d_index + l.touched : nullptr;
             a.zero_rows = (int32_t)zero_rows;
             a.stream = rows * D * gb > kCacheBytes;
+            a.flat = flat;
             const dim3 grid((unsigned)(sum_blocks + zero_blocks));
             if (g.log2_lanes == 6)
                 hipLaunchKernelGGL((k_embed_sum<Y, G, A, true>), grid, dim3(kEmbedThreads), 0, s,
