@@ -688,10 +688,11 @@ inline int64_t work_bytes(const ecc_distill_t *a) {
 // each, up to 1,024.  16 vectors leave 16 waves to a CU, four rows of 32,000
 // bf16 logits at a time (16,384 rows, temperature 2 with hard labels: 0.43 ms,
 // against 0.46 ms with 512 threads and 4 vectors; 131,072 logits: 1.77 ms,
-// against 1.97 ms with 8 vectors, and the rest read twice in both).  Rows of
-// up to 4 vectors a thread fill the CU with more waves (100,000 rows of 1,000:
-// 0.15 against 0.30 ms).  fp64, whose exponentials need registers, holds half
-// as many in half as many threads.
+// against 1.97 ms with 8 vectors, and the rest read twice in both; since
+// then, with accesses past the caches, 0.38 and 1.68 ms, 5.4 and 5.0 TB/s).
+// Rows of up to 4 vectors a thread fill the CU with more waves (100,000 rows of
+// 1,000: 0.15 against 0.30 ms).  fp64, whose exponentials need registers,
+// holds half as many in half as many threads.
 template <typename T, int MODE>
 void launch_distill(const DistillArgs &a, int64_t N, hipStream_t s) {
     const size_t lds = entries_bytes<Acc<T>>(a.K);
