@@ -715,7 +715,9 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
  *     P > 1);
  *   a parameter of D elements of type w_type    gate_rows = 0.
  * x, f and gate rows are of element type `type`, w_post, w_pre and a
- * parameter gate of w_type.  h is formed from x' before x' is rounded.
+ * parameter gate of w_type.  h is formed from x' before x' is rounded.  A
+ * row's squares are added in fp32 (fp64 for ECC_F64): their sum must lie
+ * within its range.
  * P, D >= 1, n >= 0, eps > 0; D up to ECC_NORM_MAX_DIM (half of that for
  * ECC_F64), else ECC_ERR_RANGE. */
 #define ECC_NORM_MAX_DIM 16384
@@ -791,7 +793,7 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
  *   d_labels int32 [N] or NULL; d_weight fp32 [N] or NULL.
  *   d_loss   [N] of fp32, fp64 when type is ECC_F64.
  * A weight of 0 leaves its term out.  V in [1, 2^31 - 1), N in [0, 2^31 -
- * 1), tau > 0.  d_work: ecc_distill_work_size(a) bytes (-1 for a
+ * 1), tau in [1e-15, 1e15].  d_work: ecc_distill_work_size(a) bytes (-1 for a
  * description that the call refuses). */
 #define ECC_DISTILL_MAX_TOP 1024
 typedef struct {

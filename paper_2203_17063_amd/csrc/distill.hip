@@ -658,7 +658,7 @@ static ecc_status_t check_distill(const ecc_distill_t *a) {
     ECC_ARG(a->N >= 0 && a->V >= 1, "N must be >= 0, V >= 1");
     ECC_ARG(a->K >= 0 && a->K <= kTopMax, "K = %d must lie in [0, %d]", a->K, kTopMax);
     ECC_ARG(known_type(a->type) && known_type(a->top_type), "unknown element type");
-    ECC_ARG(a->tau > 0.0 && a->tau <= 1e30, "tau must be positive");
+    ECC_ARG(a->tau >= 1e-15 && a->tau <= 1e15, "tau must lie in [1e-15, 1e15]");
     const int64_t lim = (int64_t(1) << 31) - 1;
     if (a->N >= lim || a->V >= lim || a->ld_z >= (int64_t(1) << 40)) {
         set_error("N or V is too large");

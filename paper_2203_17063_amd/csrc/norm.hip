@@ -395,8 +395,9 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
         row_sums<NT>(s, s_red, half);
         const A q = pre ? rsqrt_(fma_(s[0], inv_d, eps)) : (A)0;
         const A k = post ? rsqrt_(fma_(s[1], inv_d, eps)) : (A)1;
-        const A c = q * q * q * s[2] * inv_d;
-        const A m = post ? k * k * inv_d * (s[3] + q * s[4] - c * s[5]) : (A)0;
+        // (the sums first: the cube of a norm factor alone may pass the type's range)
+        const A c = s[2] * inv_d * q * q * q;
+        const A m = post ? (s[3] + q * s[4] - c * s[5]) * inv_d * k * k : (A)0;
         const bool group_end = row_gate && !u.split &&
                                ((row + 1) % a.gate_rows == 0 || row + 1 == r1);
         const bool group_begin = row == r0 || (row_gate && !u.split && row % a.gate_rows == 0);

@@ -256,12 +256,14 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
     df may be f or dh."""
     a, N, D, w_dtype = _norm(x, f, w_post, w_pre, gate, gate_rows, res_scale, branch_scale, eps,
                              offset, P)
+    for t, of, what in ((df, f, "df"), (dgate, gate, "dgate"), (dw_post, w_post, "dw_post"),
+                        (dw_pre, w_pre, "dw_pre")):
+        if t is not None and of is None:
+            raise ValueError("%s given without its operand" % what)
     given = [t for t in (dw_post, dw_pre, dgate if gate is not None and gate_rows == 0 else None)
              if t is not None]
     dtype = given[0].dtype if given else dtype or w_dtype
     stride = given[0].stride(0) if given and P > 1 else D
-    g = E.ecc_norm_grad_t(grad_type=_type(dtype, "the gradients"),
-                          accumulate=1 if accumulate else 0, worker_stride=stride)
 
     def rows_in(t, what):
         if t is None:
@@ -273,7 +275,10 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         return t.data_ptr(), ld
 
     def rows_out(t, like, what):
-        t = _out(t, like.shape, like.dtype, like, what)
+        if t is None:
+            t = torch.empty_like(like, memory_format=torch.contiguous_format)
+            return t, t.data_ptr(), D
+        _out(t, like.shape, like.dtype, like, what)
         _, ld = _rows(t, what)
         return t, t.data_ptr(), ld
 
@@ -281,31 +286,37 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         if t is None:
             if accumulate:
                 raise ValueError("accumulate needs %s" % what)
-            t = x.new_empty((P, stride), dtype=dtype)[:, :D]
-        elif tuple(t.shape) != (P, D) or t.dtype != dtype or (D > 1 and t.stride(1) != 1) or \
+            t = x.new_empty((P, stride), dtype=dtype)
+            return t if stride == D else t[:, :D]
+        if tuple(t.shape) != (P, D) or t.dtype != dtype or (D > 1 and t.stride(1) != 1) or \
                 (P > 1 and t.stride(0) != stride):
             raise ValueError("%s must be %s of shape %s, one stride for all" %
                              (what, dtype, (P, D)))
         _on_gpu(t, what)
         return t
 
-    g.d_dh, g.ld_dh = rows_in(dh, "dh")
-    g.d_dx_out, g.ld_dx_out = rows_in(dx_out, "dx_out")
-    dx, g.d_dx, g.ld_dx = rows_out(dx, x, "dx")
+    d_dh, ld_dh = rows_in(dh, "dh")
+    d_dxo, ld_dxo = rows_in(dx_out, "dx_out")
+    dx, d_dx, ld_dx = rows_out(dx, x, "dx")
+    d_df = d_dgate = d_post = d_pre = None
+    ld_df = ld_dgate = 0
     if f is not None:
-        df, g.d_df, g.ld_df = rows_out(df, f, "df")
+        df, d_df, ld_df = rows_out(df, f, "df")
     if gate is not None:
         if gate_rows:
-            dgate, g.d_dgate, g.ld_dgate = rows_out(dgate, gate, "dgate")
+            dgate, d_dgate, ld_dgate = rows_out(dgate, gate, "dgate")
         else:
             dgate = param(dgate, "dgate")
-            g.d_dgate = dgate.data_ptr()
+            d_dgate = dgate.data_ptr()
     if w_post is not None:
         dw_post = param(dw_post, "dw_post")
-        g.d_dw_post = dw_post.data_ptr()
+        d_post = dw_post.data_ptr()
     if w_pre is not None:
         dw_pre = param(dw_pre, "dw_pre")
-        g.d_dw_pre = dw_pre.data_ptr()
+        d_pre = dw_pre.data_ptr()
+    g = E.ecc_norm_grad_t(d_dh, ld_dh, d_dxo, ld_dxo, d_dx, ld_dx, d_df, ld_df, d_dgate, ld_dgate,
+                          d_post, d_pre, _type(dtype, "the gradients"), 1 if accumulate else 0,
+                          stride)
     if work is None:
         work = _work(E.ecc_norm_work_size(a), x)
     elif work.numel() * work.element_size() < E.ecc_norm_work_size(a):

@@ -328,6 +328,42 @@ def test_grad_accumulate_in_contributions():
     assert torch.equal(contrib, expect)
 
 
+def test_grad_zero_rows():
+    """Rows of zeros, with an eps whose norm factor has a cube beyond fp32: the
+    gradient is the incoming one times the weight and the factor."""
+    lm = _lm()
+    announce("norm grad, zero rows")
+    x = torch.zeros((4, 50), device="cuda")
+    x[2] = 1.0
+    w = torch.full((50,), 2.0, device="cuda")
+    dh = torch.full((4, 50), 3.0, device="cuda")
+    g = lm.norm_grad(x, x.clone(), dh, None, w_post=w, w_pre=w, eps=1e-30)
+    assert torch.isfinite(g["dx"]).all()
+    assert torch.allclose(g["dx"][[0, 1, 3]], torch.full((3, 50), 6e15, device="cuda"), rtol=1e-5)
+    assert torch.isfinite(g["dw_pre"]).all() and torch.isfinite(g["dw_post"]).all()
+
+
+@pytest.mark.parametrize("act,D", [(BF16, 8192), (BF16, 10000), (F64, 3000)])
+def test_grad_wide_rows_in_a_graph(act, D):
+    """Shapes whose weights fill more LDS than a kernel has by default, and those
+    that keep none there, captured and replayed."""
+    lm = _lm()
+    announce("norm grad, wide rows in a graph", act, D)
+    s = _gpu_args(_inputs(40, D, act, F32 if act != F64 else F64, "rows", gate_rows=8))
+    dh, dxo = _random((40, D), act, 90).cuda(), _random((40, D), act, 91).cuda()
+    lm.norm_grad(**s, dh=dh, dx_out=dxo)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = lm.norm_grad(**s, dh=dh, dx_out=dxo)
+    for k in range(3):
+        s["x"].copy_(_random((40, D), act, 95 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = lm.norm_grad(**s, dh=dh, dx_out=dxo)
+        assert all(torch.equal(got[k], want[k]) for k in want)
+
+
 def test_grad_no_rows():
     lm = _lm()
     announce("norm grad, no rows")
