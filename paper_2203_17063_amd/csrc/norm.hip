@@ -7,7 +7,8 @@
 // A workgroup holds a row in registers: it reads every operand of the row
 // once and writes every result once, and the weights are read once per
 // workgroup, which walks several rows.  The workgroup is as wide as makes a
-// thread hold 16 elements of the row (backward 8, for its registers).
+// thread hold 16 elements of the row (backward 8, for its registers); of rows
+// that 8, 16 or 32 lanes hold, a wave takes 8, 4 or 2 at a time.
 //
 // Forward has two sums per row, that of f^2 and then that of x'^2 (formed
 // from the squares themselves: as a combination of sums over x and f they
@@ -74,12 +75,33 @@ __device__ __forceinline__ double read_lane(double v, int lane) {
                             __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
 
+// The sum over every N = 8, 16 or 32 neighbouring lanes, in all of them.
+template <int N, typename A>
+__device__ __forceinline__ A lanes_sum(A v) {
+    if constexpr (std::is_same_v<A, float>) {
+        v += dpp_f32<kDppQuadXor1>(v);
+        v += dpp_f32<kDppQuadXor2>(v);
+        v += dpp_f32<kDppRowHalfMirror>(v);
+        if constexpr (N >= 16) v += dpp_f32<kDppRowMirror>(v);
+        if constexpr (N >= 32) v += __shfl_xor(v, 16, 64);
+        return v;
+    } else {
+        return group_sum<N>(v);
+    }
+}
+
 // K sums over the workgroup's NT threads, in every thread.  s holds [2][NT /
 // 64][K]; the two halves are used in turn, so that one barrier is enough:
 // a half is written again only after every wave has passed the barrier of
 // the other, and so has read this one.
-template <int NT, int K, typename A>
+// With LANES < 64 (NT = 64) the sums are those of every LANES neighbours.
+template <int NT, int LANES, int K, typename A>
 __device__ __forceinline__ void row_sums(A (&v)[K], A *s, int &half) {
+    if constexpr (LANES < 64) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = lanes_sum<LANES>(v[k]);
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = wave_all(v[k], OpSum{});
     if constexpr (NT > 64) {
@@ -113,20 +135,24 @@ __device__ __forceinline__ void row_sums(A (&v)[K], A *s, int &half) {
     }
 }
 
-template <typename T, int NT, int NV>
+template <typename T, int NT, int NV, int LANES>
 __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, int64_t ld_x_out,
                                                      void *h_out, int64_t ld_h) {
     using A = Acc<T>;
     constexpr int VEC = kVec<T>, E = NV * VEC;
     __shared__ A s_red[2 * (NT / 64)];
     int half = 0;
+    // the rows of a pass, this thread's among them, its place in it
+    constexpr int AT_ONCE = NT / LANES;
+    const int sub = AT_ONCE == 1 ? 0 : threadIdx.x / LANES;
+    const uint32_t tid = AT_ONCE == 1 ? threadIdx.x : threadIdx.x % LANES;
     const A res = (A)a.res, branch = (A)a.branch, eps = (A)a.eps, inv_d = (A)1 / (A)a.D;
     A wq[E], wp[E];  // branch scale, parameter gate and post-norm weight; pre-norm weight
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int64_t c = ((int64_t)v * NT + threadIdx.x) * VEC + i;
+            const int64_t c = ((int64_t)v * NT + tid) * VEC + i;
             A q = branch, p = (A)0;
             if (c < a.D) {
                 if (a.w_post) q *= (A)a.offset + load_typed<A>(a.w_post, a.w_type, c);
@@ -136,7 +162,11 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
             wq[v * VEC + i] = q;
             wp[v * VEC + i] = p;
         }
-    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+    for (int64_t first = (int64_t)blockIdx.x * AT_ONCE; first < a.N;
+         first += (int64_t)gridDim.x * AT_ONCE) {
+        // (lanes past the last row go along with it and write nothing)
+        const bool live = AT_ONCE == 1 || first + sub < a.N;
+        const int64_t row = live ? first + sub : a.N - 1;
         const T *x = reinterpret_cast<const T *>(a.x) + row * a.ld_x;
         const T *f = reinterpret_cast<const T *>(a.f) + row * a.ld_f;
         const bool row_gate = a.gate && a.gate_rows > 0;
@@ -145,7 +175,7 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
         Raw<T, VEC> rx[NV], rf[NV], rg[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const uint32_t c = (v * NT + threadIdx.x) * VEC;
+            const uint32_t c = (v * NT + tid) * VEC;
             rx[v].load_upto(x + c, (int32_t)a.D - (int32_t)c);
             if (a.f) rf[v].load_upto(f + c, (int32_t)a.D - (int32_t)c);
             if (row_gate) rg[v].load_upto(g + c, (int32_t)a.D - (int32_t)c);
@@ -159,7 +189,7 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
                 const A t = rf[e / VEC].template get<A>(e % VEC);
                 sum[0] = fma_(t, t, sum[0]);
             }
-            row_sums<NT>(sum, s_red, half);
+            row_sums<NT, LANES>(sum, s_red, half);
             k = rsqrt_(fma_(sum[0], inv_d, eps));
         }
 #pragma unroll
@@ -175,31 +205,31 @@ __global__ __launch_bounds__(NT) void k_norm_forward(NormArgs a, void *x_out, in
             T *o = reinterpret_cast<T *>(x_out) + row * ld_x_out;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const uint32_t c = (v * NT + threadIdx.x) * VEC;
+                const uint32_t c = (v * NT + tid) * VEC;
                 A t[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i];
                 Raw<T, VEC> r;
                 r.set_all(t);
-                r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
+                if (live) r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
             }
         }
         if (h_out) {
             A sum[1] = {(A)0};
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[0] = fma_(y[e], y[e], sum[0]);
-            row_sums<NT>(sum, s_red, half);
+            row_sums<NT, LANES>(sum, s_red, half);
             const A q = rsqrt_(fma_(sum[0], inv_d, eps));
             T *o = reinterpret_cast<T *>(h_out) + row * ld_h;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const uint32_t c = (v * NT + threadIdx.x) * VEC;
+                const uint32_t c = (v * NT + tid) * VEC;
                 A t[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) t[i] = y[v * VEC + i] * q * wp[v * VEC + i];
                 Raw<T, VEC> r;
                 r.set_all(t);
-                r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
+                if (live) r.store_upto(o + c, (int32_t)a.D - (int32_t)c);
             }
         }
     }
@@ -217,7 +247,7 @@ inline NormUnits norm_units(int64_t P, int64_t n, int64_t group, int64_t target)
     NormUnits u{};
     u.n = n;
     u.group = std::max<int64_t>(1, std::min(group, n));
-    const int64_t want = std::max<int64_t>(4, (P * n + target - 1) / target);
+    const int64_t want = std::max<int64_t>(1, (P * n + target - 1) / target);
     if (want >= u.group) {
         u.rows = want / u.group * u.group;
         u.per_group = 1;
@@ -248,7 +278,7 @@ struct NormGradArgs {
 // (in registers, 173 of them for a row of 4,096 bf16, one workgroup filled a
 // CU: 129 us for 8,192 such rows, 95 us with two).  Otherwise (the longest
 // rows) both are read again, and the sums over rows stay in the work buffer.
-template <typename T, int NT, int NV, bool HOLD>
+template <typename T, int NT, int NV, bool HOLD, int LANES>
 __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) void k_norm_grad(NormArgs a, NormGradArgs g) {
     using A = Acc<T>;
     constexpr int VEC = kVec<T>, KEEP = HOLD ? NV : 1;
@@ -257,6 +287,10 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
     extern __shared__ double s_weights[];  // [3][NV * CH][NT] quads
     __shared__ A s_red[2 * (NT / 64) * 6];
     int half = 0;
+    // rows at a time (several only where no gate row is shared by a few)
+    constexpr int AT_ONCE = NT / LANES;
+    const int sub = AT_ONCE == 1 ? 0 : threadIdx.x / LANES;
+    const uint32_t tid = AT_ONCE == 1 ? threadIdx.x : threadIdx.x % LANES;
     const A res = (A)a.res, branch = (A)a.branch, eps = (A)a.eps, inv_d = (A)1 / (A)a.D;
     const bool post = a.f && a.w_post, pre = a.w_pre != nullptr;
     const bool row_gate = a.f && a.gate && a.gate_rows > 0;
@@ -280,7 +314,7 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
     auto read_weights = [&](int which, int v, int c, A(&w)[Q]) {
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            const int64_t col = ((int64_t)v * NT + threadIdx.x) * VEC + c * Q + i;
+            const int64_t col = ((int64_t)v * NT + tid) * VEC + c * Q + i;
             w[i] = which == 0 ? (A)1 : which == 1 ? (A)0 : branch;
             if (col < a.D) {
                 if (which == 0 && post)
@@ -317,8 +351,8 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
         Raw<T, VEC> x, f, gate, dh, dxo;
     };
     auto fetch = [&](int64_t row, int v, Operands &o) {
-        const uint32_t c = (v * NT + threadIdx.x) * VEC;
-        const int32_t left = (int32_t)a.D - (int32_t)c;
+        const uint32_t c = (v * NT + tid) * VEC;
+        const int32_t left = AT_ONCE == 1 || row < r1 ? (int32_t)a.D - (int32_t)c : 0;
 #pragma unroll
         for (int i = 0; i < Raw<T, VEC>::kWords; ++i)
             o.x.w[i] = o.f.w[i] = o.gate.w[i] = o.dh.w[i] = o.dxo.w[i] = 0;
@@ -340,14 +374,14 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
 #pragma unroll
     for (int e = 0; e < KEEP * VEC; ++e) s_pre[e] = s_post[e] = s_gate[e] = (A)0;
     auto get = [&](const void *from, int v, bool first, A *sum) {
-        const uint32_t c = (v * NT + threadIdx.x) * VEC;
+        const uint32_t c = (v * NT + tid) * VEC;
         Raw<A, VEC> r;
         if (from && !first) r.load_upto(reinterpret_cast<const A *>(from) + at + c, (int32_t)a.D - (int32_t)c);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) sum[i] = from && !first ? r.template get<A>(i) : (A)0;
     };
     auto put = [&](void *to, int v, const A *sum) {
-        const uint32_t c = (v * NT + threadIdx.x) * VEC;
+        const uint32_t c = (v * NT + tid) * VEC;
         if (!to) return;
         A t[VEC];
 #pragma unroll
@@ -358,7 +392,9 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
     };
     constexpr int UNROLL = HOLD ? NV : 1;
     Operands op[KEEP];
-    for (int64_t row = r0; row < r1; ++row) {
+    for (int64_t first = r0; first < r1; first += AT_ONCE) {
+        const int64_t row = first + sub;
+        const bool live = AT_ONCE == 1 || row < r1;
         if constexpr (HOLD)
 #pragma unroll
             for (int v = 0; v < NV; ++v) fetch(row, v, op[v]);
@@ -392,7 +428,7 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
                 __builtin_amdgcn_sched_barrier(0);  // a quad's weights at a time
             }
         }
-        row_sums<NT>(s, s_red, half);
+        row_sums<NT, LANES>(s, s_red, half);
         const A q = pre ? rsqrt_(fma_(s[0], inv_d, eps)) : (A)0;
         const A k = post ? rsqrt_(fma_(s[1], inv_d, eps)) : (A)1;
         // (the sums first: the cube of a norm factor alone may pass the type's range)
@@ -403,8 +439,8 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
         const bool group_begin = row == r0 || (row_gate && !u.split && row % a.gate_rows == 0);
 #pragma unroll UNROLL
         for (int v = 0; v < NV; ++v) {
-            const uint32_t col = (v * NT + threadIdx.x) * VEC;
-            const int32_t left = (int32_t)a.D - (int32_t)col;
+            const uint32_t col = (v * NT + tid) * VEC;
+            const int32_t left = live ? (int32_t)a.D - (int32_t)col : 0;
             if constexpr (!HOLD) {
                 fetch(row, v, op[0]);
                 get(g.pre, v, row == r0, s_pre);
@@ -455,6 +491,18 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
             }
         }
     }
+    if constexpr (AT_ONCE > 1) {
+        // the wave's rows together
+#pragma unroll
+        for (int e = 0; e < KEEP * VEC; ++e)
+#pragma unroll
+            for (int o = LANES; o < 64; o <<= 1) {
+                s_pre[e] += __shfl_xor(s_pre[e], o, 64);
+                s_post[e] += __shfl_xor(s_post[e], o, 64);
+                s_gate[e] += __shfl_xor(s_gate[e], o, 64);
+            }
+        if (sub > 0) return;
+    }
     if constexpr (HOLD) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -466,9 +514,10 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
 }
 
 // Sums of consecutive units: result j (of `count`) adds units [j per, (j + 1)
-// per) of up to three arrays of [units][D] sums.  A workgroup takes 64
-// columns of a result; its waves take every 16th unit each, and their sums
-// are added in order.
+// per) of up to three arrays of [units][D] sums.  A workgroup takes COLS
+// columns of a result: 64, 16 where that would leave under 64 workgroups
+// (28,651 rows of 85 fp64: 60.5 us with 64, 40.9 with 16).  Its groups of COLS
+// lanes take every SLOTS-th unit each, and their sums are added in order.
 struct NormJoin {
     const void *from[3];
     void *to[3];
@@ -479,13 +528,13 @@ struct NormJoin {
 };
 constexpr int kNormJoinThreads = 1024;
 
-template <typename A>
+template <typename A, int COLS>
 __global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
-    constexpr int NW = kNormJoinThreads / 64, U = 8;
-    __shared__ A s_part[NW][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t cols = (a.D + 63) / 64;
-    const int64_t j = blockIdx.x / cols, c = blockIdx.x % cols * 64 + lane;
+    constexpr int SLOTS = kNormJoinThreads / COLS, U = 8;
+    __shared__ A s_part[SLOTS][COLS];
+    const int lane = threadIdx.x % COLS, slot = threadIdx.x / COLS;
+    const int64_t cols = (a.D + COLS - 1) / COLS;
+    const int64_t j = blockIdx.x / cols, c = blockIdx.x % cols * COLS + lane;
     const int z = blockIdx.y;
     const A *from = reinterpret_cast<const A *>(z == 0 ? a.from[0] : z == 1 ? a.from[1]
                                                                            : a.from[2]);
@@ -494,20 +543,20 @@ __global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
     const int32_t type = z == 0 ? a.type[0] : z == 1 ? a.type[1] : a.type[2];
     if (!to) return;
     A sum = (A)0;
-    for (int64_t i = wave; i < a.per; i += NW * U) {
+    for (int64_t i = slot; i < a.per; i += SLOTS * U) {
         A t[U];
 #pragma unroll
         for (int s = 0; s < U; ++s) {
-            const int64_t at = i + s * NW;
+            const int64_t at = i + s * SLOTS;
             t[s] = at < a.per && c < a.D ? from[(j * a.per + at) * a.D + c] : (A)0;
         }
 #pragma unroll
         for (int s = 0; s < U; ++s) sum += t[s];
     }
-    s_part[wave][lane] = sum;
+    s_part[slot][lane] = sum;
     __syncthreads();
-    if (wave == 0 && c < a.D) {
-        for (int w = 1; w < NW; ++w) sum += s_part[w][lane];
+    if (slot == 0 && c < a.D) {
+        for (int w = 1; w < SLOTS; ++w) sum += s_part[w][lane];
         store_param<A>(to, type, j * ld + c, sum, a.accumulate);
     }
 }
@@ -518,14 +567,19 @@ __global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
 
 // Calls f with the thread count and vectors per thread that hold a row: the
 // narrowest workgroup whose threads hold up to FULL vectors each, beyond 1,024
-// threads (WIDER) twice as many.
-template <int NT, int NV>
+// threads (WIDER) twice as many; where `several` rows may share a wave, as few
+// lanes as hold a row (308,420 rows of 106 bf16: 190 us backward, 348 us with a
+// wave to a row).
+template <int NT, int NV, int LANES = NT>
 struct RowShape {
-    static constexpr int nt = NT, nv = NV;
+    static constexpr int nt = NT, nv = NV, lanes = LANES;
 };
 template <int FULL, bool WIDER, typename F>
-void with_row_shape(int64_t vecs, F &&f) {
-    if (FULL > 1 && vecs <= 64 * (FULL / 2)) f(RowShape<64, (FULL > 1 ? FULL / 2 : 1)>{});
+void with_row_shape(int64_t vecs, bool several, F &&f) {
+    if (several && vecs <= 8) f(RowShape<64, 1, 8>{});
+    else if (several && vecs <= 16) f(RowShape<64, 1, 16>{});
+    else if (several && vecs <= 32) f(RowShape<64, 1, 32>{});
+    else if (FULL > 1 && vecs <= 64 * (FULL / 2)) f(RowShape<64, (FULL > 1 ? FULL / 2 : 1)>{});
     else if (vecs <= 64 * FULL) f(RowShape<64, FULL>{});
     else if (vecs <= 128 * FULL) f(RowShape<128, FULL>{});
     else if (vecs <= 256 * FULL) f(RowShape<256, FULL>{});
@@ -651,11 +705,14 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
                a->w_offset, a->res_scale, a->branch_scale, a->eps};
     with_type(a->type, [&](auto t) {
         using T = decltype(t);
-        with_row_shape<kForwardVecs<T>, false>((a->D + kVec<T> - 1) / kVec<T>, [&](auto shape) {
+        const int64_t vecs = (a->D + kVec<T> - 1) / kVec<T>;
+        with_row_shape<kForwardVecs<T>, false>(vecs, true, [&](auto shape) {
             constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
-            const int64_t grid = std::min<int64_t>(N, kNormCus * (2048 / NT));
-            hipLaunchKernelGGL((k_norm_forward<T, NT, NV>), dim3((unsigned)grid), dim3(NT), 0,
-                               (hipStream_t)hip_stream, n, d_x_out, ld_x_out, d_h, ld_h);
+            constexpr int LANES = decltype(shape)::lanes;
+            const int64_t grid = std::min<int64_t>((N + NT / LANES - 1) / (NT / LANES),
+                                                   kNormCus * (2048 / NT));
+            hipLaunchKernelGGL((k_norm_forward<T, NT, NV, LANES>), dim3((unsigned)grid), dim3(NT),
+                               0, (hipStream_t)hip_stream, n, d_x_out, ld_x_out, d_h, ld_h);
         });
     });
     ECC_LAUNCH_CHECK();
@@ -775,9 +832,12 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
         const bool gate_sums = g->d_dgate && (!row_gate || ga.u.split);
         ga.share = gate_sums ? work + 2 * sums : nullptr;
         ga.dgate = row_gate && !ga.u.split ? g->d_dgate : nullptr;
+        // (a shared gate row's sum is one wave's, row by row)
+        const bool several = !(a->d_f && a->d_gate) || a->gate_rows <= 1;
         if (N > 0)
-            with_row_shape<kBackwardVecs<T>, true>((D + kVec<T> - 1) / kVec<T>, [&](auto shape) {
+            with_row_shape<kBackwardVecs<T>, true>((D + kVec<T> - 1) / kVec<T>, several, [&](auto shape) {
                 constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
+                constexpr int LANES = decltype(shape)::lanes;
                 constexpr bool HOLD = NV <= kBackwardVecs<T> &&
                                       !(std::is_same_v<T, double> && NT == 1024);
                 constexpr size_t lds = HOLD ? 3 * sizeof(A) * NV * kVec<T> * NT : 0;
@@ -786,7 +846,7 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
                 // (the longest rows' sums lie there even where a group ends
                 // within its unit)
                 if (!HOLD && g->d_dgate) args.share = work + 2 * sums;
-                auto kernel = k_norm_grad<T, NT, NV, HOLD>;
+                auto kernel = k_norm_grad<T, NT, NV, HOLD, LANES>;
                 if constexpr (lds > (64 << 10))
                     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                               hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -794,7 +854,16 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
                 hipLaunchKernelGGL(kernel, dim3((unsigned)ga.u.total), dim3(NT), lds, s, n,
                                    args);
             });
-        const int64_t cols = (D + 63) / 64;
+        auto join = [&](const NormJoin &j, int arrays) {
+            const int64_t wide = (D + 63) / 64 * j.count;
+            if (wide >= 64)
+                hipLaunchKernelGGL((k_norm_join<A, 64>), dim3((unsigned)wide, arrays),
+                                   dim3(kNormJoinThreads), 0, s, j);
+            else
+                hipLaunchKernelGGL((k_norm_join<A, 16>),
+                                   dim3((unsigned)((D + 15) / 16 * j.count), arrays),
+                                   dim3(kNormJoinThreads), 0, s, j);
+        };
         if (params) {
             NormJoin j{};
             j.from[0] = ga.pre;
@@ -811,8 +880,7 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
             j.per = ga.u.per_worker;
             j.count = a->P;
             j.D = D;
-            hipLaunchKernelGGL(k_norm_join<A>, dim3((unsigned)(a->P * cols), 3),
-                               dim3(kNormJoinThreads), 0, s, j);
+            join(j, 3);
         }
         if (row_gate && ga.u.split && N > 0) {
             NormJoin j{};
@@ -823,8 +891,7 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
             j.per = ga.u.per_group;
             j.count = gate_n;
             j.D = D;
-            hipLaunchKernelGGL(k_norm_join<A>, dim3((unsigned)(gate_n * cols), 1),
-                               dim3(kNormJoinThreads), 0, s, j);
+            join(j, 1);
         }
     });
     ECC_LAUNCH_CHECK();
