@@ -21,9 +21,10 @@
 //  - rows of G without tokens, by flags that the sort has left, are zeroed by
 //    further workgroups of the first launch, behind those that add (128,000
 //    rows of 4,096: 0.62 ms, 0.68 ms dealt out among them), past the caches
-//    where G exceeds the last of them (112,882 rows of 2,378 fp32: 125 us,
-//    through them 175 us; 32,003 rows of 2,048, which it holds: 47 us past
-//    them, 33 us through them).
+//    where G exceeds the last of them (29,436 rows of 2,378 fp32: 48 us, through
+//    them 60 us; 32,003 rows of 2,048, which it holds: 47 us past them, 33 us
+//    through them), but not where most of a much larger G is zeros (136,669
+//    rows of 2,378: 246 us past them, 225 us through them; equal near 0.6 GB).
 // Every element of G is written once, by one thread, in a fixed order.
 //
 // The sort is by counting, digit by digit from the lowest: up to
@@ -731,6 +732,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_embed_join(EmbedGradArgs<Y, G,
 // host
 // ---------------------------------------------------------------------------
 constexpr int64_t kCacheBytes = 256 << 20;       // the device's last cache
+constexpr int64_t kManyZeros = 640 << 20;        // surely zeros: through the caches again
 constexpr int64_t kMaxDim = int64_t(1) << 22;  // columns of a gradient
 
 inline int64_t round16(int64_t bytes) { return (bytes + 15) & ~int64_t(15); }
@@ -981,12 +983,12 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
     const int64_t rows = (int64_t)P * V;
     const int64_t zero_rows = std::max<int64_t>({1, kZeroBytes / (D * gb), rows >> 22});
-    // (rows of at least a workgroup's share that begin at 16-byte boundaries are
-    // written as rows: 128,000 of 16 KiB 575 us with the sums, flat 602 us;
-    // 112,882 of 9,512 bytes 125 us flat, as rows 185 us)
+    // (rows of one workgroup's share up to two that begin at 16-byte boundaries
+    // are written as rows: 128,000 of 16 KiB 631 us with the sums, flat 646 us;
+    // 47,988 of 44,736 bytes 354 us flat, as rows 408 us)
     const bool flat = ld_grad == D && (P == 1 || worker_stride == V * D) &&
                       (uintptr_t)d_grad % 16 == 0 &&
-                      (D * gb < kZeroBytes || D * gb % 16 != 0);
+                      (D * gb < kZeroBytes || D * gb >= 2 * kZeroBytes || D * gb % 16 != 0);
     const int64_t zero_blocks = accumulate ? 0
                                 : flat     ? (rows * D * gb + kZeroBytes - 1) / kZeroBytes
                                            : (rows + zero_rows - 1) / zero_rows;
@@ -1022,7 +1024,7 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
             a.sum_blocks = sum_blocks;
             a.touched = n > 0 ? (const uint8_t *)d_index + l.touched : nullptr;
             a.zero_rows = (int32_t)zero_rows;
-            a.stream = rows * D * gb > kCacheBytes;
+            a.stream = rows * D * gb > kCacheBytes && (rows - l.N) * D * gb < kManyZeros;
             a.flat = flat;
             const dim3 grid((unsigned)(sum_blocks + zero_blocks));
             if (g.log2_lanes == 6)
