@@ -599,7 +599,7 @@ __global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
 // Calls f with the thread count and vectors per thread that hold a row: the
 // narrowest workgroup whose threads hold up to FULL vectors each, beyond 1,024
 // threads (WIDER) twice as many; where `several` rows may share a wave, as few
-// lanes as hold a row (308,420 rows of 106 bf16: 190 us backward, 348 us with a
+// lanes as hold a row (308,420 rows of 106 bf16: 199 us backward, 348 us with a
 // wave to a row).
 template <int NT, int NV, int LANES = NT>
 struct RowShape {
