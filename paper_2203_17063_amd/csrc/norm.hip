@@ -522,6 +522,15 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
             }
         }
     }
+    if constexpr (!HOLD) {
+        // (a short last group has units without rows: their sums are zero)
+        if (r0 >= r1)
+            for (int v = 0; v < NV; ++v) {
+                put(g.pre, v, s_pre);
+                put(g.post, v, s_post);
+                put(g.share, v, s_gate);
+            }
+    }
     if constexpr (AT_ONCE > 1) {
         // the wave's rows together
 #pragma unroll

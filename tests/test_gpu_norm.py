@@ -508,3 +508,28 @@ def test_refusals():
         lm.norm_grad(x, f, h, w_pre=w, P=4)
     with pytest.raises(ValueError):
         lm.norm_grad(x, f, h, w_pre=w, accumulate=True)
+
+
+def _strictly_within(got, want, bound_u, acc, out_type):
+    """_within, for which a NaN of either side is a difference too."""
+    assert torch.isfinite(want).all() and torch.isfinite(got).all()
+    _within(got, want, bound_u, acc, out_type)
+
+
+@pytest.mark.parametrize("act,D", [(F64, 3000), (F64, 4096), (BF16, 9001), (BF16, 16384),
+                                   (F32, 9001)])
+@pytest.mark.parametrize("N,g", [(8, 5), (1000, 900), (1000, 300)])
+def test_grad_long_rows_short_last_gate(act, D, N, g):
+    """Rows that are not held, in groups split over units, the last group short:
+    units without rows add nothing, whatever the work buffer held."""
+    announce("norm grad, long rows, short last gate", act, D, N, g)
+    wt = F64 if act == F64 else F32
+    s = _inputs(N, D, act, wt, "rows", gate_rows=g)
+    dh, dxo = _random((N, D), act, 50, 0.3), _random((N, D), act, 51, 0.3)
+    work = torch.full((3 * 1024 * D * 8,), 255, dtype=torch.uint8, device="cuda")
+    got = _lm().norm_grad(**_gpu_args(s), dh=dh.cuda(), dx_out=dxo.cuda(), res_scale=0.9,
+                          branch_scale=0.7, eps=EPS, work=work)
+    want, err = _grad_ref(s, dh, dxo, 0.9, 0.7, 0.0, 1)
+    for k in want:
+        out = act if k in ("dx", "df", "dgate") else wt
+        _strictly_within(got[k], want[k], err[k], act, out)
