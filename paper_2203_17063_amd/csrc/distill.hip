@@ -72,24 +72,25 @@ __device__ __forceinline__ double max3(double a, double b, double c) { return fm
 // Exponentials at one temperature.  fp32 works with powers of two (the
 // hardware's): with c = log2(e) / tau an exponential is 2^(z c - r), its
 // argument one multiply-add, for a reference r = fl(m c) that stands for the
-// maximum m.  r itself is exact, so what c is off by shifts a row's arguments
-// alike and falls out of every quotient.  fp64 uses exp with c = 1 / tau.
-// Only where m c would overflow (logits about as large as the type's) is m
-// subtracted first.
+// maximum m.  r is off by up to 2^-24 m c, which shifts a row's arguments alike
+// and falls out of every quotient as long as it is small: up to |m c| = 2^20,
+// where it stays below 2^-5.  Beyond, m is subtracted first (rows masked with
+// a large finite value, temperatures near 0).  fp64 uses exp with c = 1 / tau,
+// and a limit of 2^49.
 template <typename A>
 struct Temper {
     A c;
     __device__ __forceinline__ explicit Temper(double tau)
         : c(std::is_same_v<A, float> ? (A)(1.4426950408889634 / tau) : (A)(1.0 / tau)) {}
-    static constexpr A kLarge = std::is_same_v<A, float> ? (A)1e37 : (A)1e307;
+    static constexpr A kPlain = std::is_same_v<A, float> ? (A)0x1p20 : (A)0x1p49;
     __device__ __forceinline__ A power(A x) const {
         if constexpr (std::is_same_v<A, float>) return __builtin_amdgcn_exp2f(x);
         else return ::exp(x);
     }
-    // is m c - z c safe to form for every z <= m?
-    __device__ __forceinline__ bool plain(A m) const {
-        return magnitude(m) <= kLarge && magnitude(m * c) <= kLarge;
-    }
+    // does fl(m c) stand for m?
+    __device__ __forceinline__ bool plain(A m) const { return magnitude(m * c) <= kPlain; }
+    // how far m's reference lies above m c
+    __device__ __forceinline__ A shift(A m) const { return plain(m) ? -fma_(m, c, -(m * c)) : (A)0; }
     // the exponent of z above m's, and exp of it
     __device__ __forceinline__ A above(A z, A m) const {
         return plain(m) ? fma_(z, c, -(m * c)) : (z - m) * c;
@@ -97,7 +98,8 @@ struct Temper {
     __device__ __forceinline__ A operator()(A z, A m) const { return power(above(z, m)); }
     // the factor that takes sums above m to sums above a higher one
     __device__ __forceinline__ A rescale(A m, A to) const {
-        return power(plain(to) && plain(m) ? m * c - to * c : (m - to) * c);
+        return power(plain(to) && plain(m) ? m * c - to * c
+                                           : (m - to) * c + (shift(m) - shift(to)));
     }
     // the natural logarithm of exp(exponent)
     __device__ __forceinline__ A log_of(A exponent) const {

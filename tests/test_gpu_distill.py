@@ -406,3 +406,81 @@ def test_refusals():
                dict(grad=dz[:3]), dict(loss=loss[:3]), dict(labels=idx[:, 0])):
         with pytest.raises(ValueError):
             lm.distill(z, top, idx, **kw)
+
+
+def _same(a, b):
+    return torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("act", [BF16, F32, F64])
+@pytest.mark.parametrize("N,V", [(3, 40), (4, 1003), (2, 30001), (520, 2100)])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 4.0, 3.5, 0.5])
+def test_rows_of_one_large_value(act, N, V, tau):
+    """A row of one value is uniform, however large the value: as a row of zeros
+    gives.  Teachers' rows alike."""
+    lm = _lm()
+    announce("distill, rows of one large value", act, N, V, tau)
+    s = _inputs(N, V, 6, act, weight=False, absent=0.0, top_type=F64 if act == F64 else F32)
+    d = {k: v.cuda() if torch.is_tensor(v) else v for k, v in s.items()}
+    kw = dict(tau=tau, kd_weight=0.7, ce_weight=0.3)
+    z = torch.zeros_like(d["z"])
+    flat = torch.zeros_like(d["top"])
+    want, want_flat = lm.distill(**dict(d, z=z), **kw), lm.distill(**dict(d, top=flat), **kw)
+    assert all(torch.isfinite(v).all() for v in want + want_flat)
+    for value in ((-1e20, -1e30, -1e100, -1e305, 1e20, 1e200) if act == F64 else
+                  (-1e8, -1e10, -1e15, -1e30, -1e36, 1e10, 1e20, 1e30)):
+        got = lm.distill(**dict(d, z=torch.full_like(z, value)), **kw)
+        assert _same(got, want), value
+        got = lm.distill(**dict(d, top=torch.full_like(flat, value)), **kw)
+        assert _same(got, want_flat), value
+
+
+@pytest.mark.parametrize("act", [F32, F64])
+@pytest.mark.parametrize("tau,ce", [(1.0, 0.3), (2.0, 0.3), (4.0, 0.3), (3.5, 0.3), (1.5, 0.0)])
+@pytest.mark.parametrize("N,V", [(3, 300), (2, 3001), (2, 30001)])
+def test_logits_at_a_large_offset(act, tau, ce, N, V):
+    """Logits spread over some tens around offsets of any size (all of them
+    multiples of what the type resolves there), so that maxima of threads and
+    parts lie on both sides of any limit within a row."""
+    announce("distill, large offsets", act, tau, ce, N, V)
+    g = torch.Generator().manual_seed(7)
+    for at in ((2 ** k / 1.4426950408889634 * t for k in (10, 17, 19, 20, 21) for t in (1.0, tau))
+               if act == F32 else
+               (float(2 ** k) * t for k in (20, 45, 47, 49) for t in (1.0, tau))):
+        step = 2.0 ** max(-10, math.ceil(math.log2(at)) - (23 if act == F32 else 50))
+        most = int(30 / step)
+        for sign in (1.0, -1.0):
+            s = _inputs(N, V, 6, act, weight=False, absent=0.0)
+            z = torch.randint(-most, most + 1, (N, V), generator=g, dtype=F64) * step
+            offset = sign * math.floor(at / step) * step
+            d = {k: v.cuda() if torch.is_tensor(v) else v
+                 for k, v in dict(s, z=(z + offset).to(act)).items()}
+            assert torch.equal(d["z"].cpu().double() - offset, z)
+            loss, grad = _lm().distill(tau=tau, kd_weight=0.7, ce_weight=ce, **d)
+            # (the offset changes nothing)
+            want_l, want_g, el, eg = _reference(dict(s, z=z), tau, 0.7, ce)
+            acc = F64 if act == F64 else F32
+            _within(loss, want_l, el, acc, acc)
+            _within(grad, want_g, eg, acc, act)
+
+
+def test_small_temperatures():
+    """A temperature that makes z / tau large: the largest logits share the
+    probability."""
+    lm = _lm()
+    announce("distill, small temperatures")
+    for V in (200, 30000):
+        for act in (BF16, F32, F64):
+            z = torch.full((2, V), -3.0, dtype=act, device="cuda")
+            z[0, 5] = z[0, V - 7] = 9.0
+            z[1, 11] = -0.75
+            top = torch.tensor([[3.0, 3.0, 1.0], [-9.0, -11.0, -9.0]], device="cuda")
+            idx = torch.tensor([[5, V - 7, 2], [11, 0, 1]], dtype=torch.int32, device="cuda")
+            for tau in (1e-4, 1e-6, 1e-10, 1e-15):
+                loss, grad = lm.distill(z, top, idx, tau)
+                grad = grad.double() / tau
+                assert torch.isfinite(loss[0]) and loss[0].abs() <= 1e-6 * tau * tau
+                assert grad[0].abs().max() <= 1e-6
+                want = torch.zeros(V, dtype=F64, device="cuda")
+                want[11], want[1] = 0.5, -0.5
+                assert (grad[1] - want).abs().max() <= 2.0 ** -8
