@@ -4,7 +4,8 @@
 //
 // Sums are held in fp32 where the operands are fp32 or bf16 and in fp64 where
 // one of them is fp64 (Acc below); a result is rounded once, when it is
-// stored.  bf16 is rounded to nearest even (v_cvt_pk_bf16_f32).
+// stored.  bf16 is rounded to nearest even (v_cvt_pk_bf16_f32), from fp64 by
+// way of an fp32 that cannot change the outcome (on_the_way_to_bf16).
 #pragma once
 
 #include <type_traits>
@@ -64,6 +65,19 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// An fp64 value as an fp32 that rounds to the same bf16: the value itself, or of
+// its two fp32 neighbours the one whose last bit is set, which lies on the
+// same side of every middle between two bf16 (to the nearest fp32, values
+// close to such a middle would land on it and then go to the even bf16).
+__device__ __forceinline__ float on_the_way_to_bf16(float v) { return v; }
+__device__ __forceinline__ float on_the_way_to_bf16(double v) {
+    const float f = (float)v;
+    const double d = (double)f;
+    if (d == v || v != v) return f;
+    const uint32_t down = __builtin_fabs(d) > __builtin_fabs(v);  // f was rounded away from 0
+    return __uint_as_float((__float_as_uint(f) - down) | 1u);
+}
+
 template <typename A, typename T>
 __device__ __forceinline__ A load_elem(const T *p) {
     if constexpr (std::is_same_v<T, bf16_t>) return (A)bf16_value(p->bits);
@@ -71,7 +85,7 @@ __device__ __forceinline__ A load_elem(const T *p) {
 }
 template <typename A, typename T>
 __device__ __forceinline__ void store_elem(T *p, A v) {
-    if constexpr (std::is_same_v<T, bf16_t>) p->bits = (uint16_t)bf16_pair((float)v, 0.0f);
+    if constexpr (std::is_same_v<T, bf16_t>) p->bits = (uint16_t)bf16_pair(on_the_way_to_bf16(v), 0.0f);
     else *p = (T)v;
 }
 
@@ -167,7 +181,8 @@ struct Raw {
         if constexpr (std::is_same_v<T, bf16_t>) {
 #pragma unroll
             for (int i = 0; i < M; i += 2)
-                w[(first + i) / 2] = bf16_pair((float)v[i], (float)v[i + 1]);
+                w[(first + i) / 2] =
+                    bf16_pair(on_the_way_to_bf16(v[i]), on_the_way_to_bf16(v[i + 1]));
         } else if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
             for (int i = 0; i < M; ++i) w[first + i] = __float_as_uint((float)v[i]);

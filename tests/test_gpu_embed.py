@@ -5,6 +5,9 @@ Tolerances.  u = 2^-24 for fp32 sums, 2^-53 for fp64; a bf16 result (8
 significant bits) adds 2^-8 relative.  A lookup is one rounded product.  A
 gradient of m tokens adds m numbers in some order and scales once: its error
 is at most (m + 3) u * scale * sum |dy|, whatever the order."""
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 
@@ -414,3 +417,45 @@ def test_refusals():
         lm.embed_grad(index, out, accumulate=True)
     with pytest.raises(ValueError):
         lm.embed_grad(index, out, grad=grad[:, :9])
+
+
+def _bf16_bits(v):
+    """bf16 nearest to the fp64 values v (ties to even), by whole numbers."""
+    out = []
+    for x in v.reshape(-1).tolist():
+        m, e = math.frexp(abs(x))             # m in [0.5, 1)
+        n = Fraction(m) * 256                 # 8 significant bits
+        q = int(n)
+        r = n - q
+        q += r > Fraction(1, 2) or (r == Fraction(1, 2) and q % 2 == 1)
+        out.append(math.copysign(math.ldexp(q, e - 8), x))
+    return torch.tensor(out, dtype=F64).reshape(v.shape)
+
+
+def test_fp64_is_rounded_to_bf16_once():
+    """fp64 values next to the middle of two bf16 neighbours, nearer to it than
+    fp32 resolves: rounded to the nearer neighbour, in the lookup and in the
+    gradient, in whole accesses and at a row's end."""
+    lm = _lm()
+    announce("fp64 to bf16")
+    g = torch.Generator().manual_seed(3)
+    V, D = 40, 77
+    middle = (torch.randint(128, 256, (V, D), generator=g, dtype=F64) + 0.5) * \
+        2.0 ** torch.randint(-20, 20, (V, D), generator=g)
+    off = (torch.randint(0, 3, (V, D), generator=g) - 1) * 2.0 ** -35
+    sign = torch.randint(0, 2, (V, D), generator=g) * 2.0 - 1.0
+    table = sign * middle * (1.0 + off)
+    want = _bf16_bits(table)
+    ids = torch.arange(V).cuda()
+    got = lm.embed_lookup(table.cuda(), ids, dtype=BF16).cpu().double()
+    assert torch.equal(got, want)
+    index = lm.embed_index(ids, V)
+    got = lm.embed_grad(index, table.cuda(), dtype=BF16)[0].cpu().double()
+    assert torch.equal(got, want)
+    inf, top, last = float("inf"), 2.0 ** 128 - 2.0 ** 120, 2.0 ** 128 - 2.0 ** 119
+    special = torch.tensor([[inf, -inf, float("nan"), 0.0, -0.0, 1e300, -1e39,
+                             math.nextafter(last, 0.0), last, 1e-300]], dtype=F64)
+    got = lm.embed_lookup(special.cuda(), ids[:1], dtype=BF16).cpu().double()[0]
+    assert got[:2].tolist() == [inf, -inf] and torch.isnan(got[2])
+    assert got[3:].tolist() == [0.0, -0.0, inf, -inf, top, inf, 0.0] and \
+        torch.signbit(got[4])
