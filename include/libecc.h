@@ -644,8 +644,9 @@ ecc_status_t ecc_mf_error(ecc_mf_t h, const double *d_W, double *d_rmse, void *h
  *   - Arrays are row-major; a matrix has a leading dimension (elements from
  *     one row to the next, at least the row length).  Element types are
  *     ECC_F64, ECC_F32 and ECC_BF16, at the alignment of one element.
- *   - Sums, norms and softmax statistics are held in fp32, in fp64 where the
- *     operands or the result are fp64; every result is rounded once, to the
+ *   - Sums over rows and tokens are held in fp32, in fp64 where an operand or
+ *     the result is fp64; a row's own sums (norms, softmax statistics) in
+ *     fp32, in fp64 for rows of fp64.  Every result is rounded once, to the
  *     nearest, when it is stored.
  *   - P workers hold n rows each: row t of P * n belongs to worker t / n.
  *     Worker p's gradient of a parameter starts p * worker_stride elements
@@ -751,7 +752,8 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
  * are not computed; d_df, d_dw_post and d_dgate need d_f (d_dw_post also
  * d_w_post, d_dgate d_gate, d_dw_pre d_w_pre).  d_dx may be d_dx_out or
  * d_dh, and d_df may be d_f or d_dh (with the same leading dimension).
- * d_work: ecc_norm_work_size(a) bytes. */
+ * With grad_type ECC_F64 the sums over rows are fp64's, of terms of `type`'s
+ * arithmetic.  d_work: ecc_norm_work_size(a) bytes. */
 typedef struct {
     const void *d_dh;
     int64_t ld_dh;
@@ -789,7 +791,8 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
  *   d_z      N x V of `type`; d_dz the same, may be d_z (with the same
  *            leading dimension) or NULL (loss only).
  *   d_top    N x K of top_type; d_idx N x K int32, contiguous both, K in [0,
- *            ECC_DISTILL_MAX_TOP]; a teacher's logits are not NaN or +infinity.
+ *            ECC_DISTILL_MAX_TOP]; a teacher's logits are taken to fp32 first,
+ *            unless `type` is ECC_F64, and are not NaN or +infinity there.
  *   d_labels int32 [N] or NULL; d_weight fp32 [N] or NULL.
  *   d_loss   [N] of fp32, fp64 when type is ECC_F64.
  * A weight of 0 leaves its term out.  V in [1, 2^31 - 1), N in [0, 2^31 -

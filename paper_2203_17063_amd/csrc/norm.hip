@@ -22,7 +22,8 @@
 //
 // The sums over rows (gradients of the weights and of a shared gate) stay in
 // registers while a workgroup walks its unit of consecutive rows; the units'
-// sums go to the work buffer and a second launch adds them in order.
+// sums go to the work buffer and a second launch adds them in order.  They are
+// held in fp64 where the rows or the parameters' gradients are fp64.
 #include <algorithm>
 
 #include "lm_common.h"
@@ -291,13 +292,24 @@ struct NormGradArgs {
     NormUnits u;
 };
 
+// Vectors (16 bytes) a thread of the backward kernel holds of an operand's row.
+template <typename T>
+constexpr int kBackwardVecs = std::is_same_v<T, bf16_t> ? 1 : 2;
+
 // HOLD: the row's operands stay in registers between the sums and the results,
 // and the weights lie in LDS, each where the thread that needs it has put it
 // (in registers, 173 of them for a row of 4,096 bf16, one workgroup filled a
 // CU: 129 us for 8,192 such rows, 95 us with two).  Otherwise (the longest
 // rows) both are read again, and the sums over rows stay in the work buffer.
-template <typename T, int NT, int NV, bool HOLD, int LANES>
-__global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) void k_norm_grad(NormArgs a, NormGradArgs g) {
+// S: the type of the sums over rows.  fp64 sums of bf16 or fp32 rows (8,192 rows
+// of 4,096 bf16: 134 us, with sums in fp32 101 us; 8,192 rows of 8,192: 192 and
+// 171 us; 2,000 rows of 16,000, whose sums go through memory: 426 and 210 us).
+template <typename T, typename S, int NT, int NV, bool HOLD>
+constexpr int kGradWaves = HOLD && NV > kBackwardVecs<T> ? 2
+                           : NT == 64 || (HOLD && sizeof(S) == 8) ? 3 : 4;
+template <typename T, typename S, int NT, int NV, bool HOLD, int LANES>
+__global__ __launch_bounds__(NT, (kGradWaves<T, S, NT, NV, HOLD>)) void k_norm_grad(
+    NormArgs a, NormGradArgs g) {
     using A = Acc<T>;
     constexpr int VEC = kVec<T>, KEEP = HOLD ? NV : 1;
     constexpr int Q = 16 / (int)sizeof(A), CH = VEC / Q;  // accumulators of 16 bytes
@@ -398,28 +410,30 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
             o.gate.load_upto(reinterpret_cast<const T *>(a.gate) + row / a.gate_rows * a.ld_gate + c,
                              left);
     };
-    // the sums over rows of vector v's columns, in registers or (unless this is
-    // the unit's or the gate's first row) in the work buffer
+    // the sums over rows, in registers for all of the thread's columns, or for
+    // PER of them in turn (a vector's, unless fp64 sums make that too many
+    // registers), kept in the work buffer from row to row (from the unit's or
+    // the gate's first row on)
     const int64_t at = (int64_t)blockIdx.x * a.D;
-    A s_pre[KEEP * VEC], s_post[KEEP * VEC], s_gate[KEEP * VEC];
+    constexpr int PER = HOLD || std::is_same_v<S, A> ? VEC : Q, SUMS = HOLD ? NV * VEC : PER;
+    S s_pre[SUMS], s_post[SUMS], s_gate[SUMS];
 #pragma unroll
-    for (int e = 0; e < KEEP * VEC; ++e) s_pre[e] = s_post[e] = s_gate[e] = (A)0;
-    auto get = [&](const void *from, int v, bool first, A *sum) {
-        const uint32_t c = (v * NT + tid) * VEC;
-        Raw<A, VEC> r;
-        if (from && !first) r.load_upto(reinterpret_cast<const A *>(from) + at + c, (int32_t)a.D - (int32_t)c);
+    for (int e = 0; e < SUMS; ++e) s_pre[e] = s_post[e] = s_gate[e] = (S)0;
+    auto get = [&](const void *from, uint32_t c, bool first, S(&sum)[SUMS]) {
+        Raw<S, SUMS> r;
+        if (from && !first)
+            r.load_upto(reinterpret_cast<const S *>(from) + at + c, (int32_t)a.D - (int32_t)c);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] = from && !first ? r.template get<A>(i) : (A)0;
+        for (int i = 0; i < SUMS; ++i) sum[i] = from && !first ? r.template get<S>(i) : (S)0;
     };
-    auto put = [&](void *to, int v, const A *sum) {
-        const uint32_t c = (v * NT + tid) * VEC;
+    auto put = [&](void *to, uint32_t c, const S *sum) {
         if (!to) return;
-        A t[VEC];
+        S t[PER];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) t[i] = sum[i];
-        Raw<A, VEC> r;
+        for (int i = 0; i < PER; ++i) t[i] = sum[i];
+        Raw<S, PER> r;
         r.set_all(t);
-        r.store_upto(reinterpret_cast<A *>(to) + at + c, (int32_t)a.D - (int32_t)c);
+        r.store_upto(reinterpret_cast<S *>(to) + at + c, (int32_t)a.D - (int32_t)c);
     };
     constexpr int UNROLL = HOLD ? NV : 1;
     Operands op[KEEP];
@@ -472,23 +486,24 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
         for (int v = 0; v < NV; ++v) {
             const uint32_t col = (v * NT + tid) * VEC;
             const int32_t left = live ? (int32_t)a.D - (int32_t)col : 0;
-            if constexpr (!HOLD) {
-                fetch(row, v, op[0]);
-                get(g.pre, v, row == r0, s_pre);
-                get(g.post, v, row == r0, s_post);
-                get(g.share, v, group_begin, s_gate);
-            }
+            if constexpr (!HOLD) fetch(row, v, op[0]);
             const Operands &o = op[HOLD ? v : 0];
             Raw<T, VEC> rdx, rdf, rdg;
 #pragma unroll
             for (int cq = 0; cq < CH; ++cq) {
-                A wq[Q], wp[Q], wg[Q], dx[Q], df[Q], dg[Q];
+                A wq[Q], wp[Q], wg[Q], dx[Q], df[Q];
+                S dg[Q];
+                if (!HOLD && cq * Q % PER == 0) {
+                    get(g.pre, col + cq * Q, row == r0, s_pre);
+                    get(g.post, col + cq * Q, row == r0, s_post);
+                    get(g.share, col + cq * Q, group_begin, s_gate);
+                }
                 weights(0, v, cq, wq);
                 weights(1, v, cq, wp);
                 weights(2, v, cq, wg);
 #pragma unroll
                 for (int j = 0; j < Q; ++j) {
-                    const int i = cq * Q + j, e = HOLD ? v * VEC + i : i;
+                    const int i = cq * Q + j, e = HOLD ? v * VEC + i : i % PER;
                     const A x = o.x.template get<A>(i), f = o.f.template get<A>(i);
                     const A h = o.dh.template get<A>(i);
                     const A d = o.dxo.template get<A>(i) + q * (h * wp[j]) - c * x;
@@ -497,15 +512,21 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
                     const A du = gb * d;
                     dx[j] = res * d;
                     df[j] = k * (du * wq[j] - f * m);
-                    s_pre[e] = fma_(h, x * q, s_pre[e]);
-                    s_post[e] = fma_(du, f * k, s_post[e]);
-                    s_gate[e] = fma_(branch * d, f * k * wq[j], s_gate[e]);
+                    s_pre[e] = fma_((S)h, (S)(x * q), s_pre[e]);
+                    s_post[e] = fma_((S)du, (S)(f * k), s_post[e]);
+                    s_gate[e] = fma_((S)(branch * d), (S)(f * k * wq[j]), s_gate[e]);
                     dg[j] = s_gate[e];
-                    if (group_end) s_gate[e] = (A)0;
+                    if (group_end) s_gate[e] = (S)0;
                 }
                 rdx.template set_some<Q>(cq * Q, dx);
                 rdf.template set_some<Q>(cq * Q, df);
                 rdg.template set_some<Q>(cq * Q, dg);
+                if (!HOLD && (cq + 1) * Q % PER == 0) {
+                    const uint32_t first_col = col + (cq + 1) * Q - PER;
+                    put(g.pre, first_col, s_pre);
+                    put(g.post, first_col, s_post);
+                    put(g.share, first_col, s_gate);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (g.dx)
@@ -515,26 +536,22 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
             if (g.dgate && group_end)
                 rdg.store_upto(
                     reinterpret_cast<T *>(g.dgate) + row / a.gate_rows * g.ld_dgate + col, left);
-            if constexpr (!HOLD) {
-                put(g.pre, v, s_pre);
-                put(g.post, v, s_post);
-                put(g.share, v, s_gate);
-            }
         }
     }
     if constexpr (!HOLD) {
         // (a short last group has units without rows: their sums are zero)
         if (r0 >= r1)
-            for (int v = 0; v < NV; ++v) {
-                put(g.pre, v, s_pre);
-                put(g.post, v, s_post);
-                put(g.share, v, s_gate);
+            for (int i = 0; i < NV * VEC / PER; ++i) {
+                const uint32_t c = (i * PER / VEC * NT + tid) * VEC + i * PER % VEC;
+                put(g.pre, c, s_pre);
+                put(g.post, c, s_post);
+                put(g.share, c, s_gate);
             }
     }
     if constexpr (AT_ONCE > 1) {
         // the wave's rows together
 #pragma unroll
-        for (int e = 0; e < KEEP * VEC; ++e)
+        for (int e = 0; e < SUMS; ++e)
 #pragma unroll
             for (int o = LANES; o < 64; o <<= 1) {
                 s_pre[e] += __shfl_xor(s_pre[e], o, 64);
@@ -546,9 +563,10 @@ __global__ __launch_bounds__(NT, NT == 64 || (HOLD && sizeof(T) == 8) ? 3 : 4) v
     if constexpr (HOLD) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            put(g.pre, v, s_pre + v * VEC);
-            put(g.post, v, s_post + v * VEC);
-            put(g.share, v, s_gate + v * VEC);
+            const uint32_t c = (v * NT + tid) * VEC;
+            put(g.pre, c, s_pre + v * VEC);
+            put(g.post, c, s_post + v * VEC);
+            put(g.share, c, s_gate + v * VEC);
         }
     }
 }
@@ -607,14 +625,14 @@ __global__ __launch_bounds__(kNormJoinThreads) void k_norm_join(NormJoin a) {
 
 // Calls f with the thread count and vectors per thread that hold a row: the
 // narrowest workgroup whose threads hold up to FULL vectors each, beyond 1,024
-// threads (WIDER) twice as many; where `several` rows may share a wave, as few
-// lanes as hold a row (308,420 rows of 106 bf16: 199 us backward, 348 us with a
-// wave to a row).
+// threads (WIDER) twice as many, or beyond 512 (DEEP); where `several` rows may
+// share a wave, as few lanes as hold a row (308,420 rows of 106 bf16: 199 us
+// backward, 348 us with a wave to a row).
 template <int NT, int NV, int LANES = NT>
 struct RowShape {
     static constexpr int nt = NT, nv = NV, lanes = LANES;
 };
-template <int FULL, bool WIDER, typename F>
+template <int FULL, bool WIDER, bool DEEP, typename F>
 void with_row_shape(int64_t vecs, bool several, F &&f) {
     if (several && vecs <= 8) f(RowShape<64, 1, 8>{});
     else if (several && vecs <= 16) f(RowShape<64, 1, 16>{});
@@ -624,7 +642,7 @@ void with_row_shape(int64_t vecs, bool several, F &&f) {
     else if (vecs <= 128 * FULL) f(RowShape<128, FULL>{});
     else if (vecs <= 256 * FULL) f(RowShape<256, FULL>{});
     else if (vecs <= 512 * FULL) f(RowShape<512, FULL>{});
-    else if (!WIDER || vecs <= 1024 * FULL) f(RowShape<1024, FULL>{});
+    else if (!WIDER || vecs <= 1024 * FULL) f(RowShape<DEEP ? 512 : 1024, DEEP ? 2 * FULL : FULL>{});
     else f(RowShape<1024, (WIDER ? 2 : 1) * FULL>{});
 }
 // Vectors (16 bytes) a thread holds of an operand's row.
@@ -634,8 +652,11 @@ static_assert(1024 * kForwardVecs<bf16_t> * kVec<bf16_t> == ECC_NORM_MAX_DIM &&
                   1024 * kForwardVecs<float> * kVec<float> == ECC_NORM_MAX_DIM &&
                   1024 * kForwardVecs<double> * kVec<double> == ECC_NORM_MAX_DIM / 2,
               "the widest workgroup holds the longest row");
-template <typename T>
-constexpr int kBackwardVecs = std::is_same_v<T, bf16_t> ? 1 : 2;
+// fp64 sums over narrower rows: too many registers for 1,024 threads, so 512
+// hold twice as many vectors (8,192 rows of 8,192 bf16: 192 us, with 1,024
+// threads and the sums in memory 747 us).
+template <typename T, typename S>
+constexpr bool kDeep = sizeof(S) == 8 && !std::is_same_v<T, double>;
 
 inline int64_t backward_threads(int32_t type, int64_t D) {
     const int64_t vec = 16 / type_size(type), full = type == ECC_BF16 ? 1 : 2;
@@ -746,7 +767,7 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
     with_type(a->type, [&](auto t) {
         using T = decltype(t);
         const int64_t vecs = (a->D + kVec<T> - 1) / kVec<T>;
-        with_row_shape<kForwardVecs<T>, false>(vecs, true, [&](auto shape) {
+        with_row_shape<kForwardVecs<T>, false, false>(vecs, true, [&](auto shape) {
             constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
             constexpr int LANES = decltype(shape)::lanes;
             const int64_t grid = std::min<int64_t>((N + NT / LANES - 1) / (NT / LANES),
@@ -761,8 +782,8 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
 
 int64_t ecc_norm_work_size(const ecc_norm_t *a) {
     if (check_norm(a) != ECC_OK) return -1;
-    const int64_t acc = a->type == ECC_F64 ? 8 : 4;
-    return std::max<int64_t>(16, (3 * units_of(a).total * a->D * acc + 15) & ~int64_t(15));
+    // (sums of 8 bytes: whether they are is a matter of the gradients' type)
+    return std::max<int64_t>(16, 3 * units_of(a).total * a->D * 8);
 }
 
 ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *d_work,
@@ -862,10 +883,10 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
         set_error("P * n is too large for one launch");
         return ECC_ERR_RANGE;
     }
-    with_type(a->type, [&](auto t) {
+    auto run = [&](auto t, auto sum) {
         using T = decltype(t);
-        using A = Acc<T>;
-        A *work = (A *)d_work;
+        using S = decltype(sum);
+        S *work = (S *)d_work;
         const int64_t sums = ga.u.total * D;
         ga.pre = g->d_dw_pre ? work : nullptr;
         ga.post = g->d_dw_post ? work + sums : nullptr;
@@ -875,18 +896,20 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
         // (a shared gate row's sum is one wave's, row by row)
         const bool several = !(a->d_f && a->d_gate) || a->gate_rows <= 1;
         if (N > 0)
-            with_row_shape<kBackwardVecs<T>, true>((D + kVec<T> - 1) / kVec<T>, several, [&](auto shape) {
+            with_row_shape<kBackwardVecs<T>, true, kDeep<T, S>>(
+                (D + kVec<T> - 1) / kVec<T>, several, [&](auto shape) {
                 constexpr int NT = decltype(shape)::nt, NV = decltype(shape)::nv;
                 constexpr int LANES = decltype(shape)::lanes;
-                constexpr bool HOLD = NV <= kBackwardVecs<T> &&
-                                      !(std::is_same_v<T, double> && NT == 1024);
-                constexpr size_t lds = HOLD ? 3 * sizeof(A) * NV * kVec<T> * NT : 0;
+                constexpr bool HOLD = kDeep<T, S> ? NT < 1024
+                                                  : NV <= kBackwardVecs<T> &&
+                                                        !(std::is_same_v<T, double> && NT == 1024);
+                constexpr size_t lds = HOLD ? 3 * sizeof(Acc<T>) * NV * kVec<T> * NT : 0;
                 static_assert(lds <= 128 << 10, "the weights of a row in LDS");
                 NormGradArgs args = ga;
                 // (the longest rows' sums lie there even where a group ends
                 // within its unit)
                 if (!HOLD && g->d_dgate) args.share = work + 2 * sums;
-                auto kernel = k_norm_grad<T, NT, NV, HOLD, LANES>;
+                auto kernel = k_norm_grad<T, S, NT, NV, HOLD, LANES>;
                 if constexpr (lds > (64 << 10))
                     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                               hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -897,10 +920,10 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
         auto join = [&](const NormJoin &j, int arrays) {
             const int64_t wide = (D + 63) / 64 * j.count;
             if (wide >= 64)
-                hipLaunchKernelGGL((k_norm_join<A, 64>), dim3((unsigned)wide, arrays),
+                hipLaunchKernelGGL((k_norm_join<S, 64>), dim3((unsigned)wide, arrays),
                                    dim3(kNormJoinThreads), 0, s, j);
             else
-                hipLaunchKernelGGL((k_norm_join<A, 16>),
+                hipLaunchKernelGGL((k_norm_join<S, 16>),
                                    dim3((unsigned)((D + 15) / 16 * j.count), arrays),
                                    dim3(kNormJoinThreads), 0, s, j);
         };
@@ -933,6 +956,10 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
             j.D = D;
             join(j, 1);
         }
+    };
+    with_type(a->type, [&](auto t) {
+        if (params && g->grad_type == ECC_F64) run(t, double{});
+        else run(t, Acc<decltype(t)>{});
     });
     ECC_LAUNCH_CHECK();
     return ECC_OK;

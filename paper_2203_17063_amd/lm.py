@@ -4,8 +4,9 @@ libecc called on the current stream.  No arithmetic runs here.
 
 Rows (tokens, positions) may come with any number of leading dimensions as
 long as the last one is contiguous and the others collapse to rows of one
-stride.  Sums are held in fp32, or fp64 where an operand or the result is
-fp64.
+stride.  Sums over rows and tokens are held in fp32, or fp64 where an operand
+or the result is fp64; a row's own sums (norms, softmax statistics) in fp32, or
+fp64 for rows of fp64.
 """
 from __future__ import annotations
 

@@ -533,3 +533,42 @@ def test_grad_long_rows_short_last_gate(act, D, N, g):
     for k in want:
         out = act if k in ("dx", "df", "dgate") else wt
         _strictly_within(got[k], want[k], err[k], act, out)
+
+
+@pytest.mark.parametrize("act", [BF16, F32])
+@pytest.mark.parametrize("N,P,D", [(40000, 1, 64), (40000, 4, 128), (9000, 3, 512), (6000, 2, 1024),
+                                   (3000, 1, 4096), (2001, 3, 8192), (1000, 2, 16384), (1, 1, 8)])
+def test_grad_fp64_sums_over_rows(act, N, P, D):
+    """fp64 gradients of fp32 and bf16 rows are sums in fp64.  Rows of one
+    magnitude, weights and scales are powers of two, so that norm factors and
+    every row's term are exact: m additions in fp64 are within (m + 4) 2^-53 of
+    the magnitudes' sum."""
+    lm = _lm()
+    announce("norm grad, fp64 sums", act, N, P, D)
+    g = torch.Generator(device="cuda").manual_seed(N + D)
+
+    def signs(scale):
+        return ((torch.randint(0, 2, (N, D), generator=g, device="cuda") * 2 - 1) * scale).to(act)
+
+    x, f = signs(2.0), signs(4.0)
+    dh, dxo = (torch.randn((N, D), generator=g, device="cuda").to(act) for _ in range(2))
+    one = torch.ones(D, device="cuda")
+    kw = dict(eps=1e-30, P=P, dtype=F64)
+
+    def check(got, terms):
+        t = terms.view(P, N // P, D)
+        assert got.dtype == F64
+        assert ((got - t.sum(1)).abs() <= (N // P + 4) * 2.0 ** -53 * t.abs().sum(1)).all()
+
+    got = lm.norm_grad(x, None, dh, dxo, w_pre=one, **kw)
+    check(got["dw_pre"], dh.double() * x.double() / 2)
+    got = lm.norm_grad(x, f, None, dxo, w_post=2 * one, gate=one / 4, gate_rows=0,
+                       branch_scale=0.5, **kw)
+    check(got["dw_post"], dxo.double() * f.double() / 4 / 8)
+    check(got["dgate"], dxo.double() * f.double() / 4)
+    # beside a gate of rows, in groups longer than a unit, the last one short
+    rows = 700 if P == 1 else N // P
+    gate = torch.full((-(-N // rows), D), 0.25, dtype=act, device="cuda")
+    got = lm.norm_grad(x, f, None, dxo, w_post=2 * one, gate=gate, gate_rows=rows,
+                       branch_scale=0.5, **kw)
+    check(got["dw_post"], dxo.double() * f.double() / 4 / 8)
