@@ -672,6 +672,12 @@ inline NormUnits units_of(const ecc_norm_t *a) {
     return norm_units(a->P, a->n, group, target);
 }
 
+// eps in the rows' arithmetic: one that fp32 would round to zero is its least
+// number, so that rows of zeros stay zeros.
+inline double held_eps(const ecc_norm_t *a) {
+    return a->type == ECC_F64 ? a->eps : std::max(a->eps, 0x1p-149);
+}
+
 static ecc_status_t check_norm(const ecc_norm_t *a) {
     ECC_ARG(a != nullptr, "the description is NULL");
     ECC_ARG(a->P >= 1 && a->n >= 0 && a->D >= 1, "P and D must be >= 1, n >= 0");
@@ -763,7 +769,7 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
             "an output overlaps an input or the other output");
     NormArgs n{N,          a->D,      a->d_x,    a->d_f,       a->d_gate, a->d_w_post,
                a->d_w_pre, a->ld_x,   a->ld_f,   a->ld_gate,   a->gate_rows, a->w_type,
-               a->w_offset, a->res_scale, a->branch_scale, a->eps};
+               a->w_offset, a->res_scale, a->branch_scale, held_eps(a)};
     with_type(a->type, [&](auto t) {
         using T = decltype(t);
         const int64_t vecs = (a->D + kVec<T> - 1) / kVec<T>;
@@ -867,7 +873,7 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
     if (N == 0 && (!params || g->accumulate)) return ECC_OK;
     NormArgs n{N,          D,          a->d_x,    a->d_f,       a->d_gate, a->d_w_post,
                a->d_w_pre, a->ld_x,   a->ld_f,   a->ld_gate,   a->gate_rows, a->w_type,
-               a->w_offset, a->res_scale, a->branch_scale, a->eps};
+               a->w_offset, a->res_scale, a->branch_scale, held_eps(a)};
     NormGradArgs ga{};
     ga.dh = g->d_dh;
     ga.dxo = g->d_dx_out;

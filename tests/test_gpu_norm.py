@@ -572,3 +572,19 @@ def test_grad_fp64_sums_over_rows(act, N, P, D):
     got = lm.norm_grad(x, f, None, dxo, w_post=2 * one, gate=gate, gate_rows=rows,
                        branch_scale=0.5, **kw)
     check(got["dw_post"], dxo.double() * f.double() / 4 / 8)
+
+
+@pytest.mark.parametrize("act", [BF16, F32])
+def test_eps_below_fp32(act):
+    """An eps that fp32 rounds to zero: rows of zeros still give zeros."""
+    lm = _lm()
+    announce("norm, tiny eps", act)
+    x = torch.zeros((3, 70), dtype=act, device="cuda")
+    x[1] = 2.0
+    w = torch.ones(70, device="cuda")
+    for eps in (1e-50, 1e-300, 5e-324):
+        y, h = lm.norm_forward(x, x.clone(), w_post=w, w_pre=w, eps=eps)
+        assert not y[[0, 2]].any() and not h[[0, 2]].any()
+        assert torch.allclose(h[1].float(), torch.ones(70, device="cuda"), rtol=1e-2)
+        g = lm.norm_grad(x, x.clone(), torch.zeros_like(x), None, w_post=w, w_pre=w, eps=eps)
+        assert all(not g[k].any() for k in ("dx", "df", "dw_post", "dw_pre"))
