@@ -83,6 +83,8 @@ class Student:
         sequences ids (B, T); the loss of each position."""
         P, V, D = self.P, self.V, self.D
         B, T = ids.shape
+        if B % P:
+            raise ValueError("%d sequences cannot be shared equally by %d workers" % (B, P))
         w = self.views(self.W.float())
         # forward: rows are positions, worker after worker
         x0 = lm.embed_lookup(w["table"], ids, scale=self.scale)
@@ -121,7 +123,10 @@ class Student:
         self.plan.close()
 
 
-def train(steps=100, P=8, slack=2, arrive=0.8, V=67, D=96, K=8, batch=64, length=33, eta=4.0,
+BATCH = 64
+
+
+def train(steps=100, P=8, slack=2, arrive=0.8, V=67, D=96, K=8, batch=BATCH, length=33, eta=4.0,
           tau=2.0, kd_weight=0.8, ce_weight=0.2, seed=1):
     """The mean loss of every step."""
     device = "cuda"
@@ -159,6 +164,8 @@ def main():
     ap.add_argument("--slack", type=int, default=2)
     ap.add_argument("--arrive", type=float, default=0.8)
     a = ap.parse_args()
+    if a.workers < 1 or BATCH % a.workers:
+        ap.error("--workers must divide the %d sequences of a step" % BATCH)
     losses, forced = train(a.steps, a.workers, a.slack, a.arrive)
     for t in range(0, a.steps, max(1, a.steps // 10)):
         print("step %4d  loss %.4f" % (t, losses[t]))

@@ -1,5 +1,8 @@
 """Sizes and refusals of the language-model operators that need no GPU: the
 size calls, and argument errors found before anything is enqueued."""
+import os
+import sys
+
 import pytest
 
 from paper_2203_17063_amd import capi as E
@@ -70,3 +73,24 @@ def test_refused_without_a_device():
     # nothing to do is no error, with nothing to point to
     assert lib.ecc_embed_lookup(0, 8, 8, 0, None, E.ECC_I32, None, 1, 8, 1.0, None, 1, 8,
                                 None) == E.ECC_OK
+
+
+def test_example_shares_its_sequences():
+    """A batch that the workers cannot share equally is refused: their
+    gradients would be of different sequences in the different operators."""
+    torch = pytest.importorskip("torch")
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                                    "examples"))
+    import distill_lm
+    student = object.__new__(distill_lm.Student)
+    student.P, student.V, student.D = 3, 7, 4
+    with pytest.raises(ValueError, match="64 sequences"):
+        student.gradients(torch.zeros((64, 33), dtype=torch.int64), None, None, None, None, 1.0,
+                          1.0, 0.0)
+    for workers in ("3", "0", "-8", "65"):
+        with pytest.raises(SystemExit):
+            sys.argv, argv = ["distill_lm.py", "--workers", workers], sys.argv
+            try:
+                distill_lm.main()
+            finally:
+                sys.argv = argv
