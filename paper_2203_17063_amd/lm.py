@@ -4,7 +4,8 @@ libecc called on the current stream.  No arithmetic runs here.
 
 Rows (tokens, positions) may come with any number of leading dimensions as
 long as the last one is contiguous and the others collapse to rows of one
-stride.  Sums over rows and tokens are held in fp32, or fp64 where an operand
+stride.  Operands, outputs and work buffers of a call lie on one GPU, which
+need not be the current one.  Sums over rows and tokens are held in fp32, or fp64 where an operand
 or the result is fp64; a row's own sums (norms, softmax statistics) in fp32, or
 fp64 for rows of fp64.
 """
@@ -23,11 +24,32 @@ _ID_TYPES = {torch.int32: E.ECC_I32, torch.int64: E.ECC_I64}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(t):
     """The current stream of t's device."""
     if _raw_stream is not None:
         return _raw_stream(t.get_device())
     return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _launch(like, call, *args):
+    """call(*args, stream), enqueued on the current stream of like's device,
+    which is the current device meanwhile."""
+    if like.get_device() == _current_device():
+        call(*args, _stream(like))
+    else:
+        with torch.cuda.device(like.device):
+            call(*args, _stream(like))
+
+
+def _same_device(like, **others):
+    """The others lie where `like` does."""
+    device = like.get_device()
+    for what, t in others.items():
+        if t is not None and t.get_device() != device:
+            raise ValueError("%s must be on %s, not on %s" % (what, like.device, t.device))
 
 
 def _type(t, what):
@@ -84,6 +106,14 @@ def _work(size, like):
     return like.new_empty(size, dtype=torch.uint8)
 
 
+def _given_work(work, size, like):
+    """The caller's work buffer, checked."""
+    _same_device(like, work=_contiguous(work, "the work buffer"))
+    if work.numel() * work.element_size() < size:
+        raise ValueError("the work buffer is too small")
+    return work
+
+
 # ----------------------------------------------------------------------------
 # token embedding
 # ----------------------------------------------------------------------------
@@ -107,8 +137,9 @@ def embed_lookup(table, ids, scale=1.0, dtype=None, out=None, row0=0):
     ot = _type(dtype, "the result")
     out = _out(out, tuple(ids.shape) + (D,), dtype, table, "out")
     _, ld_out = _rows(out, "out")
-    E.ecc_embed_lookup(ids.numel(), V, D, row0, ids, id_type, table, tt, ld, scale, out, ot,
-                       ld_out, _stream(table))
+    _same_device(table, ids=ids, out=out)
+    _launch(table, E.ecc_embed_lookup, ids.numel(), V, D, row0, ids, id_type, table, tt, ld,
+            scale, out, ot, ld_out)
     return out
 
 
@@ -134,7 +165,8 @@ def embed_index(ids, V, P=1, row0=0, index=None):
         index = EmbedIndex(P, n, V, _work(E.ecc_embed_index_size(P, n, V), ids))
     elif (index.P, index.n, index.V) != (P, n, V):
         raise ValueError("the index was made for other sizes")
-    E.ecc_embed_index(P, n, V, row0, ids, id_type, index.data, _stream(ids))
+    _same_device(ids, index=index.data)
+    _launch(ids, E.ecc_embed_index, P, n, V, row0, ids, id_type, index.data)
     return index
 
 
@@ -159,14 +191,13 @@ def embed_grad(index, dy, scale=1.0, grad=None, dtype=torch.float32, accumulate=
     _on_gpu(grad, "grad")
     if D > 1 and grad.stride(2) != 1:
         raise ValueError("grad must be contiguous in its last dimension")
+    _same_device(grad, dy=dy, index=index.data)
     yt, gt = _type(dy, "dy"), _type(grad, "grad")
-    if work is None:
-        work = _work(E.ecc_embed_work_size(P, n, D, yt, gt), grad)
-    elif work.numel() * work.element_size() < E.ecc_embed_work_size(P, n, D, yt, gt):
-        raise ValueError("the work buffer is too small")
-    E.ecc_embed_grad(P, n, V, D, index.data, dy, yt, ld_dy, scale, grad, gt,
-                     grad.stride(1) if V > 1 else D, grad.stride(0) if P > 1 else V * D,
-                     1 if accumulate else 0, work, _stream(grad))
+    size = E.ecc_embed_work_size(P, n, D, yt, gt)
+    work = _work(size, grad) if work is None else _given_work(work, size, grad)
+    _launch(grad, E.ecc_embed_grad, P, n, V, D, index.data, dy, yt, ld_dy, scale, grad, gt,
+            grad.stride(1) if V > 1 else D, grad.stride(0) if P > 1 else V * D,
+            1 if accumulate else 0, work)
     return grad
 
 
@@ -240,7 +271,8 @@ def norm_forward(x, f=None, *, w_post=None, w_pre=None, gate=None, gate_rows=1, 
         _, ld_h = _rows(h, "h")
     elif h is not None:
         raise ValueError("h needs w_pre")
-    E.ecc_norm_forward(a, x_out, ld_xo, h, ld_h, _stream(x))
+    _same_device(x, f=f, w_post=w_post, w_pre=w_pre, gate=gate, x_out=x_out, h=h)
+    _launch(x, E.ecc_norm_forward, a, x_out, ld_xo, h, ld_h)
     return x_out, h
 
 
@@ -318,11 +350,11 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
     g = E.ecc_norm_grad_t(d_dh, ld_dh, d_dxo, ld_dxo, d_dx, ld_dx, d_df, ld_df, d_dgate, ld_dgate,
                           d_post, d_pre, _type(dtype, "the gradients"), 1 if accumulate else 0,
                           stride)
-    if work is None:
-        work = _work(E.ecc_norm_work_size(a), x)
-    elif work.numel() * work.element_size() < E.ecc_norm_work_size(a):
-        raise ValueError("the work buffer is too small")
-    E.ecc_norm_grad(a, g, work, _stream(x))
+    _same_device(x, f=f, dh=dh, dx_out=dx_out, w_post=w_post, w_pre=w_pre, gate=gate, dx=dx, df=df,
+                 dgate=dgate, dw_post=dw_post, dw_pre=dw_pre)
+    size = E.ecc_norm_work_size(a)
+    work = _work(size, x) if work is None else _given_work(work, size, x)
+    _launch(x, E.ecc_norm_grad, a, g, work)
     return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
 
 
@@ -364,11 +396,9 @@ def distill(z, top, idx, tau=1.0, kd_weight=1.0, ce_weight=0.0, labels=None, wei
     if grad is not None:
         _out(grad, z.shape, z.dtype, z, "grad")
         _, ld_dz = _rows(grad, "grad")
+    _same_device(z, top=top, idx=idx, labels=labels, weight=weight, loss=loss, grad=grad)
     size = E.ecc_distill_work_size(a)
-    if work is None:
-        # (a refused description has no size: the call says what is wrong)
-        work = _work(max(size, 16), z)
-    elif work.numel() * work.element_size() < size:
-        raise ValueError("the work buffer is too small")
-    E.ecc_distill(a, loss, grad, ld_dz, work, _stream(z))
+    # (a refused description has no size: the call says what is wrong)
+    work = _work(max(size, 16), z) if work is None else _given_work(work, size, z)
+    _launch(z, E.ecc_distill, a, loss, grad, ld_dz, work)
     return loss, grad

@@ -484,3 +484,22 @@ def test_small_temperatures():
                 want = torch.zeros(V, dtype=F64, device="cuda")
                 want[11], want[1] = 0.5, -0.5
                 assert (grad[1] - want).abs().max() <= 2.0 ** -8
+
+
+def test_work_buffers_that_do_not_hold():
+    """Work buffers on the host, too small, or with fewer elements in memory than
+    they show are refused, as are operands apart from each other."""
+    lm = _lm()
+    announce("distill, work buffers")
+    z, top = torch.zeros((2, 9000), device="cuda"), torch.zeros((2, 3), device="cuda")
+    idx = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+
+    def call(work):
+        return lm.distill(z, top, idx, work=work)
+    size = 1 << 24
+    for work in (torch.empty(size, dtype=torch.uint8), torch.empty(8, device="cuda")[:1],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(size),
+                 torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            call(work)
+    call(torch.empty(size, dtype=torch.uint8, device="cuda"))

@@ -459,3 +459,22 @@ def test_fp64_is_rounded_to_bf16_once():
     assert got[:2].tolist() == [inf, -inf] and torch.isnan(got[2])
     assert got[3:].tolist() == [0.0, -0.0, inf, -inf, top, inf, 0.0] and \
         torch.signbit(got[4])
+
+
+def test_work_buffers_that_do_not_hold():
+    """Work buffers on the host, too small, or with fewer elements in memory than
+    they show are refused, as are operands apart from each other."""
+    lm = _lm()
+    announce("embed, work buffers")
+    ids, dy = torch.zeros(6, dtype=torch.int64, device="cuda"), torch.zeros((6, 8), device="cuda")
+    index = lm.embed_index(ids, 5)
+
+    def call(work):
+        return lm.embed_grad(index, dy, work=work)
+    size = 1 << 24
+    for work in (torch.empty(size, dtype=torch.uint8), torch.empty(8, device="cuda")[:1],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(size),
+                 torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            call(work)
+    call(torch.empty(size, dtype=torch.uint8, device="cuda"))

@@ -588,3 +588,21 @@ def test_eps_below_fp32(act):
         assert torch.allclose(h[1].float(), torch.ones(70, device="cuda"), rtol=1e-2)
         g = lm.norm_grad(x, x.clone(), torch.zeros_like(x), None, w_post=w, w_pre=w, eps=eps)
         assert all(not g[k].any() for k in ("dx", "df", "dw_post", "dw_pre"))
+
+
+def test_work_buffers_that_do_not_hold():
+    """Work buffers on the host, too small, or with fewer elements in memory than
+    they show are refused, as are operands apart from each other."""
+    lm = _lm()
+    announce("norm, work buffers")
+    x, w = torch.zeros((6, 8), device="cuda"), torch.ones(8, device="cuda")
+
+    def call(work):
+        return lm.norm_grad(x, None, x.clone(), w_pre=w, work=work)
+    size = 1 << 24
+    for work in (torch.empty(size, dtype=torch.uint8), torch.empty(8, device="cuda")[:1],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(size),
+                 torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            call(work)
+    call(torch.empty(size, dtype=torch.uint8, device="cuda"))

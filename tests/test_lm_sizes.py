@@ -94,3 +94,38 @@ def test_example_shares_its_sequences():
                 distill_lm.main()
             finally:
                 sys.argv = argv
+
+
+class _On:
+    """What the device checks see of a tensor."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def get_device(self):
+        return self.device
+
+
+def test_operands_on_one_device(monkeypatch):
+    lm = pytest.importorskip("paper_2203_17063_amd.lm")
+    import contextlib
+    lm._same_device(_On(1), f=_On(1), h=None)
+    for other in (-1, 0, 2):
+        with pytest.raises(ValueError, match="^gate must be on 1"):
+            lm._same_device(_On(1), f=_On(1), h=None, gate=_On(other))
+    # a launch goes to the tensors' device and its stream
+    now = [0]
+
+    @contextlib.contextmanager
+    def device(d):
+        before, now[0] = now[0], d
+        yield
+        now[0] = before
+
+    monkeypatch.setattr(lm.torch.cuda, "device", device)
+    monkeypatch.setattr(lm, "_current_device", lambda: now[0])
+    monkeypatch.setattr(lm, "_raw_stream", lambda d: 100 + d)
+    seen = []
+    for d in (0, 3):
+        lm._launch(_On(d), lambda *args: seen.append((now[0],) + args), "a")
+    assert seen == [(0, "a", 100), (3, "a", 103)] and now == [0]
