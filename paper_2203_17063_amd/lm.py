@@ -19,37 +19,33 @@ _TYPES = {torch.float64: E.ECC_F64, torch.float32: E.ECC_F32, torch.bfloat16: E.
 _ID_TYPES = {torch.int32: E.ECC_I32, torch.int64: E.ECC_I64}
 
 
-# The current stream's handle without the object around it (2.5 us of a call of
-# 10), where torch has it.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
+# A device's current stream without the object around it (2.5 us of a call of
+# 10), and the current device, where torch has them.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _stream(t):
-    """The current stream of t's device."""
-    if _raw_stream is not None:
-        return _raw_stream(t.get_device())
-    return torch.cuda.current_stream(t.device).cuda_stream
 
 
 def _launch(like, call, *args):
     """call(*args, stream), enqueued on the current stream of like's device,
     which is the current device meanwhile."""
-    if like.get_device() == _current_device():
-        call(*args, _stream(like))
-    else:
-        with torch.cuda.device(like.device):
-            call(*args, _stream(like))
-
-
-def _same_device(like, **others):
-    """The others lie where `like` does."""
     device = like.get_device()
-    for what, t in others.items():
+    if device == _current_device():
+        call(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            call(*args, _raw_stream(device))
+
+
+def _one_gpu(first, others, names):
+    """`first` lies on a GPU, and the others (those that are not None) with it."""
+    device = first.get_device()
+    if device < 0:
+        raise ValueError("%s must be on the GPU" % names.split()[0])
+    for t in others:
         if t is not None and t.get_device() != device:
-            raise ValueError("%s must be on %s, not on %s" % (what, like.device, t.device))
+            what = names.split()[1 + [t is o for o in others].index(True)]
+            raise ValueError("%s must be on %s, not on %s" % (what, first.device, t.device))
 
 
 def _type(t, what):
@@ -60,15 +56,9 @@ def _type(t, what):
                         (what, t if isinstance(t, torch.dtype) else t.dtype)) from None
 
 
-def _on_gpu(t, what):
-    if not t.is_cuda:
-        raise ValueError("%s must be on the GPU" % what)
-
-
 def _rows(t, what, cols=None):
     """(rows, leading dimension) of a tensor seen as a matrix of its last
     dimension."""
-    _on_gpu(t, what)
     d = t.dim()
     if d < 1 or (cols is not None and t.shape[-1] != cols):
         raise ValueError("%s must have %s in its last dimension, not shape %s" %
@@ -84,7 +74,6 @@ def _rows(t, what, cols=None):
 
 
 def _contiguous(t, what):
-    _on_gpu(t, what)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % what)
     return t
@@ -108,7 +97,7 @@ def _work(size, like):
 
 def _given_work(work, size, like):
     """The caller's work buffer, checked."""
-    _same_device(like, work=_contiguous(work, "the work buffer"))
+    _one_gpu(like, (_contiguous(work, "the work buffer"),), "- work")
     if work.numel() * work.element_size() < size:
         raise ValueError("the work buffer is too small")
     return work
@@ -137,7 +126,7 @@ def embed_lookup(table, ids, scale=1.0, dtype=None, out=None, row0=0):
     ot = _type(dtype, "the result")
     out = _out(out, tuple(ids.shape) + (D,), dtype, table, "out")
     _, ld_out = _rows(out, "out")
-    _same_device(table, ids=ids, out=out)
+    _one_gpu(table, (ids, out), "table ids out")
     _launch(table, E.ecc_embed_lookup, ids.numel(), V, D, row0, ids, id_type, table, tt, ld,
             scale, out, ot, ld_out)
     return out
@@ -165,7 +154,7 @@ def embed_index(ids, V, P=1, row0=0, index=None):
         index = EmbedIndex(P, n, V, _work(E.ecc_embed_index_size(P, n, V), ids))
     elif (index.P, index.n, index.V) != (P, n, V):
         raise ValueError("the index was made for other sizes")
-    _same_device(ids, index=index.data)
+    _one_gpu(ids, (index.data,), "ids index")
     _launch(ids, E.ecc_embed_index, P, n, V, row0, ids, id_type, index.data)
     return index
 
@@ -188,10 +177,9 @@ def embed_grad(index, dy, scale=1.0, grad=None, dtype=torch.float32, accumulate=
         grad = index.data.new_empty((P, V, D), dtype=dtype)
     elif tuple(grad.shape) != (P, V, D):
         raise ValueError("grad must have shape %s, not %s" % ((P, V, D), tuple(grad.shape)))
-    _on_gpu(grad, "grad")
     if D > 1 and grad.stride(2) != 1:
         raise ValueError("grad must be contiguous in its last dimension")
-    _same_device(grad, dy=dy, index=index.data)
+    _one_gpu(grad, (dy, index.data), "grad dy index")
     yt, gt = _type(dy, "dy"), _type(grad, "grad")
     size = E.ecc_embed_work_size(P, n, D, yt, gt)
     work = _work(size, grad) if work is None else _given_work(work, size, grad)
@@ -271,7 +259,7 @@ def norm_forward(x, f=None, *, w_post=None, w_pre=None, gate=None, gate_rows=1, 
         _, ld_h = _rows(h, "h")
     elif h is not None:
         raise ValueError("h needs w_pre")
-    _same_device(x, f=f, w_post=w_post, w_pre=w_pre, gate=gate, x_out=x_out, h=h)
+    _one_gpu(x, (f, w_post, w_pre, gate, x_out, h), "x f w_post w_pre gate x_out h")
     _launch(x, E.ecc_norm_forward, a, x_out, ld_xo, h, ld_h)
     return x_out, h
 
@@ -325,7 +313,6 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
                 (P > 1 and t.stride(0) != stride):
             raise ValueError("%s must be %s of shape %s, one stride for all" %
                              (what, dtype, (P, D)))
-        _on_gpu(t, what)
         return t
 
     d_dh, ld_dh = rows_in(dh, "dh")
@@ -350,8 +337,8 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
     g = E.ecc_norm_grad_t(d_dh, ld_dh, d_dxo, ld_dxo, d_dx, ld_dx, d_df, ld_df, d_dgate, ld_dgate,
                           d_post, d_pre, _type(dtype, "the gradients"), 1 if accumulate else 0,
                           stride)
-    _same_device(x, f=f, dh=dh, dx_out=dx_out, w_post=w_post, w_pre=w_pre, gate=gate, dx=dx, df=df,
-                 dgate=dgate, dw_post=dw_post, dw_pre=dw_pre)
+    _one_gpu(x, (f, dh, dx_out, w_post, w_pre, gate, dx, df, dgate, dw_post, dw_pre),
+             "x f dh dx_out w_post w_pre gate dx df dgate dw_post dw_pre")
     size = E.ecc_norm_work_size(a)
     work = _work(size, x) if work is None else _given_work(work, size, x)
     _launch(x, E.ecc_norm_grad, a, g, work)
@@ -396,7 +383,7 @@ def distill(z, top, idx, tau=1.0, kd_weight=1.0, ce_weight=0.0, labels=None, wei
     if grad is not None:
         _out(grad, z.shape, z.dtype, z, "grad")
         _, ld_dz = _rows(grad, "grad")
-    _same_device(z, top=top, idx=idx, labels=labels, weight=weight, loss=loss, grad=grad)
+    _one_gpu(z, (top, idx, labels, weight, loss, grad), "z top idx labels weight loss grad")
     size = E.ecc_distill_work_size(a)
     # (a refused description has no size: the call says what is wrong)
     work = _work(max(size, 16), z) if work is None else _given_work(work, size, z)

@@ -109,10 +109,12 @@ class _On:
 def test_operands_on_one_device(monkeypatch):
     lm = pytest.importorskip("paper_2203_17063_amd.lm")
     import contextlib
-    lm._same_device(_On(1), f=_On(1), h=None)
+    lm._one_gpu(_On(1), (_On(1), None), "x f h")
     for other in (-1, 0, 2):
         with pytest.raises(ValueError, match="^gate must be on 1"):
-            lm._same_device(_On(1), f=_On(1), h=None, gate=_On(other))
+            lm._one_gpu(_On(1), (_On(1), None, _On(other)), "x f h gate")
+    with pytest.raises(ValueError, match="^x must be on the GPU"):
+        lm._one_gpu(_On(-1), (_On(-1),), "x f")
     # a launch goes to the tensors' device and its stream
     now = [0]
 
