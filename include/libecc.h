@@ -656,7 +656,8 @@ ecc_status_t ecc_mf_error(ecc_mf_t h, const double *d_W, double *d_rmse, void *h
  *     aligned; they carry nothing from call to call but what is stated.
  *   - Results are bitwise reproducible.  Calls are enqueued on hip_stream.
  *     Outputs must not overlap inputs, other outputs or the work buffer
- *     unless stated.  ECC_ERR_ARG for a bad size, type, leading dimension,
+ *     unless stated; rows of one leading dimension (in bytes) may lie beside
+ *     each other in one buffer, other matrices are compared with their gaps.  ECC_ERR_ARG for a bad size, type, leading dimension,
  *     NULL, alignment or overlap; ECC_ERR_RANGE for a size beyond the
  *     stated limits.
  * --------------------------------------------------------------------------- */

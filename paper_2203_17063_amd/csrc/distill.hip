@@ -745,26 +745,19 @@ ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64
     ECC_ARG((uintptr_t)d_loss % lb == 0 && (uintptr_t)d_dz % tb == 0 &&
                 (uintptr_t)d_work % 16 == 0,
             "an array is not aligned");
-    const int64_t z_bytes = row_extent(N, a->ld_z, a->V) * tb,
-                  dz_bytes = d_dz ? row_extent(N, ld_dz, a->V) * tb : 0, w_bytes = work_bytes(a);
     const bool in_place = d_dz == a->d_z && ld_dz == a->ld_z;
-    struct Range {
-        const void *p;
-        int64_t n;
-    };
-    const Range out[3] = {{d_dz, dz_bytes}, {d_loss, N * lb}, {d_work, w_bytes}};
-    const Range in[5] = {{a->d_z, z_bytes},
-                         {a->d_top, N * a->K * type_size(a->top_type)},
-                         {a->d_idx, N * a->K * 4},
-                         {a->d_labels, a->d_labels ? N * 4 : 0},
-                         {a->d_weight, a->d_weight ? N * 4 : 0}};
+    const Span out[3] = {span_of(d_dz, N, ld_dz, a->V, tb), span_of(d_loss, N * lb),
+                         span_of(d_work, work_bytes(a))};
+    const Span in[5] = {span_of(a->d_z, N, a->ld_z, a->V, tb),
+                        span_of(a->d_top, N * a->K * type_size(a->top_type)),
+                        span_of(a->d_idx, N * a->K * 4), span_of(a->d_labels, N * 4),
+                        span_of(a->d_weight, N * 4)};
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 5; ++i)
-            ECC_ARG((o == 0 && i == 0 && in_place) ||
-                        !ranges_meet(out[o].p, out[o].n, in[i].p, in[i].n),
+            ECC_ARG((o == 0 && i == 0 && in_place) || !spans_meet(out[o], in[i]),
                     "an output overlaps an input");
         for (int q = 0; q < o; ++q)
-            ECC_ARG(!ranges_meet(out[o].p, out[o].n, out[q].p, out[q].n),
+            ECC_ARG(!spans_meet(out[o], out[q]),
                     "two outputs, or an output and the work buffer, overlap");
     }
     DistillArgs d{};

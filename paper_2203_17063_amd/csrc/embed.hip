@@ -831,9 +831,9 @@ ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, con
         set_error("n * D is too large for one launch");
         return ECC_ERR_RANGE;
     }
-    const int64_t out_bytes = row_extent(n, ld_out, D) * ob;
-    ECC_ARG(!ranges_meet(d_out, out_bytes, d_table, row_extent(V, ld_table, D) * tb) &&
-                !ranges_meet(d_out, out_bytes, d_ids, n * ib),
+    const Span out = span_of(d_out, n, ld_out, D, ob);
+    ECC_ARG(!spans_meet(out, span_of(d_table, V, ld_table, D, tb)) &&
+                !spans_meet(out, span_of(d_ids, n * ib)),
             "the output overlaps an input");
     const dim3 grid((unsigned)((n * chunks + per_block - 1) / per_block));
     with_type(table_type, [&](auto t) {
@@ -872,7 +872,8 @@ ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, cons
     ECC_ARG((uintptr_t)d_index % 16 == 0, "d_index must be 16-byte aligned");
     const int64_t ib = id_type == ECC_I64 ? 8 : 4;
     ECC_ARG((uintptr_t)d_ids % ib == 0, "d_ids is not aligned to its elements");
-    ECC_ARG(!ranges_meet(d_ids, l.N * ib, d_index, l.bytes), "d_ids and d_index overlap");
+    ECC_ARG(!spans_meet(span_of(d_ids, l.N * ib), span_of(d_index, l.bytes)),
+            "d_ids and d_index overlap");
     hipStream_t s = (hipStream_t)hip_stream;
     char *base = (char *)d_index;
     uint32_t *keys = (uint32_t *)base;
@@ -964,17 +965,18 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t yb = type_size(dy_type), gb = type_size(grad_type);
     ECC_ARG((uintptr_t)d_grad % gb == 0 && (n == 0 || (uintptr_t)d_dy % yb == 0),
             "an array is not aligned to its elements");
-    const int64_t work = ecc_embed_work_size(P, n, D, dy_type, grad_type);
-    const int64_t grad_bytes = ((P - 1) * worker_stride + per_worker) * gb;
     if (n > 0) {
         ECC_ARG((uintptr_t)d_work % 16 == 0 && (uintptr_t)d_index % 16 == 0,
                 "d_work and d_index must be 16-byte aligned");
-        const int64_t dy_bytes = row_extent(l.N, ld_dy, D) * yb;
-        ECC_ARG(!ranges_meet(d_grad, grad_bytes, d_dy, dy_bytes) &&
-                    !ranges_meet(d_grad, grad_bytes, d_index, l.bytes) &&
-                    !ranges_meet(d_grad, grad_bytes, d_work, work) &&
-                    !ranges_meet(d_work, work, d_dy, dy_bytes) &&
-                    !ranges_meet(d_work, work, d_index, l.bytes),
+        // (workers' gradients that do not follow each other row by row are
+        // compared as a whole)
+        const Span grad = P == 1 || worker_stride == V * ld_grad
+                              ? span_of(d_grad, P * V, ld_grad, D, gb)
+                              : span_of(d_grad, row_extent(P, worker_stride, per_worker) * gb);
+        const Span dy = span_of(d_dy, l.N, ld_dy, D, yb), index = span_of(d_index, l.bytes),
+                   work = span_of(d_work, ecc_embed_work_size(P, n, D, dy_type, grad_type));
+        ECC_ARG(!spans_meet(grad, dy) && !spans_meet(grad, index) && !spans_meet(grad, work) &&
+                    !spans_meet(work, dy) && !spans_meet(work, index),
                 "the gradient, the work buffer and the inputs must not overlap");
     }
     if (n == 0 && accumulate) return ECC_OK;

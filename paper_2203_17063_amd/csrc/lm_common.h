@@ -8,6 +8,7 @@
 // way of an fp32 that cannot change the outcome (on_the_way_to_bf16).
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "ecc_common.h"
@@ -49,9 +50,39 @@ inline bool ranges_meet(const void *a, int64_t na, const void *b, int64_t nb) {
     return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
-// Elements between the first and the end of the last row.
+// Elements between the first and the end of the last row (up to 2^59, beyond
+// any memory, so that their bytes fit 64 bits).
 inline int64_t row_extent(int64_t rows, int64_t ld, int64_t cols) {
-    return rows > 0 ? (rows - 1) * ld + cols : 0;
+    const __int128 n = rows > 0 ? (__int128)(rows - 1) * ld + cols : 0;
+    return (int64_t)std::min<__int128>(n, int64_t(1) << 59);
+}
+
+// Memory of a matrix, in bytes: rows of `width`, `pitch` from one to the next.
+struct Span {
+    const void *p = nullptr;
+    int64_t rows = 0, pitch = 0, width = 0;
+    int64_t bytes() const { return p ? row_extent(rows, pitch, width) : 0; }
+};
+inline Span span_of(const void *p, int64_t rows, int64_t ld, int64_t cols, int64_t size) {
+    return Span{p, rows, ld * size, cols * size};
+}
+inline Span span_of(const void *p, int64_t bytes) { return Span{p, 1, bytes, bytes}; }
+
+// Do two of them share a byte?  Rows of one pitch may lie beside each other in
+// one buffer; matrices of different pitches are compared as a whole, gaps
+// included.
+inline bool spans_meet(const Span &a, const Span &b) {
+    if (!ranges_meet(a.p, a.bytes(), b.p, b.bytes())) return false;
+    const int64_t pitch = a.rows > 1 ? a.pitch : b.pitch;
+    if ((a.rows == 1 && b.rows == 1) || (b.rows > 1 && b.pitch != pitch) || a.width > pitch ||
+        b.width > pitch)
+        return true;
+    // row j of b begins d + (j - i) pitch after row i of a: between b's width
+    // ahead of it and a's width behind for one of two differences only
+    const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
+    const int64_t below = d >= 0 ? d / pitch : -((-d + pitch - 1) / pitch), rest = d - below * pitch;
+    auto there = [&](int64_t k) { return k > -a.rows && k < b.rows; };  // k = j - i
+    return (there(-below) && rest < a.width) || (there(-below - 1) && rest - pitch > -b.width);
 }
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }

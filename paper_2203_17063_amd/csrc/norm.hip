@@ -713,20 +713,14 @@ static ecc_status_t check_norm(const ecc_norm_t *a) {
     return ECC_OK;
 }
 
-// An output: NULL, or rows x D elements of `type` that meet none of the
-// inputs but one that it may stand in for (the same address and ld).
-struct Span {
-    const void *p;
-    int64_t bytes;
-};
+// Does an output meet the gate or a weight?
 static bool meets_input(const ecc_norm_t *a, const Span &o) {
     const int64_t rows = a->P * a->n, tb = type_size(a->type), wb = type_size(a->w_type);
-    const int64_t grows = a->gate_rows ? (rows + a->gate_rows - 1) / a->gate_rows : 1;
-    return (a->d_gate &&
-            ranges_meet(o.p, o.bytes, a->d_gate,
-                        a->gate_rows ? row_extent(grows, a->ld_gate, a->D) * tb : a->D * wb)) ||
-           (a->d_w_post && ranges_meet(o.p, o.bytes, a->d_w_post, a->D * wb)) ||
-           (a->d_w_pre && ranges_meet(o.p, o.bytes, a->d_w_pre, a->D * wb));
+    const Span gate = a->gate_rows ? span_of(a->d_gate, (rows + a->gate_rows - 1) / a->gate_rows,
+                                             a->ld_gate, a->D, tb)
+                                   : span_of(a->d_gate, a->D * wb);
+    return spans_meet(o, gate) || spans_meet(o, span_of(a->d_w_post, a->D * wb)) ||
+           spans_meet(o, span_of(a->d_w_pre, a->D * wb));
 }
 
 }  // namespace ecc
@@ -753,19 +747,14 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
     ECC_ARG(a->d_x, "NULL pointer");
     ECC_ARG(((uintptr_t)d_x_out | (uintptr_t)d_h) % tb == 0,
             "an array is not aligned to its elements");
-    const Span x{a->d_x, row_extent(N, a->ld_x, a->D) * tb},
-        f{a->d_f, a->d_f ? row_extent(N, a->ld_f, a->D) * tb : 0},
-        xo{d_x_out, d_x_out ? row_extent(N, ld_x_out, a->D) * tb : 0},
-        h{d_h, d_h ? row_extent(N, ld_h, a->D) * tb : 0};
-    auto clash = [](const Span &p, const Span &q) {
-        return ranges_meet(p.p, p.bytes, q.p, q.bytes);
-    };
+    const Span x = span_of(a->d_x, N, a->ld_x, a->D, tb), f = span_of(a->d_f, N, a->ld_f, a->D, tb),
+               xo = span_of(d_x_out, N, ld_x_out, a->D, tb), h = span_of(d_h, N, ld_h, a->D, tb);
     const bool xo_is_x = d_x_out == a->d_x && ld_x_out == a->ld_x;
     const bool h_is_f = d_h == a->d_f && ld_h == a->ld_f;
     const bool h_is_x = d_h == a->d_x && ld_h == a->ld_x;
-    ECC_ARG((!clash(xo, x) || xo_is_x) && !clash(xo, f) && (!clash(h, f) || h_is_f) &&
-                (!clash(h, x) || h_is_x) && !clash(xo, h) && !meets_input(a, xo) &&
-                !meets_input(a, h),
+    ECC_ARG((!spans_meet(xo, x) || xo_is_x) && !spans_meet(xo, f) &&
+                (!spans_meet(h, f) || h_is_f) && (!spans_meet(h, x) || h_is_x) &&
+                !spans_meet(xo, h) && !meets_input(a, xo) && !meets_input(a, h),
             "an output overlaps an input or the other output");
     NormArgs n{N,          a->D,      a->d_x,    a->d_f,       a->d_gate, a->d_w_post,
                a->d_w_pre, a->ld_x,   a->ld_f,   a->ld_gate,   a->gate_rows, a->w_type,
@@ -833,41 +822,29 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
             "an array is not aligned to its elements");
     // inputs and outputs, and which output may stand in for which input
     const int64_t gate_n = a->gate_rows ? (N + a->gate_rows - 1) / a->gate_rows : 0;
-    const int64_t param_bytes = ((a->P - 1) * (a->P > 1 ? g->worker_stride : 0) + D) * gb;
-    auto rows = [&](const void *p, int64_t ld) {
-        return Span{p, p ? row_extent(N, ld, D) * tb : 0};
-    };
+    auto rows = [&](const void *p, int64_t ld) { return span_of(p, N, ld, D, tb); };
+    auto param = [&](const void *p) { return span_of(p, a->P, g->worker_stride, D, gb); };
     const Span in[4] = {rows(a->d_x, a->ld_x), rows(a->d_f, a->ld_f), rows(g->d_dh, g->ld_dh),
                         rows(g->d_dx_out, g->ld_dx_out)};
-    const Span out[6] = {
-        rows(g->d_dx, g->ld_dx), rows(g->d_df, g->ld_df),
-        Span{g->d_dgate, !g->d_dgate ? 0
-                         : row_gate  ? row_extent(gate_n, g->ld_dgate, D) * tb
-                                     : param_bytes},
-        Span{g->d_dw_post, g->d_dw_post ? param_bytes : 0},
-        Span{g->d_dw_pre, g->d_dw_pre ? param_bytes : 0},
-        Span{d_work, N ? ecc_norm_work_size(a) : 0}};
+    const Span out[6] = {rows(g->d_dx, g->ld_dx),
+                         rows(g->d_df, g->ld_df),
+                         row_gate ? span_of(g->d_dgate, gate_n, g->ld_dgate, D, tb)
+                                  : param(g->d_dgate),
+                         param(g->d_dw_post),
+                         param(g->d_dw_pre),
+                         span_of(d_work, N ? ecc_norm_work_size(a) : 0)};
     const int64_t in_ld[4] = {a->ld_x, a->ld_f, g->ld_dh, g->ld_dx_out};
     const int64_t out_ld[2] = {g->ld_dx, g->ld_df};
     for (int o = 0; o < 6; ++o) {
         for (int i = 0; i < 4; ++i) {
             const bool stands_in = o < 2 && out[o].p == in[i].p && out_ld[o] == in_ld[i] &&
                                    (o == 0 ? i >= 2 : i == 1 || i == 2);
-            ECC_ARG(stands_in || !ranges_meet(out[o].p, out[o].bytes, in[i].p, in[i].bytes),
-                    "an output overlaps an input");
+            ECC_ARG(stands_in || !spans_meet(out[o], in[i]), "an output overlaps an input");
         }
         ECC_ARG(!meets_input(a, out[o]), "an output overlaps an input");
-        // (parameters of several workers lie side by side in one
-        // contribution: of them only the first worker's can be compared)
-        for (int q = 0; q < o; ++q) {
-            const bool both_params = a->P > 1 && o >= 2 && o < 5 && q >= 2 && q < 5 &&
-                                     (o != 2 || !row_gate) && (q != 2 || !row_gate);
-            const int64_t bo = both_params ? D * gb : out[o].bytes;
-            const int64_t bq = both_params ? D * gb : out[q].bytes;
-            ECC_ARG(!ranges_meet(out[o].p, out[o].bytes ? bo : 0, out[q].p,
-                                 out[q].bytes ? bq : 0),
+        for (int q = 0; q < o; ++q)
+            ECC_ARG(!spans_meet(out[o], out[q]),
                     "two outputs, or an output and the work buffer, overlap");
-        }
     }
     hipStream_t s = (hipStream_t)hip_stream;
     if (N == 0 && (!params || g->accumulate)) return ECC_OK;

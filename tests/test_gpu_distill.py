@@ -503,3 +503,23 @@ def test_work_buffers_that_do_not_hold():
         with pytest.raises(ValueError):
             call(work)
     call(torch.empty(size, dtype=torch.uint8, device="cuda"))
+
+
+def test_gradient_beside_the_logits():
+    """Logits and gradient as columns of one buffer."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("distill, gradient beside the logits")
+    N, V = 5, 301
+    d = {k: v.cuda() for k, v in _inputs(N, V, 7, BF16).items()}
+    want = lm.distill(ce_weight=0.3, **d)
+    wide = torch.full((N, 2 * V + 1), 5.0, dtype=BF16, device="cuda")
+    wide[:, :V] = d["z"]
+    d["z"] = wide[:, :V]
+    got = lm.distill(ce_weight=0.3, grad=wide[:, V:2 * V], **d)
+    assert torch.equal(got[0], want[0]) and torch.equal(wide[:, V:2 * V], want[1])
+    assert (wide[:, 2 * V] == 5).all()
+    for k in (V - 1, 1):
+        with pytest.raises(E.EccError) as e:
+            lm.distill(grad=wide[:, k:k + V], **d)
+        assert e.value.status == E.ECC_ERR_ARG

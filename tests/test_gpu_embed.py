@@ -478,3 +478,28 @@ def test_work_buffers_that_do_not_hold():
         with pytest.raises(ValueError):
             call(work)
     call(torch.empty(size, dtype=torch.uint8, device="cuda"))
+
+
+def test_rows_beside_the_table():
+    """Table, lookup and gradient as columns of one buffer."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("embed, rows beside each other")
+    n, D = 30, 19
+    wide = torch.full((n, 3 * D + 1), 5.0, device="cuda")
+    table, out, grad = (wide[:, k * D:(k + 1) * D] for k in range(3))
+    table.copy_(_random((n, D), F32, 1))
+    ids = _tokens(n, 0, n, 2).cuda()
+    lm.embed_lookup(table, ids, out=out)
+    assert torch.equal(out, table[ids])
+    index = lm.embed_index(ids, n)
+    want = lm.embed_grad(index, out.clone())
+    lm.embed_grad(index, out, grad=grad[None])
+    assert torch.equal(grad, want[0]) and (wide[:, 3 * D] == 5).all()
+    assert torch.equal(out, table[ids])
+    for k in (D - 1, 1):
+        with pytest.raises(E.EccError) as e:
+            lm.embed_lookup(table, ids, out=wide[:, k:k + D])
+        assert e.value.status == E.ECC_ERR_ARG
+    with pytest.raises(E.EccError):
+        lm.embed_grad(index, out, grad=wide[None, :, 2 * D - 1:3 * D - 1])

@@ -606,3 +606,50 @@ def test_work_buffers_that_do_not_hold():
         with pytest.raises(ValueError):
             call(work)
     call(torch.empty(size, dtype=torch.uint8, device="cuda"))
+
+
+def test_workers_gradients_that_overlap():
+    """A parameter's gradient of one worker in the place of another parameter's
+    of the next worker is refused; one beside the other is not."""
+    from paper_2203_17063_amd import capi as E
+    announce("norm grad, workers' overlap")
+    P, n, D = 3, 4, 16
+    s = _gpu_args(_inputs(P * n, D, F32, F32))
+    dh = torch.zeros((P * n, D), device="cuda")
+    flat = torch.zeros(4096, device="cuda")
+
+    def at(first, stride=64):
+        return torch.as_strided(flat, (P, D), (stride, 1), first)
+
+    for first in (64, 128, 64 + 15, 64 - 15, 128 + 3):
+        with pytest.raises(E.EccError) as e:
+            _lm().norm_grad(dh=dh, P=P, dw_post=at(0), dw_pre=at(first), **s)
+        assert e.value.status == E.ECC_ERR_ARG
+    for first in (16, 48, 64 + 16, 64 + 48, 192, 192 + 5):
+        _lm().norm_grad(dh=dh, P=P, dw_post=at(0), dw_pre=at(first), **s)
+
+
+def test_rows_beside_each_other():
+    """Operands and results as columns of one buffer, which share no element; by
+    one column less they do, and are refused."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("norm, rows beside each other")
+    N, D = 9, 37
+    s = _gpu_args(_inputs(N, D, F32, F32))
+    dh, dxo = _random((N, D), F32, 61).cuda(), _random((N, D), F32, 62).cuda()
+    want, want_g = lm.norm_forward(**s), lm.norm_grad(dh=dh, dx_out=dxo, **s)
+    wide = torch.full((N, 4 * D + 2), 5.0, device="cuda")
+    x, f, y, h = (wide[:, 1 + k * D:1 + (k + 1) * D] for k in range(4))
+    x.copy_(s["x"])
+    f.copy_(s["f"])
+    t = dict(s, x=x, f=f)
+    lm.norm_forward(x_out=y, h=h, **t)
+    assert torch.equal(y, want[0]) and torch.equal(h, want[1]) and torch.equal(x, s["x"])
+    lm.norm_grad(dh=dh, dx_out=dxo, dx=h, df=y, **t)
+    assert torch.equal(h, want_g["dx"]) and torch.equal(y, want_g["df"])
+    assert (wide[:, 0] == 5).all() and (wide[:, -1] == 5).all()
+    for k in (1 + 2 * D - 1, D + 2, 2 * D, 3):
+        with pytest.raises(E.EccError) as e:
+            lm.norm_forward(x_out=wide[:, k:k + D], h=h, **t)
+        assert e.value.status == E.ECC_ERR_ARG
