@@ -281,10 +281,15 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
                         (dw_pre, w_pre, "dw_pre")):
         if t is not None and of is None:
             raise ValueError("%s given without its operand" % what)
-    given = [t for t in (dw_post, dw_pre, dgate if gate is not None and gate_rows == 0 else None)
-             if t is not None]
+    wanted = [t for t, of in ((dw_post, w_post), (dw_pre, w_pre),
+                              (dgate, gate if gate_rows == 0 else None)) if of is not None]
+    given = [t for t in wanted if t is not None]
     dtype = given[0].dtype if given else dtype or w_dtype
     stride = given[0].stride(0) if given and P > 1 else D
+    # new ones beside given ones in wide contributions are dense, and so are
+    # those that the kernels write: the given ones are copies of them
+    apart = stride != D and len(given) < len(wanted)
+    copies = []
 
     def rows_in(t, what):
         if t is None:
@@ -307,13 +312,20 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         if t is None:
             if accumulate:
                 raise ValueError("accumulate needs %s" % what)
-            t = x.new_empty((P, stride), dtype=dtype)
-            return t if stride == D else t[:, :D]
+            t = x.new_empty((P, D), dtype=dtype)
+            return t, t.data_ptr()
         if tuple(t.shape) != (P, D) or t.dtype != dtype or (D > 1 and t.stride(1) != 1) or \
                 (P > 1 and t.stride(0) != stride):
             raise ValueError("%s must be %s of shape %s, one stride for all" %
                              (what, dtype, (P, D)))
-        return t
+        if not apart:
+            return t, t.data_ptr()
+        for other, _ in copies:   # (of the others the library sees where they are)
+            at = (t.data_ptr() - other.data_ptr()) // t.element_size()
+            if abs(at) < P * stride and min(at % stride, -at % stride) < D:
+                raise ValueError("two gradients overlap")
+        copies.append((t, t.new_empty((P, D))))
+        return t, copies[-1][1].data_ptr()
 
     d_dh, ld_dh = rows_in(dh, "dh")
     d_dxo, ld_dxo = rows_in(dx_out, "dx_out")
@@ -326,22 +338,21 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
         if gate_rows:
             dgate, d_dgate, ld_dgate = rows_out(dgate, gate, "dgate")
         else:
-            dgate = param(dgate, "dgate")
-            d_dgate = dgate.data_ptr()
+            dgate, d_dgate = param(dgate, "dgate")
     if w_post is not None:
-        dw_post = param(dw_post, "dw_post")
-        d_post = dw_post.data_ptr()
+        dw_post, d_post = param(dw_post, "dw_post")
     if w_pre is not None:
-        dw_pre = param(dw_pre, "dw_pre")
-        d_pre = dw_pre.data_ptr()
+        dw_pre, d_pre = param(dw_pre, "dw_pre")
     g = E.ecc_norm_grad_t(d_dh, ld_dh, d_dxo, ld_dxo, d_dx, ld_dx, d_df, ld_df, d_dgate, ld_dgate,
                           d_post, d_pre, _type(dtype, "the gradients"), 1 if accumulate else 0,
-                          stride)
+                          D if apart else stride)
     _one_gpu(x, (f, dh, dx_out, w_post, w_pre, gate, dx, df, dgate, dw_post, dw_pre),
              "x f dh dx_out w_post w_pre gate dx df dgate dw_post dw_pre")
     size = E.ecc_norm_work_size(a)
     work = _work(size, x) if work is None else _given_work(work, size, x)
     _launch(x, E.ecc_norm_grad, a, g, work)
+    for t, dense in copies:
+        t.copy_(dense)
     return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
 
 

@@ -653,3 +653,32 @@ def test_rows_beside_each_other():
         with pytest.raises(E.EccError) as e:
             lm.norm_forward(x_out=wide[:, k:k + D], h=h, **t)
         assert e.value.status == E.ECC_ERR_ARG
+
+
+def test_grad_given_beside_new():
+    """One parameter's gradient given as a view of wide contributions: the
+    others take no more memory than they hold."""
+    lm = _lm()
+    announce("norm grad, one given")
+    P, n, D, m = 8, 20, 64, 1 << 22
+    s = _gpu_args(_inputs(P * n, D, F32, F32, "param"))
+    dh, dxo = _random((P * n, D), F32, 61).cuda(), _random((P * n, D), F32, 62).cuda()
+    want = lm.norm_grad(dh=dh, dx_out=dxo, P=P, **s)
+    contrib = torch.full((P, m), 3.0, device="cuda")
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    got = lm.norm_grad(dh=dh, dx_out=dxo, P=P, dw_pre=contrib[:, 5:5 + D], **s)
+    assert torch.cuda.max_memory_allocated() - before < P * m
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    assert got["dw_pre"].data_ptr() == contrib[:, 5:].data_ptr()
+    contrib[:, 5:5 + D] = 3.0
+    assert (contrib == 3).all()
+    got = lm.norm_grad(dh=dh, dx_out=dxo, P=P, dw_pre=contrib[:, 5:5 + D],
+                       dgate=contrib[:, 5 + D:5 + 2 * D], **s)
+    assert all(torch.equal(got[k], want[k]) for k in want)
+    for at in (5 + D - 1, 6, 4):
+        with pytest.raises(ValueError):
+            lm.norm_grad(dh=dh, dx_out=dxo, P=P, dw_pre=contrib[:, 5:5 + D],
+                         dgate=contrib[:, at:at + D], **s)
