@@ -349,7 +349,8 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
     _one_gpu(x, (f, dh, dx_out, w_post, w_pre, gate, dx, df, dgate, dw_post, dw_pre),
              "x f dh dx_out w_post w_pre gate dx df dgate dw_post dw_pre")
     size = E.ecc_norm_work_size(a)
-    work = _work(size, x) if work is None else _given_work(work, size, x)
+    # (a refused description has no size: the call says what is wrong)
+    work = _work(max(size, 16), x) if work is None else _given_work(work, size, x)
     _launch(x, E.ecc_norm_grad, a, g, work)
     for t, dense in copies:
         t.copy_(dense)

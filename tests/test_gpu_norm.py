@@ -682,3 +682,12 @@ def test_grad_given_beside_new():
         with pytest.raises(ValueError):
             lm.norm_grad(dh=dh, dx_out=dxo, P=P, dw_pre=contrib[:, 5:5 + D],
                          dgate=contrib[:, at:at + D], **s)
+
+
+def test_grad_refusal_says_why():
+    from paper_2203_17063_amd import capi as E
+    announce("norm grad, refusal")
+    x, w = torch.zeros((4, 8), device="cuda"), torch.ones(8, device="cuda")
+    with pytest.raises(E.EccError) as e:
+        _lm().norm_grad(x, None, x.clone(), w_pre=w, eps=0.0)
+    assert e.value.status == E.ECC_ERR_ARG and "eps" in str(e.value)
