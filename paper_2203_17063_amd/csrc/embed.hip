@@ -815,7 +815,7 @@ ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, con
     ECC_ARG((uintptr_t)d_ids % ib == 0 && (uintptr_t)d_table % tb == 0 &&
                 (uintptr_t)d_out % ob == 0,
             "an array is not aligned to its elements");
-    if (V >= (int64_t(1) << 32) - 1 || D >= (int64_t(1) << 40) || n >= (int64_t(1) << 40) ||
+    if (V >= (int64_t(1) << 32) - 1 || D >= (int64_t(1) << 40) || n >= (int64_t(1) << 32) ||
         ld_table >= (int64_t(1) << 40) || ld_out >= (int64_t(1) << 40)) {
         set_error("a size is too large");
         return ECC_ERR_RANGE;
@@ -826,28 +826,32 @@ ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, con
     while ((1 << log2_lanes) < vecs && log2_lanes < 6) ++log2_lanes;
     const int64_t chunks = (vecs + (1 << log2_lanes) - 1) >> log2_lanes;
     const int64_t per_block = kEmbedThreads >> log2_lanes;
-    if (n > (int64_t(1) << 44) / chunks ||
-        (n * chunks + per_block - 1) / per_block > 0x7fffff) {
-        set_error("n * D is too large for one launch");
+    const int64_t most = 0x7fffff * per_block / chunks;  // tokens of one launch
+    if (most == 0) {
+        set_error("D is too large for one launch");
         return ECC_ERR_RANGE;
     }
     const Span out = span_of(d_out, n, ld_out, D, ob);
     ECC_ARG(!spans_meet(out, span_of(d_table, V, ld_table, D, tb)) &&
                 !spans_meet(out, span_of(d_ids, n * ib)),
             "the output overlaps an input");
-    const dim3 grid((unsigned)((n * chunks + per_block - 1) / per_block));
-    with_type(table_type, [&](auto t) {
-        with_type(out_type, [&](auto o) {
-            using T = decltype(t);
-            using O = decltype(o);
-            using A = Wider<T, O>;
-            constexpr int VEC = kVec<T> > kVec<O> ? kVec<T> : kVec<O>;
-            hipLaunchKernelGGL((k_embed_lookup<T, O, A, VEC>), grid, dim3(kEmbedThreads), 0,
-                               (hipStream_t)hip_stream, n, V, D, row0, d_ids,
-                               id_type == ECC_I64, (const T *)d_table, ld_table, (A)scale,
-                               (O *)d_out, ld_out, log2_lanes, chunks);
+    for (int64_t t0 = 0; t0 < n; t0 += most) {
+        const int64_t m = std::min(most, n - t0);
+        const dim3 grid((unsigned)((m * chunks + per_block - 1) / per_block));
+        with_type(table_type, [&](auto t) {
+            with_type(out_type, [&](auto o) {
+                using T = decltype(t);
+                using O = decltype(o);
+                using A = Wider<T, O>;
+                constexpr int VEC = kVec<T> > kVec<O> ? kVec<T> : kVec<O>;
+                hipLaunchKernelGGL((k_embed_lookup<T, O, A, VEC>), grid, dim3(kEmbedThreads), 0,
+                                   (hipStream_t)hip_stream, m, V, D, row0,
+                                   (const char *)d_ids + t0 * ib, id_type == ECC_I64,
+                                   (const T *)d_table, ld_table, (A)scale,
+                                   (O *)d_out + t0 * ld_out, ld_out, log2_lanes, chunks);
+            });
         });
-    });
+    }
     ECC_LAUNCH_CHECK();
     return ECC_OK;
 }

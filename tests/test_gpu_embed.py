@@ -503,3 +503,22 @@ def test_rows_beside_the_table():
         assert e.value.status == E.ECC_ERR_ARG
     with pytest.raises(E.EccError):
         lm.embed_grad(index, out, grad=wide[None, :, 2 * D - 1:3 * D - 1])
+
+
+def test_lookup_of_more_than_one_launch():
+    """An output of more than 32 GiB: more workgroups than one launch takes."""
+    lm = _lm()
+    n, V, D = (1 << 23) + 5, 300, 2048
+    if torch.cuda.mem_get_info()[0] < 2 * n * D + (8 << 30):
+        pytest.skip("not enough device memory")
+    announce("lookup, 34 GB")
+    table, ids = _random((V, D), BF16, 1).cuda(), torch.arange(n, device="cuda") % V
+    out = torch.full((n, D), 7.0, dtype=BF16, device="cuda")
+    lm.embed_lookup(table, ids, out=out)
+    for lo in list(range(0, n, 1 << 20)) + [n - 1000]:
+        hi = min(n, lo + 1000)
+        assert torch.equal(out[lo:hi], table[ids[lo:hi]])
+    at = torch.randint(0, n, (100000,), device="cuda")
+    assert torch.equal(out[at], table[ids[at]])
+    del out
+    torch.cuda.empty_cache()
