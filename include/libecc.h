@@ -671,7 +671,7 @@ ecc_status_t ecc_mf_error(ecc_mf_t h, const double *d_W, double *d_rmse, void *h
  * rows of D elements; zeros where ids[t] - row0 lies outside [0, V) (padding,
  * or a token of another part of a table that is split by rows).  The product
  * is formed in fp32 (fp64 when table or out is fp64).  id_type: ECC_I32 or
- * ECC_I64.  V in [1, 2^32 - 1), D in [1, 2^33], n in [0, 2^32), else
+ * ECC_I64.  V in [1, 2^32 - 1), D in [1, 2^31], n in [0, 2^32), else
  * ECC_ERR_RANGE. */
 ecc_status_t ecc_embed_lookup(int64_t n, int64_t V, int64_t D, int64_t row0, const void *d_ids,
                               int32_t id_type, const void *d_table, int32_t table_type,
