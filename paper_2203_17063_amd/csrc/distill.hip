@@ -686,6 +686,21 @@ inline int64_t work_bytes(const ecc_distill_t *a) {
     return stats_bytes(a, parts) + a->N * (a->K + 1) * (a->type == ECC_F64 ? 8 : 4);
 }
 
+// The same from a later row on.
+template <typename T>
+DistillArgs rows_from(DistillArgs a, int64_t row) {
+    a.z = (const T *)a.z + row * a.ld_z;
+    if (a.dz) a.dz = (T *)a.dz + row * a.ld_dz;
+    a.loss = (Acc<T> *)a.loss + row;
+    if (a.K > 0) {
+        a.top = (const char *)a.top + row * a.K * type_size(a.top_type);
+        a.idx += row * a.K;
+    }
+    if (a.labels) a.labels += row;
+    if (a.weight) a.weight += row;
+    return a;
+}
+
 // Rows of their own workgroups: as many threads as hold a row in 16 vectors
 // each, up to 1,024.  16 vectors leave 16 waves to a CU, four rows of 32,000
 // bf16 logits at a time (16,384 rows, temperature 2 with hard labels: 0.43 ms,
@@ -705,8 +720,12 @@ void launch_distill(const DistillArgs &a, int64_t N, hipStream_t s) {
         return;
     }
     const int64_t vecs = a.V / kVec<T>;
+    // (a launch has fewer than 2^32 threads)
     auto launch = [&](auto kernel, int threads) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)N), dim3(threads), lds, s, a);
+        const int64_t most = (int64_t(1) << 31) / threads;
+        for (int64_t row = 0; row < N; row += most)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(most, N - row)), dim3(threads), lds,
+                               s, rows_from<T>(a, row));
     };
     constexpr bool f64 = std::is_same_v<T, double>;
     constexpr int H = f64 ? 8 : 16, W = f64 ? 2 : 4, MOST = f64 ? 512 : 1024;

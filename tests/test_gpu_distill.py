@@ -523,3 +523,24 @@ def test_gradient_beside_the_logits():
         with pytest.raises(E.EccError) as e:
             lm.distill(grad=wide[:, k:k + V], **d)
         assert e.value.status == E.ECC_ERR_ARG
+
+
+@pytest.mark.parametrize("act,V,K,in_place", [(BF16, 3, 2, False), (F32, 2, 0, True)])
+def test_more_rows_than_one_launch_takes(act, V, K, in_place):
+    """Rows of more than 2^32 threads: all repeats of some rows give the same."""
+    lm = _lm()
+    N = 2 * (1 << 31) // 64 + 1003      # (64 threads to a row)
+    announce("distill, many launches", act, N, V, K)
+    n = 997
+    s = {k: v.cuda() for k, v in _inputs(n, V, K, act, absent=0.1).items()}
+    d = {k: v.repeat(-(-N // n), *[1] * (v.dim() - 1))[:N] for k, v in s.items()}
+    want = lm.distill(tau=2.0, kd_weight=0.7, ce_weight=0.3, **s)
+    loss, grad = lm.distill(tau=2.0, kd_weight=0.7, ce_weight=0.3,
+                            grad=d["z"] if in_place else True, **d)
+    for got, w in ((loss, want[0]), (grad, want[1])):
+        whole = N // n * n
+        step = n * 4096
+        for at in range(0, whole, step):
+            hi = min(whole, at + step)
+            assert (got[at:hi].view(-1, n, *w.shape[1:]) == w).all()
+        assert torch.equal(got[whole:], w[:N - whole])
