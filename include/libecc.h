@@ -754,6 +754,7 @@ ecc_status_t ecc_norm_forward(const ecc_norm_t *a, void *d_x_out, int64_t ld_x_o
  * are not computed; d_df, d_dw_post and d_dgate need d_f (d_dw_post also
  * d_w_post, d_dgate d_gate, d_dw_pre d_w_pre).  d_dx may be d_dx_out or
  * d_dh, and d_df may be d_f or d_dh (with the same leading dimension).
+ * P below 2^22 (2^26 for rows of up to 1 KiB), else ECC_ERR_RANGE.
  * With grad_type ECC_F64 the sums over rows are fp64's, of terms of `type`'s
  * arithmetic.  d_work: ecc_norm_work_size(a) bytes. */
 typedef struct {

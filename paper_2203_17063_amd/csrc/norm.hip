@@ -862,8 +862,8 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
     ga.ld_df = g->ld_df;
     ga.ld_dgate = g->ld_dgate;
     ga.u = units_of(a);
-    if (ga.u.total > 0x7fffff) {
-        set_error("P * n is too large for one launch");
+    if (ga.u.total >= (int64_t(1) << 32) / backward_threads(a->type, D)) {
+        set_error("P = %d workers are too many for one launch", a->P);
         return ECC_ERR_RANGE;
     }
     auto run = [&](auto t, auto sum) {
@@ -900,15 +900,23 @@ ecc_status_t ecc_norm_grad(const ecc_norm_t *a, const ecc_norm_grad_t *g, void *
                 hipLaunchKernelGGL(kernel, dim3((unsigned)ga.u.total), dim3(NT), lds, s, n,
                                    args);
             });
-        auto join = [&](const NormJoin &j, int arrays) {
-            const int64_t wide = (D + 63) / 64 * j.count;
-            if (wide >= 64)
-                hipLaunchKernelGGL((k_norm_join<S, 64>), dim3((unsigned)wide, arrays),
-                                   dim3(kNormJoinThreads), 0, s, j);
-            else
-                hipLaunchKernelGGL((k_norm_join<S, 16>),
-                                   dim3((unsigned)((D + 15) / 16 * j.count), arrays),
-                                   dim3(kNormJoinThreads), 0, s, j);
+        // (as many results at a time as a launch of fewer than 2^32 threads has)
+        auto join = [&](NormJoin j, int arrays) {
+            const int64_t results = j.count;
+            const bool wide = (D + 63) / 64 * results >= 64;
+            const int64_t blocks = wide ? (D + 63) / 64 : (D + 15) / 16;
+            const int64_t most = (int64_t(1) << 31) / kNormJoinThreads / blocks;
+            for (int64_t at = 0; at < results; at += most) {
+                j.count = std::min(most, results - at);
+                const dim3 grid((unsigned)(blocks * j.count), arrays), threads(kNormJoinThreads);
+                if (wide) hipLaunchKernelGGL((k_norm_join<S, 64>), grid, threads, 0, s, j);
+                else hipLaunchKernelGGL((k_norm_join<S, 16>), grid, threads, 0, s, j);
+                for (int z = 0; z < arrays; ++z) {
+                    j.from[z] = j.from[z] ? (const S *)j.from[z] + j.count * j.per * D : nullptr;
+                    j.to[z] = j.to[z] ? (char *)j.to[z] + j.count * j.ld[z] * type_size(j.type[z])
+                                      : nullptr;
+                }
+            }
         };
         if (params) {
             NormJoin j{};

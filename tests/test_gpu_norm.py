@@ -691,3 +691,20 @@ def test_grad_refusal_says_why():
     with pytest.raises(E.EccError) as e:
         _lm().norm_grad(x, None, x.clone(), w_pre=w, eps=0.0)
     assert e.value.status == E.ECC_ERR_ARG and "eps" in str(e.value)
+
+
+def test_grad_of_many_workers():
+    """A row each of 70,000 workers: more workgroups in the join than one launch
+    of fewer than 2^32 threads has.  A worker's gradient is its row's term,
+    within 100 u."""
+    announce("norm grad, many workers")
+    P, D = 70000, 4096
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((P, D), generator=g, device="cuda").to(BF16)
+    dh = torch.randn((P, D), generator=g, device="cuda").to(BF16)
+    got = _lm().norm_grad(x, None, dh, None, w_pre=torch.ones(D, device="cuda"), eps=EPS,
+                          P=P)["dw_pre"]
+    for lo in range(0, P, 10000):
+        v = x[lo:lo + 10000].double()
+        want = dh[lo:lo + 10000].double() * v * torch.rsqrt((v * v).mean(1, keepdim=True) + EPS)
+        assert ((got[lo:lo + 10000] - want).abs() <= 101 * 2.0 ** -24 * want.abs()).all()
