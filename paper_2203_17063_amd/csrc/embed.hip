@@ -111,7 +111,8 @@ __device__ __forceinline__ uint32_t bins_scan(uint32_t v, uint32_t *sums) {
 // of its tokens.  The one CU's LDS bounds it: rows and positions travel in one
 // word where that holds them (PACK: tables below 2^18 rows).
 template <int ITEMS, bool PACK>
-__global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t V, int64_t row0,
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t worker0, int64_t n,
+                                                             int64_t V, int64_t row0,
                                                              const void *ids, int id64,
                                                              int passes,
                                                              uint32_t *__restrict__ keys_out,
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t 
     auto key_at = [](uint32_t i) { return i + i / ITEMS; };
     auto pos_at = [](uint32_t i) { return i + i / ITEMS * 2; };
     const int tid = threadIdx.x;
-    const int64_t first = (int64_t)blockIdx.x * n;
+    const int64_t worker = worker0 + blockIdx.x, first = worker * n;
     constexpr int rb = kSmallBits, bins = kSmallBins;
     constexpr uint32_t mask = bins - 1;
     auto count_at = [&](uint32_t digit) {
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t 
         return s_count + i + 8 * (i >> rb);
     };
     // (cleared before the barriers that lie ahead of the flags set below)
-    uint8_t *const flags = touched + blockIdx.x * V;
+    uint8_t *const flags = touched + worker * V;
     const int64_t whole = min((int64_t)(-(uintptr_t)flags & 15), V);  // before 16-byte accesses
     const int64_t quads16 = (V - whole) / 16, behind = whole + 16 * quads16;
     if (tid < whole) flags[tid] = 0;
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(int64_t n, int64_t 
             __syncthreads();
         }
     }
-    const uint32_t key0 = blockIdx.x * (uint32_t)(V + 1);
+    const uint32_t key0 = (uint32_t)worker * (uint32_t)(V + 1);
     for (int i = tid; i < n; i += kSortThreads) {
         const uint32_t row = s_key[key_at(i)] >> LOW;
         const int32_t t = (int32_t)(first + (PACK ? s_key[key_at(i)] & ((1u << kPosBits) - 1)
@@ -886,27 +887,26 @@ ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, cons
     const int id64 = id_type == ECC_I64;
     if (n <= kSmallSort) {
         const int passes = (key_bits(V + 1) + kSmallBits - 1) / kSmallBits;
-        const dim3 grid((unsigned)P), block(kSortThreads);
         const bool pack = key_bits(V + 1) + kPosBits <= 32;
-#define ECC_SORT(ITEMS)                                                                         \
-    if (pack)                                                                                   \
-        hipLaunchKernelGGL((k_embed_sort<ITEMS, true>), grid, block, 0, s, n, V, row0, d_ids,    \
-                           id64, passes, keys, order, touched);                                 \
-    else                                                                                        \
-        hipLaunchKernelGGL((k_embed_sort<ITEMS, false>), grid, block, 0, s, n, V, row0, d_ids,   \
-                           id64, passes, keys, order, touched)
-        if (n <= kSortThreads) {
-            ECC_SORT(1);
-        } else if (n <= 2 * kSortThreads) {
-            ECC_SORT(2);
-        } else if (n <= 4 * kSortThreads) {
-            ECC_SORT(4);
-        } else if (n <= 8 * kSortThreads) {
-            ECC_SORT(8);
-        } else {
-            ECC_SORT(16);
+        // (a launch has fewer than 2^32 threads)
+        constexpr int64_t kMost = (int64_t(1) << 31) / kSortThreads;
+        for (int64_t worker0 = 0; worker0 < P; worker0 += kMost) {
+            const dim3 grid((unsigned)std::min(kMost, P - worker0)), block(kSortThreads);
+            auto sort = [&](auto items) {
+                constexpr int ITEMS = decltype(items)::value;
+                if (pack)
+                    hipLaunchKernelGGL((k_embed_sort<ITEMS, true>), grid, block, 0, s, worker0, n,
+                                       V, row0, d_ids, id64, passes, keys, order, touched);
+                else
+                    hipLaunchKernelGGL((k_embed_sort<ITEMS, false>), grid, block, 0, s, worker0, n,
+                                       V, row0, d_ids, id64, passes, keys, order, touched);
+            };
+            if (n <= kSortThreads) sort(std::integral_constant<int, 1>{});
+            else if (n <= 2 * kSortThreads) sort(std::integral_constant<int, 2>{});
+            else if (n <= 4 * kSortThreads) sort(std::integral_constant<int, 4>{});
+            else if (n <= 8 * kSortThreads) sort(std::integral_constant<int, 8>{});
+            else sort(std::integral_constant<int, 16>{});
         }
-#undef ECC_SORT
         ECC_LAUNCH_CHECK();
         return ECC_OK;
     }

@@ -522,3 +522,23 @@ def test_lookup_of_more_than_one_launch():
     assert torch.equal(out[at], table[ids[at]])
     del out
     torch.cuda.empty_cache()
+
+
+def test_index_of_many_workers():
+    """Four million workers of two tokens and their gradients: more workgroups
+    than one launch of fewer than 2^32 threads has."""
+    lm = _lm()
+    P, n, V = (1 << 22) + 3, 2, 3
+    announce("index, many workers", P, n, V)
+    ids = torch.randint(-1, V + 1, (P * n,), generator=torch.Generator().manual_seed(1))
+    index = lm.embed_index(ids.cuda(), V, P=P)
+    key, order = _index_ref(ids, V, P, 0)
+    N = P * n
+    at = (4 * N + 15) // 16 * 16
+    data = index.data.cpu()
+    assert torch.equal(data[:4 * N].view(torch.int32).long(), key)
+    assert torch.equal(data[at:at + 4 * N].view(torch.int32).long(), order)
+    dy = _random((N, 2), F32, 2)
+    ref, mass, count = _grad_ref(ids, dy, V, P, 1.0)
+    got = lm.embed_grad(index, dy.cuda())
+    _check_grad(got, ref, mass, count, 2.0 ** -24, 2.0 ** -24)
