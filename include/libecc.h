@@ -695,8 +695,9 @@ ecc_status_t ecc_embed_index(int32_t P, int64_t n, int64_t V, int64_t row0, cons
  * V).  Rows of d_dy whose token lies outside the table are not read.
  * Tokens are added in order within pieces of up to 64 sorted tokens, and the
  * pieces of a token in order.  worker_stride >= (V - 1) * ld_grad + D when
- * P > 1.  D up to 2^22, P * V below 2^29 (else ECC_ERR_RANGE).  d_work:
- * ecc_embed_work_size(...) bytes (-1 for arguments that the call refuses). */
+ * P > 1.  D up to 2^22, P * n and P * (V + 1) as for the index, else
+ * ECC_ERR_RANGE.  d_work: ecc_embed_work_size(...) bytes (-1 for arguments
+ * that the call refuses). */
 int64_t ecc_embed_work_size(int32_t P, int64_t n, int64_t D, int32_t dy_type, int32_t grad_type);
 ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const void *d_index,
                             const void *d_dy, int32_t dy_type, int64_t ld_dy, double scale,

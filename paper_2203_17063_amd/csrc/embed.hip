@@ -988,13 +988,15 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t per_block = kEmbedThreads >> g.log2_lanes;
     const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
     const int64_t rows = (int64_t)P * V;
-    const int64_t zero_rows = std::max<int64_t>({1, kZeroBytes / (D * gb), rows >> 22});
+    const int64_t zero_rows = std::max(kZeroBytes / (D * gb), (rows >> 22) + 1);
     // (rows of one workgroup's share up to two that begin at 16-byte boundaries
     // are written as rows: 128,000 of 16 KiB 631 us with the sums, flat 646 us;
-    // 47,988 of 44,736 bytes 354 us flat, as rows 408 us)
+    // 47,988 of 44,736 bytes 354 us flat, as rows 408 us), and so is a gradient
+    // of more shares than one launch takes beside the sums
     const bool flat = ld_grad == D && (P == 1 || worker_stride == V * D) &&
                       (uintptr_t)d_grad % 16 == 0 &&
-                      (D * gb < kZeroBytes || D * gb >= 2 * kZeroBytes || D * gb % 16 != 0);
+                      (D * gb < kZeroBytes || D * gb >= 2 * kZeroBytes || D * gb % 16 != 0) &&
+                      rows * D * gb / kZeroBytes < int64_t(1) << 22;
     const int64_t zero_blocks = accumulate ? 0
                                 : flat     ? (rows * D * gb + kZeroBytes - 1) / kZeroBytes
                                            : (rows + zero_rows - 1) / zero_rows;

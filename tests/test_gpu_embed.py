@@ -542,3 +542,45 @@ def test_index_of_many_workers():
     ref, mass, count = _grad_ref(ids, dy, V, P, 1.0)
     got = lm.embed_grad(index, dy.cuda())
     _check_grad(got, ref, mass, count, 2.0 ** -24, 2.0 ** -24)
+
+
+def test_grad_of_more_than_128_gib():
+    """A contiguous gradient of 137 GB, most of it zeros."""
+    lm = _lm()
+    V, D, n = (1 << 25) + 3, 1024, 1000
+    if torch.cuda.mem_get_info()[0] < 4 * V * D + (8 << 30):
+        pytest.skip("not enough device memory")
+    announce("grad, 137 GB")
+    ids = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(5))
+    ids[0], ids[1], ids[2] = 0, V - 1, V - 1
+    dy = torch.randn((n, D), device="cuda")
+    grad = torch.empty((1, V, D), device="cuda")
+    grad.fill_(3.0)
+    index = lm.embed_index(ids.cuda(), V)
+    lm.embed_grad(index, dy, grad=grad)
+    rows, inverse = torch.unique(ids.cuda(), return_inverse=True)
+    want = torch.zeros((rows.numel(), D), dtype=F64, device="cuda").index_add_(0, inverse,
+                                                                             dy.double())
+    assert (grad[0, rows].double() - want).abs().max() <= 1e-5
+    # every other element is zero
+    step = 1 << 21
+    nonzero = sum(int(torch.count_nonzero(grad[0, lo:lo + step])) for lo in range(0, V, step))
+    assert nonzero == int(torch.count_nonzero(grad[0, rows]))
+    del grad
+    torch.cuda.empty_cache()
+
+
+def test_grad_of_many_rows():
+    """P V beyond 2^29 rows."""
+    lm = _lm()
+    announce("grad, many rows")
+    P, V, D, n = 2, (1 << 28) + 100, 1, 5000
+    if torch.cuda.mem_get_info()[0] < (16 << 30):
+        pytest.skip("not enough device memory")
+    ids, dy = _tokens(P * n, 0, V, 3).cuda(), _random((P * n, D), F32, 4).cuda()
+    ids[0], ids[n - 1], ids[-1] = 0, V - 1, V - 1
+    grad = torch.full((P, V, D), 2.0, device="cuda")
+    lm.embed_grad(lm.embed_index(ids, V, P=P), dy, grad=grad)
+    rows = torch.arange(P * n, device="cuda") // n * V + ids
+    want = torch.zeros(P * V, dtype=F64, device="cuda").index_add_(0, rows, dy[:, 0].double())
+    assert (grad.view(-1).double() - want).abs().max() <= 1e-5
