@@ -989,13 +989,21 @@ ecc_status_t ecc_embed_grad(int32_t P, int64_t n, int64_t V, int64_t D, const vo
     const int64_t sum_blocks = (g.tiles * g.chunks + per_block - 1) / per_block;
     const int64_t rows = (int64_t)P * V;
     const int64_t zero_rows = std::max(kZeroBytes / (D * gb), (rows >> 22) + 1);
-    // (rows of one workgroup's share up to two that begin at 16-byte boundaries
-    // are written as rows: 128,000 of 16 KiB 631 us with the sums, flat 646 us;
-    // 47,988 of 44,736 bytes 354 us flat, as rows 408 us), and so is a gradient
-    // of more shares than one launch takes beside the sums
+    // Zeros as rows or flat, where the rows follow each other.  Rows of 16 KiB up
+    // to 24 that begin at 16-byte boundaries are written as rows: a gradient of
+    // 64,000 rows of 17 KiB with 64,000 and 16,000 tokens 348 and 231 us, flat
+    // 370 and 245; of 128,000 rows of 16 KiB 590 and 596, of 64,000 of 20 KiB 405
+    // and 418, but with few tokens 213 and 194.  From 24 KiB on the last share
+    // of a row is small, and flat is faster where the gradient exceeds the last
+    // cache (64,000 rows of 24 KiB with 64,000, 16,000 and 100 tokens 480, 319
+    // and 231 us, as rows 493, 346 and 283; of 28 KiB 562, 376 and 266, as rows
+    // 568, 402 and 331), slower by 1 us where it does not (4,000 rows of 28 KiB 40
+    // and 39 us).  A gradient of more shares than one launch takes beside the
+    // sums is written as rows.
+    const int64_t flat_from = rows * D * gb > kCacheBytes ? 3 * kZeroBytes / 2 : 2 * kZeroBytes;
     const bool flat = ld_grad == D && (P == 1 || worker_stride == V * D) &&
                       (uintptr_t)d_grad % 16 == 0 &&
-                      (D * gb < kZeroBytes || D * gb >= 2 * kZeroBytes || D * gb % 16 != 0) &&
+                      (D * gb < kZeroBytes || D * gb >= flat_from || D * gb % 16 != 0) &&
                       rows * D * gb / kZeroBytes < int64_t(1) << 22;
     const int64_t zero_blocks = accumulate ? 0
                                 : flat     ? (rows * D * gb + kZeroBytes - 1) / kZeroBytes
