@@ -584,3 +584,91 @@ def test_grad_of_many_rows():
     rows = torch.arange(P * n, device="cuda") // n * V + ids
     want = torch.zeros(P * V, dtype=F64, device="cuda").index_add_(0, rows, dy[:, 0].double())
     assert (grad.view(-1).double() - want).abs().max() <= 1e-5
+
+
+def _grad_on_device(ids, dy, V, cols):
+    """The gradient's columns `cols` and their masses in 64 bits on the GPU, a
+    token at a time off the sorted order."""
+    r = ids.long()
+    held = (r >= 0) & (r < V)
+    y = dy[held][:, cols].double()
+    zero = torch.zeros((V, len(cols)), dtype=F64, device="cuda")
+    g, s = zero.clone(), zero
+    order = torch.sort(r[held], stable=True)
+    rows, count = torch.unique_consecutive(order.values, return_counts=True)
+    for out, v in ((g, y), (s, y.abs())):
+        c = torch.cumsum(v[order.indices], 0)[torch.cumsum(count, 0) - 1]
+        out[rows] = torch.cat([c[:1], c[1:] - c[:-1]])
+    m = torch.zeros((V, 1), dtype=F64, device="cuda")
+    m[rows, 0] = count.double()
+    return g, s, m
+
+
+@pytest.mark.parametrize("n,D,tile,V,common", [
+    (131072, 4096, 32, 3000, 0.3), (131071, 4103, 32, 100, 0.0), (262144, 4096, 64, 5000, 0.5),
+    (262147, 4099, 64, 701, 0.01), (70001, 4096, 16, 997, 0.9), (131072, 8192, 64, 1, 0.0)])
+def test_grad_longer_tiles(n, D, tile, V, common):
+    """Sums over so many tokens that tiles hold 16, 32 and 64 of them: runs
+    shorter than a tile, of its length and around it, of twice that, and of
+    thousands of tiles, tokens outside the table in between."""
+    lm = _lm()
+    announce("grad, longer tiles", n, D, tile, V, common)
+    rng = np.random.default_rng(n + D)
+    t = rng.integers(0, V, n)
+    t[rng.random(n) < common] = V // 2
+    t[rng.random(n) < 0.02] = -1
+    if V > 600:
+        # runs of given lengths, at what place the others leave them
+        at = 0
+        for k, length in enumerate([tile - 1, tile, tile + 1, 2 * tile, 2 * tile - 1, 2 * tile + 1,
+                                    1, 2, 3 * tile, 5] * 6):
+            t[t == 10 + 3 * k] = V // 2
+            t[at:at + length] = 10 + 3 * k
+            at += length
+    ids = torch.from_numpy(t).cuda()
+    dy = torch.randn((n, D), dtype=BF16, device="cuda",
+                     generator=torch.Generator(device="cuda").manual_seed(n))
+    dy[ids < 0] = float("nan")
+    grad = lm.embed_grad(lm.embed_index(ids, V), dy)[0]
+    assert torch.isfinite(grad).all()
+    cols = list(range(8)) + [500, 511, 512, 513, 1024, D // 2, D - 513, D - 512] + \
+        list(range(D - 8, D))
+    g, s, m = _grad_on_device(ids, dy, V, cols)
+    # (the reference's running sums: a few units of 2^-53 of the whole column)
+    tol = (m + 4) * 2.0 ** -24 * s + 1e-9
+    assert ((grad[:, cols].double() - g).abs() <= tol).all()
+    again = lm.embed_grad(lm.embed_index(ids, V), dy)[0]
+    assert torch.equal(grad, again)
+
+
+@pytest.mark.parametrize("gt,V,D,n", [
+    (F32, 40000, 2048, 45000),     # above 256 MiB, few rows without tokens
+    (F64, 9001, 4099, 9100),       # the same, rows of odd lengths
+    (F32, 3000, 4096, 500),        # rows of 16 KiB
+    (F32, 3001, 5120, 2000),       # of 20 KiB
+    (F64, 1501, 3500, 900),        # of 28,000 bytes
+    (F32, 40001, 4096, 30000),     # of 16 KiB, above 256 MiB
+    (BF16, 1201, 16385, 700),      # of 32 KiB and two bytes
+    (BF16, 33000, 10240, 25000),   # of 20 KiB, above 256 MiB
+    (F32, 3001, 7000, 2500),       # of 28,000 bytes
+    (F32, 15001, 6144, 10000),     # of 24 KiB, above 256 MiB
+    (F32, 14999, 8191, 15000)])    # of 4 bytes less than 32 KiB, above 256 MiB
+def test_grad_zeros(gt, V, D, n):
+    """Rows without tokens in large gradients and in rows of 16 to 32 KiB: all
+    of them zeros, the others complete."""
+    lm = _lm()
+    announce("grad, zeros", gt, V, D, n)
+    yt = F32 if gt != BF16 else BF16
+    ids = _tokens(n, -1, V, n).cuda()
+    dy = torch.randn((n, D), dtype=yt, device="cuda",
+                     generator=torch.Generator(device="cuda").manual_seed(n))
+    grad = torch.full((1, V, D), float("nan"), dtype=gt, device="cuda")
+    lm.embed_grad(lm.embed_index(ids, V), dy, grad=grad)
+    touched = torch.zeros(V, dtype=torch.bool, device="cuda")
+    touched[ids[ids >= 0]] = True
+    assert torch.isfinite(grad).all() and not grad[0, ~touched].any()
+    cols = [0, 1, 2, 3, D // 2, D - 3, D - 2, D - 1]
+    g, s, m = _grad_on_device(ids, dy, V, cols)
+    u = _unit(yt, gt)
+    tol = (m + 4) * u * s + HALF_ULP[gt] * g.abs() + 1e-9
+    assert ((grad[0][:, cols].double() - g).abs() <= tol).all()

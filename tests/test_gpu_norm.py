@@ -708,3 +708,19 @@ def test_grad_of_many_workers():
         v = x[lo:lo + 10000].double()
         want = dh[lo:lo + 10000].double() * v * torch.rsqrt((v * v).mean(1, keepdim=True) + EPS)
         assert ((got[lo:lo + 10000] - want).abs() <= 101 * 2.0 ** -24 * want.abs()).all()
+
+
+def test_forward_is_finite():
+    """No NaN or infinity where the inputs have none (a comparison with a bound
+    lets NaN pass)."""
+    lm = _lm()
+    announce("norm, finite")
+    for act, wt in ((BF16, BF16), (BF16, F32), (F32, F32), (F64, F64)):
+        for N, D in SIZES + [(3, 12001), (3, 16384), (4099, 96)]:
+            if act == F64 and D > 8192:
+                continue
+            for gate in ("none", "rows", "param"):
+                for post, pre in ((True, True), (True, False), (False, True)):
+                    s = _gpu_args(_inputs(N, D, act, wt, gate, 2, post, pre))
+                    for v in lm.norm_forward(res_scale=0.9, branch_scale=0.7, eps=EPS, **s):
+                        assert v is None or torch.isfinite(v).all(), (act, wt, N, D, gate)
