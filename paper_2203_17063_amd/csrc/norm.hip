@@ -301,9 +301,10 @@ constexpr int kBackwardVecs = std::is_same_v<T, bf16_t> ? 1 : 2;
 // (in registers, 173 of them for a row of 4,096 bf16, one workgroup filled a
 // CU: 129 us for 8,192 such rows, 95 us with two).  Otherwise (the longest
 // rows) both are read again, and the sums over rows stay in the work buffer.
-// S: the type of the sums over rows.  fp64 sums of bf16 or fp32 rows (8,192 rows
-// of 4,096 bf16: 134 us, with sums in fp32 101 us; 8,192 rows of 8,192: 192 and
-// 171 us; 2,000 rows of 16,000, whose sums go through memory: 426 and 210 us).
+// S: the type of the sums over rows, fp64 where the parameters' gradients are
+// (8,192 rows of 4,096 bf16: 120 us, with sums in fp32 97 us; 8,192 rows of
+// 8,192: 193 and 172 us; 2,000 rows of 16,000, whose sums go through memory: 425
+// and 210 us).
 template <typename T, typename S, int NT, int NV, bool HOLD>
 constexpr int kGradWaves = HOLD && NV > kBackwardVecs<T> ? 2
                            : NT == 64 || (HOLD && sizeof(S) == 8) ? 3 : 4;

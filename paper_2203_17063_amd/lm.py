@@ -2,12 +2,16 @@
 read from torch tensors and checked, outputs and work buffers allocated, and
 libecc called on the current stream.  No arithmetic runs here.
 
+The calls are not recorded for torch's differentiation: results of inputs that
+require gradients do not, and the gradients are the calls named *_grad (and
+distill's second result).
+
 Rows (tokens, positions) may come with any number of leading dimensions as
 long as the last one is contiguous and the others collapse to rows of one
 stride.  Operands, outputs and work buffers of a call lie on one GPU, which
-need not be the current one.  Sums over rows and tokens are held in fp32, or fp64 where an operand
-or the result is fp64; a row's own sums (norms, softmax statistics) in fp32, or
-fp64 for rows of fp64.
+need not be the current one.  Sums over rows and tokens are held in fp32, or
+fp64 where an operand or the result is fp64; a row's own sums (norms, softmax
+statistics) in fp32, or fp64 for rows of fp64.
 """
 from __future__ import annotations
 
@@ -352,8 +356,9 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
     # (a refused description has no size: the call says what is wrong)
     work = _work(max(size, 16), x) if work is None else _given_work(work, size, x)
     _launch(x, E.ecc_norm_grad, a, g, work)
-    for t, dense in copies:
-        t.copy_(dense)
+    with torch.no_grad():
+        for t, dense in copies:
+            t.copy_(dense)
     return {"dx": dx, "df": df, "dgate": dgate, "dw_post": dw_post, "dw_pre": dw_pre}
 
 
