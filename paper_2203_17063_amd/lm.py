@@ -324,6 +324,8 @@ def norm_grad(x, f=None, dh=None, dx_out=None, *, w_post=None, w_pre=None, gate=
                              (what, dtype, (P, D)))
         if not apart:
             return t, t.data_ptr()
+        if stride < D:
+            raise ValueError("workers' gradients overlap")
         for other, _ in copies:   # (of the others the library sees where they are)
             at = (t.data_ptr() - other.data_ptr()) // t.element_size()
             if abs(at) < P * stride and min(at % stride, -at % stride) < D:

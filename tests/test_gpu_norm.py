@@ -724,3 +724,21 @@ def test_forward_is_finite():
                     s = _gpu_args(_inputs(N, D, act, wt, gate, 2, post, pre))
                     for v in lm.norm_forward(res_scale=0.9, branch_scale=0.7, eps=EPS, **s):
                         assert v is None or torch.isfinite(v).all(), (act, wt, N, D, gate)
+
+
+def test_workers_gradients_in_one_place():
+    """A gradient whose workers share memory is refused, alone and beside one
+    that was not given."""
+    from paper_2203_17063_amd import capi as E
+    announce("norm grad, workers in one place")
+    P, D = 3, 16
+    s = _gpu_args(_inputs(P * 4, D, F32, F32))
+    dh, flat = torch.zeros((P * 4, D), device="cuda"), torch.zeros(4096, device="cuda")
+    for stride in (0, 1, D - 1):
+        t = torch.as_strided(flat, (P, D), (stride, 1))
+        with pytest.raises(ValueError):
+            _lm().norm_grad(dh=dh, P=P, dw_post=t, **s)
+        with pytest.raises(E.EccError) as e:
+            _lm().norm_grad(dh=dh, P=P, dw_post=t, dw_pre=torch.as_strided(flat, (P, D),
+                                                                          (stride, 1), 512), **s)
+        assert e.value.status == E.ECC_ERR_ARG
