@@ -820,6 +820,118 @@ int64_t ecc_distill_work_size(const ecc_distill_t *a);
 ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64_t ld_dz,
                          void *d_work, void *hip_stream);
 
+/* Cross entropy straight from hidden states, loss and gradients, for P * n
+ * rows h_r (D elements) and a table E of V rows:
+ *   z_r = scale * E h_r
+ *   loss[r] = w_r (log sum_j exp(z_r[j]) - z_r[y_r])
+ *   dz_r[j] = scale * w_r (softmax(z_r)[j] - [j = y_r])
+ *   dh_r = sum_j dz_r[j] E_j,   dE_p[j] = sum over worker p's rows of dz_r[j] h_r
+ * A row whose label y_r lies outside [0, V), or whose weight is 0, is not
+ * read: its loss and gradient are 0 (d_weight NULL: all 1).  The logits exist
+ * for a piece of rows at a time, 4 GiB of them and their gradients at most.
+ *   d_h        P * n rows of `type`, ECC_F32 or ECC_BF16; d_table V rows of it
+ *   d_labels   int32 [P * n];  d_weight  fp32 [P * n] or NULL
+ *   d_loss     fp32 [P * n]
+ *   d_dh       P * n rows of `type`, or NULL
+ *   d_dtable   per worker V rows of grad_type (ECC_F32 or `type`) at
+ *              ld_dtable, written, or with accumulate = 1 added to; or NULL
+ *              (both NULL: the loss alone).
+ * Products are formed in fp32 from bf16 operands, or from fp32 ones to fp32's
+ * precision (as products of three bf16 pieces each; operands must be finite,
+ * and elements below 2^-117 lose bits).  dz is rounded to bf16 for a gradient
+ * that is bf16 itself.  V up to ECC_CROSS_ENTROPY_MAX_VOCAB, D up to
+ * ECC_CROSS_ENTROPY_MAX_DIM, P times n (rounded up to 64) below 2^31 - 1024, P * V * D
+ * below about 2^36, else ECC_ERR_RANGE.  d_work: ecc_cross_entropy_work_size(a, 1)
+ * bytes, or (a, 0) for the loss alone (-1 for a description that the call
+ * refuses; the size depends on where the arrays lie). */
+#define ECC_CROSS_ENTROPY_MAX_VOCAB (1 << 22)
+#define ECC_CROSS_ENTROPY_MAX_DIM (1 << 16)
+typedef struct {
+    int64_t n, V, D;
+    int32_t P;
+    int32_t type, grad_type;
+    int32_t pad;
+    const void *d_h;
+    int64_t ld_h;
+    const void *d_table;
+    int64_t ld_table;
+    const int32_t *d_labels;
+    const float *d_weight;
+    double scale;
+} ecc_cross_entropy_t;
+int64_t ecc_cross_entropy_work_size(const ecc_cross_entropy_t *a, int32_t gradient);
+ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void *d_dh,
+                               int64_t ld_dh, void *d_dtable, int64_t ld_dtable,
+                               int64_t worker_stride, int32_t accumulate, void *d_work,
+                               void *hip_stream);
+
+/* The gated feed-forward block up to its inner width, for P * n rows x of D
+ * elements and two matrices of F rows of D:
+ *   g = x Wg^T,  u = x Wu^T,  y = act(g) u
+ * (act(g) = g / (1 + exp(-g)), or g (1 + erf(g / sqrt 2)) / 2), and its
+ * gradients for a given dy:
+ *   dg = dy u act'(g),  du = dy act(g)
+ *   dx = dg Wg + du Wu,  dWg_p = dg_p^T x_p,  dWu_p = du_p^T x_p
+ * (g and u are formed again).  x, Wg, Wu, y, dy and dx are of `type`, ECC_F32
+ * or ECC_BF16; the weights' gradients are dense F x D matrices of grad_type
+ * (ECC_F32 or `type`) per worker, both or neither NULL; d_dx may be NULL.
+ * Products are formed as for ecc_cross_entropy.  dg and du are rounded to bf16
+ * for a gradient that is bf16 itself.  D and F up to ECC_FFN_MAX_DIM, P times
+ * n (rounded up to 64) up to ECC_FFN_MAX_ROWS, and products of fewer than 2^36
+ * or so elements, else ECC_ERR_RANGE.  d_work: ecc_ffn_work_size(a, 0) bytes
+ * for the forward call, (a, 1) for the gradients (-1 for a description that
+ * the call refuses; the size depends on where the arrays lie). */
+#define ECC_ACT_SILU 0
+#define ECC_ACT_GELU 1
+#define ECC_FFN_MAX_DIM (1 << 20)
+#define ECC_FFN_MAX_ROWS (1 << 22)
+typedef struct {
+    int64_t n, D, F;
+    int32_t P;
+    int32_t type, grad_type, act;
+    const void *d_x;
+    int64_t ld_x;
+    const void *d_w_gate;
+    int64_t ld_gate;
+    const void *d_w_up;
+    int64_t ld_up;
+} ecc_ffn_t;
+int64_t ecc_ffn_work_size(const ecc_ffn_t *a, int32_t gradient);
+ecc_status_t ecc_ffn_forward(const ecc_ffn_t *a, void *d_y, int64_t ld_y, void *d_work,
+                             void *hip_stream);
+ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, void *d_dx,
+                          int64_t ld_dx, void *d_dw_gate, void *d_dw_up, int64_t worker_stride,
+                          int32_t accumulate, void *d_work, void *hip_stream);
+
+/* The norm of every worker's gradients over `count` tensors, and gradients
+ * scaled to at most a norm:
+ *   d_norms[p] = sqrt(sum over the tensors' elements of worker p of g^2)
+ *   out = g * max_norm / d_norms[p] where d_norms[p] > max_norm, else g.
+ * Squares are added in fp64; their sum must lie within its range.  A norm that
+ * is not finite leaves the worker's gradients as they are (ECC_CLIP_KEEP) or
+ * makes them zeros (ECC_CLIP_ZERO: the worker then contributes nothing).
+ * h_tensors is read on the host during the call.  A tensor holds n elements
+ * per worker, the workers' `stride` elements apart.  d_out NULL: in place (not
+ * written where nothing changes); else out_type elements at d_out, workers
+ * out_stride apart, e.g. the parameter's place in every contribution to a
+ * collective; d_out may be d_grad itself.  P up to 65535, up to 2^20 tensors,
+ * fewer than 2^45 elements, else ECC_ERR_RANGE.  d_work:
+ * ecc_grad_norm_work_size bytes (-1 for tensors that the calls refuse). */
+#define ECC_CLIP_KEEP 0
+#define ECC_CLIP_ZERO 1
+typedef struct {
+    const void *d_grad;
+    void *d_out;
+    int64_t n, stride, out_stride;
+    int32_t type, out_type;
+} ecc_tensor_t;
+int64_t ecc_grad_norm_work_size(int32_t P, int32_t count, const ecc_tensor_t *h_tensors);
+ecc_status_t ecc_grad_norm(int32_t P, int32_t count, const ecc_tensor_t *h_tensors,
+                           double *d_norms, void *d_work, void *hip_stream);
+ecc_status_t ecc_clip_grads(int32_t P, int32_t count, const ecc_tensor_t *h_tensors,
+                            double max_norm, int32_t nonfinite, double *d_norms, void *d_work,
+                            void *hip_stream);
+
 /* ---------------------------------------------------------------------------
  * Plain streaming copy d_dst[i] = d_src[i], 0 <= i < n, enqueued on
  * hip_stream.  Both buffers 8-byte aligned and not overlapping

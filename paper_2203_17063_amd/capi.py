@@ -34,6 +34,10 @@ ECC_GATHER_CHUNK = 2048
 ECC_NORM_MAX_DIM = 16384
 ECC_DISTILL_MAX_TOP = 1024
 ECC_F64, ECC_F32, ECC_BF16, ECC_I32, ECC_I64 = 0, 1, 2, 3, 4
+ECC_CROSS_ENTROPY_MAX_VOCAB, ECC_CROSS_ENTROPY_MAX_DIM = 1 << 22, 1 << 16
+ECC_ACT_SILU, ECC_ACT_GELU = 0, 1
+ECC_FFN_MAX_DIM, ECC_FFN_MAX_ROWS = 1 << 20, 1 << 22
+ECC_CLIP_KEEP, ECC_CLIP_ZERO = 0, 1
 
 STATUS_NAMES = {0: "ECC_OK", 1: "ECC_ERR_ARG", 2: "ECC_ERR_OVERLAP", 3: "ECC_ERR_RANGE",
                 4: "ECC_ERR_ALLOC", 5: "ECC_ERR_DEVICE", 6: "ECC_ERR_STATE"}
@@ -85,6 +89,29 @@ class ecc_distill_t(ctypes.Structure):
                 ("d_idx", ctypes.c_void_p), ("d_labels", ctypes.c_void_p),
                 ("d_weight", ctypes.c_void_p), ("tau", ctypes.c_double),
                 ("kd_weight", ctypes.c_double), ("ce_weight", ctypes.c_double)]
+
+
+class ecc_cross_entropy_t(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("V", ctypes.c_int64), ("D", ctypes.c_int64),
+                ("P", ctypes.c_int32), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("pad", ctypes.c_int32), ("d_h", ctypes.c_void_p), ("ld_h", ctypes.c_int64),
+                ("d_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64),
+                ("d_labels", ctypes.c_void_p), ("d_weight", ctypes.c_void_p),
+                ("scale", ctypes.c_double)]
+
+
+class ecc_ffn_t(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("D", ctypes.c_int64), ("F", ctypes.c_int64),
+                ("P", ctypes.c_int32), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("d_x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("d_w_gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
+                ("d_w_up", ctypes.c_void_p), ("ld_up", ctypes.c_int64)]
+
+
+class ecc_tensor_t(ctypes.Structure):
+    _fields_ = [("d_grad", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
 
 
 _lib = None
@@ -153,6 +180,17 @@ _SIGS = [
                                      ctypes.POINTER(ecc_norm_grad_t), _VP, _VP]),
     ("ecc_distill_work_size", _I64, [ctypes.POINTER(ecc_distill_t)]),
     ("ecc_distill", ctypes.c_int, [ctypes.POINTER(ecc_distill_t), _VP, _VP, _I64, _VP, _VP]),
+    ("ecc_cross_entropy_work_size", _I64, [ctypes.POINTER(ecc_cross_entropy_t), _I32]),
+    ("ecc_cross_entropy", ctypes.c_int, [ctypes.POINTER(ecc_cross_entropy_t), _VP, _VP, _I64, _VP,
+                                         _I64, _I64, _I32, _VP, _VP]),
+    ("ecc_ffn_work_size", _I64, [ctypes.POINTER(ecc_ffn_t), _I32]),
+    ("ecc_ffn_forward", ctypes.c_int, [ctypes.POINTER(ecc_ffn_t), _VP, _I64, _VP, _VP]),
+    ("ecc_ffn_grad", ctypes.c_int, [ctypes.POINTER(ecc_ffn_t), _VP, _I64, _VP, _I64, _VP, _VP,
+                                    _I64, _I32, _VP, _VP]),
+    ("ecc_grad_norm_work_size", _I64, [_I32, _I32, ctypes.POINTER(ecc_tensor_t)]),
+    ("ecc_grad_norm", ctypes.c_int, [_I32, _I32, ctypes.POINTER(ecc_tensor_t), _VP, _VP, _VP]),
+    ("ecc_clip_grads", ctypes.c_int, [_I32, _I32, ctypes.POINTER(ecc_tensor_t), _D, _I32, _VP,
+                                      _VP, _VP]),
     ("ecc_solve", ctypes.c_int, [_VP, _VP, _VP, _D, _D, _VP, _VP, _VP, _VP, _I32, _D, _VP, _VP,
                                  _VP, _VP]),
 ]
@@ -515,3 +553,40 @@ def ecc_distill_work_size(a: ecc_distill_t) -> int:
 
 def ecc_distill(a: ecc_distill_t, d_loss, d_dz, ld_dz, d_work, hip_stream=None):
     _check(lib().ecc_distill(a, _ptr(d_loss), _ptr(d_dz), ld_dz, _ptr(d_work), hip_stream))
+
+
+def ecc_cross_entropy_work_size(a: ecc_cross_entropy_t, gradient) -> int:
+    return int(lib().ecc_cross_entropy_work_size(a, gradient))
+
+
+def ecc_cross_entropy(a: ecc_cross_entropy_t, d_loss, d_dh, ld_dh, d_dtable, ld_dtable,
+                      worker_stride, accumulate, d_work, hip_stream=None):
+    _check(lib().ecc_cross_entropy(a, _ptr(d_loss), _ptr(d_dh), ld_dh, _ptr(d_dtable), ld_dtable,
+                                   worker_stride, accumulate, _ptr(d_work), hip_stream))
+
+
+def ecc_ffn_work_size(a: ecc_ffn_t, gradient) -> int:
+    return int(lib().ecc_ffn_work_size(a, gradient))
+
+
+def ecc_ffn_forward(a: ecc_ffn_t, d_y, ld_y, d_work, hip_stream=None):
+    _check(lib().ecc_ffn_forward(a, _ptr(d_y), ld_y, _ptr(d_work), hip_stream))
+
+
+def ecc_ffn_grad(a: ecc_ffn_t, d_dy, ld_dy, d_dx, ld_dx, d_dw_gate, d_dw_up, worker_stride,
+                 accumulate, d_work, hip_stream=None):
+    _check(lib().ecc_ffn_grad(a, _ptr(d_dy), ld_dy, _ptr(d_dx), ld_dx, _ptr(d_dw_gate),
+                              _ptr(d_dw_up), worker_stride, accumulate, _ptr(d_work), hip_stream))
+
+
+def ecc_grad_norm_work_size(P, count, h_tensors) -> int:
+    return int(lib().ecc_grad_norm_work_size(P, count, h_tensors))
+
+
+def ecc_grad_norm(P, count, h_tensors, d_norms, d_work, hip_stream=None):
+    _check(lib().ecc_grad_norm(P, count, h_tensors, _ptr(d_norms), _ptr(d_work), hip_stream))
+
+
+def ecc_clip_grads(P, count, h_tensors, max_norm, nonfinite, d_norms, d_work, hip_stream=None):
+    _check(lib().ecc_clip_grads(P, count, h_tensors, max_norm, nonfinite, _ptr(d_norms),
+                                _ptr(d_work), hip_stream))

@@ -1,0 +1,414 @@
+// The gated feed-forward block up to its inner width, and its gradients:
+//   g = x Wg^T,  u = x Wu^T,  y = act(g) u
+//   dg = dy u act'(g),  du = dy act(g)
+//   dx = dg Wg + du Wu,  dWg_p = dg_p^T x_p,  dWu_p = du_p^T x_p.
+// Forward is one product kernel: a wave holds the same columns of g and u, so
+// that y is formed from the sums in registers and rounded once.  Backward forms
+// g and u again instead of keeping them (a third of its operations), and dg and
+// du from them in registers; they are stored beside each other as one matrix
+// [dg | du], so that dx is one product over both along k, and the weights'
+// gradients one product with both stacked.  dg and du are rounded to bf16
+// where the gradient is bf16 itself, and kept as three pieces (gemm.h) where
+// it is fp32.
+#include "gemm.h"
+#include "pack.h"
+
+namespace ecc {
+namespace {
+
+// act(g) and its derivative.
+template <int ACT>
+__device__ __forceinline__ void activation(float g, float &a, float &da) {
+    if constexpr (ACT == ECC_ACT_SILU) {
+        const float q = 1.0f / (1.0f + expf(-g));
+        a = g * q;
+        da = q * (1.0f + g * (1.0f - q));
+    } else {
+        const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
+        a = g * c;
+        da = c + g * (expf(-0.5f * g * g) * 0.39894228040143268f);
+    }
+}
+
+template <typename T, int ACT>
+struct FfnOut {
+    static constexpr bool kPair = true;
+    T *y;
+    int64_t ld;
+    template <int MI, int NI>
+    __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
+                                           f32x4 (&acc)[MI][NI]) const {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI / 2; ++j) {
+                const int32_t m = t.m + 16 * i, n = t.n + 16 * j;
+                if (m >= g.M || n >= g.N) continue;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float a, da;
+                    activation<ACT>(acc[i][j][e], a, da);
+                    v[e] = a * acc[i][j + NI / 2][e];
+                }
+                Raw<T, 4> x;
+                x.set_all(v);
+                x.store_upto(y + m * ld + n, g.N - n);
+            }
+    }
+};
+
+template <typename T, int ACT>
+struct FfnGradOut {
+    static constexpr bool kPair = true;
+    const T *dy;
+    int64_t ld_dy;
+    bf16_t *d;            // [piece][row][dg | du], each F_pad long
+    int64_t F_pad, plane;
+    int32_t pieces;
+    template <int MI, int NI>
+    __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
+                                           f32x4 (&acc)[MI][NI]) const {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI / 2; ++j) {
+                const int32_t m = t.m + 16 * i, n = t.n + 16 * j;
+                if (m >= g.M || n >= F_pad) continue;
+                Raw<T, 4> x;
+                x.load_upto(dy + m * ld_dy + n, (int64_t)g.N - n);
+                float dg[4], du[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float a, da;
+                    activation<ACT>(acc[i][j][e], a, da);
+                    const float v = x.template get<float>(e);
+                    dg[e] = n + e < g.N ? v * acc[i][j + NI / 2][e] * da : 0.0f;
+                    du[e] = n + e < g.N ? v * a : 0.0f;
+                }
+                bf16_t *to = d + m * 2 * F_pad + n;
+                for (int which = 0; which < pieces; ++which) {
+                    Raw<bf16_t, 4> p;
+                    set_piece(p, dg, which, pieces > 1);
+                    p.store(to + which * plane);
+                    set_piece(p, du, which, pieces > 1);
+                    p.store(to + which * plane + F_pad);
+                }
+            }
+    }
+};
+
+struct Plan {
+    int64_t N, n_pad, rows, Dp, Fp;
+    int np, pd;                   // pieces of the operands, of dg and du
+    bool pack_x, pack_gate, pack_up;
+    int64_t splits_x, splits_w;
+    int64_t x, gate, up, x_t, w_t, d, d_t, parts, bytes;
+};
+
+Plan make_plan(const ecc_ffn_t *a, bool gradient) {
+    Plan p{};
+    p.N = a->P * a->n;
+    p.n_pad = pad64(a->n);
+    p.rows = a->P * p.n_pad;
+    p.Dp = pad64(a->D);
+    p.Fp = pad64(a->F);
+    p.np = a->type == ECC_F32 ? 3 : 1;
+    p.pd = a->type == ECC_F32 || a->grad_type == ECC_F32 ? 3 : 1;
+    p.pack_x = !as_it_lies(a->d_x, a->ld_x, a->D, a->type);
+    p.pack_gate = !as_it_lies(a->d_w_gate, a->ld_gate, a->D, a->type);
+    p.pack_up = !as_it_lies(a->d_w_up, a->ld_up, a->D, a->type);
+    // (a pair of matrices has one pitch)
+    if (p.pack_gate || p.pack_up || a->ld_gate != a->ld_up) p.pack_gate = p.pack_up = true;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += (bytes + 255) & ~int64_t(255);
+        return here;
+    };
+    p.x = take(p.pack_x ? p.np * 2 * pad64(p.N) * p.Dp : 0);
+    p.gate = take(p.pack_gate ? p.np * 2 * p.Fp * p.Dp : 0);
+    p.up = take(p.pack_up ? p.np * 2 * p.Fp * p.Dp : 0);
+    if (gradient) {
+        p.x_t = take(p.np * 2 * a->D * p.rows);
+        p.w_t = take(p.np * 2 * a->D * 2 * p.Fp);
+        p.d = take(p.pd * 2 * pad64(p.N) * 2 * p.Fp);
+        p.d_t = take(p.pd * 2 * 2 * a->F * p.rows);
+        p.splits_x = gemm_splits(p.N, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1);
+        p.splits_w = gemm_splits(2 * a->F, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pd), a->P);
+        p.parts = take(std::max(split_bytes(p.N, a->D, p.splits_x, 1),
+                                split_bytes(2 * a->F, a->D, p.splits_w, a->P)));
+    }
+    p.bytes = std::max<int64_t>(at, 16);
+    return p;
+}
+
+ecc_status_t check(const ecc_ffn_t *a) {
+    ECC_ARG(a, "NULL description");
+    ECC_ARG(a->n >= 0 && a->F >= 1 && a->D >= 1 && a->P >= 1, "a size is out of range");
+    ECC_ARG(a->type == ECC_F32 || a->type == ECC_BF16, "the operands must be fp32 or bf16");
+    ECC_ARG(a->grad_type == ECC_F32 || a->grad_type == a->type,
+            "the weights' gradients must be fp32 or of the operands' type");
+    ECC_ARG(a->act == ECC_ACT_SILU || a->act == ECC_ACT_GELU, "unknown activation");
+    ECC_ARG(a->ld_x >= a->D && a->ld_gate >= a->D && a->ld_up >= a->D,
+            "a leading dimension is below D");
+    if (a->F > ECC_FFN_MAX_DIM || a->D > ECC_FFN_MAX_DIM || a->n > ECC_FFN_MAX_ROWS ||
+        (__int128)a->P * pad64(a->n) > ECC_FFN_MAX_ROWS || a->ld_x >= (int64_t(1) << 40) ||
+        a->ld_gate >= (int64_t(1) << 40) || a->ld_up >= (int64_t(1) << 40) ||
+        !gemm_in_range(a->P * a->n, 2 * a->F, 1) || !gemm_in_range(a->P * a->n, a->D, 1) ||
+        !gemm_in_range(2 * a->F, a->D, a->P)) {
+        set_error("the sizes are beyond what the library supports");
+        return ECC_ERR_RANGE;
+    }
+    if (a->n == 0) return ECC_OK;
+    const int64_t size = type_size(a->type);
+    ECC_ARG(a->d_x && a->d_w_gate && a->d_w_up, "NULL pointer");
+    ECC_ARG((uintptr_t)a->d_x % size == 0 && (uintptr_t)a->d_w_gate % size == 0 &&
+                (uintptr_t)a->d_w_up % size == 0,
+            "an array is not aligned");
+    return ECC_OK;
+}
+
+// The projections' operands, packed where they have to be.
+GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) {
+    PackArgs k{};
+    k.cols = a->D;
+    k.pieces = p.np;
+    k.ld_rows = p.Dp;
+    GemmArgs g{};
+    g.a = GemmOperand{(const bf16_t *)a->d_x, a->ld_x, 0};
+    g.b = GemmOperand{(const bf16_t *)a->d_w_gate, a->ld_gate, 0};
+    g.b2 = (const bf16_t *)a->d_w_up;
+    auto pack = [&](const void *src, int64_t ld, int64_t rows, int64_t to) {
+        k.src = src;
+        k.ld = ld;
+        k.n = k.total = rows;
+        k.rows_packed = k.n_pad = pad64(rows);
+        k.rows = (bf16_t *)(w + to);
+        k.plane_rows = k.rows_packed * p.Dp;
+        launch_pack(k, a->type, s);
+        return GemmOperand{k.rows, p.Dp, k.plane_rows};
+    };
+    if (p.pack_x) g.a = pack(a->d_x, a->ld_x, p.N, p.x);
+    if (p.pack_gate) {
+        g.b = pack(a->d_w_gate, a->ld_gate, a->F, p.gate);
+        g.b2 = pack(a->d_w_up, a->ld_up, a->F, p.up).p;
+    }
+    g.M = (int32_t)p.N;
+    g.N = (int32_t)a->F;
+    g.K = (int32_t)p.Dp;
+    g.batches = g.splits = 1;
+    set_products(g, p.np, p.np);
+    return g;
+}
+
+template <typename F>
+void with_kind(const ecc_ffn_t *a, F &&f) {
+    auto act = [&](auto t) {
+        if (a->act == ECC_ACT_SILU) f(t, std::integral_constant<int, ECC_ACT_SILU>{});
+        else f(t, std::integral_constant<int, ECC_ACT_GELU>{});
+    };
+    if (a->type == ECC_F32) act(float{});
+    else act(bf16_t{});
+}
+
+// Gradients of weights that no row reached.
+template <typename T>
+__global__ __launch_bounds__(256) void k_ffn_zero(int64_t rows, int64_t F, int64_t D, T *g,
+                                                  int64_t stride) {
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        T *to = g + r / F * stride + r % F * D;
+        for (int64_t d = threadIdx.x; d < D; d += 256) store_elem<float>(to + d, 0.0f);
+    }
+}
+
+}  // namespace
+}  // namespace ecc
+
+using namespace ecc;
+
+extern "C" {
+
+int64_t ecc_ffn_work_size(const ecc_ffn_t *a, int32_t gradient) {
+    if (check(a) != ECC_OK) return -1;
+    return make_plan(a, gradient != 0).bytes;
+}
+
+ecc_status_t ecc_ffn_forward(const ecc_ffn_t *a, void *d_y, int64_t ld_y, void *d_work,
+                             void *hip_stream) {
+    clear_error();
+    const ecc_status_t st = check(a);
+    if (st != ECC_OK) return st;
+    ECC_ARG(ld_y >= a->F, "a leading dimension is below F");
+    if (ld_y >= (int64_t(1) << 40)) {
+        set_error("a leading dimension is too large");
+        return ECC_ERR_RANGE;
+    }
+    if (a->n == 0) return ECC_OK;
+    const int64_t size = type_size(a->type);
+    ECC_ARG(d_y && d_work, "NULL pointer");
+    ECC_ARG((uintptr_t)d_y % size == 0 && (uintptr_t)d_work % 16 == 0, "an array is not aligned");
+    const Plan p = make_plan(a, false);
+    const Span in[3] = {span_of(a->d_x, p.N, a->ld_x, a->D, size),
+                        span_of(a->d_w_gate, a->F, a->ld_gate, a->D, size),
+                        span_of(a->d_w_up, a->F, a->ld_up, a->D, size)};
+    const Span out[2] = {span_of(d_y, p.N, ld_y, a->F, size), span_of(d_work, p.bytes)};
+    for (const Span &o : out)
+        for (const Span &i : in) ECC_ARG(!spans_meet(o, i), "an output overlaps an input");
+    ECC_ARG(!spans_meet(out[0], out[1]), "an output and the work buffer overlap");
+    hipStream_t s = (hipStream_t)hip_stream;
+    const GemmArgs g = projections(a, p, (char *)d_work, s);
+    with_kind(a, [&](auto t, auto act) {
+        using T = decltype(t);
+        launch_gemm(g, FfnOut<T, decltype(act)::value>{(T *)d_y, ld_y}, s);
+    });
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, void *d_dx,
+                          int64_t ld_dx, void *d_dw_gate, void *d_dw_up, int64_t worker_stride,
+                          int32_t accumulate, void *d_work, void *hip_stream) {
+    clear_error();
+    const ecc_status_t st = check(a);
+    if (st != ECC_OK) return st;
+    const int64_t D = a->D, F = a->F, size = type_size(a->type), gsize = type_size(a->grad_type);
+    const int32_t P = a->P;
+    ECC_ARG(ld_dy >= F, "a leading dimension is below F");
+    ECC_ARG(!d_dx || ld_dx >= D, "a leading dimension is below D");
+    ECC_ARG(!d_dw_gate == !d_dw_up, "the weights' gradients are formed together");
+    ECC_ARG(!d_dw_gate || P == 1 || worker_stride >= F * D, "workers' gradients overlap");
+    ECC_ARG(accumulate == 0 || accumulate == 1, "accumulate must be 0 or 1");
+    if (ld_dy >= (int64_t(1) << 40) || ld_dx >= (int64_t(1) << 40) ||
+        worker_stride >= (int64_t(1) << 56)) {
+        set_error("a stride is too large");
+        return ECC_ERR_RANGE;
+    }
+    ECC_ARG((uintptr_t)d_dy % size == 0 && (uintptr_t)d_dx % size == 0 &&
+                (uintptr_t)d_dw_gate % gsize == 0 && (uintptr_t)d_dw_up % gsize == 0 &&
+                (uintptr_t)d_work % 16 == 0,
+            "an array is not aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    const Span weights[2] = {
+        P == 1 ? span_of(d_dw_gate, F * D * gsize) : span_of(d_dw_gate, P, worker_stride, F * D, gsize),
+        P == 1 ? span_of(d_dw_up, F * D * gsize) : span_of(d_dw_up, P, worker_stride, F * D, gsize)};
+    ECC_ARG(!spans_meet(weights[0], weights[1]), "two outputs overlap");
+    if (a->n == 0) {
+        if (d_dw_gate && !accumulate) {
+            const int64_t rows = P * F;
+            const dim3 grid((unsigned)std::min<int64_t>(rows, 4096));
+            for (void *to : {d_dw_gate, d_dw_up}) {
+                if (a->grad_type == ECC_F32)
+                    hipLaunchKernelGGL(k_ffn_zero<float>, grid, dim3(256), 0, s, rows, F, D,
+                                       (float *)to, worker_stride);
+                else
+                    hipLaunchKernelGGL(k_ffn_zero<bf16_t>, grid, dim3(256), 0, s, rows, F, D,
+                                       (bf16_t *)to, worker_stride);
+            }
+            ECC_LAUNCH_CHECK();
+        }
+        return ECC_OK;
+    }
+    ECC_ARG(d_dy && d_work, "NULL pointer");
+    const Plan p = make_plan(a, true);
+    const Span in[4] = {span_of(a->d_x, p.N, a->ld_x, D, size),
+                        span_of(a->d_w_gate, F, a->ld_gate, D, size),
+                        span_of(a->d_w_up, F, a->ld_up, D, size),
+                        span_of(d_dy, p.N, ld_dy, F, size)};
+    const Span out[4] = {span_of(d_dx, p.N, ld_dx, D, size), weights[0], weights[1],
+                         span_of(d_work, p.bytes)};
+    for (int o = 0; o < 4; ++o) {
+        for (const Span &i : in) ECC_ARG(!spans_meet(out[o], i), "an output overlaps an input");
+        for (int q = 0; q < o; ++q)
+            ECC_ARG(!spans_meet(out[o], out[q]),
+                    "two outputs, or an output and the work buffer, overlap");
+    }
+    char *w = (char *)d_work;
+    // dg and du
+    const GemmArgs g = projections(a, p, w, s);
+    bf16_t *d = (bf16_t *)(w + p.d);
+    const int64_t plane = pad64(p.N) * 2 * p.Fp;
+    with_kind(a, [&](auto t, auto act) {
+        using T = decltype(t);
+        launch_gemm(g, FfnGradOut<T, decltype(act)::value>{(const T *)d_dy, ld_dy, d, p.Fp, plane,
+                                                           p.pd},
+                    s);
+    });
+    PackArgs k{};
+    if (d_dx) {
+        // [Wg | Wu] transposed, as long as [dg | du]
+        k.cols = D;
+        k.pieces = p.np;
+        k.n = k.total = F;
+        k.rows_packed = k.n_pad = p.Fp;
+        k.ld_cols = 2 * p.Fp;
+        k.plane_cols = D * 2 * p.Fp;
+        for (int i = 0; i < 2; ++i) {
+            k.src = i ? a->d_w_up : a->d_w_gate;
+            k.ld = i ? a->ld_up : a->ld_gate;
+            k.cols_out = (bf16_t *)(w + p.w_t) + i * p.Fp;
+            launch_pack(k, a->type, s);
+        }
+        GemmArgs x{};
+        x.a = GemmOperand{d, 2 * p.Fp, plane};
+        x.b = GemmOperand{(bf16_t *)(w + p.w_t), 2 * p.Fp, k.plane_cols};
+        x.M = (int32_t)p.N;
+        x.N = (int32_t)D;
+        x.K = (int32_t)(2 * p.Fp);
+        x.batches = 1;
+        x.splits = (int32_t)p.splits_x;
+        set_products(x, p.np, p.np);
+        MatrixOut to{};
+        to.out = d_dx;
+        to.ld = ld_dx;
+        to.type = a->type;
+        launch_product(x, to, (float *)(w + p.parts), s);
+    }
+    if (d_dw_gate) {
+        // x and [dg | du] transposed, workers padded to multiples of 64 rows
+        k = PackArgs{};
+        k.n = a->n;
+        k.n_pad = p.n_pad;
+        k.total = p.N;
+        k.rows_packed = k.ld_cols = p.rows;
+        k.src = a->d_x;
+        k.ld = a->ld_x;
+        k.cols = D;
+        k.pieces = p.np;
+        k.cols_out = (bf16_t *)(w + p.x_t);
+        k.plane_cols = D * p.rows;
+        launch_pack(k, a->type, s);
+        k.ld = 2 * p.Fp;
+        k.cols = F;
+        k.pieces = 1;
+        const int64_t plane_t = 2 * F * p.rows;
+        for (int which = 0; which < p.pd; ++which)
+            for (int i = 0; i < 2; ++i) {
+                k.src = d + which * plane + i * p.Fp;
+                k.cols_out = (bf16_t *)(w + p.d_t) + which * plane_t + i * F * p.rows;
+                launch_pack(k, ECC_BF16, s);
+            }
+        GemmArgs x{};
+        x.a = GemmOperand{(bf16_t *)(w + p.d_t), p.rows, plane_t};
+        x.b = GemmOperand{(bf16_t *)(w + p.x_t), p.rows, D * p.rows};
+        x.M = (int32_t)(2 * F);
+        x.N = (int32_t)D;
+        x.K = (int32_t)p.n_pad;
+        x.batches = P;
+        x.splits = (int32_t)p.splits_w;
+        set_products(x, p.pd, p.np);
+        MatrixOut to{};
+        to.out = d_dw_gate;
+        to.out2 = d_dw_up;
+        to.second = (int32_t)F;
+        to.ld = D;
+        to.batch_stride = worker_stride;
+        to.type = a->grad_type;
+        to.add = accumulate;
+        launch_product(x, to, (float *)(w + p.parts), s);
+    }
+    ECC_LAUNCH_CHECK();
+    return ECC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,378 @@
+// Products of the language-model operators on the matrix cores:
+//     C[m, n] = sum over k of A[m, k] B[n, k]
+// for operands of bf16 whose rows are contiguous along k, sums in fp32.
+//
+// fp32 operands take the same path as three pieces of bf16 each (split3), laid
+// out as planes: hi + mid + lo is the fp32 value (24 bits in 3 x 8), and the
+// six products of pieces down to 2^-16 of the largest (mid mid, hi lo, lo hi,
+// hi mid, mid hi, hi hi, in this order) leave out terms of 2^-24 of an
+// element's product, below fp32's own rounding.  The loop over k just walks
+// the planes one product after another.
+//
+// The kernel: a workgroup holds a tile of BM x BN sums in registers, each wave
+// (BM / WM) x (BN / WN) as 16 x 16 blocks.  Steps of 64 along k are brought
+// into LDS by direct 16-byte loads, one step ahead of the products, in two
+// buffers; a row of a step is 128 bytes, its 16-byte chunks stored at chunk ^
+// (row & 7), so that the reads of 16 rows touch every bank once (the loads
+// write LDS lane after lane, so the exchange is in the addresses they read).
+// Rows behind the last one are read as the last row and not stored.
+// Workgroups go round the eight XCDs, each of which walks a contiguous part of
+// the tiles in bands of four tile rows, so that its L2 serves the operands of
+// neighbours.
+// 256 x 256 with 8 waves is bound by the matrix cores and LDS: 8,192^3 at 1.25
+// PFLOP/s, 4,096^3 at 1.13; 128 x 128 with 4 waves reaches 1.03 and 0.98, and
+// is for products that leave CUs without a large tile.  (256 x 256 with 4
+// waves needs 256 sums a lane and spills: 0.29 PFLOP/s.)
+#pragma once
+
+#include "lm_common.h"
+
+namespace ecc {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kGemmK = 64;        // elements along k of one step
+constexpr int kGemmGroup = 4;     // tile rows of a band
+// Row pitch of an operand: 32-bit offsets reach the rows of a tile.
+constexpr int64_t kGemmMaxLd = int64_t(1) << 23;
+
+// Rows of `ld` elements (a multiple of 8, 16-byte aligned), pieces `plane`
+// elements apart.
+struct GemmOperand {
+    const bf16_t *p;
+    int64_t ld, plane;
+};
+
+struct GemmArgs {
+    GemmOperand a, b;
+    const bf16_t *b2;      // the second matrix of pairs (Epi::kPair), like b
+    int32_t M, N;          // rows of A and of B (of one of the pair)
+    int32_t K;             // along k, a multiple of kGemmK: of every batch
+    int32_t tiles_m, tiles_n, batches, splits;
+    // Batches are ranges along k: [batch * K, + K), or those of the device
+    // array ranges (begin, end), cut to [k_lo, k_hi) and counted from k_lo.
+    const int2 *ranges;
+    int32_t k_lo, k_hi;
+    // Rows of A that hold anything, from m_lo on (device; NULL: all): tiles
+    // behind them are left out.
+    const int32_t *live;
+    int32_t m_lo;
+    int32_t nprod;         // products of pieces
+    uint8_t pa[6], pb[6];
+};
+
+// The products of an operand of `na` pieces with one of `nb`, small ones first.
+inline void set_products(GemmArgs &g, int na, int nb) {
+    static const uint8_t both[6][2] = {{1, 1}, {0, 2}, {2, 0}, {0, 1}, {1, 0}, {0, 0}};
+    g.nprod = 0;
+    for (auto &p : both) {
+        if (p[0] >= na || p[1] >= nb) continue;
+        g.pa[g.nprod] = p[0];
+        g.pb[g.nprod++] = p[1];
+    }
+}
+
+// Where a lane's sums lie: acc[i][j][e] is row m + 16 i, column n + 16 j + e
+// of the tile's matrix (of pairs: acc[i][j] and acc[i][j + NI / 2] are the
+// first's and the second's column n + 16 j + e).
+struct GemmTile {
+    int32_t m, n;
+    int32_t batch, split;
+    int32_t k;        // elements along k that the tile has summed
+    int32_t tile_n;   // 64-column tile of the wave
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes a lane from base + offset into LDS, lane after lane.
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, uint16_t *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, -1, 0x00020000),
+        (lds_void *)to, 16, (int)offset, 0, 0, 0);
+}
+
+template <int BM, int BN, int WM, int WN, class Epi>
+__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
+    constexpr int NW = WM * WN;
+    constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
+    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // loads of 8 rows a wave
+    static_assert(BN / WN == 64, "a wave's columns: 64, or 32 of each of a pair");
+    // (four arrays: the compiler tells the loads of one buffer from the reads
+    // of the other by their names)
+    __shared__ __attribute__((aligned(1024))) uint16_t s_a0[BM * kGemmK];
+    __shared__ __attribute__((aligned(1024))) uint16_t s_b0[BN * kGemmK];
+    __shared__ __attribute__((aligned(1024))) uint16_t s_a1[BM * kGemmK];
+    __shared__ __attribute__((aligned(1024))) uint16_t s_b1[BN * kGemmK];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // the tile: blocks go round the XCDs, each takes a contiguous share
+    const int per = (int)((gridDim.x + 7) >> 3), more = (int)(gridDim.x - ((per - 1) << 3));
+    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    int t = xcd * per + at - max(0, xcd - more);
+    const int tiles = g.tiles_m * g.tiles_n;
+    const int part = t / tiles;
+    t -= part * tiles;
+    const int split = part % g.splits, batch = part / g.splits;
+    const int band = kGemmGroup * g.tiles_n;
+    const int first = t / band * kGemmGroup, in = t % band;
+    const int rows = min(kGemmGroup, g.tiles_m - first);
+    const int tm = first + in % rows, tn = in / rows;
+    const int m0 = tm * BM, n0 = tn * (Epi::kPair ? BN / 2 : BN);
+    if (g.live && m0 + g.m_lo >= *g.live) return;
+
+    // the range along k, in steps; this split's share of all products' steps
+    int k0 = batch * g.K, k1 = k0 + g.K;
+    if (g.ranges) {
+        const int2 r = g.ranges[batch];
+        k0 = max(r.x, g.k_lo) - g.k_lo;
+        k1 = max(k0, min(r.y, g.k_hi) - g.k_lo);
+    }
+    const int ksteps = (k1 - k0) / kGemmK;
+    const int all = ksteps * g.nprod;
+    int step = (int)((int64_t)all * split / g.splits);
+    const int end = (int)((int64_t)all * (split + 1) / g.splits);
+
+    uint32_t oa[LA], ob[LB];
+    const int sub = lane >> 3, chunk = ((lane & 7) ^ sub) * 16;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const int r = min((wave * LA + i) * 8 + sub, g.M - 1 - m0);
+        oa[i] = (uint32_t)(r * (int64_t)g.a.ld * 2 + chunk);
+    }
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        int r = (wave * LB + i) * 8 + sub;
+        if constexpr (Epi::kPair) r = r / 64 * 32 + r % 32;
+        r = min(r, g.N - 1 - n0);
+        ob[i] = (uint32_t)(r * (int64_t)g.b.ld * 2 + chunk);
+    }
+    const bf16_t *pa = g.a.p + (int64_t)m0 * g.a.ld + k0;
+    const int64_t b_at = (int64_t)n0 * g.b.ld + k0;
+    int prod = ksteps ? step / ksteps : 0, ks = ksteps ? step % ksteps : 0;
+
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+
+    // brings the next step into a buffer
+    auto load = [&](uint16_t *sa, uint16_t *sb) {
+        const bf16_t *a = pa + g.pa[prod] * g.a.plane + ks * kGemmK;
+        const int64_t at_b = b_at + g.pb[prod] * g.b.plane + ks * kGemmK;
+        if (++ks == ksteps) ks = 0, ++prod;
+#pragma unroll
+        for (int i = 0; i < LA; ++i) load_to_lds(a, oa[i], sa + (wave * LA + i) * 8 * kGemmK);
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const bf16_t *b = g.b.p;
+            if constexpr (Epi::kPair)
+                if ((wave * LB + i) / 4 & 1) b = g.b2;
+            load_to_lds(b + at_b, ob[i], sb + (wave * LB + i) * 8 * kGemmK);
+        }
+    };
+    const int ra = wm * (BM / WM) + (lane & 15), rb = wn * (BN / WN) + (lane & 15);
+    const int x = lane & 7, q = lane >> 4;
+    auto multiply = [&](const uint16_t *sa, const uint16_t *sb) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 fa[MI], fb[NI];
+            const int c = ((kk * 4 + q) ^ x) * 8;
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                fb[j] = *reinterpret_cast<const bf16x8 *>(sb + (rb + j * 16) * kGemmK + c);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+                fa[i] = *reinterpret_cast<const bf16x8 *>(sa + (ra + i * 16) * kGemmK + c);
+            // (B first: a lane then holds four neighbouring columns)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j],
+                                                                       0, 0, 0);
+        }
+    };
+    if (step < end) {
+        load(s_a0, s_b0);
+        for (;;) {
+            __syncthreads();  // the step is in LDS, and the other buffer is read
+            if (step + 1 < end) load(s_a1, s_b1);
+            multiply(s_a0, s_b0);
+            if (++step >= end) break;
+            __syncthreads();
+            if (step + 1 < end) load(s_a0, s_b0);
+            multiply(s_a1, s_b1);
+            if (++step >= end) break;
+        }
+    }
+    const int n_wave = n0 + wn * (Epi::kPair ? 32 : 64);
+    epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64}, g, acc);
+}
+
+// Launches tiles of BM x BN (of pairs: BN / 2 columns).
+template <int BM, int BN, int WM, int WN, class Epi>
+void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
+    g.tiles_m = (g.M + BM - 1) / BM;
+    const int cols = Epi::kPair ? BN / 2 : BN;
+    g.tiles_n = (g.N + cols - 1) / cols;
+    const int64_t grid = (int64_t)g.tiles_m * g.tiles_n * g.batches * g.splits;
+    if (grid > 0)
+        hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, Epi>), dim3((unsigned)grid),
+                           dim3(64 * WM * WN), 0, s, g, epi);
+}
+
+// Large tiles where they fill the CUs once, else small ones.
+inline bool large_tiles(int64_t M, int64_t N, int64_t batches) {
+    return ((M + 255) / 256) * ((N + 255) / 256) * batches >= 224;
+}
+template <class Epi>
+void launch_gemm(const GemmArgs &g, const Epi &epi, hipStream_t s) {
+    if (large_tiles(g.M, (int64_t)g.N * (Epi::kPair ? 2 : 1), (int64_t)g.batches * g.splits))
+        launch_gemm_tile<256, 256, 2, 4>(g, epi, s);
+    else launch_gemm_tile<128, 128, 2, 2>(g, epi, s);
+}
+
+// Parts along k of a product whose tiles would leave most CUs without one:
+// each of at least 8 steps, joined by k_gemm_join.
+inline int32_t gemm_splits(int64_t M, int64_t N, int64_t steps, int64_t batches) {
+    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128) * batches;
+    if (tiles >= 224 || steps < 16) return 1;
+    return (int32_t)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, steps / 8));
+}
+inline int64_t split_bytes(int64_t M, int64_t N, int64_t splits, int64_t batches) {
+    return splits > 1 ? splits * batches * M * ((N + 3) & ~int64_t(3)) * 4 : 0;
+}
+// (grids of fewer than 2^32 threads)
+inline bool gemm_in_range(int64_t M, int64_t N, int64_t batches) {
+    return (__int128)((M + 127) / 128) * ((N + 127) / 128) * batches < (int64_t(1) << 22);
+}
+
+// A plain matrix out of the sums: rows of out (from row `second` on those of
+// out2), batches apart, rounded to `type` once, what was there or `sums`
+// (fp32, dense) added before; or fp32 parts of a split product.
+struct MatrixOut {
+    static constexpr bool kPair = false;
+    void *out, *out2;
+    int64_t ld, batch_stride;
+    int32_t type, second;
+    int32_t add;              // to what out holds
+    int32_t skip_empty;       // batches without a range along k are left alone
+    const int32_t *row_map;   // out's row of each row; negative: none
+    const float *sums;
+    float *to_sums;           // fp32 sums in out's place
+    float *parts;
+
+    __device__ __forceinline__ void put(const GemmArgs &g, int32_t batch, int32_t m, int32_t n,
+                                        f32x4 v) const {
+        if (m >= g.M || n >= g.N) return;
+        int64_t r = m;
+        if (row_map) {
+            r = row_map[m];
+            if (r < 0) return;
+        }
+        const int w = min(4, g.N - n);
+        if (sums || to_sums) {
+            const int64_t at = ((int64_t)batch * g.M + m) * g.N + n;
+            if (sums) v += load4(sums + at, w);
+            if (to_sums) return store4(to_sums + at, v, w);
+        }
+        char *base = (char *)out;
+        if (second && r >= second) {
+            base = (char *)out2;
+            r -= second;
+        }
+        const int64_t at = batch * batch_stride + r * ld + n;
+        if (type == ECC_F32) {
+            float *p = (float *)base + at;
+            if (add) v += load4(p, w);
+            store4(p, v, w);
+        } else {
+            bf16_t *p = (bf16_t *)base + at;
+            Raw<bf16_t, 4> x;
+            if (add) {
+                x.load_upto(p, w);
+                for (int e = 0; e < 4; ++e) v[e] += x.get<float>(e);
+            }
+            const float y[4] = {v[0], v[1], v[2], v[3]};
+            x.set_all(y);
+            x.store_upto(p, w);
+        }
+    }
+    __device__ static __forceinline__ f32x4 load4(const float *p, int w) {
+        Raw<float, 4> x;
+        x.load_upto(p, w);
+        return f32x4{x.get<float>(0), x.get<float>(1), x.get<float>(2), x.get<float>(3)};
+    }
+    __device__ static __forceinline__ void store4(float *p, f32x4 v, int w) {
+        Raw<float, 4> x;
+        const float y[4] = {v[0], v[1], v[2], v[3]};
+        x.set_all(y);
+        x.store_upto(p, w);
+    }
+    template <int MI, int NI>
+    __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
+                                           f32x4 (&acc)[MI][NI]) const {
+        if (parts) {
+            const int64_t ld4 = (g.N + 3) & ~3;
+            float *p = parts + (int64_t)(t.batch * g.splits + t.split) * g.M * ld4;
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    if (t.m + 16 * i < g.M && t.n + 16 * j < g.N)
+                        *reinterpret_cast<f32x4 *>(p + (t.m + 16 * i) * ld4 + t.n + 16 * j) =
+                            acc[i][j];
+            return;
+        }
+        if (skip_empty && t.k == 0) return;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                put(g, t.batch, t.m + 16 * i, t.n + 16 * j, acc[i][j]);
+    }
+};
+
+// Adds the parts of a split product in their order: one thread per four
+// columns of a row.
+static __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, MatrixOut out,
+                                                          int64_t quads) {
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= quads) return;
+    const int32_t per_row = (g.N + 3) / 4;
+    const int64_t row = i / per_row;
+    const int32_t n = (int32_t)(i - row * per_row) * 4;
+    const int32_t batch = (int32_t)(row / g.M), m = (int32_t)(row - (int64_t)batch * g.M);
+    if (g.live && m / 128 * 128 + g.m_lo >= *g.live) return;  // (that tile was left out)
+    if (out.skip_empty && g.ranges) {
+        const int2 r = g.ranges[batch];
+        if (min(r.y, g.k_hi) <= max(r.x, g.k_lo)) return;
+    }
+    const int64_t ld4 = (g.N + 3) & ~3;
+    const float *p = out.parts + ((int64_t)batch * g.splits * g.M + m) * ld4 + n;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+    for (int32_t s = 1; s < g.splits; ++s)
+        v += *reinterpret_cast<const f32x4 *>(p + s * (int64_t)g.M * ld4);
+    out.parts = nullptr;
+    out.put(g, batch, m, n, v);
+}
+
+// A product into a plain matrix, split along k as gemm_splits says; parts: work
+// memory of split_bytes.
+inline void launch_product(GemmArgs g, MatrixOut out, float *parts, hipStream_t s) {
+    if (g.splits == 1) {
+        launch_gemm(g, out, s);
+        return;
+    }
+    out.parts = parts;
+    launch_gemm_tile<128, 128, 2, 2>(g, out, s);
+    const int64_t quads = (int64_t)g.batches * g.M * ((g.N + 3) / 4);
+    hipLaunchKernelGGL(k_gemm_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, out,
+                       quads);
+}
+
+}  // namespace ecc

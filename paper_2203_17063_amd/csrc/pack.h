@@ -1,0 +1,150 @@
+// Operands of the products (gemm.h) out of the caller's matrices: bf16 planes
+// whose rows are a multiple of 64 long, 16-byte aligned and padded with zeros,
+// in the matrix's own order or transposed.
+#pragma once
+
+#include "lm_common.h"
+
+namespace ecc {
+
+constexpr int64_t pad64(int64_t n) { return (n + 63) & ~int64_t(63); }
+
+// An fp32 value as three bf16 that add up to it: each the nearest to what the
+// ones before leave (8 + 8 + 8 bits and the signs hold all 24).  Values that
+// would round to an infinity are cut off instead; infinities and NaN are their
+// first piece's.  (Pieces below 2^-133 of values below 2^-117 are lost.)
+__device__ __forceinline__ void split3(float v, float (&piece)[3]) {
+    float hi = bf16_value(bf16_pair(v, 0.0f) & 0xffffu);
+    const uint32_t bits = __float_as_uint(v);
+    if (__builtin_isinf(hi)) hi = __uint_as_float(bits & 0xffff0000u);
+    float rest = v - hi;
+    if ((bits & 0x7f800000u) == 0x7f800000u) rest = 0.0f;  // infinity or NaN
+    piece[0] = hi;
+    piece[1] = bf16_value(bf16_pair(rest, 0.0f) & 0xffffu);
+    piece[2] = rest - piece[1];
+}
+
+// Piece `which` of values v as bf16.
+template <int N>
+__device__ __forceinline__ void set_piece(Raw<bf16_t, N> &x, const float (&v)[N], int which,
+                                          bool split) {
+    float y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        float p[3] = {v[e], 0.0f, 0.0f};
+        if (split) split3(v[e], p);
+        y[e] = which == 0 ? p[0] : which == 1 ? p[1] : p[2];
+    }
+    x.set_all(y);
+}
+
+// Where packed rows come from: row_map (negative: zeros), or rows of workers
+// padded from n to n_pad rows each.
+struct PackArgs {
+    const void *src;
+    int64_t ld;
+    int64_t cols;
+    int64_t rows_packed;       // a multiple of 64
+    int64_t n, n_pad, total;   // total: source rows
+    const int32_t *row_map;
+    const int32_t *live;       // row blocks from *live - row0 on are left alone
+    int64_t row0;
+    int32_t pieces;
+    bf16_t *rows;              // [pieces][rows_packed][ld_rows] or NULL
+    int64_t ld_rows;           // >= cols, a multiple of 64: zeros up to there
+    bf16_t *cols_out;          // [pieces][cols][ld_cols] or NULL
+    int64_t ld_cols;
+    int64_t plane_rows, plane_cols;
+    int32_t col_blocks;
+};
+
+constexpr int kTile = 64;  // rows and columns of a block
+
+// A block of 64 x 64 values in LDS, as [column][row].
+struct PackTile {
+    float v[kTile][kTile + 1];
+};
+
+// Writes the block's pieces: `mine[p]` are this thread's 8 columns c8 .. + 7 of
+// row p * 32 + r.  Loads and stores are of 16 bytes, eight to a row.
+__device__ __forceinline__ void write_block(PackTile &s, const float (&mine)[2][8], int64_t row0,
+                                            int64_t col0, int64_t cols, bf16_t *rows,
+                                            int64_t ld_rows, int64_t plane_rows, int pieces_rows,
+                                            bf16_t *cols_out, int64_t ld_cols, int64_t plane_cols,
+                                            int pieces_cols) {
+    const int c8 = (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
+    if (rows && col0 + c8 < ld_rows) {
+        for (int which = 0; which < pieces_rows; ++which)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                Raw<bf16_t, 8> x;
+                set_piece(x, mine[p], which, pieces_rows > 1);
+                x.store(rows + which * plane_rows + (row0 + p * 32 + r) * ld_rows + col0 + c8);
+            }
+    }
+    if (!cols_out) return;
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s.v[c8 + e][p * 32 + r] = mine[p][e];
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        const int c = p * 32 + r;
+        if (col0 + c >= cols) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = s.v[c][c8 + e];
+        for (int which = 0; which < pieces_cols; ++which) {
+            Raw<bf16_t, 8> x;
+            set_piece(x, v, which, pieces_cols > 1);
+            x.store(cols_out + which * plane_cols + (col0 + c) * ld_cols + row0 + c8);
+        }
+    }
+}
+
+// One workgroup per block of 64 x 64, columns first.  Bound by memory: each
+// value is read once and written once per layout and piece.
+template <typename T>
+static __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+    __shared__ PackTile s;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.col_blocks) * kTile;
+    const int64_t col0 = (int64_t)(blockIdx.x % a.col_blocks) * kTile;
+    if (a.live && row0 + a.row0 >= *a.live) return;
+    const int c8 = (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
+    float mine[2][8];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        int64_t row = row0 + p * 32 + r;
+        if (a.row_map) row = a.row_map[row];
+        else {
+            const int64_t w = row / a.n_pad, i = row - w * a.n_pad;
+            row = i < a.n ? w * a.n + i : -1;
+            if (row >= a.total) row = -1;
+        }
+        Raw<T, 8> x;
+        x.load_upto((const T *)a.src + (row < 0 ? 0 : row * a.ld) + (row < 0 ? 0 : col0 + c8),
+                    row < 0 ? 0 : a.cols - col0 - c8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine[p][e] = x.template get<float>(e);
+    }
+    write_block(s, mine, row0, col0, a.cols, a.rows, a.ld_rows, a.plane_rows, a.pieces, a.cols_out,
+                a.ld_cols, a.plane_cols, a.pieces);
+}
+
+inline void launch_pack(PackArgs a, int32_t type, hipStream_t s) {
+    a.col_blocks = (int32_t)((a.cols + kTile - 1) / kTile);
+    const int64_t grid = a.rows_packed / kTile * a.col_blocks;
+    if (grid <= 0) return;
+    if (type == ECC_F32)
+        hipLaunchKernelGGL(k_pack<float>, dim3((unsigned)grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(k_pack<bf16_t>, dim3((unsigned)grid), dim3(256), 0, s, a);
+}
+
+// Can a product take a bf16 matrix as it lies?
+inline bool as_it_lies(const void *p, int64_t ld, int64_t cols, int32_t type) {
+    return type == ECC_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 64 == 0 &&
+           ld < (int64_t(1) << 23);
+}
+
+}  // namespace ecc

@@ -408,3 +408,251 @@ def distill(z, top, idx, tau=1.0, kd_weight=1.0, ce_weight=0.0, labels=None, wei
     work = _work(max(size, 16), z) if work is None else _given_work(work, size, z)
     _launch(z, E.ecc_distill, a, loss, grad, ld_dz, work)
     return loss, grad
+
+
+# ----------------------------------------------------------------------------
+# cross entropy from hidden states
+# ----------------------------------------------------------------------------
+
+def _product_type(t, what):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("%s must be float32 or bfloat16, not %s" % (what, t.dtype))
+    return _TYPES[t.dtype]
+
+
+def cross_entropy(h, table, labels, weight=None, scale=1.0, P=1, grad=True, dtype=None, loss=None,
+                  dh=None, dtable=None, accumulate=False, work=None):
+    """(loss, dh, dtable) of the logits scale * h table^T, which are never held
+    as a whole: per row of h (..., D) weight (log sum exp of its logits - the
+    logit of its label), and the gradients of the losses' sum in h and, per
+    worker (P, V, D), in the table.
+
+    labels: int32, outside [0, V) for none; weight: fp32.  grad: None for the
+    loss only.  dtype: of dtable, float32 or the table's (which it is by
+    default); dtable: written, or with accumulate added to; its rows and
+    workers may be strided."""
+    if table.dim() != 2:
+        raise ValueError("table must be a matrix")
+    V, D = table.shape
+    t = _product_type(h, "h")
+    if table.dtype != h.dtype:
+        raise TypeError("table must be %s like h, not %s" % (h.dtype, table.dtype))
+    N, ld_h = _rows(h, "h", D)
+    _, ld_table = _rows(table, "table")
+    shape = h.shape[:-1]
+    for v, kind, what in ((labels, torch.int32, "labels"), (weight, torch.float32, "weight")):
+        if v is None and what == "weight":
+            continue
+        if v.shape != shape or v.dtype != kind:
+            raise ValueError("%s must be %s of shape %s, not %s of %s" %
+                             (what, kind, tuple(shape), tuple(v.shape), v.dtype))
+        _contiguous(v, what)
+    if P < 1 or N % P:
+        raise ValueError("%d rows cannot be shared equally by %d workers" % (N, P))
+    if not grad and (dh is not None or dtable is not None or accumulate):
+        raise ValueError("gradients given without grad")
+    if dtable is not None:
+        if tuple(dtable.shape) != (P, V, D):
+            raise ValueError("dtable must have shape %s, not %s" % ((P, V, D), tuple(dtable.shape)))
+        if D > 1 and dtable.stride(2) != 1:
+            raise ValueError("dtable must be contiguous in its last dimension")
+        dtype = dtable.dtype
+    elif accumulate:
+        raise ValueError("accumulate needs dtable")
+    dtype = dtype or table.dtype
+    if dtype not in (torch.float32, table.dtype):
+        raise TypeError("dtable must be float32 or %s, not %s" % (table.dtype, dtype))
+    loss = _out(loss, shape, torch.float32, h, "loss")
+    _contiguous(loss, "loss")
+    ld_dh = ld_dt = stride = 0
+    if grad:
+        dh = _out(dh, h.shape, h.dtype, h, "dh")
+        _, ld_dh = _rows(dh, "dh")
+        if dtable is None:
+            dtable = table.new_empty((P, V, D), dtype=dtype)
+        ld_dt = dtable.stride(1) if V > 1 else D
+        stride = dtable.stride(0) if P > 1 else V * D
+    _one_gpu(h, (table, labels, weight, loss, dh, dtable), "h table labels weight loss dh dtable")
+    a = E.ecc_cross_entropy_t(N // P, V, D, P, t, _TYPES[dtype], 0, h.data_ptr(), ld_h,
+                              table.data_ptr(), ld_table, labels.data_ptr(),
+                              None if weight is None else weight.data_ptr(), scale)
+    size = E.ecc_cross_entropy_work_size(a, 1 if grad else 0)
+    # (a refused description has no size: the call says what is wrong)
+    work = _work(max(size, 16), h) if work is None else _given_work(work, size, h)
+    _launch(h, E.ecc_cross_entropy, a, loss, dh, ld_dh, dtable, ld_dt, stride,
+            1 if accumulate else 0, work)
+    return loss, dh, dtable
+
+
+# ----------------------------------------------------------------------------
+# the gated feed-forward block
+# ----------------------------------------------------------------------------
+
+_ACTS = {"silu": E.ECC_ACT_SILU, "gelu": E.ECC_ACT_GELU}
+
+
+def _ffn(x, w_gate, w_up, act, P, dtype):
+    """The ecc_ffn_t of tensors; rows and inner width."""
+    if w_gate.dim() != 2 or w_gate.shape != w_up.shape:
+        raise ValueError("w_gate and w_up must be matrices of one shape, not %s and %s" %
+                         (tuple(w_gate.shape), tuple(w_up.shape)))
+    F, D = w_gate.shape
+    t = _product_type(x, "x")
+    if w_gate.dtype != x.dtype or w_up.dtype != x.dtype:
+        raise TypeError("the weights must be %s like x, not %s and %s" %
+                        (x.dtype, w_gate.dtype, w_up.dtype))
+    if act not in _ACTS:
+        raise ValueError("act must be one of %s, not %r" % (", ".join(_ACTS), act))
+    if dtype not in (torch.float32, x.dtype):
+        raise TypeError("the weights' gradients must be float32 or %s, not %s" % (x.dtype, dtype))
+    N, ld_x = _rows(x, "x", D)
+    if P < 1 or N % P:
+        raise ValueError("%d rows cannot be shared equally by %d workers" % (N, P))
+    a = E.ecc_ffn_t(N // P, D, F, P, t, _TYPES[dtype], _ACTS[act], x.data_ptr(), ld_x,
+                    w_gate.data_ptr(), _rows(w_gate, "w_gate")[1], w_up.data_ptr(),
+                    _rows(w_up, "w_up")[1])
+    return a, N, F
+
+
+def gated_ffn(x, w_gate, w_up, act="silu", out=None, work=None):
+    """act(x w_gate^T) * (x w_up^T), of shape (..., F), for weights (F, D).
+    act: "silu" or "gelu" (by erf)."""
+    a, _, F = _ffn(x, w_gate, w_up, act, 1, x.dtype)
+    out = _out(out, x.shape[:-1] + (F,), x.dtype, x, "out")
+    _, ld = _rows(out, "out")
+    _one_gpu(x, (w_gate, w_up, out), "x w_gate w_up out")
+    size = E.ecc_ffn_work_size(a, 0)
+    # (a refused description has no size: the call says what is wrong)
+    work = _work(max(size, 16), x) if work is None else _given_work(work, size, x)
+    _launch(x, E.ecc_ffn_forward, a, out, ld, work)
+    return out
+
+
+def gated_ffn_grad(x, w_gate, w_up, dy, act="silu", P=1, dtype=None, dx=None, dw_gate=None,
+                   dw_up=None, accumulate=False, work=None):
+    """The gradients of gated_ffn for a given dy: a dict of dx, and dw_gate and
+    dw_up per worker, (P, F, D) of dtype (float32, or the weights' type, which
+    it is by default).  Given ones of the weights may be views of contributions
+    whose workers lie one common stride apart, and accumulate adds to them."""
+    given = [w for w in (dw_gate, dw_up) if w is not None]
+    if len(given) == 1 or (accumulate and not given):
+        raise ValueError("the weights' gradients are given together" if given else
+                         "accumulate needs dw_gate and dw_up")
+    dtype = given[0].dtype if given else dtype or w_gate.dtype
+    a, N, F = _ffn(x, w_gate, w_up, act, P, dtype)
+    D = w_gate.shape[1]
+    rows, ld_dy = _rows(dy, "dy", F)
+    if rows != N or dy.dtype != x.dtype:
+        raise ValueError("dy must have %d rows of %s, not %s of %s" %
+                         (N, x.dtype, tuple(dy.shape), dy.dtype))
+    dx = _out(dx, x.shape, x.dtype, x, "dx")
+    _, ld_dx = _rows(dx, "dx")
+    if not given:
+        dw_gate, dw_up = (x.new_empty((P, F, D), dtype=dtype) for _ in range(2))
+    stride = dw_gate.stride(0) if P > 1 else F * D
+    for w in (dw_gate, dw_up):
+        if tuple(w.shape) != (P, F, D) or w.dtype != dtype or not w[0].is_contiguous() or \
+                (P > 1 and w.stride(0) != stride):
+            raise ValueError("dw_gate and dw_up must be dense matrices of %s per worker, of shape "
+                             "%s, one stride for both" % (dtype, (P, F, D)))
+    _one_gpu(x, (w_gate, w_up, dy, dx, dw_gate, dw_up), "x w_gate w_up dy dx dw_gate dw_up")
+    size = E.ecc_ffn_work_size(a, 1)
+    # (a refused description has no size: the call says what is wrong)
+    work = _work(max(size, 16), x) if work is None else _given_work(work, size, x)
+    _launch(x, E.ecc_ffn_grad, a, dy, ld_dy, dx, ld_dx, dw_gate, dw_up, stride,
+            1 if accumulate else 0, work)
+    return {"dx": dx, "dw_gate": dw_gate, "dw_up": dw_up}
+
+
+# ----------------------------------------------------------------------------
+# norms and clipping of gradients
+# ----------------------------------------------------------------------------
+
+def _worker_parts(t, P, what):
+    """(elements per worker, elements from one worker to the next)."""
+    if P is None:
+        return _contiguous(t, what).numel(), 0
+    if t.dim() < 1 or t.shape[0] != P:
+        raise ValueError("%s must have %d workers in its first dimension, not shape %s" %
+                         (what, P, tuple(t.shape)))
+    if t.is_contiguous():
+        n = t.numel() // P
+        return n, n
+    if not t[0].is_contiguous():
+        raise ValueError("%s must be contiguous for each worker" % what)
+    return t[0].numel(), t.stride(0)
+
+
+def _tensors(grads, out, P):
+    """The array of ecc_tensor_t, and the first tensor."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("there are no gradients")
+    if P is not None and P < 1:
+        raise ValueError("P must be >= 1")
+    outs = [None] * len(grads) if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError("%d outputs for %d gradients" % (len(outs), len(grads)))
+    a = (E.ecc_tensor_t * len(grads))()
+    device = grads[0].get_device()
+    if device < 0:
+        raise ValueError("grads must be on the GPU")
+    for e, g, o in zip(a, grads, outs):
+        e.type = _type(g, "a gradient")
+        e.d_grad = g.data_ptr()
+        e.n, e.stride = _worker_parts(g, P, "a gradient")
+        if g.get_device() != device:
+            raise ValueError("grads must be on one GPU")
+        if o is not None:
+            e.out_type = _type(o, "an output")
+            e.d_out = o.data_ptr()
+            n, e.out_stride = _worker_parts(o, P, "an output")
+            if o.shape != g.shape:
+                raise ValueError("an output must have its gradient's shape %s, not %s" %
+                                 (tuple(g.shape), tuple(o.shape)))
+            if o.get_device() != device:
+                raise ValueError("grads and out must be on one GPU")
+    return a, grads[0]
+
+
+def _norms(norms, P, like):
+    norms = _out(norms, (1 if P is None else P,), torch.float64, like, "norms")
+    _contiguous(norms, "norms")
+    _one_gpu(like, (norms,), "grads norms")
+    return norms
+
+
+def grad_norm(grads, P=None, norms=None, work=None):
+    """The global norm over the tensors `grads`, float64 of shape (1,), or with
+    P given, tensors of shape (P, ...), each worker's, of shape (P,)."""
+    a, like = _tensors(grads, None, P)
+    norms = _norms(norms, P, like)
+    size = E.ecc_grad_norm_work_size(P or 1, len(a), a)
+    # (refused tensors have no size: the call says what is wrong)
+    work = _work(max(size, 16), like) if work is None else _given_work(work, size, like)
+    _launch(like, E.ecc_grad_norm, P or 1, len(a), a, norms, work)
+    return norms
+
+
+_NONFINITE = {"keep": E.ECC_CLIP_KEEP, "zero": E.ECC_CLIP_ZERO}
+
+
+def clip_grads(grads, max_norm, P=None, out=None, nonfinite="keep", norms=None, work=None):
+    """Scales gradients to at most max_norm, each worker's by its own norm, and
+    returns the norms before that (see grad_norm).
+
+    out: tensors of the gradients' shapes and any type to write instead (e.g.
+    the parameters' places in the workers' contributions); None in a place, or
+    for all: in place.  nonfinite: "keep" leaves the gradients of a worker whose
+    norm is infinite or NaN as they are, "zero" makes them zeros."""
+    if nonfinite not in _NONFINITE:
+        raise ValueError("nonfinite must be one of %s, not %r" %
+                         (", ".join(_NONFINITE), nonfinite))
+    a, like = _tensors(grads, out, P)
+    norms = _norms(norms, P, like)
+    size = E.ecc_grad_norm_work_size(P or 1, len(a), a)
+    # (refused tensors have no size: the call says what is wrong)
+    work = _work(max(size, 16), like) if work is None else _given_work(work, size, like)
+    _launch(like, E.ecc_clip_grads, P or 1, len(a), a, max_norm, _NONFINITE[nonfinite], norms,
+            work)
+    return norms
