@@ -20,7 +20,7 @@ namespace ecc {
 namespace {
 
 // Bytes of logits and their gradients at a time.
-constexpr int64_t kPieceBytes = int64_t(1) << 32;
+constexpr int64_t kPieceBytes = int64_t(5) << 30;
 
 struct Rows {
     int32_t *map;      // packed row -> position, -1: none
@@ -275,7 +275,7 @@ struct Plan {
     int np;                      // pieces of the operands
     int pz, pzt;                 // of dz for dh, for dE
     bool pack_table;
-    int64_t splits_h, splits_e;
+    GemmShape shape_h, shape_e;
     // offsets into the work buffer
     int64_t map, label, weight, live, ranges, counts, table, table_t, h, h_t, z, dz, dzt, stats,
         picked, terms, sums, parts, bytes;
@@ -298,6 +298,10 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
                         (gradient ? 4 * p.Vp + 2 * p.pz * p.Vp + 2 * p.pzt * p.Vp : 0);
     p.R = std::max<int64_t>(256, kPieceBytes / row & ~int64_t(255));
     p.R = std::max<int64_t>(64, std::min(p.R, p.rows));
+    p.pieces_of_rows = (p.rows + p.R - 1) / p.R;
+    // (pieces of equal length)
+    if (p.pieces_of_rows > 1)
+        p.R = (p.rows / p.pieces_of_rows + 255 + (p.rows % p.pieces_of_rows > 0)) & ~int64_t(255);
     p.pieces_of_rows = (p.rows + p.R - 1) / p.R;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -323,10 +327,13 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
         p.dzt = take(2 * p.pzt * a->V * p.R);
         p.terms = take(12 * p.R);
         p.sums = take(p.pieces_of_rows > 1 && a->grad_type != ECC_F32 ? 4 * a->P * a->V * a->D : 0);
-        p.splits_h = gemm_splits(p.R, a->D, p.Vp / kGemmK * (p.np == 3 ? 6 : 1), 1);
-        p.splits_e = gemm_splits(a->V, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pzt), a->P);
-        p.parts = take(std::max(split_bytes(p.R, a->D, p.splits_h, 1),
-                                split_bytes(a->V, a->D, p.splits_e, a->P)));
+        p.shape_h = gemm_shape(p.R, a->D, p.Vp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+        // (a worker's rows in a piece)
+        p.shape_e = gemm_shape(a->V, a->D,
+                               std::min(p.n_pad, p.R) / kGemmK * (p.np == 3 ? 6 : p.pzt), a->P,
+                               true);
+        p.parts = take(std::max(split_bytes(p.R, a->D, p.shape_h.splits, 1),
+                                split_bytes(a->V, a->D, p.shape_e.splits, a->P)));
     }
     p.bytes = std::max<int64_t>(at, 16);
     return p;
@@ -495,7 +502,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         g.M = (int32_t)R;
         g.N = (int32_t)V;
         g.K = (int32_t)p.Dp;
-        g.batches = g.splits = 1;
+        g.batches = 1;
         g.live = rows.live;
         g.m_lo = (int32_t)r0;
         set_products(g, p.np, p.np);
@@ -535,7 +542,6 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             d.N = (int32_t)D;
             d.K = (int32_t)p.Vp;
             d.batches = 1;
-            d.splits = (int32_t)p.splits_h;
             d.live = rows.live;
             d.m_lo = (int32_t)r0;
             set_products(d, p.pz, p.np);
@@ -544,7 +550,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             out.ld = ld_dh;
             out.type = a->type;
             out.row_map = rows.map + r0;
-            launch_product(d, out, (float *)(w + p.parts), s);
+            launch_product(d, out, p.shape_h, (float *)(w + p.parts), s);
         }
         if (d_dtable) {
             const bool first = r0 == 0, last = r0 + R >= p.rows;
@@ -554,7 +560,6 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             d.M = (int32_t)V;
             d.N = (int32_t)D;
             d.batches = P;
-            d.splits = (int32_t)p.splits_e;
             d.ranges = rows.ranges;
             d.k_lo = (int32_t)r0;
             d.k_hi = (int32_t)(r0 + R);
@@ -573,7 +578,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
                 out.add = last && accumulate;
                 out.skip_empty = !first && !last;
             }
-            launch_product(d, out, (float *)(w + p.parts), s);
+            launch_product(d, out, p.shape_e, (float *)(w + p.parts), s);
         }
     }
     ECC_LAUNCH_CHECK();

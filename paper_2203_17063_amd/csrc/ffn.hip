@@ -102,7 +102,7 @@ struct Plan {
     int64_t N, n_pad, rows, Dp, Fp;
     int np, pd;                   // pieces of the operands, of dg and du
     bool pack_x, pack_gate, pack_up;
-    int64_t splits_x, splits_w;
+    GemmShape shape_x, shape_w;
     int64_t x, gate, up, x_t, w_t, d, d_t, parts, bytes;
 };
 
@@ -134,10 +134,10 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
         p.w_t = take(p.np * 2 * a->D * 2 * p.Fp);
         p.d = take(p.pd * 2 * pad64(p.N) * 2 * p.Fp);
         p.d_t = take(p.pd * 2 * 2 * a->F * p.rows);
-        p.splits_x = gemm_splits(p.N, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1);
-        p.splits_w = gemm_splits(2 * a->F, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pd), a->P);
-        p.parts = take(std::max(split_bytes(p.N, a->D, p.splits_x, 1),
-                                split_bytes(2 * a->F, a->D, p.splits_w, a->P)));
+        p.shape_x = gemm_shape(p.N, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+        p.shape_w = gemm_shape(2 * a->F, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pd), a->P, true);
+        p.parts = take(std::max(split_bytes(p.N, a->D, p.shape_x.splits, 1),
+                                split_bytes(2 * a->F, a->D, p.shape_w.splits, a->P)));
     }
     p.bytes = std::max<int64_t>(at, 16);
     return p;
@@ -197,7 +197,7 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
     g.M = (int32_t)p.N;
     g.N = (int32_t)a->F;
     g.K = (int32_t)p.Dp;
-    g.batches = g.splits = 1;
+    g.batches = 1;
     set_products(g, p.np, p.np);
     return g;
 }
@@ -356,13 +356,12 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         x.N = (int32_t)D;
         x.K = (int32_t)(2 * p.Fp);
         x.batches = 1;
-        x.splits = (int32_t)p.splits_x;
         set_products(x, p.np, p.np);
         MatrixOut to{};
         to.out = d_dx;
         to.ld = ld_dx;
         to.type = a->type;
-        launch_product(x, to, (float *)(w + p.parts), s);
+        launch_product(x, to, p.shape_x, (float *)(w + p.parts), s);
     }
     if (d_dw_gate) {
         // x and [dg | du] transposed, workers padded to multiples of 64 rows
@@ -395,7 +394,6 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         x.N = (int32_t)D;
         x.K = (int32_t)p.n_pad;
         x.batches = P;
-        x.splits = (int32_t)p.splits_w;
         set_products(x, p.pd, p.np);
         MatrixOut to{};
         to.out = d_dw_gate;
@@ -405,7 +403,7 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         to.batch_stride = worker_stride;
         to.type = a->grad_type;
         to.add = accumulate;
-        launch_product(x, to, (float *)(w + p.parts), s);
+        launch_product(x, to, p.shape_w, (float *)(w + p.parts), s);
     }
     ECC_LAUNCH_CHECK();
     return ECC_OK;

@@ -9,20 +9,29 @@
 // element's product, below fp32's own rounding.  The loop over k just walks
 // the planes one product after another.
 //
-// The kernel: a workgroup holds a tile of BM x BN sums in registers, each wave
-// (BM / WM) x (BN / WN) as 16 x 16 blocks.  Steps of 64 along k are brought
-// into LDS by direct 16-byte loads, one step ahead of the products, in two
-// buffers; a row of a step is 128 bytes, its 16-byte chunks stored at chunk ^
-// (row & 7), so that the reads of 16 rows touch every bank once (the loads
-// write LDS lane after lane, so the exchange is in the addresses they read).
-// Rows behind the last one are read as the last row and not stored.
-// Workgroups go round the eight XCDs, each of which walks a contiguous part of
-// the tiles in bands of four tile rows, so that its L2 serves the operands of
-// neighbours.
-// 256 x 256 with 8 waves is bound by the matrix cores and LDS: 8,192^3 at 1.25
-// PFLOP/s, 4,096^3 at 1.13; 128 x 128 with 4 waves reaches 1.03 and 0.98, and
-// is for products that leave CUs without a large tile.  (256 x 256 with 4
-// waves needs 256 sums a lane and spills: 0.29 PFLOP/s.)
+// The kernel: a workgroup of eight waves holds a tile of BM x BN sums in
+// registers, as 16 x 16 blocks.  Steps of 64 along k are brought into LDS by
+// direct 16-byte loads; a row of a step is 128 bytes, its 16-byte chunks stored
+// at chunk ^ (row & 7), so that no reads of a wave meet in a bank (counted: 0
+// conflicts; the loads write LDS lane after lane, so the exchange is in the
+// addresses that they read).  Rows behind the last one are read as the last row
+// and not stored.  Workgroups go round the eight XCDs, each of which walks a
+// contiguous part of the tiles in bands of four tile rows, so that its L2 serves
+// the operands of neighbours.
+//
+// 256 x 256: the waves are two groups, the upper and the lower half of the tile,
+// that take turns: while one reads a whole step from LDS into registers, the
+// other keeps the matrix cores busy with the step that it has read, and issues
+// loads.  A's steps have two buffers (a half is free once its group has read
+// it), B's three, all 160 KiB of a CU, so that loads have three or four turns
+// to arrive.  8,192^3: 1.26 PFLOP/s, 4,096 x 4,096 x 128,000: 1.37 (zeros, which
+// draw less power: 1.56 and 1.66; without loads 2.10).  A plain double buffer
+// of both made 1.11 and 1.14, two groups over it 1.21 and 1.20; products of
+// 32 x 32 blocks 1.15 and 1.25; loads between the products 1.20 and 1.31.
+//
+// 128 x 128, four buffers of both, one meeting of the waves a step: for products
+// whose large tiles would leave CUs idle.  2,048^2 x 16,384: 0.89 PFLOP/s (four
+// waves 0.79).
 #pragma once
 
 #include "lm_common.h"
@@ -59,17 +68,18 @@ struct GemmArgs {
     const int32_t *live;
     int32_t m_lo;
     int32_t nprod;         // products of pieces
-    uint8_t pa[6], pb[6];
+    int64_t a_piece[6], b_piece[6];  // where each one's pieces begin
 };
 
-// The products of an operand of `na` pieces with one of `nb`, small ones first.
+// The products of operands (set before) of `na` and `nb` pieces, small ones
+// first.
 inline void set_products(GemmArgs &g, int na, int nb) {
     static const uint8_t both[6][2] = {{1, 1}, {0, 2}, {2, 0}, {0, 1}, {1, 0}, {0, 0}};
     g.nprod = 0;
     for (auto &p : both) {
         if (p[0] >= na || p[1] >= nb) continue;
-        g.pa[g.nprod] = p[0];
-        g.pb[g.nprod++] = p[1];
+        g.a_piece[g.nprod] = p[0] * g.a.plane;
+        g.b_piece[g.nprod++] = p[1] * g.b.plane;
     }
 }
 
@@ -85,11 +95,48 @@ struct GemmTile {
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// 16 bytes a lane from base + offset into LDS, lane after lane.
-__device__ __forceinline__ void load_to_lds(const void *base, uint32_t offset, uint16_t *to) {
+// A value that all lanes share, in a scalar register.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Where the next step of an operand lies; products of pieces follow each other.
+// Behind the last step nothing is read, so that loads need no condition.
+struct GemmCursor {
+    int prod, left, todo;   // steps left of this product, of all
+    const bf16_t *next;
+    __device__ __forceinline__ int bytes() const { return uniform(~((todo - 1) >> 31)); }
+    __device__ __forceinline__ void step(int ksteps, int nprod, const bf16_t *base,
+                                         const int64_t *piece) {
+        next += kGemmK;
+        --todo;
+        if (--left == 0) {
+            left = ksteps;
+            prod = min(prod + 1, nprod - 1);
+            next = base + piece[prod];
+        }
+    }
+};
+// 16 bytes a lane from base + offset into LDS, lane after lane; zeros where
+// `bytes` from base on are none.
+__device__ __forceinline__ void load_to_lds(const void *base, int bytes, uint32_t offset,
+                                            uint16_t *to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, -1, 0x00020000),
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000),
         (lds_void *)to, 16, (int)offset, 0, 0, 0);
+}
+
+// This wave's direct loads are in LDS; its reads of LDS are in registers.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4 << 14));
+}
+__device__ __forceinline__ void wait_reads() { __builtin_amdgcn_s_waitcnt(0xc07f); }
+// Where all waves of a workgroup meet; nothing moves across.
+__device__ __forceinline__ void phase_end() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int BM, int BN, int WM, int WN, class Epi>
@@ -100,10 +147,12 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
     static_assert(BN / WN == 64, "a wave's columns: 64, or 32 of each of a pair");
     // (four arrays: the compiler tells the loads of one buffer from the reads
     // of the other by their names)
-    __shared__ __attribute__((aligned(1024))) uint16_t s_a0[BM * kGemmK];
-    __shared__ __attribute__((aligned(1024))) uint16_t s_b0[BN * kGemmK];
-    __shared__ __attribute__((aligned(1024))) uint16_t s_a1[BM * kGemmK];
-    __shared__ __attribute__((aligned(1024))) uint16_t s_b1[BN * kGemmK];
+    // (separate arrays: the compiler tells the loads into one from the reads of
+    // another by their names)
+    constexpr int kA = BM * kGemmK, kB = BN * kGemmK, kSmall = BM == 256 ? 8 : 1;
+    __shared__ __attribute__((aligned(1024))) uint16_t s_a0[kA], s_a1[kA], s_b0[kB], s_b1[kB],
+        s_b2[kB], s_a2[kSmall == 1 ? kA : 8], s_a3[kSmall == 1 ? kA : 8],
+        s_b3[kSmall == 1 ? kB : 8];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -111,29 +160,29 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
     // the tile: blocks go round the XCDs, each takes a contiguous share
     const int per = (int)((gridDim.x + 7) >> 3), more = (int)(gridDim.x - ((per - 1) << 3));
     const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
-    int t = xcd * per + at - max(0, xcd - more);
+    int t = xcd * per + at - max(0, xcd - more);  // (uniform: from scalars alone)
     const int tiles = g.tiles_m * g.tiles_n;
     const int part = t / tiles;
     t -= part * tiles;
-    const int split = part % g.splits, batch = part / g.splits;
+    const int split = uniform(part % g.splits), batch = uniform(part / g.splits);
     const int band = kGemmGroup * g.tiles_n;
     const int first = t / band * kGemmGroup, in = t % band;
     const int rows = min(kGemmGroup, g.tiles_m - first);
-    const int tm = first + in % rows, tn = in / rows;
+    const int tm = uniform(first + in % rows), tn = uniform(in / rows);
     const int m0 = tm * BM, n0 = tn * (Epi::kPair ? BN / 2 : BN);
-    if (g.live && m0 + g.m_lo >= *g.live) return;
+    if (g.live && m0 + g.m_lo >= uniform(*g.live)) return;
 
     // the range along k, in steps; this split's share of all products' steps
     int k0 = batch * g.K, k1 = k0 + g.K;
     if (g.ranges) {
         const int2 r = g.ranges[batch];
-        k0 = max(r.x, g.k_lo) - g.k_lo;
-        k1 = max(k0, min(r.y, g.k_hi) - g.k_lo);
+        k0 = uniform(max(r.x, g.k_lo) - g.k_lo);
+        k1 = uniform(max(k0, min(r.y, g.k_hi) - g.k_lo));
     }
     const int ksteps = (k1 - k0) / kGemmK;
     const int all = ksteps * g.nprod;
-    int step = (int)((int64_t)all * split / g.splits);
-    const int end = (int)((int64_t)all * (split + 1) / g.splits);
+    const int step = uniform((int)((int64_t)all * split / g.splits));
+    const int end = uniform((int)((int64_t)all * (split + 1) / g.splits));
 
     uint32_t oa[LA], ob[LB];
     const int sub = lane >> 3, chunk = ((lane & 7) ^ sub) * 16;
@@ -149,9 +198,17 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
         r = min(r, g.N - 1 - n0);
         ob[i] = (uint32_t)(r * (int64_t)g.b.ld * 2 + chunk);
     }
-    const bf16_t *pa = g.a.p + (int64_t)m0 * g.a.ld + k0;
-    const int64_t b_at = (int64_t)n0 * g.b.ld + k0;
-    int prod = ksteps ? step / ksteps : 0, ks = ksteps ? step % ksteps : 0;
+    // where the next step lies; the products of pieces follow each other
+    const bf16_t *a_base = g.a.p + (int64_t)m0 * g.a.ld + k0;
+    const bf16_t *b_base = g.b.p + (int64_t)n0 * g.b.ld + k0;
+    if constexpr (Epi::kPair) {
+        static_assert(LB == 2 || LB == 4, "a wave loads rows of one of the pair");
+        if (wave * LB / 4 & 1) b_base += g.b2 - g.b.p;
+    }
+    const int prod0 = uniform(ksteps ? step / ksteps : 0);
+    GemmCursor at_a{prod0, (prod0 + 1) * ksteps - step, end - step, nullptr}, at_b = at_a;
+    at_a.next = a_base + g.a_piece[prod0] + (ksteps - at_a.left) * kGemmK;
+    at_b.next = b_base + g.b_piece[prod0] + (ksteps - at_b.left) * kGemmK;
 
     f32x4 acc[MI][NI];
 #pragma unroll
@@ -159,54 +216,122 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 
-    // brings the next step into a buffer
-    auto load = [&](uint16_t *sa, uint16_t *sb) {
-        const bf16_t *a = pa + g.pa[prod] * g.a.plane + ks * kGemmK;
-        const int64_t at_b = b_at + g.pb[prod] * g.b.plane + ks * kGemmK;
-        if (++ks == ksteps) ks = 0, ++prod;
+    // bring this wave's rows of the next step of A or B into a buffer
+    auto load_a = [&](uint16_t *to) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) load_to_lds(a, oa[i], sa + (wave * LA + i) * 8 * kGemmK);
+        for (int i = 0; i < LA; ++i)
+            load_to_lds(at_a.next, at_a.bytes(), oa[i], to + (wave * LA + i) * 8 * kGemmK);
+        at_a.step(ksteps, g.nprod, a_base, g.a_piece);
+    };
+    auto load_b = [&](uint16_t *to) {
 #pragma unroll
-        for (int i = 0; i < LB; ++i) {
-            const bf16_t *b = g.b.p;
-            if constexpr (Epi::kPair)
-                if ((wave * LB + i) / 4 & 1) b = g.b2;
-            load_to_lds(b + at_b, ob[i], sb + (wave * LB + i) * 8 * kGemmK);
-        }
+        for (int i = 0; i < LB; ++i)
+            load_to_lds(at_b.next, at_b.bytes(), ob[i], to + (wave * LB + i) * 8 * kGemmK);
+        at_b.step(ksteps, g.nprod, b_base, g.b_piece);
     };
     const int ra = wm * (BM / WM) + (lane & 15), rb = wn * (BN / WN) + (lane & 15);
     const int x = lane & 7, q = lane >> 4;
-    auto multiply = [&](const uint16_t *sa, const uint16_t *sb) {
+    struct Held {
+        bf16x8 a[2][MI], b[2][NI];
+    } f;
+    auto read = [&](const uint16_t *sa, const uint16_t *sb) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 fa[MI], fb[NI];
             const int c = ((kk * 4 + q) ^ x) * 8;
 #pragma unroll
             for (int j = 0; j < NI; ++j)
-                fb[j] = *reinterpret_cast<const bf16x8 *>(sb + (rb + j * 16) * kGemmK + c);
+                f.b[kk][j] = *reinterpret_cast<const bf16x8 *>(sb + (rb + j * 16) * kGemmK + c);
 #pragma unroll
             for (int i = 0; i < MI; ++i)
-                fa[i] = *reinterpret_cast<const bf16x8 *>(sa + (ra + i * 16) * kGemmK + c);
-            // (B first: a lane then holds four neighbouring columns)
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j],
-                                                                       0, 0, 0);
+                f.a[kk][i] = *reinterpret_cast<const bf16x8 *>(sa + (ra + i * 16) * kGemmK + c);
         }
     };
-    if (step < end) {
-        load(s_a0, s_b0);
-        for (;;) {
-            __syncthreads();  // the step is in LDS, and the other buffer is read
-            if (step + 1 < end) load(s_a1, s_b1);
-            multiply(s_a0, s_b0);
-            if (++step >= end) break;
-            __syncthreads();
-            if (step + 1 < end) load(s_a0, s_b0);
-            multiply(s_a1, s_b1);
-            if (++step >= end) break;
+    // (B first: a lane then holds four neighbouring columns)
+    auto multiply = [&] {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int jj = 0; jj < NI; ++jj) {
+                    const int j = i & 1 ? NI - 1 - jj : jj;
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b[kk][j], f.a[kk][i],
+                                                                       acc[i][j], 0, 0, 0);
+                }
+    };
+    const int steps = end - step;
+    if (steps > 0) {
+        if constexpr (BM == 256) {
+            const bool late = wave >= 4;
+            load_a(s_a0);
+            load_b(s_b0);
+            if (late) {
+                load_b(s_b1);
+                load_a(s_a1);
+                load_b(s_b2);
+            } else {
+                load_a(s_a1);
+                load_b(s_b1);
+            }
+            wait_loads<8>();
+            phase_end();
+            if (late) phase_end();
+            auto turn = [&](uint16_t *a, uint16_t *b, uint16_t *b_two) {
+                read(a, b);
+                wait_reads();
+                phase_end();
+                load_a(a);
+                if (late) load_b(b);
+                else load_b(b_two);
+                __builtin_amdgcn_s_setprio(1);
+                multiply();
+                __builtin_amdgcn_s_setprio(0);
+                wait_loads<8>();
+                phase_end();
+            };
+            for (int t = 0;;) {
+                turn(s_a0, s_b0, s_b2);
+                if (++t >= steps) break;
+                turn(s_a1, s_b1, s_b0);
+                if (++t >= steps) break;
+                turn(s_a0, s_b2, s_b1);
+                if (++t >= steps) break;
+                turn(s_a1, s_b0, s_b2);
+                if (++t >= steps) break;
+                turn(s_a0, s_b1, s_b0);
+                if (++t >= steps) break;
+                turn(s_a1, s_b2, s_b1);
+                if (++t >= steps) break;
+            }
+            wait_loads<0>();
+            if (!late) phase_end();
+        } else {
+            load_a(s_a0);
+            load_b(s_b0);
+            load_a(s_a1);
+            load_b(s_b1);
+            load_a(s_a2);
+            load_b(s_b2);
+            auto turn = [&](uint16_t *a, uint16_t *b, uint16_t *next_a, uint16_t *next_b) {
+                wait_loads<2 * (LA + LB)>();
+                phase_end();  // the step is in LDS, and the one before is read
+                load_a(next_a);
+                load_b(next_b);
+                read(a, b);
+                multiply();
+                wait_reads();
+            };
+            for (int t = 0;;) {
+                turn(s_a0, s_b0, s_a3, s_b3);
+                if (++t >= steps) break;
+                turn(s_a1, s_b1, s_a0, s_b0);
+                if (++t >= steps) break;
+                turn(s_a2, s_b2, s_a1, s_b1);
+                if (++t >= steps) break;
+                turn(s_a3, s_b3, s_a2, s_b2);
+                if (++t >= steps) break;
+            }
+            wait_loads<0>();
         }
     }
     const int n_wave = n0 + wn * (Epi::kPair ? 32 : 64);
@@ -225,24 +350,41 @@ void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
                            dim3(64 * WM * WN), 0, s, g, epi);
 }
 
-// Large tiles where they fill the CUs once, else small ones.
-inline bool large_tiles(int64_t M, int64_t N, int64_t batches) {
-    return ((M + 255) / 256) * ((N + 255) / 256) * batches >= 224;
+// Tiles, and parts along k of a product whose tiles would leave CUs idle (the
+// parts are joined by k_gemm_join): what takes the least by the times that a
+// round of 256 tiles takes, in us: 1.5 a step and 8 before and after them for
+// large tiles, 0.6 and 4 for small ones, and the join at 4 TB/s.  (M x N and
+// `steps` of all products, per batch.)  4,136 x 1,001 of 516 steps: 3 parts of
+// large tiles, 0.25 ms, against 0.65 ms for small tiles in one.
+struct GemmShape {
+    bool large;
+    int32_t splits;
+};
+inline GemmShape gemm_shape(int64_t M, int64_t N, int64_t steps, int64_t batches, bool may_split) {
+    GemmShape best{false, 1};
+    double least = 1e30;
+    for (int large = 0; large < 2; ++large) {
+        const int64_t tile = large ? 256 : 128;
+        const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile) * batches;
+        for (int64_t s = 1; s <= 32 && (s == 1 || (may_split && s * 4 <= steps)); ++s) {
+            const double rounds = (double)((tiles * s + 255) / 256), part = (double)((steps + s - 1) / s);
+            double us = rounds * (large ? 1.5 * part + 8.0 : 0.6 * part + 4.0);
+            if (s > 1) us += 4.0 + (double)(s + 1) * batches * M * N * 4.0 / 4e6;
+            if (us < least) least = us, best = GemmShape{large != 0, (int32_t)s};
+        }
+    }
+    return best;
 }
 template <class Epi>
-void launch_gemm(const GemmArgs &g, const Epi &epi, hipStream_t s) {
-    if (large_tiles(g.M, (int64_t)g.N * (Epi::kPair ? 2 : 1), (int64_t)g.batches * g.splits))
+void launch_gemm(GemmArgs g, const Epi &epi, hipStream_t s) {
+    g.splits = 1;
+    if (gemm_shape(g.M, (int64_t)g.N * (Epi::kPair ? 2 : 1), (int64_t)g.K / kGemmK * g.nprod,
+                   g.batches, false)
+            .large)
         launch_gemm_tile<256, 256, 2, 4>(g, epi, s);
-    else launch_gemm_tile<128, 128, 2, 2>(g, epi, s);
+    else launch_gemm_tile<128, 128, 4, 2>(g, epi, s);
 }
 
-// Parts along k of a product whose tiles would leave most CUs without one:
-// each of at least 8 steps, joined by k_gemm_join.
-inline int32_t gemm_splits(int64_t M, int64_t N, int64_t steps, int64_t batches) {
-    const int64_t tiles = ((M + 127) / 128) * ((N + 127) / 128) * batches;
-    if (tiles >= 224 || steps < 16) return 1;
-    return (int32_t)std::max<int64_t>(1, std::min((512 + tiles - 1) / tiles, steps / 8));
-}
 inline int64_t split_bytes(int64_t M, int64_t N, int64_t splits, int64_t batches) {
     return splits > 1 ? splits * batches * M * ((N + 3) & ~int64_t(3)) * 4 : 0;
 }
@@ -347,7 +489,7 @@ static __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, MatrixOut 
     const int64_t row = i / per_row;
     const int32_t n = (int32_t)(i - row * per_row) * 4;
     const int32_t batch = (int32_t)(row / g.M), m = (int32_t)(row - (int64_t)batch * g.M);
-    if (g.live && m / 128 * 128 + g.m_lo >= *g.live) return;  // (that tile was left out)
+    if (g.live && m + g.m_lo >= *g.live) return;
     if (out.skip_empty && g.ranges) {
         const int2 r = g.ranges[batch];
         if (min(r.y, g.k_hi) <= max(r.x, g.k_lo)) return;
@@ -361,15 +503,14 @@ static __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, MatrixOut 
     out.put(g, batch, m, n, v);
 }
 
-// A product into a plain matrix, split along k as gemm_splits says; parts: work
-// memory of split_bytes.
-inline void launch_product(GemmArgs g, MatrixOut out, float *parts, hipStream_t s) {
-    if (g.splits == 1) {
-        launch_gemm(g, out, s);
-        return;
-    }
-    out.parts = parts;
-    launch_gemm_tile<128, 128, 2, 2>(g, out, s);
+// A product into a plain matrix; parts: work memory of split_bytes.
+inline void launch_product(GemmArgs g, MatrixOut out, GemmShape shape, float *parts,
+                           hipStream_t s) {
+    g.splits = shape.splits;
+    if (g.splits > 1) out.parts = parts;
+    if (shape.large) launch_gemm_tile<256, 256, 2, 4>(g, out, s);
+    else launch_gemm_tile<128, 128, 4, 2>(g, out, s);
+    if (g.splits == 1) return;
     const int64_t quads = (int64_t)g.batches * g.M * ((g.N + 3) / 4);
     hipLaunchKernelGGL(k_gemm_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, out,
                        quads);
