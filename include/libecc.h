@@ -844,8 +844,8 @@ ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64
  * below about 2^36, else ECC_ERR_RANGE.  d_work: ecc_cross_entropy_work_size(a, 1)
  * bytes, or (a, 0) for the loss alone (-1 for a description that the call
  * refuses; the size depends on where the arrays lie). */
-#define ECC_CROSS_ENTROPY_MAX_VOCAB (1 << 22)
-#define ECC_CROSS_ENTROPY_MAX_DIM (1 << 16)
+#define ECC_CROSS_ENTROPY_MAX_VOCAB 4194304
+#define ECC_CROSS_ENTROPY_MAX_DIM 65536
 typedef struct {
     int64_t n, V, D;
     int32_t P;
@@ -883,8 +883,8 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
  * the call refuses; the size depends on where the arrays lie). */
 #define ECC_ACT_SILU 0
 #define ECC_ACT_GELU 1
-#define ECC_FFN_MAX_DIM (1 << 20)
-#define ECC_FFN_MAX_ROWS (1 << 22)
+#define ECC_FFN_MAX_DIM 1048576
+#define ECC_FFN_MAX_ROWS 4194304
 typedef struct {
     int64_t n, D, F;
     int32_t P;

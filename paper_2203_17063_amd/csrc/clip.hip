@@ -217,9 +217,10 @@ __global__ __launch_bounds__(kThreads) void k_clip_many(ClipArgs a) {
     __shared__ double s[kThreads / 64];
     clip_chunk(a.table, a, s);
 }
-__global__ __launch_bounds__(kAddThreads) void k_norm_only(ClipArgs a) {
-    __shared__ double s[kAddThreads / 64];
-    const double norm = norm_of<kAddThreads>(a, blockIdx.x, s);
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_only(ClipArgs a) {
+    __shared__ double s[THREADS / 64];
+    const double norm = norm_of<THREADS>(a, blockIdx.x, s);
     if (threadIdx.x == 0) a.norms[blockIdx.x] = norm;
 }
 
@@ -413,8 +414,11 @@ ecc_status_t run(int32_t P, int32_t count, const ecc_tensor_t *t, const Cut &cut
         if (many) hipLaunchKernelGGL(k_norm_many, grid, block, 0, s, a);
         else hipLaunchKernelGGL(k_norm_few, grid, block, 0, s, some, a);
     }
-    if (!clip || cut.chunks == 0 || cut.chunks > kFewChunks)
-        hipLaunchKernelGGL(k_norm_only, dim3((unsigned)P), dim3(kAddThreads), 0, s, a);
+    // (few sums in the order in which the scaling adds them: the same norms)
+    if (cut.chunks > kFewChunks)
+        hipLaunchKernelGGL(k_norm_only<kAddThreads>, dim3((unsigned)P), dim3(kAddThreads), 0, s, a);
+    else if (!clip || cut.chunks == 0)
+        hipLaunchKernelGGL(k_norm_only<kThreads>, dim3((unsigned)P), block, 0, s, a);
     if (!clip || cut.chunks == 0) {
     } else if (many) hipLaunchKernelGGL(k_clip_many, grid, block, 0, s, a);
     else hipLaunchKernelGGL(k_clip_few, grid, block, 0, s, some, a);
