@@ -7,12 +7,17 @@
 //   1. z as fp32, with every row's maximum and sum of exponentials per 64
 //      columns formed from the sums in registers (alone where only the loss is
 //      wanted: z is not stored then);
-//   2. a wave per row joins them: loss, maximum, weight / sum;
-//   3. dz as bf16 (the pieces of gemm.h where a gradient is fp32), in both
-//      orders;
+//   2. a wave per row joins them: loss, maximum, 1 / sum (vocabularies of up to
+//      32 times 64 join them in the next launch);
+//   3. softmax - [label] as bf16 (as the pieces of gemm.h where a gradient is
+//      fp32), in both orders;
 //   4. dh, scattered to the rows' places, and dE, added up over pieces in fp32.
-// dz is rounded to bf16 for gradients that are bf16 themselves: one rounding of
-// the terms beside the one of the result.
+// What is rounded to bf16 for gradients that are bf16 themselves is softmax -
+// [label], one rounding of the terms beside the one of the result: weights and
+// the scale are factors of dh's rows afterwards.  For dE they are rounded with
+// the term, unless a worker's weights are all alike and one factor does: a
+// label's term is near the weight in most rows of a model that learns, and
+// would be off by one and the same half step everywhere (0.0037 of dE).
 #include "gemm.h"
 #include "pack.h"
 
@@ -26,9 +31,12 @@ struct Rows {
     int32_t *map;      // packed row -> position, -1: none
     int32_t *label;
     float *weight;
+    float *factor;     // weight * scale: of dh's row
+    float *inside;     // of its terms in dE
     int32_t *live;     // packed rows that hold anything (a multiple of 64)
     int2 *ranges;      // of every worker
     int32_t *counts;   // rows per worker, rounded up
+    float *outside;    // of every worker's dE
 };
 
 struct Positions {
@@ -74,8 +82,13 @@ __global__ __launch_bounds__(kMapThreads) void k_ce_count(Positions q, Rows rows
 // Every worker's rows in order, each worker's from a multiple of 64 on: a
 // workgroup per worker, which first adds up the counts of those before it.
 __global__ __launch_bounds__(kMapThreads) void k_ce_map(Positions q, Rows rows, int32_t P,
-                                                        int64_t capacity, float *loss) {
+                                                        int64_t capacity, float scale,
+                                                        float *loss) {
     __shared__ int s_sum[kMapThreads / 64 + 1];
+    __shared__ float s_least[kMapThreads / 64], s_most[kMapThreads / 64];
+    __shared__ int s_odd;   // a weight that is NaN
+    if (threadIdx.x == 0) s_odd = 0;
+    float least = __builtin_inff(), most = -__builtin_inff();
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int32_t p = blockIdx.x;
     int before = 0;
@@ -112,7 +125,12 @@ __global__ __launch_bounds__(kMapThreads) void k_ce_map(Positions q, Rows rows, 
                 const int64_t from = base + i + e;
                 rows.map[row] = (int32_t)from;
                 rows.label[row] = q.labels[from];
-                rows.weight[row] = q.weight ? q.weight[from] : 1.0f;
+                const float w = q.weight ? q.weight[from] : 1.0f;
+                rows.weight[row] = w;
+                rows.factor[row] = w * scale;
+                least = fminf(least, w);
+                most = fmaxf(most, w);
+                if (w != w) s_odd = 1;
                 ++row;
             }
     }
@@ -123,18 +141,44 @@ __global__ __launch_bounds__(kMapThreads) void k_ce_map(Positions q, Rows rows, 
     for (int64_t r = at + threadIdx.x; r < (last ? capacity : end); r += kMapThreads) {
         rows.map[r] = -1;
         rows.label[r] = -1;
-        rows.weight[r] = 0.0f;
+        rows.weight[r] = rows.factor[r] = 0.0f;
     }
+    // weights that are all alike become a factor of the whole sum
+    for (int d = 32; d; d >>= 1) {
+        least = fminf(least, __shfl_xor(least, d, 64));
+        most = fmaxf(most, __shfl_xor(most, d, 64));
+    }
+    if (lane == 0) s_least[wave] = least, s_most[wave] = most;
+    __syncthreads();
+    for (int w = 0; w < kMapThreads / 64; ++w) {
+        least = fminf(least, s_least[w]);
+        most = fmaxf(most, s_most[w]);
+    }
+    const bool alike = least == most && !s_odd;
+    if (threadIdx.x == 0) rows.outside[p] = alike ? least * scale : 1.0f;
+    for (int r = before + threadIdx.x; r < end; r += kMapThreads)
+        rows.inside[r] = alike || r >= at ? 1.0f : rows.factor[r];
 }
 
-// Zeros for the rows of dh that do not count: a wave per position.
-template <typename T>
-__global__ __launch_bounds__(256) void k_ce_dead(Positions q, int64_t first, int64_t N, int64_t D,
-                                                 T *dh, int64_t ld) {
-    const int64_t i = first + blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
-    if (i >= N || q.counts(i)) return;
-    for (int64_t d = threadIdx.x & 63; d < D; d += 64) store_elem<float>(dh + i * ld + d, 0.0f);
-}
+// Zeros for the rows of dh that do not count: positions first .. + count - 1,
+// a wave's.
+struct Unread {
+    Positions q;
+    int64_t N, D;
+    void *dh;        // NULL: none
+    int64_t ld;
+    int32_t type;
+    __device__ __forceinline__ void zero(int64_t first, int count) const {
+        for (int64_t i = first; i < min(N, first + count); ++i) {
+            if (q.counts(i)) continue;
+            for (int64_t d = threadIdx.x & 63; d < D; d += 64) {
+                if (type == ECC_F32) ((float *)dh)[i * ld + d] = 0.0f;
+                else ((bf16_t *)dh)[i * ld + d].bits = 0;
+            }
+        }
+    }
+};
+constexpr int kUnread = 16;  // positions of a wave
 
 // Logits and what the softmax needs of them, per row and 64 columns.
 struct LogitsOut {
@@ -186,82 +230,125 @@ struct LogitsOut {
 };
 
 struct RowTerms {
-    float *most, *soft, *hard;  // dz = exp(z - most) soft - [label] hard
+    float *most, *soft;  // softmax = exp(z - most) soft
 };
 
-// A wave per packed row: the loss, and the terms of its gradient.
-__global__ __launch_bounds__(256) void k_ce_rows(int32_t first, int32_t M, const int32_t *live,
-                                                 const float2 *stats, int32_t tiles,
-                                                 const float *picked, Rows rows, float scale,
-                                                 float *loss, RowTerms out) {
-    const int32_t m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (m >= M || first + m >= *live) return;
-    const int32_t to = rows.map[first + m];
-    float most = 0.0f, soft = 0.0f, hard = 0.0f;
-    if (to >= 0) {
-        const float2 *s = stats + (int64_t)m * tiles;
-        float top = -__builtin_inff();
-        for (int32_t i = lane; i < tiles; i += 64) top = fmaxf(top, s[i].x);
-        top = wave_all(top, OpMax());
-        const float from = top == -__builtin_inff() ? 0.0f : top;
-        float sum = 0.0f;
-        for (int32_t i = lane; i < tiles; i += 64) {
-            const float2 v = s[i];
-            // (a tile of NaN has a sum of NaN, and so has the row)
-            sum += v.y * (v.x == -__builtin_inff() ? 1.0f : expf(v.x - from));
-        }
-        sum = wave_all(sum, OpSum());
-        const float w = rows.weight[first + m];
-        most = from;
-        hard = w * scale;
-        soft = hard / sum;
-        if (lane == 0) loss[to] = w * ((from - picked[m]) + logf(sum));
+// A row's maximum and sum from its tiles', by `lanes` neighbouring lanes.
+__device__ __forceinline__ void join_tiles(const float2 *s, int32_t tiles, int lane, int lanes,
+                                           float &most, float &sum) {
+    most = -__builtin_inff();
+    for (int32_t i = lane; i < tiles; i += lanes) most = fmaxf(most, s[i].x);
+    for (int d = lanes / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    if (most == -__builtin_inff()) most = 0.0f;
+    sum = 0.0f;
+    for (int32_t i = lane; i < tiles; i += lanes) {
+        const float2 v = s[i];
+        // (a tile of NaN has a sum of NaN, and so has the row)
+        sum += v.y * (v.x == -__builtin_inff() ? 1.0f : expf(v.x - most));
     }
-    if (out.most && lane == 0) {
-        out.most[m] = most;
-        out.soft[m] = soft;
-        out.hard[m] = hard;
+    for (int d = lanes / 2; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+}
+
+struct RowArgs {
+    int32_t first, M, tiles;
+    const float2 *stats;
+    const float *picked;
+    Rows rows;
+    float *loss;
+    RowTerms out;
+    Unread unread;
+};
+
+// A wave per packed row: the loss, and the terms of its gradient.  Then waves
+// for the positions that do not count.
+__global__ __launch_bounds__(256) void k_ce_rows(RowArgs a) {
+    const int64_t wave = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (wave >= a.M) {
+        a.unread.zero((wave - a.M) * kUnread, kUnread);
+        return;
+    }
+    const int32_t m = (int32_t)wave;
+    if (a.first + m >= *a.rows.live) return;
+    const int32_t to = a.rows.map[a.first + m];
+    if (to < 0) return;
+    float most, sum;
+    join_tiles(a.stats + (int64_t)m * a.tiles, a.tiles, lane, 64, most, sum);
+    if (lane == 0) {
+        a.loss[to] = a.rows.weight[a.first + m] * ((most - a.picked[m]) + logf(sum));
+        if (a.out.most) {
+            a.out.most[m] = most;
+            a.out.soft[m] = 1.0f / sum;
+        }
     }
 }
 
 struct DzArgs {
     const float *z;
     int64_t ld;               // of z and of dz, a multiple of 64
-    int32_t V, first;
-    const int32_t *live, *label;
-    RowTerms row;
+    int32_t V;
+    RowArgs r;
     bf16_t *dz, *dzt;
     int64_t plane, plane_t, ld_t;
     int32_t pieces, pieces_t;
-    int32_t col_blocks;
+    int32_t col_blocks, blocks;
 };
+constexpr int32_t kFewTiles = 32;
 
-// dz in both orders, blocks of 64 x 64.  Bound by memory: 4 bytes read and 2
-// written for each order and piece.
+// softmax - [label] in both orders, blocks of 64 x 64.  Bound by memory: 4 bytes
+// read and 2 written for each order and piece.  FEW: the blocks join the tiles
+// of their rows by themselves, and zero the positions that do not count.
+template <bool FEW>
 __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
     __shared__ PackTile s;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.col_blocks) * kTile;
-    const int64_t col0 = (int64_t)(blockIdx.x % a.col_blocks) * kTile;
-    if (row0 + a.first >= *a.live) return;
+    __shared__ float s_most[kTile], s_soft[kTile];
+    const RowArgs &q = a.r;
+    if (FEW && (int32_t)blockIdx.x >= a.blocks) {
+        q.unread.zero((((int64_t)blockIdx.x - a.blocks) * 4 + (threadIdx.x >> 6)) * kUnread,
+                      kUnread);
+        return;
+    }
+    const int32_t row0 = (int32_t)(blockIdx.x / a.col_blocks) * kTile;
+    const int32_t col0 = (int32_t)(blockIdx.x % a.col_blocks) * kTile;
+    if (row0 + q.first >= *q.rows.live) return;
     const int c8 = (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
-    float mine[2][8];
+    Raw<float, 8> x[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+        x[p].load(a.z + (int64_t)(row0 + p * 32 + r) * a.ld + col0 + c8);
+    if constexpr (FEW) {
+        const int i = threadIdx.x >> 2;
+        const int32_t to = q.rows.map[q.first + row0 + i];
+        float most = 0.0f, sum = 1.0f;
+        if (to >= 0) join_tiles(q.stats + (int64_t)(row0 + i) * q.tiles, q.tiles, threadIdx.x & 3, 4,
+                                most, sum);
+        if ((threadIdx.x & 3) == 0) {
+            s_most[i] = most;
+            s_soft[i] = 1.0f / sum;
+            if (to >= 0 && col0 == 0)
+                q.loss[to] = q.rows.weight[q.first + row0 + i] *
+                             ((most - q.picked[row0 + i]) + logf(sum));
+        }
+        __syncthreads();
+    }
+    float mine[2][8], by[2];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const int64_t m = row0 + p * 32 + r;
-        Raw<float, 8> x;
-        x.load(a.z + m * a.ld + col0 + c8);
-        const int32_t y = a.label[m];
-        const float most = a.row.most[m], soft = a.row.soft[m], hard = a.row.hard[m];
+        const int32_t m = row0 + p * 32 + r;
+        const int32_t y = q.rows.label[q.first + m];
+        const float most = FEW ? s_most[p * 32 + r] : q.out.most[m];
+        const float soft = FEW ? s_soft[p * 32 + r] : q.out.soft[m];
+        by[p] = q.rows.inside[q.first + m];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int32_t j = (int32_t)col0 + c8 + e;
-            float v = expf(x.get<float>(e) - most) * soft;
-            if (j == y) v -= hard;
+            const int32_t j = col0 + c8 + e;
+            float v = expf(x[p].get<float>(e) - most) * soft;
+            if (j == y) v -= 1.0f;
             mine[p][e] = y >= 0 && j < a.V ? v : 0.0f;
         }
     }
-    write_block(s, mine, row0, col0, a.V, a.dz, a.ld, a.plane, a.pieces, a.dzt, a.ld_t, a.plane_t,
-                a.pieces_t);
+    write_block(s, mine, by, row0, col0, a.V, a.dz, a.ld, a.plane, a.pieces, a.dzt, a.ld_t,
+                a.plane_t, a.pieces_t);
 }
 
 // ---------------------------------------------------------------------------
@@ -277,8 +364,8 @@ struct Plan {
     bool pack_table;
     GemmShape shape_h, shape_e;
     // offsets into the work buffer
-    int64_t map, label, weight, live, ranges, counts, table, table_t, h, h_t, z, dz, dzt, stats,
-        picked, terms, sums, parts, bytes;
+    int64_t map, label, weight, factor, inside, live, ranges, counts, outside, table, table_t, h, h_t,
+        z, dz, dzt, stats, picked, terms, sums, parts[2], bytes;
 };
 
 Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
@@ -312,9 +399,12 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.map = take(4 * p.rows);
     p.label = take(4 * p.rows);
     p.weight = take(4 * p.rows);
+    p.factor = take(4 * p.rows);
+    p.inside = take(4 * p.rows);
     p.live = take(4);
     p.ranges = take(8 * (int64_t)a->P);
     p.counts = take(4 * (int64_t)a->P);
+    p.outside = take(4 * (int64_t)a->P);
     p.table = take(p.pack_table ? p.np * 2 * p.Vp * p.Dp : 0);
     p.h = take(p.np * 2 * p.R * p.Dp);
     p.stats = take(8 * p.R * p.tiles);
@@ -325,15 +415,15 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
         p.z = take(4 * p.R * p.Vp);
         p.dz = take(2 * p.pz * p.R * p.Vp);
         p.dzt = take(2 * p.pzt * a->V * p.R);
-        p.terms = take(12 * p.R);
+        p.terms = take(8 * p.R);
         p.sums = take(p.pieces_of_rows > 1 && a->grad_type != ECC_F32 ? 4 * a->P * a->V * a->D : 0);
         p.shape_h = gemm_shape(p.R, a->D, p.Vp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
         // (a worker's rows in a piece)
         p.shape_e = gemm_shape(a->V, a->D,
                                std::min(p.n_pad, p.R) / kGemmK * (p.np == 3 ? 6 : p.pzt), a->P,
                                true);
-        p.parts = take(std::max(split_bytes(p.R, a->D, p.shape_h.splits, 1),
-                                split_bytes(a->V, a->D, p.shape_e.splits, a->P)));
+        p.parts[0] = take(split_bytes(p.R, a->D, p.shape_h.splits, 1));
+        p.parts[1] = take(split_bytes(a->V, a->D, p.shape_e.splits, a->P));
     }
     p.bytes = std::max<int64_t>(at, 16);
     return p;
@@ -361,14 +451,6 @@ ecc_status_t check(const ecc_cross_entropy_t *a) {
                 (uintptr_t)a->d_labels % 4 == 0 && (uintptr_t)a->d_weight % 4 == 0,
             "an array is not aligned");
     return ECC_OK;
-}
-
-template <typename T>
-void zero_dead(const Positions &q, int64_t N, int64_t D, void *dh, int64_t ld, hipStream_t s) {
-    const int64_t most = int64_t(1) << 25;
-    for (int64_t i = 0; i < N; i += most)
-        hipLaunchKernelGGL(k_ce_dead<T>, dim3((unsigned)((std::min(most, N - i) + 3) / 4)),
-                           dim3(256), 0, s, q, i, std::min(N, i + most), D, (T *)dh, ld);
 }
 
 // The gradient of a table without rows to learn from.
@@ -451,16 +533,14 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
     }
     char *w = (char *)d_work;
     const Rows rows{(int32_t *)(w + p.map), (int32_t *)(w + p.label), (float *)(w + p.weight),
-                    (int32_t *)(w + p.live), (int2 *)(w + p.ranges), (int32_t *)(w + p.counts)};
+                    (float *)(w + p.factor), (float *)(w + p.inside), (int32_t *)(w + p.live),
+                    (int2 *)(w + p.ranges), (int32_t *)(w + p.counts), (float *)(w + p.outside)};
     const Positions q{a->d_labels, a->d_weight, a->n, (int32_t)V};
     if (P > 1)
         hipLaunchKernelGGL(k_ce_count, dim3((unsigned)P), dim3(kMapThreads), 0, s, q, rows);
     hipLaunchKernelGGL(k_ce_map, dim3((unsigned)P), dim3(kMapThreads), 0, s, q, rows, P, p.rows,
-                       (float *)d_loss);
-    if (d_dh) {
-        if (a->type == ECC_F32) zero_dead<float>(q, N, D, d_dh, ld_dh, s);
-        else zero_dead<bf16_t>(q, N, D, d_dh, ld_dh, s);
-    }
+                       (float)a->scale, (float *)d_loss);
+    Packing packing;
     if (p.pack_table || d_dh) {
         PackArgs k{};
         k.src = a->d_table;
@@ -475,7 +555,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         k.cols_out = d_dh ? (bf16_t *)(w + p.table_t) : nullptr;
         k.ld_cols = p.Vp;
         k.plane_cols = D * p.Vp;
-        launch_pack(k, a->type, s);
+        packing.add(k);
     }
     for (int64_t r0 = 0; r0 < p.rows; r0 += p.R) {
         const int64_t R = std::min(p.R, p.rows - r0);
@@ -494,7 +574,9 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         k.cols_out = d_dtable ? (bf16_t *)(w + p.h_t) : nullptr;
         k.ld_cols = R;
         k.plane_cols = D * R;
-        launch_pack(k, a->type, s);
+        packing.add(k);
+        packing.launch(a->type, s);
+        packing = Packing{};
         GemmArgs g{};
         g.a = GemmOperand{k.rows, p.Dp, k.plane_rows};
         g.b = p.pack_table ? GemmOperand{(bf16_t *)(w + p.table), p.Dp, p.Vp * p.Dp}
@@ -510,21 +592,30 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
                                (float2 *)(w + p.stats), p.tiles, rows.label + r0,
                                (float *)(w + p.picked)};
         launch_gemm(g, logits, s);
-        float *terms = gradient ? (float *)(w + p.terms) : nullptr;
-        const RowTerms row{terms, gradient ? terms + R : nullptr,
-                           gradient ? terms + 2 * R : nullptr};
-        hipLaunchKernelGGL(k_ce_rows, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, s, (int32_t)r0,
-                           (int32_t)R, rows.live, logits.stats, p.tiles, logits.picked, rows,
-                           (float)a->scale, (float *)d_loss, row);
+        RowArgs row{};
+        row.first = (int32_t)r0;
+        row.M = (int32_t)R;
+        row.tiles = p.tiles;
+        row.stats = logits.stats;
+        row.picked = logits.picked;
+        row.rows = rows;
+        row.loss = (float *)d_loss;
+        // (positions that do not count: with the first piece)
+        row.unread = Unread{q, d_dh && r0 == 0 ? N : 0, D, d_dh, ld_dh, a->type};
+        const int64_t unread = (row.unread.N + kUnread - 1) / kUnread;
+        const bool few = gradient && p.tiles <= kFewTiles;
+        if (!few) {
+            float *terms = gradient ? (float *)(w + p.terms) : nullptr;
+            row.out = RowTerms{terms, gradient ? terms + R : nullptr};
+            hipLaunchKernelGGL(k_ce_rows, dim3((unsigned)((R + unread + 3) / 4)), dim3(256), 0, s,
+                               row);
+        }
         if (!gradient) continue;
         DzArgs z{};
         z.z = logits.z;
         z.ld = p.Vp;
         z.V = (int32_t)V;
-        z.first = (int32_t)r0;
-        z.live = rows.live;
-        z.label = rows.label + r0;
-        z.row = row;
+        z.r = row;
         z.dz = d_dh ? (bf16_t *)(w + p.dz) : nullptr;
         z.dzt = d_dtable ? (bf16_t *)(w + p.dzt) : nullptr;
         z.plane = R * p.Vp;
@@ -533,7 +624,15 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         z.pieces = p.pz;
         z.pieces_t = p.pzt;
         z.col_blocks = p.tiles;
-        hipLaunchKernelGGL(k_ce_dz, dim3((unsigned)(R / kTile * p.tiles)), dim3(256), 0, s, z);
+        z.blocks = (int32_t)(R / kTile * p.tiles);
+        if (few)
+            hipLaunchKernelGGL(k_ce_dz<true>, dim3((unsigned)(z.blocks + (unread + 3) / 4)),
+                               dim3(256), 0, s, z);
+        else hipLaunchKernelGGL(k_ce_dz<false>, dim3((unsigned)z.blocks), dim3(256), 0, s, z);
+        Product products[2];
+        GemmShape shapes[2];
+        float *parts[2];
+        int count = 0;
         if (d_dh) {
             GemmArgs d{};
             d.a = GemmOperand{z.dz, p.Vp, z.plane};
@@ -550,7 +649,10 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             out.ld = ld_dh;
             out.type = a->type;
             out.row_map = rows.map + r0;
-            launch_product(d, out, p.shape_h, (float *)(w + p.parts), s);
+            out.row_scale = rows.factor + r0;
+            products[count] = Product{d, out};
+            shapes[count] = p.shape_h;
+            parts[count++] = (float *)(w + p.parts[0]);
         }
         if (d_dtable) {
             const bool first = r0 == 0, last = r0 + R >= p.rows;
@@ -569,6 +671,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             out.ld = ld_dtable;
             out.batch_stride = worker_stride;
             out.type = a->grad_type;
+            out.scale = rows.outside;
             if (a->grad_type == ECC_F32 || p.pieces_of_rows == 1) {
                 out.add = accumulate || !first;
                 out.skip_empty = out.add;
@@ -578,8 +681,11 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
                 out.add = last && accumulate;
                 out.skip_empty = !first && !last;
             }
-            launch_product(d, out, p.shape_e, (float *)(w + p.parts), s);
+            products[count] = Product{d, out};
+            shapes[count] = p.shape_e;
+            parts[count++] = (float *)(w + p.parts[1]);
         }
+        launch_products(products, count, shapes, parts, s);
     }
     ECC_LAUNCH_CHECK();
     return ECC_OK;

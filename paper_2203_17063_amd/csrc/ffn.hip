@@ -103,7 +103,7 @@ struct Plan {
     int np, pd;                   // pieces of the operands, of dg and du
     bool pack_x, pack_gate, pack_up;
     GemmShape shape_x, shape_w;
-    int64_t x, gate, up, x_t, w_t, d, d_t, parts, bytes;
+    int64_t x, gate, up, x_t, w_t, d, d_t, parts[2], bytes;
 };
 
 Plan make_plan(const ecc_ffn_t *a, bool gradient) {
@@ -136,8 +136,8 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
         p.d_t = take(p.pd * 2 * 2 * a->F * p.rows);
         p.shape_x = gemm_shape(p.N, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
         p.shape_w = gemm_shape(2 * a->F, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pd), a->P, true);
-        p.parts = take(std::max(split_bytes(p.N, a->D, p.shape_x.splits, 1),
-                                split_bytes(2 * a->F, a->D, p.shape_w.splits, a->P)));
+        p.parts[0] = take(split_bytes(p.N, a->D, p.shape_x.splits, 1));
+        p.parts[1] = take(split_bytes(2 * a->F, a->D, p.shape_w.splits, a->P));
     }
     p.bytes = std::max<int64_t>(at, 16);
     return p;
@@ -179,6 +179,7 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
     g.a = GemmOperand{(const bf16_t *)a->d_x, a->ld_x, 0};
     g.b = GemmOperand{(const bf16_t *)a->d_w_gate, a->ld_gate, 0};
     g.b2 = (const bf16_t *)a->d_w_up;
+    Packing packing;
     auto pack = [&](const void *src, int64_t ld, int64_t rows, int64_t to) {
         k.src = src;
         k.ld = ld;
@@ -186,7 +187,7 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
         k.rows_packed = k.n_pad = pad64(rows);
         k.rows = (bf16_t *)(w + to);
         k.plane_rows = k.rows_packed * p.Dp;
-        launch_pack(k, a->type, s);
+        packing.add(k);
         return GemmOperand{k.rows, p.Dp, k.plane_rows};
     };
     if (p.pack_x) g.a = pack(a->d_x, a->ld_x, p.N, p.x);
@@ -194,6 +195,7 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
         g.b = pack(a->d_w_gate, a->ld_gate, a->F, p.gate);
         g.b2 = pack(a->d_w_up, a->ld_up, a->F, p.up).p;
     }
+    packing.launch(a->type, s);
     g.M = (int32_t)p.N;
     g.N = (int32_t)a->F;
     g.K = (int32_t)p.Dp;
@@ -334,9 +336,15 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
                                                            p.pd},
                     s);
     });
-    PackArgs k{};
+    // the other order of everything: [Wg | Wu] transposed, as long as [dg | du],
+    // x and [dg | du] with workers padded to multiples of 64 rows
+    Packing packing;
+    Product products[2];
+    GemmShape shapes[2];
+    float *parts[2];
+    int count = 0;
     if (d_dx) {
-        // [Wg | Wu] transposed, as long as [dg | du]
+        PackArgs k{};
         k.cols = D;
         k.pieces = p.np;
         k.n = k.total = F;
@@ -347,7 +355,7 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
             k.src = i ? a->d_w_up : a->d_w_gate;
             k.ld = i ? a->ld_up : a->ld_gate;
             k.cols_out = (bf16_t *)(w + p.w_t) + i * p.Fp;
-            launch_pack(k, a->type, s);
+            packing.add(k);
         }
         GemmArgs x{};
         x.a = GemmOperand{d, 2 * p.Fp, plane};
@@ -361,11 +369,12 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         to.out = d_dx;
         to.ld = ld_dx;
         to.type = a->type;
-        launch_product(x, to, p.shape_x, (float *)(w + p.parts), s);
+        products[count] = Product{x, to};
+        shapes[count] = p.shape_x;
+        parts[count++] = (float *)(w + p.parts[0]);
     }
     if (d_dw_gate) {
-        // x and [dg | du] transposed, workers padded to multiples of 64 rows
-        k = PackArgs{};
+        PackArgs k{};
         k.n = a->n;
         k.n_pad = p.n_pad;
         k.total = p.N;
@@ -376,17 +385,20 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         k.pieces = p.np;
         k.cols_out = (bf16_t *)(w + p.x_t);
         k.plane_cols = D * p.rows;
-        launch_pack(k, a->type, s);
+        packing.add(k);
         k.ld = 2 * p.Fp;
         k.cols = F;
         k.pieces = 1;
         const int64_t plane_t = 2 * F * p.rows;
-        for (int which = 0; which < p.pd; ++which)
+        for (int which = 0; which < p.pd; ++which) {
+            Packing gradients;
             for (int i = 0; i < 2; ++i) {
                 k.src = d + which * plane + i * p.Fp;
                 k.cols_out = (bf16_t *)(w + p.d_t) + which * plane_t + i * F * p.rows;
-                launch_pack(k, ECC_BF16, s);
+                gradients.add(k);
             }
+            gradients.launch(ECC_BF16, s);
+        }
         GemmArgs x{};
         x.a = GemmOperand{(bf16_t *)(w + p.d_t), p.rows, plane_t};
         x.b = GemmOperand{(bf16_t *)(w + p.x_t), p.rows, D * p.rows};
@@ -403,8 +415,12 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         to.batch_stride = worker_stride;
         to.type = a->grad_type;
         to.add = accumulate;
-        launch_product(x, to, p.shape_w, (float *)(w + p.parts), s);
+        products[count] = Product{x, to};
+        shapes[count] = p.shape_w;
+        parts[count++] = (float *)(w + p.parts[1]);
     }
+    packing.launch(a->type, s);
+    launch_products(products, count, shapes, parts, s);
     ECC_LAUNCH_CHECK();
     return ECC_OK;
 }

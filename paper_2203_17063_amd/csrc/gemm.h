@@ -140,7 +140,8 @@ __device__ __forceinline__ void phase_end() {
 }
 
 template <int BM, int BN, int WM, int WN, class Epi>
-__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int block,
+                                          int blocks) {
     constexpr int NW = WM * WN;
     constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
     constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // loads of 8 rows a wave
@@ -158,8 +159,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
     const int wm = wave / WN, wn = wave % WN;
 
     // the tile: blocks go round the XCDs, each takes a contiguous share
-    const int per = (int)((gridDim.x + 7) >> 3), more = (int)(gridDim.x - ((per - 1) << 3));
-    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int per = (blocks + 7) >> 3, more = blocks - ((per - 1) << 3);
+    const int xcd = block & 7, at = block >> 3;
     int t = xcd * per + at - max(0, xcd - more);  // (uniform: from scalars alone)
     const int tiles = g.tiles_m * g.tiles_n;
     const int part = t / tiles;
@@ -338,13 +339,22 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
     epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64}, g, acc);
 }
 
-// Launches tiles of BM x BN (of pairs: BN / 2 columns).
 template <int BM, int BN, int WM, int WN, class Epi>
-void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
+__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
+    gemm_tile<BM, BN, WM, WN>(g, epi, blockIdx.x, gridDim.x);
+}
+
+// Tiles of BM x BN (of pairs: BN / 2 columns): their number.
+template <int BM, int BN, class Epi>
+int64_t set_tiles(GemmArgs &g) {
     g.tiles_m = (g.M + BM - 1) / BM;
     const int cols = Epi::kPair ? BN / 2 : BN;
     g.tiles_n = (g.N + cols - 1) / cols;
-    const int64_t grid = (int64_t)g.tiles_m * g.tiles_n * g.batches * g.splits;
+    return (int64_t)g.tiles_m * g.tiles_n * g.batches * g.splits;
+}
+template <int BM, int BN, int WM, int WN, class Epi>
+void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
+    const int64_t grid = set_tiles<BM, BN, Epi>(g);
     if (grid > 0)
         hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, Epi>), dim3((unsigned)grid),
                            dim3(64 * WM * WN), 0, s, g, epi);
@@ -404,6 +414,8 @@ struct MatrixOut {
     int32_t add;              // to what out holds
     int32_t skip_empty;       // batches without a range along k are left alone
     const int32_t *row_map;   // out's row of each row; negative: none
+    const float *row_scale;   // the sums' factor, of each row
+    const float *scale;       // of each batch
     const float *sums;
     float *to_sums;           // fp32 sums in out's place
     float *parts;
@@ -416,6 +428,8 @@ struct MatrixOut {
             r = row_map[m];
             if (r < 0) return;
         }
+        if (row_scale) v *= row_scale[m];
+        if (scale) v *= scale[batch];
         const int w = min(4, g.N - n);
         if (sums || to_sums) {
             const int64_t at = ((int64_t)batch * g.M + m) * g.N + n;
@@ -481,10 +495,7 @@ struct MatrixOut {
 
 // Adds the parts of a split product in their order: one thread per four
 // columns of a row.
-static __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, MatrixOut out,
-                                                          int64_t quads) {
-    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-    if (i >= quads) return;
+__device__ __forceinline__ void join_parts(const GemmArgs &g, MatrixOut out, int64_t i) {
     const int32_t per_row = (g.N + 3) / 4;
     const int64_t row = i / per_row;
     const int32_t n = (int32_t)(i - row * per_row) * 4;
@@ -503,17 +514,59 @@ static __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs g, MatrixOut 
     out.put(g, batch, m, n, v);
 }
 
-// A product into a plain matrix; parts: work memory of split_bytes.
-inline void launch_product(GemmArgs g, MatrixOut out, GemmShape shape, float *parts,
-                           hipStream_t s) {
-    g.splits = shape.splits;
-    if (g.splits > 1) out.parts = parts;
-    if (shape.large) launch_gemm_tile<256, 256, 2, 4>(g, out, s);
-    else launch_gemm_tile<128, 128, 4, 2>(g, out, s);
-    if (g.splits == 1) return;
-    const int64_t quads = (int64_t)g.batches * g.M * ((g.N + 3) / 4);
-    hipLaunchKernelGGL(k_gemm_join, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, out,
-                       quads);
+// A product into a plain matrix, and two of them in one launch: of few tiles
+// each, that leave CUs to each other.
+struct Product {
+    GemmArgs g;
+    MatrixOut out;
+};
+struct TwoProducts {
+    Product p[2];
+    int64_t first[2];   // blocks, or quads to join, of the first; of both
+};
+static __global__ __launch_bounds__(512) void k_gemm_two(TwoProducts t) {
+    const int second = (int)blockIdx.x >= t.first[0];
+    const Product &p = t.p[second];
+    const int before = second ? (int)t.first[0] : 0;
+    gemm_tile<128, 128, 4, 2>(p.g, p.out, (int)blockIdx.x - before,
+                              (int)(second ? t.first[1] : t.first[0]) - before);
+}
+static __global__ __launch_bounds__(256) void k_gemm_join(TwoProducts t) {
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i < t.first[0]) join_parts(t.p[0].g, t.p[0].out, i);
+    else if (i < t.first[1]) join_parts(t.p[1].g, t.p[1].out, i - t.first[0]);
+}
+
+inline int64_t quads_to_join(const Product &p) {
+    return p.g.splits > 1 ? (int64_t)p.g.batches * p.g.M * ((p.g.N + 3) / 4) : 0;
+}
+
+// Up to two products (count) of the given shapes; parts: work memory of
+// split_bytes for each.
+inline void launch_products(Product (&p)[2], int count, const GemmShape (&shape)[2],
+                            float *const (&parts)[2], hipStream_t s) {
+    TwoProducts t{};
+    int64_t quads[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+        p[i].g.splits = shape[i].splits;
+        if (shape[i].splits > 1) p[i].out.parts = parts[i];
+        quads[i] = quads_to_join(p[i]);
+        t.p[i] = p[i];
+    }
+    if (count == 2 && !shape[0].large && !shape[1].large) {
+        t.first[0] = set_tiles<128, 128, MatrixOut>(t.p[0].g);
+        t.first[1] = t.first[0] + set_tiles<128, 128, MatrixOut>(t.p[1].g);
+        hipLaunchKernelGGL(k_gemm_two, dim3((unsigned)t.first[1]), dim3(512), 0, s, t);
+    } else {
+        for (int i = 0; i < count; ++i)
+            if (shape[i].large) launch_gemm_tile<256, 256, 2, 4>(p[i].g, p[i].out, s);
+            else launch_gemm_tile<128, 128, 4, 2>(p[i].g, p[i].out, s);
+    }
+    t.first[0] = quads[0];
+    t.first[1] = quads[0] + quads[1];
+    if (t.first[1] > 0)
+        hipLaunchKernelGGL(k_gemm_join, dim3((unsigned)((t.first[1] + 255) / 256)), dim3(256), 0, s,
+                           t);
 }
 
 }  // namespace ecc

@@ -66,8 +66,10 @@ struct PackTile {
 };
 
 // Writes the block's pieces: `mine[p]` are this thread's 8 columns c8 .. + 7 of
-// row p * 32 + r.  Loads and stores are of 16 bytes, eight to a row.
-__device__ __forceinline__ void write_block(PackTile &s, const float (&mine)[2][8], int64_t row0,
+// row p * 32 + r, times by[p] in the transposed order.  Loads and stores are of
+// 16 bytes, eight to a row.
+__device__ __forceinline__ void write_block(PackTile &s, const float (&mine)[2][8],
+                                            const float (&by)[2], int64_t row0,
                                             int64_t col0, int64_t cols, bf16_t *rows,
                                             int64_t ld_rows, int64_t plane_rows, int pieces_rows,
                                             bf16_t *cols_out, int64_t ld_cols, int64_t plane_cols,
@@ -86,7 +88,7 @@ __device__ __forceinline__ void write_block(PackTile &s, const float (&mine)[2][
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s.v[c8 + e][p * 32 + r] = mine[p][e];
+        for (int e = 0; e < 8; ++e) s.v[c8 + e][p * 32 + r] = mine[p][e] * by[p];
     __syncthreads();
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
@@ -103,16 +105,17 @@ __device__ __forceinline__ void write_block(PackTile &s, const float (&mine)[2][
     }
 }
 
-// One workgroup per block of 64 x 64, columns first.  Bound by memory: each
-// value is read once and written once per layout and piece.
+// A block of 64 x 64, columns first.  Bound by memory: each value is read once
+// and written once per layout and piece.
 template <typename T>
-static __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+__device__ __forceinline__ void pack_block(const PackArgs &a, int64_t block) {
     __shared__ PackTile s;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.col_blocks) * kTile;
-    const int64_t col0 = (int64_t)(blockIdx.x % a.col_blocks) * kTile;
+    const int64_t row0 = block / a.col_blocks * kTile;
+    const int64_t col0 = block % a.col_blocks * kTile;
     if (a.live && row0 + a.row0 >= *a.live) return;
     const int c8 = (threadIdx.x & 7) * 8, r = threadIdx.x >> 3;
     float mine[2][8];
+    const float by[2] = {1.0f, 1.0f};
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
         int64_t row = row0 + p * 32 + r;
@@ -128,18 +131,42 @@ static __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) mine[p][e] = x.template get<float>(e);
     }
-    write_block(s, mine, row0, col0, a.cols, a.rows, a.ld_rows, a.plane_rows, a.pieces, a.cols_out,
-                a.ld_cols, a.plane_cols, a.pieces);
+    write_block(s, mine, by, row0, col0, a.cols, a.rows, a.ld_rows, a.plane_rows, a.pieces,
+                a.cols_out, a.ld_cols, a.plane_cols, a.pieces);
 }
 
-inline void launch_pack(PackArgs a, int32_t type, hipStream_t s) {
-    a.col_blocks = (int32_t)((a.cols + kTile - 1) / kTile);
-    const int64_t grid = a.rows_packed / kTile * a.col_blocks;
-    if (grid <= 0) return;
-    if (type == ECC_F32)
-        hipLaunchKernelGGL(k_pack<float>, dim3((unsigned)grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(k_pack<bf16_t>, dim3((unsigned)grid), dim3(256), 0, s, a);
+// Up to four matrices in one launch, one after another.
+struct PackList {
+    PackArgs a[4];
+    int32_t count;
+    int32_t first[4];   // their first blocks
+};
+
+template <typename T>
+static __global__ __launch_bounds__(256) void k_pack(PackList l) {
+    int i = 0;
+    for (int k = 1; k < l.count; ++k)
+        if ((int32_t)blockIdx.x >= l.first[k]) i = k;
+    pack_block<T>(l.a[i], (int32_t)blockIdx.x - l.first[i]);
 }
+
+// Matrices of one type to pack.
+struct Packing {
+    PackList l{};
+    int64_t blocks = 0;
+    void add(PackArgs a) {
+        a.col_blocks = (int32_t)((a.cols + kTile - 1) / kTile);
+        l.first[l.count] = (int32_t)blocks;
+        l.a[l.count++] = a;
+        blocks += a.rows_packed / kTile * a.col_blocks;
+    }
+    void launch(int32_t type, hipStream_t s) {
+        if (blocks == 0) return;
+        if (type == ECC_F32)
+            hipLaunchKernelGGL(k_pack<float>, dim3((unsigned)blocks), dim3(256), 0, s, l);
+        else hipLaunchKernelGGL(k_pack<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, s, l);
+    }
+};
 
 // Can a product take a bf16 matrix as it lies?
 inline bool as_it_lies(const void *p, int64_t ld, int64_t cols, int32_t type) {
