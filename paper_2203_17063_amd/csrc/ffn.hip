@@ -98,6 +98,151 @@ struct FfnGradOut {
     }
 };
 
+// ---------------------------------------------------------------------------
+// few rows (single tokens)
+// ---------------------------------------------------------------------------
+
+// Bound by the weights' bytes, which are read once, straight into the matrix
+// cores' registers: a workgroup forms 16 columns of g and u for all rows, its
+// eight waves share the elements along D in turn, kAhead loads of each wave
+// under way at once, and add up in LDS in their order.  Operands need no
+// alignment and fp32 is split where it is loaded, so that nothing is packed.
+constexpr int kFewRows = 64;
+constexpr int kFewWaves = 8;
+
+// 16 bytes of a lane's share of a step: 8 bf16, or 4 fp32.
+template <typename T>
+struct FewStep;
+template <>
+struct FewStep<bf16_t> {
+    static constexpr int kStep = 64, kLane = 16, kFrags = 2, kPieces = 1;
+    Raw<bf16_t, 8> raw[2];
+    __device__ __forceinline__ void load(const bf16_t *row, int64_t k, int64_t D) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) raw[j].load_upto(row + k + j * 8, D - k - j * 8);
+    }
+    __device__ __forceinline__ void frags(bf16x8 (&f)[2][1]) const {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[j][0] = __builtin_bit_cast(bf16x8, raw[j]);
+    }
+};
+template <>
+struct FewStep<float> {
+    static constexpr int kStep = 32, kLane = 8, kFrags = 1, kPieces = 3;
+    Raw<float, 8> raw;
+    __device__ __forceinline__ void load(const float *row, int64_t k, int64_t D) {
+        raw.load_upto(row + k, D - k);
+    }
+    __device__ __forceinline__ void frags(bf16x8 (&f)[1][3]) const {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = raw.get<float>(e);
+#pragma unroll
+        for (int which = 0; which < 3; ++which) {
+            Raw<bf16_t, 8> x;
+            set_piece(x, v, which, true);
+            f[0][which] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+};
+
+template <typename T, int ACT, int MB>
+__global__ __launch_bounds__(64 * kFewWaves) void k_ffn_few(const T *x, int64_t ld_x,
+                                                            const T *w_gate, int64_t ld_gate,
+                                                            const T *w_up, int64_t ld_up, T *y,
+                                                            int64_t ld_y, int32_t M, int32_t F,
+                                                            int64_t D) {
+    using S = FewStep<T>;
+    constexpr int kAhead = MB == 4 ? 2 : 4;
+    __shared__ f32x4 s_acc[kFewWaves][2][MB][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+    const int32_t f0 = blockIdx.x * 16;
+    const T *rows[2] = {w_gate + min(f0 + c, F - 1) * ld_gate, w_up + min(f0 + c, F - 1) * ld_up};
+    const T *mine[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) mine[i] = x + min(i * 16 + c, M - 1) * ld_x;
+    f32x4 acc[2][MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[0][i] = acc[1][i] = f32x4{0, 0, 0, 0};
+    for (int64_t k = (int64_t)wave * S::kStep; k < D; k += kFewWaves * kAhead * S::kStep) {
+        S w[kAhead][2], a[kAhead][MB];
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h) {
+            const int64_t at = k + h * kFewWaves * S::kStep + q * S::kLane;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) w[h][g].load(rows[g], at, D);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) a[h][i].load(mine[i], at, D);
+        }
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h) {
+            bf16x8 fw[2][S::kFrags][S::kPieces];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) w[h][g].frags(fw[g]);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                bf16x8 fa[S::kFrags][S::kPieces];
+                a[h][i].frags(fa);
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int j = 0; j < S::kFrags; ++j) {
+                        auto add = [&](int pw, int pa) {
+                            acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                fw[g][j][pw], fa[j][pa], acc[g][i], 0, 0, 0);
+                        };
+                        if constexpr (S::kPieces == 3) {
+                            add(1, 1);
+                            add(0, 2);
+                            add(2, 0);
+                            add(0, 1);
+                            add(1, 0);
+                        }
+                        add(0, 0);
+                    }
+            }
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) s_acc[wave][g][i][lane] = acc[g][i];
+    __syncthreads();
+    // a lane's four columns of a row
+    if (wave >= MB) return;
+    f32x4 g = s_acc[0][0][wave][lane], u = s_acc[0][1][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) {
+        g += s_acc[w][0][wave][lane];
+        u += s_acc[w][1][wave][lane];
+    }
+    const int32_t m = wave * 16 + c, n = f0 + q * 4;
+    if (m >= M || n >= F) return;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float b, db;
+        activation<ACT>(g[e], b, db);
+        v[e] = b * u[e];
+    }
+    Raw<T, 4> out;
+    out.set_all(v);
+    out.store_upto(y + m * ld_y + n, F - n);
+}
+
+template <typename T, int ACT>
+void launch_few(const ecc_ffn_t *a, void *d_y, int64_t ld_y, hipStream_t s) {
+    const int32_t M = (int32_t)(a->P * a->n), F = (int32_t)a->F;
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((F + 15) / 16)), dim3(64 * kFewWaves), 0, s,
+                           (const T *)a->d_x, a->ld_x, (const T *)a->d_w_gate, a->ld_gate,
+                           (const T *)a->d_w_up, a->ld_up, (T *)d_y, ld_y, M, F, a->D);
+    };
+    if (M <= 16) launch(k_ffn_few<T, ACT, 1>);
+    else if (M <= 32) launch(k_ffn_few<T, ACT, 2>);
+    else launch(k_ffn_few<T, ACT, 4>);
+}
+
 struct Plan {
     int64_t N, n_pad, rows, Dp, Fp;
     int np, pd;                   // pieces of the operands, of dg and du
@@ -259,6 +404,13 @@ ecc_status_t ecc_ffn_forward(const ecc_ffn_t *a, void *d_y, int64_t ld_y, void *
         for (const Span &i : in) ECC_ARG(!spans_meet(o, i), "an output overlaps an input");
     ECC_ARG(!spans_meet(out[0], out[1]), "an output and the work buffer overlap");
     hipStream_t s = (hipStream_t)hip_stream;
+    if (p.N <= kFewRows) {
+        with_kind(a, [&](auto t, auto act) {
+            launch_few<decltype(t), decltype(act)::value>(a, d_y, ld_y, s);
+        });
+        ECC_LAUNCH_CHECK();
+        return ECC_OK;
+    }
     const GemmArgs g = projections(a, p, (char *)d_work, s);
     with_kind(a, [&](auto t, auto act) {
         using T = decltype(t);

@@ -15,6 +15,8 @@ statistics) in fp32, or fp64 for rows of fp64.
 """
 from __future__ import annotations
 
+import struct
+
 import torch
 
 from . import capi as E
@@ -575,44 +577,50 @@ def _worker_parts(t, P, what):
     if t.dim() < 1 or t.shape[0] != P:
         raise ValueError("%s must have %d workers in its first dimension, not shape %s" %
                          (what, P, tuple(t.shape)))
+    n = t.numel() // P
     if t.is_contiguous():
-        n = t.numel() // P
         return n, n
     if not t[0].is_contiguous():
         raise ValueError("%s must be contiguous for each worker" % what)
-    return t[0].numel(), t.stride(0)
+    return n, t.stride(0)
+
+
+# An ecc_tensor_t: two addresses, three sizes, two types.
+_TENSOR = struct.Struct("=QQqqqii")
 
 
 def _tensors(grads, out, P):
-    """The array of ecc_tensor_t, and the first tensor."""
+    """The array of ecc_tensor_t, their number, and the first tensor."""
     grads = list(grads)
     if not grads:
         raise ValueError("there are no gradients")
     if P is not None and P < 1:
         raise ValueError("P must be >= 1")
-    outs = [None] * len(grads) if out is None else list(out)
-    if len(outs) != len(grads):
-        raise ValueError("%d outputs for %d gradients" % (len(outs), len(grads)))
-    a = (E.ecc_tensor_t * len(grads))()
+    count = len(grads)
+    outs = (None,) * count if out is None else list(out)
+    if len(outs) != count:
+        raise ValueError("%d outputs for %d gradients" % (len(outs), count))
     device = grads[0].get_device()
     if device < 0:
         raise ValueError("grads must be on the GPU")
-    for e, g, o in zip(a, grads, outs):
-        e.type = _type(g, "a gradient")
-        e.d_grad = g.data_ptr()
-        e.n, e.stride = _worker_parts(g, P, "a gradient")
+    data, at, size = bytearray(count * _TENSOR.size), 0, _TENSOR.size
+    for g, o in zip(grads, outs):
         if g.get_device() != device:
             raise ValueError("grads must be on one GPU")
-        if o is not None:
-            e.out_type = _type(o, "an output")
-            e.d_out = o.data_ptr()
-            n, e.out_stride = _worker_parts(o, P, "an output")
+        n, stride = _worker_parts(g, P, "a gradient")
+        if o is None:
+            _TENSOR.pack_into(data, at, g.data_ptr(), 0, n, stride, 0, _type(g, "a gradient"), 0)
+        else:
             if o.shape != g.shape:
                 raise ValueError("an output must have its gradient's shape %s, not %s" %
                                  (tuple(g.shape), tuple(o.shape)))
             if o.get_device() != device:
                 raise ValueError("grads and out must be on one GPU")
-    return a, grads[0]
+            _TENSOR.pack_into(data, at, g.data_ptr(), o.data_ptr(), n, stride,
+                              _worker_parts(o, P, "an output")[1], _type(g, "a gradient"),
+                              _type(o, "an output"))
+        at += size
+    return (E.ecc_tensor_t * count).from_buffer(data), grads[0]
 
 
 def _norms(norms, P, like):
