@@ -195,37 +195,56 @@ struct LogitsOut {
     __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
                                            f32x4 (&acc)[MI][NI]) const {
         const bool first = (threadIdx.x & 63) < 16;
+        const int32_t n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
+        const bool whole = n0 + 16 * NI <= g.N;   // no column is behind the last
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int32_t m = t.m + 16 * i;
             const bool row = m < g.M;
             const int32_t y = row ? label[m] : -1;
-            float most = -__builtin_inff();
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int32_t n = t.n + 16 * j;
-                acc[i][j] *= scale;
-                if (z && row && n < ld) *reinterpret_cast<f32x4 *>(z + m * ld + n) = acc[i][j];
+            for (int j = 0; j < NI; ++j) acc[i][j] *= scale;
+            if (z && row) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (n + e == y && y >= 0) picked[m] = acc[i][j][e];
-                    if (n + e < g.N) most = fmaxf(most, acc[i][j][e]);
-                }
+                for (int j = 0; j < NI; ++j)
+                    if (whole || t.n + 16 * j < ld)
+                        *reinterpret_cast<f32x4 *>(z + m * ld + t.n + 16 * j) = acc[i][j];
             }
-            most = fmaxf(most, __shfl_xor(most, 16, 64));
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            const float from = most == -__builtin_inff() ? 0.0f : most;
-            float sum = 0.0f;
+            if (y >= n0 && y < n0 + 16 * NI) {
 #pragma unroll
-            for (int j = 0; j < NI; ++j)
+                for (int j = 0; j < NI; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (t.n + 16 * j + e < g.N) sum += expf(acc[i][j][e] - from);
-            sum += __shfl_xor(sum, 16, 64);
-            sum += __shfl_xor(sum, 32, 64);
+                    for (int e = 0; e < 4; ++e)
+                        if (t.n + 16 * j + e == y) picked[m] = acc[i][j][e];
+            }
+            float most = -__builtin_inff(), sum = 0.0f;
+            if (whole) {
+                sums_of<NI, true>(acc[i], t.n, g.N, most, sum);
+            } else {
+                sums_of<NI, false>(acc[i], t.n, g.N, most, sum);
+            }
             if (first && row && t.tile_n < tiles)
                 stats[(int64_t)m * tiles + t.tile_n] = make_float2(most, sum);
         }
+    }
+    template <int NI, bool WHOLE>
+    __device__ static __forceinline__ void sums_of(const f32x4 (&v)[NI], int32_t n, int32_t N,
+                                                   float &most, float &sum) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (WHOLE || n + 16 * j + e < N) most = fmaxf(most, v[j][e]);
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const float from = most == -__builtin_inff() ? 0.0f : most;
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (WHOLE || n + 16 * j + e < N) sum += exp_fast(v[j][e] - from);
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
     }
 };
 
@@ -342,7 +361,7 @@ __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int32_t j = col0 + c8 + e;
-            float v = expf(x[p].get<float>(e) - most) * soft;
+            float v = exp_fast(x[p].get<float>(e) - most) * soft;
             if (j == y) v -= 1.0f;
             mine[p][e] = y >= 0 && j < a.V ? v : 0.0f;
         }
@@ -675,11 +694,16 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
             if (a->grad_type == ECC_F32 || p.pieces_of_rows == 1) {
                 out.add = accumulate || !first;
                 out.skip_empty = out.add;
+            } else if (!last) {
+                // pieces of a bf16 gradient are added up in fp32
+                out.out = w + p.sums;
+                out.ld = D;
+                out.batch_stride = V * D;
+                out.type = ECC_F32;
+                out.add = out.skip_empty = !first;
             } else {
-                out.sums = first ? nullptr : (const float *)(w + p.sums);
-                out.to_sums = last ? nullptr : (float *)(w + p.sums);
-                out.add = last && accumulate;
-                out.skip_empty = !first && !last;
+                out.sums = (const float *)(w + p.sums);
+                out.add = accumulate;
             }
             products[count] = Product{d, out};
             shapes[count] = p.shape_e;

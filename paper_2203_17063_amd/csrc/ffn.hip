@@ -20,13 +20,13 @@ namespace {
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float &a, float &da) {
     if constexpr (ACT == ECC_ACT_SILU) {
-        const float q = 1.0f / (1.0f + expf(-g));
+        const float q = recip_fast(1.0f + exp_fast(-g));
         a = g * q;
         da = q * (1.0f + g * (1.0f - q));
     } else {
         const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
         a = g * c;
-        da = c + g * (expf(-0.5f * g * g) * 0.39894228040143268f);
+        da = c + g * (exp_fast(-0.5f * g * g) * 0.39894228040143268f);
     }
 }
 

@@ -433,8 +433,7 @@ struct MatrixOut {
     int32_t held, padded;     // or workers' rows held of those padded to (0: all)
     const float *row_scale;   // the sums' factor, of each row
     const float *scale;       // of each batch
-    const float *sums;
-    float *to_sums;           // fp32 sums in out's place
+    const float *sums;        // added before (dense)
     float *parts;
 
     __device__ __forceinline__ void put(const GemmArgs &g, int32_t batch, int32_t m, int32_t n,
@@ -453,11 +452,7 @@ struct MatrixOut {
         if (row_scale) v *= row_scale[m];
         if (scale) v *= scale[batch];
         const int w = min(4, g.N - n);
-        if (sums || to_sums) {
-            const int64_t at = ((int64_t)batch * g.M + m) * g.N + n;
-            if (sums) v += load4(sums + at, w);
-            if (to_sums) return store4(to_sums + at, v, w);
-        }
+        if (sums) v += load4(sums + ((int64_t)batch * g.M + m) * g.N + n, w);
         char *base = (char *)out;
         if (second && r >= second) {
             base = (char *)out2;
@@ -515,6 +510,68 @@ struct MatrixOut {
     }
 };
 
+// The same for rows that are the output's own and not split, with what happens
+// to each element settled beforehand (large tiles: asked element by element, a
+// table gradient of 128,000 x 4,096 takes 3.5 to 3.9 ms per 4,096 rows).
+enum { kWrite = 0, kAdd = 1, kFromSums = 2 };  // kFromSums: sums, and out with `add`
+template <typename T, int MODE>
+struct BlockOut {
+    static constexpr bool kPair = false, kLds = false;
+    MatrixOut o;
+    template <int MI, int NI>
+    __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
+                                           f32x4 (&acc)[MI][NI]) const {
+        if (o.skip_empty && t.k == 0) return;
+        const float by = o.scale ? o.scale[t.batch] : 1.0f;
+        const int32_t n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
+        const bool whole = n0 + 16 * NI <= g.N;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int32_t m = t.m + 16 * i;
+            if (m >= g.M) continue;
+            const bool last = o.second && m >= o.second;
+            T *to = (T *)(last ? o.out2 : o.out) + t.batch * o.batch_stride +
+                    (int64_t)(last ? m - o.second : m) * o.ld + t.n;
+            const float *sums =
+                MODE == kFromSums ? o.sums + ((int64_t)t.batch * g.M + m) * g.N + t.n : nullptr;
+            if (whole) row<NI, true>(to, sums, acc[i], by, 0);
+            else row<NI, false>(to, sums, acc[i], by, g.N - t.n);
+        }
+    }
+    template <int NI, bool WHOLE>
+    __device__ __forceinline__ void row(T *to, const float *sums, const f32x4 (&v)[NI], float by,
+                                        int32_t n) const {
+        Raw<T, 4> old[NI];
+        Raw<float, 4> sum[NI];
+        const bool add = MODE == kAdd || (MODE == kFromSums && o.add);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            if (add) {
+                if (WHOLE) old[j].load(to + 16 * j);
+                else old[j].load_upto(to + 16 * j, n - 16 * j);
+            }
+            if (MODE == kFromSums) {
+                if (WHOLE) sum[j].load(sums + 16 * j);
+                else sum[j].load_upto(sums + 16 * j, n - 16 * j);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = v[j][e] * by;
+                if (MODE == kFromSums) y[e] += sum[j].template get<float>(e);
+                if (add) y[e] += old[j].template get<float>(e);
+            }
+            Raw<T, 4> x;
+            x.set_all(y);
+            if (WHOLE) x.store(to + 16 * j);
+            else x.store_upto(to + 16 * j, n - 16 * j);
+        }
+    }
+};
+
 // Adds the parts of a split product in their order: one thread per four
 // columns of a row.
 __device__ __forceinline__ void join_parts(const GemmArgs &g, MatrixOut out, int64_t i) {
@@ -563,6 +620,24 @@ inline int64_t quads_to_join(const Product &p) {
     return p.g.splits > 1 ? (int64_t)p.g.batches * p.g.M * ((p.g.N + 3) / 4) : 0;
 }
 
+// A product of large tiles.
+inline void launch_large(const Product &p, hipStream_t s) {
+    const MatrixOut &o = p.out;
+    auto block = [&](auto t, auto mode) {
+        using B = BlockOut<decltype(t), decltype(mode)::value>;
+        launch_gemm_tile<256, 256, 2, 4>(p.g, B{o}, s);
+    };
+    auto typed = [&](auto mode) {
+        if (o.type == ECC_F32) block(float{}, mode);
+        else block(bf16_t{}, mode);
+    };
+    if (o.parts || o.row_map || o.padded || o.row_scale)
+        launch_gemm_tile<256, 256, 2, 4>(p.g, o, s);
+    else if (o.sums) block(bf16_t{}, std::integral_constant<int, kFromSums>{});
+    else if (o.add) typed(std::integral_constant<int, kAdd>{});
+    else typed(std::integral_constant<int, kWrite>{});
+}
+
 // Up to two products (count) of the given shapes; parts: work memory of
 // split_bytes for each.
 inline void launch_products(Product (&p)[2], int count, const GemmShape (&shape)[2],
@@ -581,7 +656,7 @@ inline void launch_products(Product (&p)[2], int count, const GemmShape (&shape)
         hipLaunchKernelGGL(k_gemm_two, dim3((unsigned)t.first[1]), dim3(512), 0, s, t);
     } else {
         for (int i = 0; i < count; ++i)
-            if (shape[i].large) launch_gemm_tile<256, 256, 2, 4>(p[i].g, p[i].out, s);
+            if (shape[i].large) launch_large(p[i], s);
             else launch_gemm_tile<128, 128, 4, 2>(p[i].g, p[i].out, s);
     }
     t.first[0] = quads[0];

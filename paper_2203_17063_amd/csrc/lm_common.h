@@ -247,6 +247,21 @@ private:
 template <typename T>
 constexpr int kVec = 16 / (int)sizeof(T);
 
+// exp(x) within 2 ulp by the power of two of the hardware (1 ulp): x log2(e) as
+// a product and what it is rounded by, the latter to first order.  0 below -104
+// (the smallest results are flushed to 0 anyway), that of 88 above it; NaN stays.
+__device__ __forceinline__ float exp_fast(float x) {
+    constexpr float kLog2e = 1.44269502f, kLog2eLow = 1.92596303e-8f, kLn2 = 0.69314718f;
+    x = x < -104.0f ? -104.0f : x;
+    x = x > 88.0f ? 88.0f : x;
+    const float t = x * kLog2e;
+    const float r = __builtin_fmaf(x, kLog2eLow, __builtin_fmaf(x, kLog2e, -t));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e * kLn2, r, e);
+}
+// 1 / x within 1 ulp, 0 beyond 2^126
+__device__ __forceinline__ float recip_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_f32(float v) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, false));
