@@ -182,7 +182,7 @@ constexpr int kUnread = 16;  // positions of a wave
 
 // Logits and what the softmax needs of them, per row and 64 columns.
 struct LogitsOut {
-    static constexpr bool kPair = false, kLds = false;
+    static constexpr bool kPair = false;
     float *z;          // NULL: not kept
     int64_t ld;
     float scale;

@@ -16,7 +16,11 @@
 namespace ecc {
 namespace {
 
-// act(g) and its derivative.
+// act(g) and its derivative.  The error function is Abramowitz and Stegun's
+// 7.1.26 (Hastings), within 1.5e-7 of it: half of 1 - erf(|x|) is a polynomial
+// in 1 / (1 + p |x|) times exp(-x^2), at x = g / sqrt 2 the exponential that the
+// derivative needs too.  For negative g that half is the factor itself, so that
+// small values keep their digits.
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float &a, float &da) {
     if constexpr (ACT == ECC_ACT_SILU) {
@@ -24,15 +28,22 @@ __device__ __forceinline__ void activation(float g, float &a, float &da) {
         a = g * q;
         da = q * (1.0f + g * (1.0f - q));
     } else {
-        const float c = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
+        const float e = exp_fast(-0.5f * g * g);
+        const float t = recip_fast(__builtin_fmaf(__builtin_fabsf(g), 0.3275911f * 0.70710678f, 1.0f));
+        float h = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+        h = __builtin_fmaf(t, h, 1.421413741f);
+        h = __builtin_fmaf(t, h, -0.284496736f);
+        h = __builtin_fmaf(t, h, 0.254829592f);
+        h *= 0.5f * t * e;
+        const float c = g < 0.0f ? h : 1.0f - h;
         a = g * c;
-        da = c + g * (exp_fast(-0.5f * g * g) * 0.39894228040143268f);
+        da = c + g * e * 0.39894228f;
     }
 }
 
 template <typename T, int ACT>
 struct FfnOut {
-    static constexpr bool kPair = true, kLds = false;
+    static constexpr bool kPair = true;
     T *y;
     int64_t ld;
     template <int MI, int NI>
@@ -58,136 +69,82 @@ struct FfnOut {
     }
 };
 
-// dg and du out of the sums, in both orders.  A wave turns its block round in
-// its part of LDS, so that memory is written in rows of 256 bytes (of the other
-// order: two of 64) instead of 8 bytes a lane: 8,192 rows, D 4,096, F 12,288: XXX
 template <typename T, int ACT>
 struct FfnGradOut {
-    static constexpr bool kPair = true, kLds = true;
+    static constexpr bool kPair = true;
     const T *dy;
     int64_t ld_dy;
-    int32_t n, n_pad;     // workers' rows among the product's (n_pad 0: all rows)
-    int32_t pieces;
-    bf16_t *d;            // [piece][row][dg | du], each F_pad long; NULL: none
+    bf16_t *d;            // [piece][row][dg | du], each F_pad long
     int64_t F_pad, plane;
-    bf16_t *dt;           // [piece][dg's columns, du's][ld_t rows]; NULL: none
-    int64_t ld_t, plane_t;
-
-    // dy's row of a row of the product, -1: none
-    __device__ __forceinline__ int64_t source(int32_t m, int32_t M) const {
-        if (m >= M) return -1;
-        if (!n_pad) return m;
-        const int32_t w = m / n_pad, i = m - w * n_pad;
-        return i < n ? (int64_t)w * n + i : -1;
-    }
+    int32_t pieces;
     template <int MI, int NI>
     __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
-                                           f32x4 (&acc)[MI][NI], uint16_t *lds) const {
-        static_assert(NI == 4, "32 columns of each of the pair");
-        // (some rows at a time: all at once would not fit the registers)
-        constexpr int G = ACT == ECC_ACT_SILU && sizeof(T) == 2 && MI > 2 ? 4 : 2;
+                                           f32x4 (&acc)[MI][NI]) const {
+        const int32_t m0 = t.m & ~15, n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
+        if (m0 + 16 * MI <= g.M && n0 + 8 * NI <= g.N) {
+            // (a block inside: the loads of some rows go together)
+            constexpr int G = MI < 4 ? MI : 4;
 #pragma unroll
-        for (int i0 = 0; i0 < MI; i0 += G) {
-            Raw<T, 4> x[G][2];
-            bool held[G];
+            for (int i0 = 0; i0 < MI; i0 += G) {
+                Raw<T, 4> x[G][NI / 2];
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const int64_t row = source(t.m + 16 * (i0 + i), g.M);
-                held[i] = row >= 0;
+                for (int i = 0; i < G; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    x[i][j].load_upto(dy + (held[i] ? row * ld_dy + t.n + 16 * j : 0),
-                                      held[i] ? (int64_t)g.N - t.n - 16 * j : 0);
+                    for (int j = 0; j < NI / 2; ++j)
+                        x[i][j].load(dy + (t.m + 16 * (i0 + i)) * ld_dy + t.n + 16 * j);
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI / 2; ++j)
+                        put(t.m + 16 * (i0 + i), t.n + 16 * j, x[i][j], acc[i0 + i][j],
+                            acc[i0 + i][j + NI / 2]);
             }
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    f32x4 &first = acc[i0 + i][j], &second = acc[i0 + i][j + 2];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float a, da;
-                        activation<ACT>(first[e], a, da);
-                        const float v = x[i][j].template get<float>(e);
-                        const bool in = held[i] && t.n + 16 * j + e < g.N;
-                        const float dg = v * second[e] * da, du = v * a;
-                        first[e] = in ? dg : 0.0f;
-                        second[e] = in ? du : 0.0f;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            return;
         }
-        const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
-        const int32_t m0 = t.m - c, n0 = t.n - q * 4;  // the wave's block
-        uint32_t *words = reinterpret_cast<uint32_t *>(lds);
-        for (int which = 0; which < pieces; ++which) {
-            // (the pieces are formed in each turn: kept from turn to turn, all
-            // of them would not fit the registers)
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(acc[i][j]));
-            if (dt) {
-                // [column][row]: two rows to a word, a lane and its neighbour
-                // exchange halves of their four columns; words are stored at
-                // word ^ 8 (column / 2), free of conflicts
-                constexpr int kRow = MI * 8;
+            for (int j = 0; j < NI / 2; ++j) {
+                const int32_t m = t.m + 16 * i, n = t.n + 16 * j;
+                if (m >= g.M || n >= F_pad) continue;
+                Raw<T, 4> x;
+                x.load_upto(dy + m * ld_dy + n, (int64_t)g.N - n);
+                // (columns behind the last are zeros: their weights' rows are
+                // the last one's again, or not finite with it)
+                f32x4 first = acc[i][j], second = acc[i][j + NI / 2];
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                        Raw<bf16_t, 4> p;
-                        set_piece(p, v, which, pieces > 1);
-                        const bool odd = c & 1;
-                        const uint32_t give = odd ? p.w[0] : p.w[1];
-                        const uint32_t keep = odd ? p.w[1] : p.w[0];
-                        const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp(
-                            (int)give, kDppQuadXor1, 0xf, 0xf, false);
-                        const uint32_t lo = odd ? got : keep, hi = odd ? keep : got;
-                        const int col = j * 16 + q * 4 + (odd ? 2 : 0);
-                        const int at = (i * 8 + c / 2) ^ (8 * (col / 2 % MI));
-                        words[col * kRow + at] = (lo & 0xffffu) | hi << 16;
-                        words[(col + 1) * kRow + at] = lo >> 16 | (hi & 0xffff0000u);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                constexpr int kLanes = MI * 2;     // of 8 rows each: a column
-                for (int it = 0; it < 64; it += 64 / kLanes) {
-                    const int col = it + lane / kLanes, r = lane % kLanes;
-                    const int at = (r * 4) ^ (8 * (col / 2 % MI));
-                    Raw<bf16_t, 8> v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v.w[e] = words[col * kRow + at + e];
-                    const int32_t f = n0 + col % 32, m = m0 + r * 8;
-                    if (f < g.N && m < ld_t)
-                        v.store(dt + which * plane_t + ((col < 32 ? 0 : g.N) + f) * ld_t + m);
-                }
+                for (int e = 0; e < 4; ++e)
+                    if (n + e >= g.N) first[e] = second[e] = 0.0f;
+                put(m, n, x, first, second);
             }
-            if (d) {
-                // [row][column], 16-byte chunks stored at chunk ^ (row & 7)
+    }
+    __device__ __forceinline__ void put(int32_t m, int32_t n, const Raw<T, 4> &x,
+                                        const f32x4 &first, const f32x4 &second) const {
+        float dg[4], du[4];
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
+        for (int e = 0; e < 4; ++e) {
+            float a, da;
+            activation<ACT>(first[e], a, da);
+            const float v = x.template get<float>(e);
+            dg[e] = v * second[e] * da;
+            du[e] = v * a;
+        }
+        bf16_t *to = d + m * 2 * F_pad + n;
+        store_pieces(to, dg);
+        store_pieces(to + F_pad, du);
+    }
+    // (a piece is what is left, rounded; then it is taken off)
+    __device__ __forceinline__ void store_pieces(bf16_t *to, float (&v)[4]) const {
+        Raw<bf16_t, 4> p;
+        p.set_all(v);
+        p.store(to);
+        if (pieces == 1) return;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                        Raw<bf16_t, 4> p;
-                        set_piece(p, v, which, pieces > 1);
-                        const int row = i * 16 + c, chunk = j * 2 + q / 2;
-                        p.store(reinterpret_cast<bf16_t *>(lds) + row * 64 +
-                                (chunk ^ (row & 7)) * 8 + (q & 1) * 4);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                for (int it = 0; it < MI * 16; it += 8) {
-                    const int row = it + lane / 8, chunk = lane % 8;
-                    Raw<bf16_t, 8> v;
-                    v.load(reinterpret_cast<const bf16_t *>(lds) + row * 64 +
-                           (chunk ^ (row & 7)) * 8);
-                    const int32_t m = m0 + row, f = n0 + chunk % 4 * 8;
-                    if (m < g.M && f < F_pad)
-                        v.store(d + which * plane + m * 2 * F_pad + (chunk < 4 ? 0 : F_pad) + f);
-                }
-            }
+        for (int which = 1; which < 3; ++which) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] -= p.get<float>(e);
+            p.set_all(v);
+            p.store(to + which * plane);
         }
     }
 };
@@ -339,8 +296,6 @@ void launch_few(const ecc_ffn_t *a, void *d_y, int64_t ld_y, hipStream_t s) {
 
 struct Plan {
     int64_t N, n_pad, rows, Dp, Fp;
-    int64_t M;                    // rows of the backward products
-    bool padded;                  // workers of n rows among n_pad each
     int np, pd;                   // pieces of the operands, of dg and du
     bool pack_x, pack_gate, pack_up;
     GemmShape shape_x, shape_w;
@@ -356,9 +311,7 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
     p.Fp = pad64(a->F);
     p.np = a->type == ECC_F32 ? 3 : 1;
     p.pd = a->type == ECC_F32 || a->grad_type == ECC_F32 ? 3 : 1;
-    p.padded = gradient && a->P > 1 && p.n_pad != a->n;
-    p.M = p.padded ? p.rows : p.N;
-    p.pack_x = p.padded || !as_it_lies(a->d_x, a->ld_x, a->D, a->type);
+    p.pack_x = !as_it_lies(a->d_x, a->ld_x, a->D, a->type);
     p.pack_gate = !as_it_lies(a->d_w_gate, a->ld_gate, a->D, a->type);
     p.pack_up = !as_it_lies(a->d_w_up, a->ld_up, a->D, a->type);
     // (a pair of matrices has one pitch)
@@ -369,17 +322,17 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
         at += (bytes + 255) & ~int64_t(255);
         return here;
     };
-    p.x = take(p.pack_x ? p.np * 2 * pad64(p.M) * p.Dp : 0);
+    p.x = take(p.pack_x ? p.np * 2 * pad64(p.N) * p.Dp : 0);
     p.gate = take(p.pack_gate ? p.np * 2 * p.Fp * p.Dp : 0);
     p.up = take(p.pack_up ? p.np * 2 * p.Fp * p.Dp : 0);
     if (gradient) {
         p.x_t = take(p.np * 2 * a->D * p.rows);
         p.w_t = take(p.np * 2 * a->D * 2 * p.Fp);
-        p.d = take(p.pd * 2 * p.M * 2 * p.Fp);
+        p.d = take(p.pd * 2 * pad64(p.N) * 2 * p.Fp);
         p.d_t = take(p.pd * 2 * 2 * a->F * p.rows);
-        p.shape_x = gemm_shape(p.M, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+        p.shape_x = gemm_shape(p.N, a->D, 2 * p.Fp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
         p.shape_w = gemm_shape(2 * a->F, a->D, p.n_pad / kGemmK * (p.np == 3 ? 6 : p.pd), a->P, true);
-        p.parts[0] = take(split_bytes(p.M, a->D, p.shape_x.splits, 1));
+        p.parts[0] = take(split_bytes(p.N, a->D, p.shape_x.splits, 1));
         p.parts[1] = take(split_bytes(2 * a->F, a->D, p.shape_w.splits, a->P));
     }
     p.bytes = std::max<int64_t>(at, 16);
@@ -423,25 +376,23 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
     g.b = GemmOperand{(const bf16_t *)a->d_w_gate, a->ld_gate, 0};
     g.b2 = (const bf16_t *)a->d_w_up;
     Packing packing;
-    auto pack = [&](const void *src, int64_t ld, int64_t rows, int64_t to, bool padded) {
+    auto pack = [&](const void *src, int64_t ld, int64_t rows, int64_t to) {
         k.src = src;
         k.ld = ld;
-        k.n = padded ? a->n : rows;
-        k.n_pad = padded ? p.n_pad : pad64(rows);
-        k.total = rows;
-        k.rows_packed = padded ? p.rows : pad64(rows);
+        k.n = k.total = rows;
+        k.rows_packed = k.n_pad = pad64(rows);
         k.rows = (bf16_t *)(w + to);
         k.plane_rows = k.rows_packed * p.Dp;
         packing.add(k);
         return GemmOperand{k.rows, p.Dp, k.plane_rows};
     };
-    if (p.pack_x) g.a = pack(a->d_x, a->ld_x, p.N, p.x, p.padded);
+    if (p.pack_x) g.a = pack(a->d_x, a->ld_x, p.N, p.x);
     if (p.pack_gate) {
-        g.b = pack(a->d_w_gate, a->ld_gate, a->F, p.gate, false);
-        g.b2 = pack(a->d_w_up, a->ld_up, a->F, p.up, false).p;
+        g.b = pack(a->d_w_gate, a->ld_gate, a->F, p.gate);
+        g.b2 = pack(a->d_w_up, a->ld_up, a->F, p.up).p;
     }
     packing.launch(a->type, s);
-    g.M = (int32_t)p.M;
+    g.M = (int32_t)p.N;
     g.N = (int32_t)a->F;
     g.K = (int32_t)p.Dp;
     g.batches = 1;
@@ -581,25 +532,15 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
     // dg and du
     const GemmArgs g = projections(a, p, w, s);
     bf16_t *d = (bf16_t *)(w + p.d);
-    const int64_t plane = p.M * 2 * p.Fp, plane_t = 2 * F * p.rows;
+    const int64_t plane = pad64(p.N) * 2 * p.Fp;
     with_kind(a, [&](auto t, auto act) {
         using T = decltype(t);
-        FfnGradOut<T, decltype(act)::value> out{};
-        out.dy = (const T *)d_dy;
-        out.ld_dy = ld_dy;
-        out.n = (int32_t)a->n;
-        out.n_pad = p.padded ? (int32_t)p.n_pad : 0;
-        out.pieces = p.pd;
-        out.d = d_dx ? d : nullptr;
-        out.F_pad = p.Fp;
-        out.plane = plane;
-        out.dt = d_dw_gate ? (bf16_t *)(w + p.d_t) : nullptr;
-        out.ld_t = p.rows;
-        out.plane_t = plane_t;
-        launch_gemm(g, out, s);
+        launch_gemm(g, FfnGradOut<T, decltype(act)::value>{(const T *)d_dy, ld_dy, d, p.Fp, plane,
+                                                           p.pd},
+                    s);
     });
-    // the operands' other order: [Wg | Wu] transposed, as long as [dg | du], and
-    // x with workers padded to multiples of 64 rows
+    // the other order of everything: [Wg | Wu] transposed, as long as [dg | du],
+    // x and [dg | du] with workers padded to multiples of 64 rows
     Packing packing;
     Product products[2];
     GemmShape shapes[2];
@@ -622,7 +563,7 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         GemmArgs x{};
         x.a = GemmOperand{d, 2 * p.Fp, plane};
         x.b = GemmOperand{(bf16_t *)(w + p.w_t), 2 * p.Fp, k.plane_cols};
-        x.M = (int32_t)p.M;
+        x.M = (int32_t)p.N;
         x.N = (int32_t)D;
         x.K = (int32_t)(2 * p.Fp);
         x.batches = 1;
@@ -630,8 +571,6 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         MatrixOut to{};
         to.out = d_dx;
         to.ld = ld_dx;
-        to.held = (int32_t)a->n;
-        to.padded = p.padded ? (int32_t)p.n_pad : 0;
         to.type = a->type;
         products[count] = Product{x, to};
         shapes[count] = p.shape_x;
@@ -650,6 +589,18 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
         k.cols_out = (bf16_t *)(w + p.x_t);
         k.plane_cols = D * p.rows;
         packing.add(k);
+        k.ld = 2 * p.Fp;
+        k.cols = F;
+        k.pieces = 1;
+        const int64_t plane_t = 2 * F * p.rows;
+        Packing gradients;
+        for (int which = 0; which < p.pd; ++which)
+            for (int i = 0; i < 2; ++i) {
+                k.src = d + which * plane + i * p.Fp;
+                k.cols_out = (bf16_t *)(w + p.d_t) + which * plane_t + i * F * p.rows;
+                gradients.add(k);
+            }
+        gradients.launch(ECC_BF16, s);
         GemmArgs x{};
         x.a = GemmOperand{(bf16_t *)(w + p.d_t), p.rows, plane_t};
         x.b = GemmOperand{(bf16_t *)(w + p.x_t), p.rows, D * p.rows};

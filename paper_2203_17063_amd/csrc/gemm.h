@@ -93,11 +93,6 @@ struct GemmTile {
     int32_t tile_n;   // 64-column tile of the wave
 };
 
-// LDS of a wave for an epilogue that wants it (Epi::kLds), in 16-bit elements:
-// its block of sums.
-template <int MI>
-constexpr int kWaveLds = MI * 16 * 64;
-
 typedef __attribute__((address_space(3))) void lds_void;
 
 // A value that all lanes share, in a scalar register.
@@ -341,18 +336,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int
         }
     }
     const int n_wave = n0 + wn * (Epi::kPair ? 32 : 64);
-    const GemmTile tile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64};
-    if constexpr (Epi::kLds) {
-        __syncthreads();  // nobody reads LDS any more, and no load is under way
-        uint16_t *mine;
-        if constexpr (BM == 256)
-            mine = (wave < 4 ? wave < 2 ? s_a0 : s_a1 : wave < 6 ? s_b0 : s_b1) +
-                   (wave & 1) * kWaveLds<MI>;
-        else mine = (wave < 4 ? s_a0 : s_a1) + (wave & 3) * kWaveLds<MI>;
-        epi.finish(tile, g, acc, mine);
-    } else {
-        epi.finish(tile, g, acc);
-    }
+    epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64}, g, acc);
 }
 
 template <int BM, int BN, int WM, int WN, class Epi>
@@ -423,14 +407,13 @@ inline bool gemm_in_range(int64_t M, int64_t N, int64_t batches) {
 // out2), batches apart, rounded to `type` once, what was there or `sums`
 // (fp32, dense) added before; or fp32 parts of a split product.
 struct MatrixOut {
-    static constexpr bool kPair = false, kLds = false;
+    static constexpr bool kPair = false;
     void *out, *out2;
     int64_t ld, batch_stride;
     int32_t type, second;
     int32_t add;              // to what out holds
     int32_t skip_empty;       // batches without a range along k are left alone
     const int32_t *row_map;   // out's row of each row; negative: none
-    int32_t held, padded;     // or workers' rows held of those padded to (0: all)
     const float *row_scale;   // the sums' factor, of each row
     const float *scale;       // of each batch
     const float *sums;        // added before (dense)
@@ -443,11 +426,6 @@ struct MatrixOut {
         if (row_map) {
             r = row_map[m];
             if (r < 0) return;
-        }
-        if (padded) {
-            const int32_t w = m / padded, i = m - w * padded;
-            if (i >= held) return;
-            r = (int64_t)w * held + i;
         }
         if (row_scale) v *= row_scale[m];
         if (scale) v *= scale[batch];
@@ -516,7 +494,7 @@ struct MatrixOut {
 enum { kWrite = 0, kAdd = 1, kFromSums = 2 };  // kFromSums: sums, and out with `add`
 template <typename T, int MODE>
 struct BlockOut {
-    static constexpr bool kPair = false, kLds = false;
+    static constexpr bool kPair = false;
     MatrixOut o;
     template <int MI, int NI>
     __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
@@ -631,7 +609,7 @@ inline void launch_large(const Product &p, hipStream_t s) {
         if (o.type == ECC_F32) block(float{}, mode);
         else block(bf16_t{}, mode);
     };
-    if (o.parts || o.row_map || o.padded || o.row_scale)
+    if (o.parts || o.row_map || o.row_scale)
         launch_gemm_tile<256, 256, 2, 4>(p.g, o, s);
     else if (o.sums) block(bf16_t{}, std::integral_constant<int, kFromSums>{});
     else if (o.add) typed(std::integral_constant<int, kAdd>{});

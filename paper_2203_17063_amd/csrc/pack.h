@@ -135,11 +135,11 @@ __device__ __forceinline__ void pack_block(const PackArgs &a, int64_t block) {
                 a.cols_out, a.ld_cols, a.plane_cols, a.pieces);
 }
 
-// Up to four matrices in one launch, one after another.
+// Up to eight matrices in one launch, one after another.
 struct PackList {
-    PackArgs a[4];
+    PackArgs a[8];
     int32_t count;
-    int32_t first[4];   // their first blocks
+    int32_t first[8];   // their first blocks
 };
 
 template <typename T>
