@@ -204,12 +204,12 @@ struct LogitsOut {
             const int32_t y = row ? label[m] : -1;
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] *= scale;
-            if (z && row) {
-#pragma unroll
-                for (int j = 0; j < NI; ++j)
-                    if (whole || t.n + 16 * j < ld)
-                        *reinterpret_cast<f32x4 *>(z + m * ld + t.n + 16 * j) = acc[i][j];
-            }
+            if (z)
+                turn<NI>(t.lds, acc[i], [&](int r, int col, f32x4 v) {
+                    const int32_t to = (t.m & ~15) + 16 * i + r;
+                    if (to < g.M && (whole || n0 + col < ld))
+                        *reinterpret_cast<f32x4 *>(z + to * ld + n0 + col) = v;
+                });
             if (y >= n0 && y < n0 + 16 * NI) {
 #pragma unroll
                 for (int j = 0; j < NI; ++j)

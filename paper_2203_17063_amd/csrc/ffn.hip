@@ -49,23 +49,27 @@ struct FfnOut {
     template <int MI, int NI>
     __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
                                            f32x4 (&acc)[MI][NI]) const {
+        const int32_t m0 = t.m & ~15, n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i) {
+            f32x4 v[NI / 2];
 #pragma unroll
-            for (int j = 0; j < NI / 2; ++j) {
-                const int32_t m = t.m + 16 * i, n = t.n + 16 * j;
-                if (m >= g.M || n >= g.N) continue;
-                float v[4];
+            for (int j = 0; j < NI / 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, da;
                     activation<ACT>(acc[i][j][e], a, da);
-                    v[e] = a * acc[i][j + NI / 2][e];
+                    v[j][e] = a * acc[i][j + NI / 2][e];
                 }
+            turn<NI / 2>(t.lds, v, [&](int row, int col, f32x4 u) {
+                const int32_t m = m0 + 16 * i + row, n = n0 + col;
+                if (m >= g.M || n >= g.N) return;
+                const float w[4] = {u[0], u[1], u[2], u[3]};
                 Raw<T, 4> x;
-                x.set_all(v);
+                x.set_all(w);
                 x.store_upto(y + m * ld + n, g.N - n);
-            }
+            });
+        }
     }
 };
 
@@ -81,57 +85,49 @@ struct FfnGradOut {
     __device__ __forceinline__ void finish(const GemmTile &t, const GemmArgs &g,
                                            f32x4 (&acc)[MI][NI]) const {
         const int32_t m0 = t.m & ~15, n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
-        if (m0 + 16 * MI <= g.M && n0 + 8 * NI <= g.N) {
-            // (a block inside: the loads of some rows go together)
-            constexpr int G = MI < 4 ? MI : 4;
+        const bool whole = m0 + 16 * MI <= g.M && n0 + 8 * NI <= g.N;
+        // (the loads of some rows go together)
+        constexpr int G = MI < 4 ? MI : 4;
 #pragma unroll
-            for (int i0 = 0; i0 < MI; i0 += G) {
-                Raw<T, 4> x[G][NI / 2];
+        for (int i0 = 0; i0 < MI; i0 += G) {
+            Raw<T, 4> x[G][NI / 2];
 #pragma unroll
-                for (int i = 0; i < G; ++i)
+            for (int i = 0; i < G; ++i)
 #pragma unroll
-                    for (int j = 0; j < NI / 2; ++j)
-                        x[i][j].load(dy + (t.m + 16 * (i0 + i)) * ld_dy + t.n + 16 * j);
+                for (int j = 0; j < NI / 2; ++j) {
+                    const int32_t m = t.m + 16 * (i0 + i), n = t.n + 16 * j;
+                    if (whole) x[i][j].load(dy + m * ld_dy + n);
+                    else x[i][j].load_upto(dy + (m < g.M ? m * ld_dy + n : 0),
+                                           m < g.M ? (int64_t)g.N - n : 0);
+                }
 #pragma unroll
-                for (int i = 0; i < G; ++i)
+            for (int i = 0; i < G; ++i) {
+                f32x4 dg[NI / 2], du[NI / 2];
 #pragma unroll
-                    for (int j = 0; j < NI / 2; ++j)
-                        put(t.m + 16 * (i0 + i), t.n + 16 * j, x[i][j], acc[i0 + i][j],
-                            acc[i0 + i][j + NI / 2]);
+                for (int j = 0; j < NI / 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float a, da;
+                        activation<ACT>(acc[i0 + i][j][e], a, da);
+                        const float v = x[i][j].template get<float>(e);
+                        // (columns behind the last are zeros: what was summed
+                        // for them is the last one's again)
+                        const bool in = whole || t.n + 16 * j + e < g.N;
+                        dg[j][e] = in ? v * acc[i0 + i][j + NI / 2][e] * da : 0.0f;
+                        du[j][e] = in ? v * a : 0.0f;
+                    }
+                auto put = [&](const f32x4 (&v)[NI / 2], int64_t at) {
+                    turn<NI / 2>(t.lds, v, [&](int row, int col, f32x4 u) {
+                        const int32_t m = m0 + 16 * (i0 + i) + row, n = n0 + col;
+                        if (!whole && (m >= g.M || n >= F_pad)) return;
+                        float w[4] = {u[0], u[1], u[2], u[3]};
+                        store_pieces(d + m * 2 * F_pad + at + n, w);
+                    });
+                };
+                put(dg, 0);
+                put(du, F_pad);
             }
-            return;
         }
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI / 2; ++j) {
-                const int32_t m = t.m + 16 * i, n = t.n + 16 * j;
-                if (m >= g.M || n >= F_pad) continue;
-                Raw<T, 4> x;
-                x.load_upto(dy + m * ld_dy + n, (int64_t)g.N - n);
-                // (columns behind the last are zeros: their weights' rows are
-                // the last one's again, or not finite with it)
-                f32x4 first = acc[i][j], second = acc[i][j + NI / 2];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e >= g.N) first[e] = second[e] = 0.0f;
-                put(m, n, x, first, second);
-            }
-    }
-    __device__ __forceinline__ void put(int32_t m, int32_t n, const Raw<T, 4> &x,
-                                        const f32x4 &first, const f32x4 &second) const {
-        float dg[4], du[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float a, da;
-            activation<ACT>(first[e], a, da);
-            const float v = x.template get<float>(e);
-            dg[e] = v * second[e] * da;
-            du[e] = v * a;
-        }
-        bf16_t *to = d + m * 2 * F_pad + n;
-        store_pieces(to, dg);
-        store_pieces(to + F_pad, du);
     }
     // (a piece is what is left, rounded; then it is taken off)
     __device__ __forceinline__ void store_pieces(bf16_t *to, float (&v)[4]) const {

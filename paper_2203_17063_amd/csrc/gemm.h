@@ -91,7 +91,27 @@ struct GemmTile {
     int32_t batch, split;
     int32_t k;        // elements along k that the tile has summed
     int32_t tile_n;   // 64-column tile of the wave
+    f32x4 *lds;       // 4 KiB of the wave's own
 };
+
+// Turns 16 rows of a wave's block round: quads of a column of lanes (v[j]: row
+// lane & 15, columns 16 j + 4 (lane / 16)) become rows, f(row, column, quad) for
+// NQ neighbouring rows of lanes after each other, so that 16 lanes (NQ = 4: 8
+// for NQ = 2) reach a row's 16 NQ columns with one access.  Chunks are stored at
+// chunk ^ row, free of conflicts.
+template <int NQ, class F>
+__device__ __forceinline__ void turn(f32x4 *lds, const f32x4 (&v)[NQ], F &&f) {
+    constexpr int CH = NQ * 4;
+    const int lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) lds[c * CH + ((j * 4 + q) ^ (c & (CH - 1)))] = v[j];
+    const int first = lane / CH, chunk = lane % CH;
+#pragma unroll
+    for (int it = 0; it < NQ; ++it) {
+        const int row = it * (64 / CH) + first;
+        f(row, chunk * 4, lds[row * CH + (chunk ^ (row & (CH - 1)))]);
+    }
+}
 
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -336,7 +356,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int
         }
     }
     const int n_wave = n0 + wn * (Epi::kPair ? 32 : 64);
-    epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64}, g, acc);
+    __syncthreads();  // nobody reads LDS any more: 4 KiB of it are the wave's
+    f32x4 *lds = reinterpret_cast<f32x4 *>(BM == 256 || wave < 4 ? s_a0 : s_a1) +
+                 (BM == 256 ? wave : wave & 3) * 256;
+    epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64, lds}, g, acc);
 }
 
 template <int BM, int BN, int WM, int WN, class Epi>
@@ -501,52 +524,43 @@ struct BlockOut {
                                            f32x4 (&acc)[MI][NI]) const {
         if (o.skip_empty && t.k == 0) return;
         const float by = o.scale ? o.scale[t.batch] : 1.0f;
-        const int32_t n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
-        const bool whole = n0 + 16 * NI <= g.N;
+        const int32_t m0 = t.m & ~15, n0 = t.n - (threadIdx.x >> 4 & 3) * 4;
+        const bool whole = m0 + 16 * MI <= g.M && n0 + 16 * NI <= g.N;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int32_t m = t.m + 16 * i;
-            if (m >= g.M) continue;
-            const bool last = o.second && m >= o.second;
-            T *to = (T *)(last ? o.out2 : o.out) + t.batch * o.batch_stride +
-                    (int64_t)(last ? m - o.second : m) * o.ld + t.n;
-            const float *sums =
-                MODE == kFromSums ? o.sums + ((int64_t)t.batch * g.M + m) * g.N + t.n : nullptr;
-            if (whole) row<NI, true>(to, sums, acc[i], by, 0);
-            else row<NI, false>(to, sums, acc[i], by, g.N - t.n);
-        }
+        for (int i = 0; i < MI; ++i)
+            turn<NI>(t.lds, acc[i], [&](int row, int col, f32x4 v) {
+                const int32_t m = m0 + 16 * i + row, n = n0 + col;
+                if (whole) put<true>(t, g, m, n, v * by);
+                else if (m < g.M && n < g.N) put<false>(t, g, m, n, v * by);
+            });
     }
-    template <int NI, bool WHOLE>
-    __device__ __forceinline__ void row(T *to, const float *sums, const f32x4 (&v)[NI], float by,
-                                        int32_t n) const {
-        Raw<T, 4> old[NI];
-        Raw<float, 4> sum[NI];
-        const bool add = MODE == kAdd || (MODE == kFromSums && o.add);
+    template <bool WHOLE>
+    __device__ __forceinline__ void put(const GemmTile &t, const GemmArgs &g, int32_t m, int32_t n,
+                                        f32x4 v) const {
+        const bool last = o.second && m >= o.second;
+        T *to = (T *)(last ? o.out2 : o.out) + t.batch * o.batch_stride +
+                (int64_t)(last ? m - o.second : m) * o.ld + n;
+        const int32_t w = g.N - n;
+        if (MODE == kFromSums) {
+            const float *from = o.sums + ((int64_t)t.batch * g.M + m) * g.N + n;
+            Raw<float, 4> sum;
+            if (WHOLE) sum.load(from);
+            else sum.load_upto(from, w);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            if (add) {
-                if (WHOLE) old[j].load(to + 16 * j);
-                else old[j].load_upto(to + 16 * j, n - 16 * j);
-            }
-            if (MODE == kFromSums) {
-                if (WHOLE) sum[j].load(sums + 16 * j);
-                else sum[j].load_upto(sums + 16 * j, n - 16 * j);
-            }
+            for (int e = 0; e < 4; ++e) v[e] += sum.template get<float>(e);
         }
+        if (MODE == kAdd || (MODE == kFromSums && o.add)) {
+            Raw<T, 4> old;
+            if (WHOLE) old.load(to);
+            else old.load_upto(to, w);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = v[j][e] * by;
-                if (MODE == kFromSums) y[e] += sum[j].template get<float>(e);
-                if (add) y[e] += old[j].template get<float>(e);
-            }
-            Raw<T, 4> x;
-            x.set_all(y);
-            if (WHOLE) x.store(to + 16 * j);
-            else x.store_upto(to + 16 * j, n - 16 * j);
+            for (int e = 0; e < 4; ++e) v[e] += old.template get<float>(e);
         }
+        Raw<T, 4> x;
+        const float y[4] = {v[0], v[1], v[2], v[3]};
+        x.set_all(y);
+        if (WHOLE) x.store(to);
+        else x.store_upto(to, w);
     }
 };
 
