@@ -604,21 +604,34 @@ def _tensors(grads, out, P):
     if device < 0:
         raise ValueError("grads must be on the GPU")
     data, at, size = bytearray(count * _TENSOR.size), 0, _TENSOR.size
+    pack, types = _TENSOR.pack_into, _TYPES
     for g, o in zip(grads, outs):
         if g.get_device() != device:
             raise ValueError("grads must be on one GPU")
-        n, stride = _worker_parts(g, P, "a gradient")
-        if o is None:
-            _TENSOR.pack_into(data, at, g.data_ptr(), 0, n, stride, 0, _type(g, "a gradient"), 0)
+        shape = g.shape
+        if P is None:
+            n, stride = _contiguous(g, "a gradient").numel(), 0
+        elif len(shape) and shape[0] == P and g.is_contiguous():
+            n = stride = g.numel() // P
         else:
-            if o.shape != g.shape:
+            n, stride = _worker_parts(g, P, "a gradient")
+        kind = types.get(g.dtype)
+        if kind is None:
+            _type(g, "a gradient")
+        if o is None:
+            pack(data, at, g.data_ptr(), 0, n, stride, 0, kind, 0)
+        else:
+            if o.shape != shape:
                 raise ValueError("an output must have its gradient's shape %s, not %s" %
-                                 (tuple(g.shape), tuple(o.shape)))
+                                 (tuple(shape), tuple(o.shape)))
             if o.get_device() != device:
                 raise ValueError("grads and out must be on one GPU")
-            _TENSOR.pack_into(data, at, g.data_ptr(), o.data_ptr(), n, stride,
-                              _worker_parts(o, P, "an output")[1], _type(g, "a gradient"),
-                              _type(o, "an output"))
+            out_kind = types.get(o.dtype)
+            if out_kind is None:
+                _type(o, "an output")
+            pack(data, at, g.data_ptr(), o.data_ptr(), n, stride,
+                 stride if o.is_contiguous() else _worker_parts(o, P, "an output")[1], kind,
+                 out_kind)
         at += size
     return (E.ecc_tensor_t * count).from_buffer(data), grads[0]
 
