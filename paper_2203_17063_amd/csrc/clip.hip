@@ -18,6 +18,7 @@
 // into the work buffer first, so that nothing is copied from the host and a
 // captured call holds all that it needs.
 #include <algorithm>
+#include <new>
 #include <vector>
 
 #include "lm_common.h"
@@ -471,9 +472,15 @@ ecc_status_t ecc_clip_grads(int32_t P, int32_t count, const ecc_tensor_t *h_tens
     ECC_ARG(d_norms && d_work, "NULL pointer");
     ECC_ARG((uintptr_t)d_norms % 8 == 0 && (uintptr_t)d_work % 16 == 0, "an array is not aligned");
     const Cut cut = make_cut(P, count, h_tensors);
-    ECC_ARG(!outputs_meet(P, count, h_tensors, span_of(d_work, cut.bytes(P, count)),
-                          span_of(d_norms, 8 * (int64_t)P)),
-            "outputs overlap each other, another gradient, the norms or the work buffer");
+    bool meet = true;
+    try {
+        meet = outputs_meet(P, count, h_tensors, span_of(d_work, cut.bytes(P, count)),
+                            span_of(d_norms, 8 * (int64_t)P));
+    } catch (const std::bad_alloc &) {
+        set_error("out of host memory");
+        return ECC_ERR_ALLOC;
+    }
+    ECC_ARG(!meet, "outputs overlap each other, another gradient, the norms or the work buffer");
     return run(P, count, h_tensors, cut, true, max_norm, nonfinite == ECC_CLIP_ZERO, d_norms,
                d_work, (hipStream_t)hip_stream);
 }

@@ -315,6 +315,69 @@ def test_on_another_stream_and_in_a_graph():
             assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_one_gradient():
+    """Either gradient alone is what both calls together give."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("cross entropy, one gradient")
+    P, n, D, V = 2, 70, 100, 333
+    for dtype, kind in ((BF16, E.ECC_BF16), (F32, E.ECC_F32)):
+        h, table, y, w = _inputs(P * n, D, V, dtype, 13)
+        want = lm.cross_entropy(h, table, y, w, P=P)
+        a = E.ecc_cross_entropy_t(n, V, D, P, kind, kind, 0, h.data_ptr(), D, table.data_ptr(), D,
+                                  y.data_ptr(), w.data_ptr(), 1.0)
+        work = torch.empty(E.ecc_cross_entropy_work_size(a, 1), dtype=torch.uint8, device="cuda")
+        stream = torch.cuda.current_stream().cuda_stream
+        for which in (1, 2):
+            loss = torch.full_like(want[0], math.nan)
+            dh = torch.full_like(want[1], math.nan) if which == 1 else None
+            dt = torch.full_like(want[2], math.nan) if which == 2 else None
+            E.ecc_cross_entropy(a, loss, dh, D, dt, D, V * D, 0, work, stream)
+            assert torch.equal(loss, want[0])
+            assert torch.equal(*((dh, want[1]) if which == 1 else (dt, want[2])))
+
+
+def test_single_rows_and_far_rows():
+    """A vector and its label, and rows further apart than 32 bits reach."""
+    lm = _lm()
+    announce("cross entropy, single and far rows")
+    for dtype in (BF16, F32):
+        h, table, y, w = _inputs(40, 64, 150, dtype, 14)
+        y.clamp_(0, 149)
+        want = lm.cross_entropy(h[3], table, y[3])
+        assert want[0].shape == () and want[1].shape == (64,)
+        assert torch.equal(want[1], lm.cross_entropy(h[3:4], table, y[3:4])[1][0])
+    h, table, y, w = _inputs(40, 64, 40, BF16, 15)
+    want = lm.cross_entropy(h, table, y, w)
+    pitch = (1 << 27) + 8
+    far = torch.empty(40 * pitch, dtype=BF16, device="cuda").view(40, pitch)
+    wide = [far[:, 64 * i:64 * (i + 1)] for i in range(4)]
+    wide[0].copy_(h)
+    wide[1].copy_(table)
+    got = lm.cross_entropy(wide[0], wide[1], y, w, dh=wide[2], dtable=wide[3][None])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_alike_weights():
+    """Weights that are all alike are a factor of the sums: a label's term, near
+    the weight in every row of a model that knows nothing yet, is off by no
+    common half step of bf16."""
+    lm = _lm()
+    announce("cross entropy, alike weights")
+    N, D, V = 512, 128, 2000
+    h, table, y, _ = _inputs(N, D, V, BF16, 16, size=0.1)
+    y.random_(0, V, generator=torch.Generator(device="cuda").manual_seed(1))
+    for value in (1.0 / 515, 0.37, 3.0):
+        w = torch.full((N,), value, device="cuda")
+        _, dh, dt = _check(h, table, y, w)
+        want = _reference(h, table, y, w, 1.0, 1, BF16)
+        for got, (exact, _) in ((dh, want[1]), (dt, want[2])):
+            # rounding the result leaves 2^-8 / sqrt(3) at most, and the terms
+            # that are not labels as much of a small share
+            error = (got.double() - exact).norm() / exact.norm()
+            assert error <= 2.0 ** -8 / math.sqrt(3) * 1.1, float(error)
+
+
 def test_work_buffers():
     from paper_2203_17063_amd import capi as E
     lm = _lm()

@@ -286,6 +286,54 @@ def test_on_another_stream_and_in_a_graph():
             assert torch.equal(y, want_y) and all(torch.equal(got[i], want[i]) for i in got)
 
 
+def test_single_rows_and_far_rows():
+    """A vector, rows around the number that is taken without packing, and rows
+    further apart than 32 bits reach."""
+    lm = _lm()
+    announce("ffn, single and far rows")
+    for dtype in (BF16, F32):
+        for N in (15, 16, 17, 32, 33, 48, 64, 65):
+            x, wg, wu, _ = _inputs(N, 200, 90, dtype, 10)
+            within(lm.gated_ffn(x, wg, wu), *_forward(x, wg, wu, "silu"), N)
+        assert torch.equal(lm.gated_ffn(x[3], wg, wu), lm.gated_ffn(x[3:4], wg, wu)[0])
+        got = lm.gated_ffn_grad(x[3], wg, wu, lm.gated_ffn(x[3], wg, wu))
+        assert got["dx"].shape == (200,) and got["dw_gate"].shape == (1, 90, 200)
+    pitch = (1 << 27) + 8
+    for N in (40, 70):
+        x, wg, wu, dy = _inputs(N, 64, 40, BF16, 11)
+        y, want = lm.gated_ffn(x, wg, wu), lm.gated_ffn_grad(x, wg, wu, dy)
+        far = torch.empty(N * pitch, dtype=BF16, device="cuda").view(N, pitch)
+        wide = [far[:, 64 * i:64 * (i + 1)] for i in range(6)]
+        wide[0].copy_(x)
+        wide[1][:40].copy_(wg)
+        wide[2][:40].copy_(wu)
+        wide[3][:, :40].copy_(dy)
+        args = wide[0], wide[1][:40], wide[2][:40]
+        assert torch.equal(lm.gated_ffn(*args, out=wide[4][:, :40]), y)
+        got = lm.gated_ffn_grad(*args, wide[3][:, :40], dx=wide[5])
+        assert all(torch.equal(got[k], want[k]) for k in got)
+
+
+def test_one_gradient():
+    """dx alone, and the weights' alone, are what both together give."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("ffn, one gradient")
+    P, n, D, F = 2, 70, 100, 90
+    for dtype, kind in ((BF16, E.ECC_BF16), (F32, E.ECC_F32)):
+        x, wg, wu, dy = _inputs(P * n, D, F, dtype, 12)
+        want = lm.gated_ffn_grad(x, wg, wu, dy, P=P)
+        a = E.ecc_ffn_t(n, D, F, P, kind, kind, E.ECC_ACT_SILU, x.data_ptr(), D, wg.data_ptr(), D,
+                        wu.data_ptr(), D)
+        work = torch.empty(E.ecc_ffn_work_size(a, 1), dtype=torch.uint8, device="cuda")
+        stream = torch.cuda.current_stream().cuda_stream
+        new = {k: torch.full_like(v, math.nan) for k, v in want.items()}
+        E.ecc_ffn_grad(a, dy, F, new["dx"], D, None, None, 0, 0, work, stream)
+        assert torch.equal(new["dx"], want["dx"])
+        E.ecc_ffn_grad(a, dy, F, None, 0, new["dw_gate"], new["dw_up"], F * D, 0, work, stream)
+        assert all(torch.equal(new[k], want[k]) for k in want)
+
+
 def test_work_buffers():
     """A work buffer full of NaN changes nothing, and neither does its place;
     buffers that do not hold are refused."""
