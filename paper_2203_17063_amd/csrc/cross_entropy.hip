@@ -248,6 +248,31 @@ struct LogitsOut {
     }
 };
 
+// The same from the parts of a product that is split along D: a wave per row
+// and 64 columns.
+__global__ __launch_bounds__(256) void k_ce_logits(LogitsOut out, const float *parts,
+                                                   int32_t splits, int32_t M, int32_t N,
+                                                   const int32_t *live, int32_t first) {
+    const int64_t wave = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+    const int32_t m = (int32_t)(wave / out.tiles), tile = (int32_t)(wave % out.tiles);
+    if (m >= M || m + first >= *live) return;
+    const int32_t lane = threadIdx.x & 63, n = tile * 64 + lane;
+    const int64_t ld4 = (N + 3) & ~3;
+    float v = 0.0f;
+    if (n < N) {
+        const float *p = parts + m * ld4 + n;
+        v = *p;
+        for (int32_t s = 1; s < splits; ++s) v += p[s * (int64_t)M * ld4];
+        v *= out.scale;
+        if (n == out.label[m]) out.picked[m] = v;
+    }
+    if (out.z) out.z[m * out.ld + n] = v;
+    const float most = wave_all(n < N ? v : -__builtin_inff(), OpMax());
+    const float from = most == -__builtin_inff() ? 0.0f : most;
+    const float sum = wave_all(n < N ? exp_fast(v - from) : 0.0f, OpSum());
+    if (lane == 0) out.stats[(int64_t)m * out.tiles + tile] = make_float2(most, sum);
+}
+
 struct RowTerms {
     float *most, *soft;  // softmax = exp(z - most) soft
 };
@@ -381,10 +406,10 @@ struct Plan {
     int np;                      // pieces of the operands
     int pz, pzt;                 // of dz for dh, for dE
     bool pack_table;
-    GemmShape shape_h, shape_e;
+    GemmShape shape_z, shape_h, shape_e;
     // offsets into the work buffer
     int64_t map, label, weight, factor, inside, live, ranges, counts, outside, table, table_t, h, h_t,
-        z, dz, dzt, stats, picked, terms, sums, parts[2], bytes;
+        z, dz, dzt, stats, picked, terms, sums, parts[2], parts_z, bytes;
 };
 
 Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
@@ -428,6 +453,8 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.h = take(p.np * 2 * p.R * p.Dp);
     p.stats = take(8 * p.R * p.tiles);
     p.picked = take(4 * p.R);
+    p.shape_z = gemm_shape(p.R, a->V, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+    p.parts_z = take(split_bytes(p.R, a->V, p.shape_z.splits, 1));
     if (gradient) {
         p.table_t = take(p.np * 2 * a->D * p.Vp);
         p.h_t = take(p.np * 2 * a->D * p.R);
@@ -610,7 +637,15 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         const LogitsOut logits{gradient ? (float *)(w + p.z) : nullptr, p.Vp, (float)a->scale,
                                (float2 *)(w + p.stats), p.tiles, rows.label + r0,
                                (float *)(w + p.picked)};
-        launch_gemm(g, logits, s);
+        if (p.shape_z.splits > 1) {
+            float *parts = (float *)(w + p.parts_z);
+            g.splits = p.shape_z.splits;
+            launch_tiles({Product{g, parts_alone(parts)}, {}}, 1, {p.shape_z, {}}, s);
+            hipLaunchKernelGGL(k_ce_logits, dim3((unsigned)((R * p.tiles + 3) / 4)), dim3(256), 0,
+                               s, logits, parts, g.splits, g.M, g.N, rows.live, g.m_lo);
+        } else {
+            launch_gemm(g, logits, s);
+        }
         RowArgs row{};
         row.first = (int32_t)r0;
         row.M = (int32_t)R;

@@ -145,6 +145,61 @@ struct FfnGradOut {
     }
 };
 
+// The same from the parts of two products that are split along D (few tiles, a
+// long sum): a thread per four columns of a row.
+struct FfnParts {
+    const float *g, *u;
+    int32_t splits, M, N;
+};
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void k_ffn_join(FfnParts p, FfnOut<T, ACT> out, int64_t quads) {
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= quads) return;
+    const int32_t per = (p.N + 3) / 4;
+    const int64_t m = i / per;
+    const int32_t n = (int32_t)(i - m * per) * 4;
+    const f32x4 g = sum_of_parts(p.g, p.splits, p.M, p.N, m, n);
+    const f32x4 u = sum_of_parts(p.u, p.splits, p.M, p.N, m, n);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a, da;
+        activation<ACT>(g[e], a, da);
+        v[e] = a * u[e];
+    }
+    Raw<T, 4> x;
+    x.set_all(v);
+    x.store_upto(out.y + m * out.ld + n, p.N - n);
+}
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void k_ffn_grad_join(FfnParts p, FfnGradOut<T, ACT> out,
+                                                       int64_t quads) {
+    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
+    if (i >= quads) return;
+    const int32_t per = (int32_t)(out.F_pad / 4);
+    const int64_t m = i / per;
+    const int32_t n = (int32_t)(i - m * per) * 4;
+    float dg[4] = {0, 0, 0, 0}, du[4] = {0, 0, 0, 0};
+    if (n < p.N) {
+        const f32x4 g = sum_of_parts(p.g, p.splits, p.M, p.N, m, n);
+        const f32x4 u = sum_of_parts(p.u, p.splits, p.M, p.N, m, n);
+        Raw<T, 4> x;
+        x.load_upto(out.dy + m * out.ld_dy + n, (int64_t)p.N - n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (n + e >= p.N) continue;
+            float a, da;
+            activation<ACT>(g[e], a, da);
+            const float v = x.template get<float>(e);
+            dg[e] = v * u[e] * da;
+            du[e] = v * a;
+        }
+    }
+    bf16_t *to = out.d + m * 2 * out.F_pad + n;
+    out.store_pieces(to, dg);
+    out.store_pieces(to + out.F_pad, du);
+}
+
 // ---------------------------------------------------------------------------
 // few rows (single tokens)
 // ---------------------------------------------------------------------------
@@ -294,7 +349,8 @@ struct Plan {
     int64_t N, n_pad, rows, Dp, Fp;
     int np, pd;                   // pieces of the operands, of dg and du
     bool pack_x, pack_gate, pack_up;
-    GemmShape shape_x, shape_w;
+    GemmShape shape_f, shape_x, shape_w;
+    int64_t parts_f[2];
     int64_t x, gate, up, x_t, w_t, d, d_t, parts[2], bytes;
 };
 
@@ -321,6 +377,9 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
     p.x = take(p.pack_x ? p.np * 2 * pad64(p.N) * p.Dp : 0);
     p.gate = take(p.pack_gate ? p.np * 2 * p.Fp * p.Dp : 0);
     p.up = take(p.pack_up ? p.np * 2 * p.Fp * p.Dp : 0);
+    p.shape_f = gemm_shape(p.N, a->F, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 2, true);
+    if (!gradient && p.N <= kFewRows) p.shape_f.splits = 1;
+    for (int64_t &at_f : p.parts_f) at_f = take(split_bytes(p.N, a->F, p.shape_f.splits, 1));
     if (gradient) {
         p.x_t = take(p.np * 2 * a->D * p.rows);
         p.w_t = take(p.np * 2 * a->D * 2 * p.Fp);
@@ -396,6 +455,19 @@ GemmArgs projections(const ecc_ffn_t *a, const Plan &p, char *w, hipStream_t s) 
     return g;
 }
 
+// Both projections into parts, where that is quicker.
+bool split_projections(GemmArgs g, const Plan &p, char *w, FfnParts &parts, hipStream_t s) {
+    if (p.shape_f.splits == 1) return false;
+    float *to[2] = {(float *)(w + p.parts_f[0]), (float *)(w + p.parts_f[1])};
+    g.splits = p.shape_f.splits;
+    GemmArgs u = g;
+    u.b.p = g.b2;
+    launch_tiles({Product{g, parts_alone(to[0])}, Product{u, parts_alone(to[1])}}, 2,
+                 {p.shape_f, p.shape_f}, s);
+    parts = FfnParts{to[0], to[1], g.splits, g.M, g.N};
+    return true;
+}
+
 template <typename F>
 void with_kind(const ecc_ffn_t *a, F &&f) {
     auto act = [&](auto t) {
@@ -459,9 +531,17 @@ ecc_status_t ecc_ffn_forward(const ecc_ffn_t *a, void *d_y, int64_t ld_y, void *
         return ECC_OK;
     }
     const GemmArgs g = projections(a, p, (char *)d_work, s);
+    FfnParts parts{};
+    const bool split = split_projections(g, p, (char *)d_work, parts, s);
     with_kind(a, [&](auto t, auto act) {
         using T = decltype(t);
-        launch_gemm(g, FfnOut<T, decltype(act)::value>{(T *)d_y, ld_y}, s);
+        constexpr int ACT = decltype(act)::value;
+        const FfnOut<T, ACT> out{(T *)d_y, ld_y};
+        const int64_t quads = p.N * ((a->F + 3) / 4);
+        if (split)
+            hipLaunchKernelGGL((k_ffn_join<T, ACT>), dim3((unsigned)((quads + 255) / 256)),
+                               dim3(256), 0, s, parts, out, quads);
+        else launch_gemm(g, out, s);
     });
     ECC_LAUNCH_CHECK();
     return ECC_OK;
@@ -529,11 +609,17 @@ ecc_status_t ecc_ffn_grad(const ecc_ffn_t *a, const void *d_dy, int64_t ld_dy, v
     const GemmArgs g = projections(a, p, w, s);
     bf16_t *d = (bf16_t *)(w + p.d);
     const int64_t plane = pad64(p.N) * 2 * p.Fp;
+    FfnParts halves{};
+    const bool split = split_projections(g, p, w, halves, s);
     with_kind(a, [&](auto t, auto act) {
         using T = decltype(t);
-        launch_gemm(g, FfnGradOut<T, decltype(act)::value>{(const T *)d_dy, ld_dy, d, p.Fp, plane,
-                                                           p.pd},
-                    s);
+        constexpr int ACT = decltype(act)::value;
+        const FfnGradOut<T, ACT> out{(const T *)d_dy, ld_dy, d, p.Fp, plane, p.pd};
+        const int64_t quads = p.N * (p.Fp / 4);
+        if (split)
+            hipLaunchKernelGGL((k_ffn_grad_join<T, ACT>), dim3((unsigned)((quads + 255) / 256)),
+                               dim3(256), 0, s, halves, out, quads);
+        else launch_gemm(g, out, s);
     });
     // the other order of everything: [Wg | Wu] transposed, as long as [dg | du],
     // x and [dg | du] with workers padded to multiples of 64 rows

@@ -630,8 +630,24 @@ inline void launch_large(const Product &p, hipStream_t s) {
     else typed(std::integral_constant<int, kWrite>{});
 }
 
-// Up to two products (count) of the given shapes; parts: work memory of
-// split_bytes for each.
+// Up to two products (count) of the given shapes, small ones in one launch.
+inline void launch_tiles(const Product (&p)[2], int count, const GemmShape (&shape)[2],
+                         hipStream_t s) {
+    if (count == 2 && !shape[0].large && !shape[1].large) {
+        TwoProducts t{};
+        t.p[0] = p[0];
+        t.p[1] = p[1];
+        t.first[0] = set_tiles<128, 128, MatrixOut>(t.p[0].g);
+        t.first[1] = t.first[0] + set_tiles<128, 128, MatrixOut>(t.p[1].g);
+        hipLaunchKernelGGL(k_gemm_two, dim3((unsigned)t.first[1]), dim3(512), 0, s, t);
+        return;
+    }
+    for (int i = 0; i < count; ++i)
+        if (shape[i].large) launch_large(p[i], s);
+        else launch_gemm_tile<128, 128, 4, 2>(p[i].g, p[i].out, s);
+}
+
+// The same into their matrices; parts: work memory of split_bytes for each.
 inline void launch_products(Product (&p)[2], int count, const GemmShape (&shape)[2],
                             float *const (&parts)[2], hipStream_t s) {
     TwoProducts t{};
@@ -642,20 +658,29 @@ inline void launch_products(Product (&p)[2], int count, const GemmShape (&shape)
         quads[i] = quads_to_join(p[i]);
         t.p[i] = p[i];
     }
-    if (count == 2 && !shape[0].large && !shape[1].large) {
-        t.first[0] = set_tiles<128, 128, MatrixOut>(t.p[0].g);
-        t.first[1] = t.first[0] + set_tiles<128, 128, MatrixOut>(t.p[1].g);
-        hipLaunchKernelGGL(k_gemm_two, dim3((unsigned)t.first[1]), dim3(512), 0, s, t);
-    } else {
-        for (int i = 0; i < count; ++i)
-            if (shape[i].large) launch_large(p[i], s);
-            else launch_gemm_tile<128, 128, 4, 2>(p[i].g, p[i].out, s);
-    }
+    launch_tiles(p, count, shape, s);
     t.first[0] = quads[0];
     t.first[1] = quads[0] + quads[1];
     if (t.first[1] > 0)
         hipLaunchKernelGGL(k_gemm_join, dim3((unsigned)((t.first[1] + 255) / 256)), dim3(256), 0, s,
                            t);
+}
+
+// The parts of a split product alone, [split][row][N rounded up to 4].
+inline MatrixOut parts_alone(float *parts) {
+    MatrixOut out{};
+    out.parts = parts;
+    return out;
+}
+// Four columns of a row of them, added in their order.
+__device__ __forceinline__ f32x4 sum_of_parts(const float *parts, int32_t splits, int64_t M,
+                                              int32_t N, int64_t m, int32_t n) {
+    const int64_t ld4 = (N + 3) & ~3;
+    const float *p = parts + m * ld4 + n;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+    for (int32_t s = 1; s < splits; ++s)
+        v += *reinterpret_cast<const f32x4 *>(p + s * M * ld4);
+    return v;
 }
 
 }  // namespace ecc
