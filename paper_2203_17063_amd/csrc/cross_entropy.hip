@@ -79,85 +79,115 @@ __global__ __launch_bounds__(kMapThreads) void k_ce_count(Positions q, Rows rows
     }
 }
 
+// A thread's positions from i on: labels and weights, and which count.
+struct Taken {
+    int32_t y[kMapRows];
+    float w[kMapRows];
+    uint32_t held;
+    __device__ __forceinline__ void load(const Positions &q, int64_t base, int64_t i) {
+#pragma unroll
+        for (int e = 0; e < kMapRows; ++e) {
+            y[e] = i + e < q.n ? q.labels[base + i + e] : -1;
+            w[e] = q.weight && i + e < q.n ? q.weight[base + i + e] : 1.0f;
+        }
+        held = 0;
+#pragma unroll
+        for (int e = 0; e < kMapRows; ++e)
+            if (y[e] >= 0 && y[e] < q.V && w[e] != 0.0f) held |= 1u << e;
+    }
+};
+
 // Every worker's rows in order, each worker's from a multiple of 64 on: a
-// workgroup per worker, which first adds up the counts of those before it.
+// workgroup per worker, which first adds up the counts of those before it, and
+// looks whether its weights are all alike.
 __global__ __launch_bounds__(kMapThreads) void k_ce_map(Positions q, Rows rows, int32_t P,
                                                         int64_t capacity, float scale,
                                                         float *loss) {
-    __shared__ int s_sum[kMapThreads / 64 + 1];
-    __shared__ float s_least[kMapThreads / 64], s_most[kMapThreads / 64];
+    constexpr int kWaves = kMapThreads / 64;
+    __shared__ int s_sum[kWaves];
+    __shared__ float s_least[kWaves], s_most[kWaves];
     __shared__ int s_odd;   // a weight that is NaN
-    if (threadIdx.x == 0) s_odd = 0;
-    float least = __builtin_inff(), most = -__builtin_inff();
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int32_t p = blockIdx.x;
+    const int64_t base = p * q.n, step = kMapThreads * kMapRows;
+    if (threadIdx.x == 0) s_odd = 0;
     int before = 0;
     for (int32_t i = threadIdx.x; i < p; i += kMapThreads) before += rows.counts[i];
     before = wave_scan(before);
     if (lane == 63) s_sum[wave] = before;
-    __syncthreads();
-    before = 0;
-    for (int w = 0; w < kMapThreads / 64; ++w) before += s_sum[w];
-    __syncthreads();
-    int at = before;
-    const int64_t base = p * q.n;
-    for (int64_t i0 = 0; i0 < q.n; i0 += kMapThreads * kMapRows) {
-        const int64_t i = i0 + threadIdx.x * kMapRows;
-        uint32_t held = 0;
+    Taken t;
+    float least = __builtin_inff(), most = -__builtin_inff();
+    bool odd = false;
+    for (int64_t i = threadIdx.x * kMapRows; i < q.n; i += step) {
+        t.load(q, base, i);
 #pragma unroll
         for (int e = 0; e < kMapRows; ++e)
-            if (i + e < q.n) {
-                if (q.counts(base + i + e)) held |= 1u << e;
-                else loss[base + i + e] = 0.0f;
-            }
-        const int mine = __popc(held), upto = wave_scan(mine);
-        if (lane == 63) s_sum[wave] = upto;
-        __syncthreads();
-        int row = at + upto - mine;
-        for (int w = 0; w < kMapThreads / 64; ++w) {
-            if (w < wave) row += s_sum[w];
-            at += s_sum[w];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kMapRows; ++e)
-            if (held >> e & 1) {
-                const int64_t from = base + i + e;
-                rows.map[row] = (int32_t)from;
-                rows.label[row] = q.labels[from];
-                const float w = q.weight ? q.weight[from] : 1.0f;
-                rows.weight[row] = w;
-                rows.factor[row] = w * scale;
-                least = fminf(least, w);
-                most = fmaxf(most, w);
-                if (w != w) s_odd = 1;
-                ++row;
+            if (t.held >> e & 1) {
+                least = fminf(least, t.w[e]);
+                most = fmaxf(most, t.w[e]);
+                odd = odd || t.w[e] != t.w[e];
             }
     }
-    const int end = (at + 63) & ~63;
-    if (threadIdx.x == 0) rows.ranges[p] = make_int2(before, end);
-    const bool last = p == P - 1;
-    if (last && threadIdx.x == 0) *rows.live = end;
-    for (int64_t r = at + threadIdx.x; r < (last ? capacity : end); r += kMapThreads) {
-        rows.map[r] = -1;
-        rows.label[r] = -1;
-        rows.weight[r] = rows.factor[r] = 0.0f;
-    }
-    // weights that are all alike become a factor of the whole sum
     for (int d = 32; d; d >>= 1) {
         least = fminf(least, __shfl_xor(least, d, 64));
         most = fmaxf(most, __shfl_xor(most, d, 64));
     }
     if (lane == 0) s_least[wave] = least, s_most[wave] = most;
     __syncthreads();
-    for (int w = 0; w < kMapThreads / 64; ++w) {
+    if (odd) s_odd = 1;
+    before = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        before += s_sum[w];
         least = fminf(least, s_least[w]);
         most = fmaxf(most, s_most[w]);
     }
+    __syncthreads();
+    // weights that are all alike become a factor of the whole sum
     const bool alike = least == most && !s_odd;
-    if (threadIdx.x == 0) rows.outside[p] = alike ? least * scale : 1.0f;
-    for (int r = before + threadIdx.x; r < end; r += kMapThreads)
-        rows.inside[r] = alike || r >= at ? 1.0f : rows.factor[r];
+    int at = before;
+    for (int64_t i0 = 0; i0 < q.n; i0 += step) {
+        const int64_t i = i0 + threadIdx.x * kMapRows;
+        // (of up to one step, the positions are those at hand)
+        if (q.n > step) t.load(q, base, i);
+        else if (i >= q.n) t.held = 0;
+        const int mine = __popc(t.held), upto = wave_scan(mine);
+        if (lane == 63) s_sum[wave] = upto;
+        __syncthreads();
+        int row = at + upto - mine;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) row += s_sum[w];
+            at += s_sum[w];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kMapRows; ++e) {
+            const int64_t from = base + i + e;
+            if (t.held >> e & 1) {
+                const float factor = t.w[e] * scale;
+                rows.map[row] = (int32_t)from;
+                rows.label[row] = t.y[e];
+                rows.weight[row] = t.w[e];
+                rows.factor[row] = factor;
+                rows.inside[row] = alike ? 1.0f : factor;
+                ++row;
+            } else if (i + e < q.n) {
+                loss[from] = 0.0f;
+            }
+        }
+    }
+    const int end = (at + 63) & ~63;
+    const bool last = p == P - 1;
+    if (threadIdx.x == 0) {
+        rows.ranges[p] = make_int2(before, end);
+        rows.outside[p] = alike ? least * scale : 1.0f;
+        if (last) *rows.live = end;
+    }
+    for (int64_t r = at + threadIdx.x; r < (last ? capacity : end); r += kMapThreads) {
+        rows.map[r] = -1;
+        rows.label[r] = -1;
+        rows.weight[r] = rows.factor[r] = 0.0f;
+        rows.inside[r] = 1.0f;
+    }
 }
 
 // Zeros for the rows of dh that do not count: positions first .. + count - 1,

@@ -159,21 +159,20 @@ __device__ __forceinline__ void phase_end() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int BM, int BN, int WM, int WN, class Epi>
+template <int BM, int BN, int WM, int WN, int STAGES, class Epi>
 __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int block,
                                           int blocks) {
     constexpr int NW = WM * WN;
     constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
     constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // loads of 8 rows a wave
     static_assert(BN / WN == 64, "a wave's columns: 64, or 32 of each of a pair");
-    // (four arrays: the compiler tells the loads of one buffer from the reads
-    // of the other by their names)
     // (separate arrays: the compiler tells the loads into one from the reads of
     // another by their names)
-    constexpr int kA = BM * kGemmK, kB = BN * kGemmK, kSmall = BM == 256 ? 8 : 1;
+    constexpr int kA = BM * kGemmK, kB = BN * kGemmK;
+    constexpr bool kThree = BM == 256, kFour = STAGES == 4;
     __shared__ __attribute__((aligned(1024))) uint16_t s_a0[kA], s_a1[kA], s_b0[kB], s_b1[kB],
-        s_b2[kB], s_a2[kSmall == 1 ? kA : 8], s_a3[kSmall == 1 ? kA : 8],
-        s_b3[kSmall == 1 ? kB : 8];
+        s_b2[kThree || kFour ? kB : 8], s_a2[kFour ? kA : 8], s_a3[kFour ? kA : 8],
+        s_b3[kFour ? kB : 8];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -326,6 +325,22 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int
             }
             wait_loads<0>();
             if (!late) phase_end();
+        } else if constexpr (STAGES == 2) {
+            // (two steps at most)
+            load_a(s_a0);
+            load_b(s_b0);
+            load_a(s_a1);
+            load_b(s_b1);
+            wait_loads<LA + LB>();
+            phase_end();
+            read(s_a0, s_b0);
+            multiply();
+            wait_loads<0>();
+            phase_end();
+            if (steps > 1) {
+                read(s_a1, s_b1);
+                multiply();
+            }
         } else {
             load_a(s_a0);
             load_b(s_b0);
@@ -362,9 +377,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int
     epi.finish(GemmTile{m0 + ra, n_wave + q * 4, batch, split, k1 - k0, n_wave / 64, lds}, g, acc);
 }
 
-template <int BM, int BN, int WM, int WN, class Epi>
+template <int BM, int BN, int WM, int WN, int STAGES, class Epi>
 __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmArgs g, Epi epi) {
-    gemm_tile<BM, BN, WM, WN>(g, epi, blockIdx.x, gridDim.x);
+    gemm_tile<BM, BN, WM, WN, STAGES>(g, epi, blockIdx.x, gridDim.x);
 }
 
 // Tiles of BM x BN (of pairs: BN / 2 columns): their number.
@@ -375,12 +390,24 @@ int64_t set_tiles(GemmArgs &g) {
     g.tiles_n = (g.N + cols - 1) / cols;
     return (int64_t)g.tiles_m * g.tiles_n * g.batches * g.splits;
 }
-template <int BM, int BN, int WM, int WN, class Epi>
-void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
+template <int BM, int BN, int WM, int WN, int STAGES, class Epi>
+void launch_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
     const int64_t grid = set_tiles<BM, BN, Epi>(g);
     if (grid > 0)
-        hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, Epi>), dim3((unsigned)grid),
+        hipLaunchKernelGGL((k_gemm<BM, BN, WM, WN, STAGES, Epi>), dim3((unsigned)grid),
                            dim3(64 * WM * WN), 0, s, g, epi);
+}
+template <class Epi>
+void launch_large_tiles(const GemmArgs &g, const Epi &epi, hipStream_t s) {
+    launch_tile<256, 256, 2, 4, 3>(g, epi, s);
+}
+template <class Epi>
+void launch_small_tiles(const GemmArgs &g, const Epi &epi, hipStream_t s) {
+    launch_tile<128, 128, 4, 2, 4>(g, epi, s);
+}
+template <class Epi>
+void launch_short_tiles(const GemmArgs &g, const Epi &epi, hipStream_t s) {
+    launch_tile<128, 128, 4, 2, 2>(g, epi, s);
 }
 
 // Tiles, and parts along k of a product whose tiles would leave CUs idle (the
@@ -389,12 +416,19 @@ void launch_gemm_tile(GemmArgs g, const Epi &epi, hipStream_t s) {
 // large tiles, 0.6 and 4 for small ones, and the join at 4 TB/s.  (M x N and
 // `steps` of all products, per batch.)  4,136 x 1,001 of 516 steps: 3 parts of
 // large tiles, 0.25 ms, against 0.65 ms for small tiles in one.
+// Products of one or two steps take short tiles instead: small ones of 64 KiB of
+// LDS, two to a CU, so that one's results are written while the other begins.
+// 5,000 rows x 2 x 2,178 columns of two steps: 18 us against 25 us; gradients of
+// 100,003 x 237 for each of 15 workers, of one: 329 us against 367 us.
 struct GemmShape {
     bool large;
     int32_t splits;
+    bool brief;
 };
+constexpr int kShortSteps = 2;
 inline GemmShape gemm_shape(int64_t M, int64_t N, int64_t steps, int64_t batches, bool may_split) {
-    GemmShape best{false, 1};
+    GemmShape best{false, 1, steps <= kShortSteps};
+    if (best.brief) return best;
     double least = 1e30;
     for (int large = 0; large < 2; ++large) {
         const int64_t tile = large ? 256 : 128;
@@ -403,7 +437,7 @@ inline GemmShape gemm_shape(int64_t M, int64_t N, int64_t steps, int64_t batches
             const double rounds = (double)((tiles * s + 255) / 256), part = (double)((steps + s - 1) / s);
             double us = rounds * (large ? 1.5 * part + 8.0 : 0.6 * part + 4.0);
             if (s > 1) us += 4.0 + (double)(s + 1) * batches * M * N * 4.0 / 4e6;
-            if (us < least) least = us, best = GemmShape{large != 0, (int32_t)s};
+            if (us < least) least = us, best = GemmShape{large != 0, (int32_t)s, false};
         }
     }
     return best;
@@ -411,11 +445,11 @@ inline GemmShape gemm_shape(int64_t M, int64_t N, int64_t steps, int64_t batches
 template <class Epi>
 void launch_gemm(GemmArgs g, const Epi &epi, hipStream_t s) {
     g.splits = 1;
-    if (gemm_shape(g.M, (int64_t)g.N * (Epi::kPair ? 2 : 1), (int64_t)g.K / kGemmK * g.nprod,
-                   g.batches, false)
-            .large)
-        launch_gemm_tile<256, 256, 2, 4>(g, epi, s);
-    else launch_gemm_tile<128, 128, 4, 2>(g, epi, s);
+    const GemmShape shape = gemm_shape(g.M, (int64_t)g.N * (Epi::kPair ? 2 : 1),
+                                       (int64_t)g.K / kGemmK * g.nprod, g.batches, false);
+    if (shape.brief) launch_short_tiles(g, epi, s);
+    else if (shape.large) launch_large_tiles(g, epi, s);
+    else launch_small_tiles(g, epi, s);
 }
 
 inline int64_t split_bytes(int64_t M, int64_t N, int64_t splits, int64_t batches) {
@@ -599,7 +633,7 @@ static __global__ __launch_bounds__(512) void k_gemm_two(TwoProducts t) {
     const int second = (int)blockIdx.x >= t.first[0];
     const Product &p = t.p[second];
     const int before = second ? (int)t.first[0] : 0;
-    gemm_tile<128, 128, 4, 2>(p.g, p.out, (int)blockIdx.x - before,
+    gemm_tile<128, 128, 4, 2, 4>(p.g, p.out, (int)blockIdx.x - before,
                               (int)(second ? t.first[1] : t.first[0]) - before);
 }
 static __global__ __launch_bounds__(256) void k_gemm_join(TwoProducts t) {
@@ -612,20 +646,20 @@ inline int64_t quads_to_join(const Product &p) {
     return p.g.splits > 1 ? (int64_t)p.g.batches * p.g.M * ((p.g.N + 3) / 4) : 0;
 }
 
-// A product of large tiles.
-inline void launch_large(const Product &p, hipStream_t s) {
+// A product of large or short tiles.
+inline void launch_blocks(const Product &p, bool brief, hipStream_t s) {
     const MatrixOut &o = p.out;
-    auto block = [&](auto t, auto mode) {
-        using B = BlockOut<decltype(t), decltype(mode)::value>;
-        launch_gemm_tile<256, 256, 2, 4>(p.g, B{o}, s);
+    auto tiles = [&](const auto &epi) {
+        if (brief) launch_short_tiles(p.g, epi, s);
+        else launch_large_tiles(p.g, epi, s);
     };
     auto typed = [&](auto mode) {
-        if (o.type == ECC_F32) block(float{}, mode);
-        else block(bf16_t{}, mode);
+        constexpr int MODE = decltype(mode)::value;
+        if (o.type == ECC_F32) tiles(BlockOut<float, MODE>{o});
+        else tiles(BlockOut<bf16_t, MODE>{o});
     };
-    if (o.parts || o.row_map || o.row_scale)
-        launch_gemm_tile<256, 256, 2, 4>(p.g, o, s);
-    else if (o.sums) block(bf16_t{}, std::integral_constant<int, kFromSums>{});
+    if (o.parts || o.row_map || o.row_scale) tiles(o);
+    else if (o.sums) tiles(BlockOut<bf16_t, kFromSums>{o});
     else if (o.add) typed(std::integral_constant<int, kAdd>{});
     else typed(std::integral_constant<int, kWrite>{});
 }
@@ -633,7 +667,8 @@ inline void launch_large(const Product &p, hipStream_t s) {
 // Up to two products (count) of the given shapes, small ones in one launch.
 inline void launch_tiles(const Product (&p)[2], int count, const GemmShape (&shape)[2],
                          hipStream_t s) {
-    if (count == 2 && !shape[0].large && !shape[1].large) {
+    auto small = [&](int i) { return !shape[i].large && !shape[i].brief; };
+    if (count == 2 && small(0) && small(1)) {
         TwoProducts t{};
         t.p[0] = p[0];
         t.p[1] = p[1];
@@ -643,8 +678,8 @@ inline void launch_tiles(const Product (&p)[2], int count, const GemmShape (&sha
         return;
     }
     for (int i = 0; i < count; ++i)
-        if (shape[i].large) launch_large(p[i], s);
-        else launch_gemm_tile<128, 128, 4, 2>(p[i].g, p[i].out, s);
+        if (small(i)) launch_small_tiles(p[i].g, p[i].out, s);
+        else launch_blocks(p[i], shape[i].brief, s);
 }
 
 // The same into their matrices; parts: work memory of split_bytes for each.
