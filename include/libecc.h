@@ -838,14 +838,18 @@ ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64
  *              (both NULL: the loss alone).
  * Products are formed in fp32 from bf16 operands, or from fp32 ones to fp32's
  * precision (as products of three bf16 pieces each; operands must be finite,
- * and elements below 2^-117 lose bits).  dz is rounded to bf16 for a gradient
- * that is bf16 itself.  V up to ECC_CROSS_ENTROPY_MAX_VOCAB, D up to
- * ECC_CROSS_ENTROPY_MAX_DIM, P times n (rounded up to 64) below 2^31 - 1024, P * V * D
- * below about 2^36, else ECC_ERR_RANGE.  d_work: ecc_cross_entropy_work_size(a, 1)
- * bytes, or (a, 0) for the loss alone (-1 for a description that the call
- * refuses; the size depends on where the arrays lie). */
+ * and elements below 2^-117 lose bits).  For a gradient that is bf16 itself,
+ * what is rounded to bf16 before its product is softmax - [label]; the weights
+ * and the scale are factors in fp32, but for dE where a worker's weights differ:
+ * there they are rounded with it.  V up to ECC_CROSS_ENTROPY_MAX_VOCAB, D up to
+ * ECC_CROSS_ENTROPY_MAX_DIM, P times n (rounded up to 64) up to
+ * ECC_CROSS_ENTROPY_MAX_ROWS, P * V * D below about 2^36, else ECC_ERR_RANGE.
+ * d_work: ecc_cross_entropy_work_size(a, 1) bytes, or (a, 0) for the loss alone
+ * (-1 for a description that the call refuses; the size depends on where the
+ * arrays lie). */
 #define ECC_CROSS_ENTROPY_MAX_VOCAB 4194304
 #define ECC_CROSS_ENTROPY_MAX_DIM 65536
+#define ECC_CROSS_ENTROPY_MAX_ROWS 536870912
 typedef struct {
     int64_t n, V, D;
     int32_t P;
@@ -868,8 +872,8 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
 /* The gated feed-forward block up to its inner width, for P * n rows x of D
  * elements and two matrices of F rows of D:
  *   g = x Wg^T,  u = x Wu^T,  y = act(g) u
- * (act(g) = g / (1 + exp(-g)), or g (1 + erf(g / sqrt 2)) / 2), and its
- * gradients for a given dy:
+ * (act(g) = g / (1 + exp(-g)), or g (1 + erf(g / sqrt 2)) / 2 with erf within
+ * 1.5e-7), and its gradients for a given dy:
  *   dg = dy u act'(g),  du = dy act(g)
  *   dx = dg Wg + du Wu,  dWg_p = dg_p^T x_p,  dWu_p = du_p^T x_p
  * (g and u are formed again).  x, Wg, Wu, y, dy and dx are of `type`, ECC_F32

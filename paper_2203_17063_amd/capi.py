@@ -35,6 +35,7 @@ ECC_NORM_MAX_DIM = 16384
 ECC_DISTILL_MAX_TOP = 1024
 ECC_F64, ECC_F32, ECC_BF16, ECC_I32, ECC_I64 = 0, 1, 2, 3, 4
 ECC_CROSS_ENTROPY_MAX_VOCAB, ECC_CROSS_ENTROPY_MAX_DIM = 1 << 22, 1 << 16
+ECC_CROSS_ENTROPY_MAX_ROWS = 1 << 29
 ECC_ACT_SILU, ECC_ACT_GELU = 0, 1
 ECC_FFN_MAX_DIM, ECC_FFN_MAX_ROWS = 1 << 20, 1 << 22
 ECC_CLIP_KEEP, ECC_CLIP_ZERO = 0, 1

@@ -513,8 +513,10 @@ ecc_status_t check(const ecc_cross_entropy_t *a) {
             "the table's gradient must be fp32 or of the operands' type");
     ECC_ARG(a->scale == a->scale && __builtin_fabs(a->scale) <= 3e38, "the scale must be finite");
     ECC_ARG(a->ld_h >= a->D && a->ld_table >= a->D, "a leading dimension is below D");
+    // (rows: grids of fewer than 2^32 threads, k_ce_rows' being the largest)
     if (a->V > ECC_CROSS_ENTROPY_MAX_VOCAB || a->D > ECC_CROSS_ENTROPY_MAX_DIM ||
-        a->n > (int64_t(1) << 31) || (__int128)a->P * pad64(a->n) >= (int64_t(1) << 31) - 1024 ||
+        a->n > ECC_CROSS_ENTROPY_MAX_ROWS ||
+        (__int128)a->P * pad64(a->n) > ECC_CROSS_ENTROPY_MAX_ROWS ||
         a->ld_h >= (int64_t(1) << 40) || a->ld_table >= (int64_t(1) << 40) ||
         !gemm_in_range(a->V, a->D, a->P)) {
         set_error("the sizes are beyond what the library supports");

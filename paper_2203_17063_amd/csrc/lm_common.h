@@ -1,5 +1,5 @@
-// Shared by the language-model operators (embed.hip, norm.hip, distill.hip):
-// element types, accesses of several elements at any element alignment, and
+// Shared by the language-model operators (embed.hip, norm.hip, distill.hip,
+// ffn.hip, cross_entropy.hip, clip.hip): element types, accesses of several elements at any element alignment, and
 // the sums a wave or a workgroup forms.
 //
 // Sums are held in fp32 where the operands are fp32 or bf16 and in fp64 where

@@ -4,14 +4,15 @@ libecc called on the current stream.  No arithmetic runs here.
 
 The calls are not recorded for torch's differentiation: results of inputs that
 require gradients do not, and the gradients are the calls named *_grad (and
-distill's second result).
+further results of distill and cross_entropy).
 
 Rows (tokens, positions) may come with any number of leading dimensions as
 long as the last one is contiguous and the others collapse to rows of one
 stride.  Operands, outputs and work buffers of a call lie on one GPU, which
 need not be the current one.  Sums over rows and tokens are held in fp32, or
 fp64 where an operand or the result is fp64; a row's own sums (norms, softmax
-statistics) in fp32, or fp64 for rows of fp64.
+statistics) in fp32, or fp64 for rows of fp64; norms of whole gradients in fp64.
+cross_entropy and gated_ffn are products of fp32 or bf16 operands, not fp64.
 """
 from __future__ import annotations
 

@@ -71,6 +71,18 @@ def test_cross_entropy_refused(bad):
     assert E.ecc_last_error() != ""
 
 
+@pytest.mark.parametrize("P", [1, 64])
+def test_cross_entropy_rows(P):
+    # (a launch has fewer than 2^32 threads, some of them 64 for each row)
+    most = E.ECC_CROSS_ENTROPY_MAX_ROWS // P
+    assert E.ecc_cross_entropy_work_size(_ce(P=P, n=most, V=3, D=1), 1) > 20 * most * P
+    a = _ce(P=P, n=most + 1, V=3, D=1)
+    assert E.ecc_cross_entropy_work_size(a, 1) == -1
+    with pytest.raises(E.EccError) as e:
+        E.ecc_cross_entropy(a, 4 << 20, None, 0, None, 0, 0, 0, 1 << 30)
+    assert e.value.status == E.ECC_ERR_RANGE
+
+
 def test_cross_entropy_outputs_refused():
     a, work = _ce(), 1 << 32
     good = dict(d_loss=4 << 20, d_dh=5 << 20, ld_dh=64, d_dtable=6 << 20, ld_dtable=64,
