@@ -18,7 +18,11 @@
 // the term, unless a worker's weights are all alike and one factor does: a
 // label's term is near the weight in most rows of a model that learns, and
 // would be off by one and the same half step everywhere (0.0037 of dE).
-#include "gemm.h"
+//
+// Up to 64 rows of one worker take kernels of their own, which need no packed
+// and no transposed table (its two passes are most of such a call): 61 rows,
+// D 96, V 1,003, fp32: 23 us against 47 us, in three launches instead of seven;
+// 8 rows, D 4,096, V 128,000, bf16: 0.93 ms against 1.28 ms.
 #include "pack.h"
 
 namespace ecc {
@@ -257,6 +261,18 @@ struct LogitsOut {
                 stats[(int64_t)m * tiles + t.tile_n] = make_float2(most, sum);
         }
     }
+    // 64 columns of a row, one per lane.
+    __device__ __forceinline__ void row(int32_t m, int32_t tile, int32_t N, int32_t y,
+                                        float v) const {
+        const int32_t n = tile * 64 + (threadIdx.x & 63);
+        const bool in = n < N;
+        if (in && n == y) picked[m] = v;
+        if (z) z[m * ld + n] = in ? v : 0.0f;
+        const float most = wave_all(in ? v : -__builtin_inff(), OpMax());
+        const float from = most == -__builtin_inff() ? 0.0f : most;
+        const float sum = wave_all(in ? exp_fast(v - from) : 0.0f, OpSum());
+        if ((threadIdx.x & 63) == 0) stats[(int64_t)m * tiles + tile] = make_float2(most, sum);
+    }
     template <int NI, bool WHOLE>
     __device__ static __forceinline__ void sums_of(const f32x4 (&v)[NI], int32_t n, int32_t N,
                                                    float &most, float &sum) {
@@ -294,13 +310,8 @@ __global__ __launch_bounds__(256) void k_ce_logits(LogitsOut out, const float *p
         v = *p;
         for (int32_t s = 1; s < splits; ++s) v += p[s * (int64_t)M * ld4];
         v *= out.scale;
-        if (n == out.label[m]) out.picked[m] = v;
     }
-    if (out.z) out.z[m * out.ld + n] = v;
-    const float most = wave_all(n < N ? v : -__builtin_inff(), OpMax());
-    const float from = most == -__builtin_inff() ? 0.0f : most;
-    const float sum = wave_all(n < N ? exp_fast(v - from) : 0.0f, OpSum());
-    if (lane == 0) out.stats[(int64_t)m * out.tiles + tile] = make_float2(most, sum);
+    out.row(m, tile, N, out.label[m], v);
 }
 
 struct RowTerms {
@@ -426,6 +437,316 @@ __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// few rows of one worker
+// ---------------------------------------------------------------------------
+
+// The rows stay where they are (those that do not count have label -1), and
+// nothing is packed: the table is read once for the logits and once for dh, by
+// kernels that are bound by that and by their latency (1 row, D 3,268, V 49,125,
+// bf16: 92 us for 321 MB of logits' operands; gradients 233 us for 642 MB).
+struct FewArgs {
+    const void *h, *table;
+    int64_t ld_h, ld_table;
+    Positions q;
+    int64_t D;
+    LogitsOut out;
+    Rows rows;
+    float *loss;
+    float scale;
+};
+
+// What k_ce_map leaves, by a wave.
+__device__ __forceinline__ void few_rows(const FewArgs &a) {
+    const int32_t r = threadIdx.x & 63, n = (int32_t)a.q.n;
+    const bool held = r < n && a.q.counts(r);
+    const float w = held ? (a.q.weight ? a.q.weight[r] : 1.0f) : 0.0f;
+    const float least = -wave_all(held ? -w : -__builtin_inff(), OpMax());
+    const float most = wave_all(held ? w : -__builtin_inff(), OpMax());
+    const bool alike = least == most && !__any(w != w);
+    const float factor = w * a.scale;
+    a.rows.map[r] = held ? r : -1;
+    a.rows.label[r] = held ? a.q.labels[r] : -1;
+    a.rows.weight[r] = w;
+    a.rows.factor[r] = factor;
+    a.rows.inside[r] = alike ? 1.0f : factor;
+    if (r < n && !held) a.loss[r] = 0.0f;
+    if (r == 0) {
+        *a.rows.live = kTile;
+        *a.rows.outside = alike ? least * a.scale : 1.0f;
+    }
+}
+
+__global__ __launch_bounds__(64) void k_ce_few_rows(FewArgs a) { few_rows(a); }
+
+// Logits of 64 columns: four waves for 16 of them each, by two (fp32, which is
+// bound by its splitting: four) that share the elements along D in turn and add
+// up in LDS; then a wave per row.
+template <typename T>
+constexpr int kFewThreads = std::is_same_v<T, float> ? 1024 : 512;
+template <typename T, int MB>
+__global__ __launch_bounds__(kFewThreads<T>) void k_ce_few(FewArgs a) {
+    using S = FewStep<T>;
+    // (fp32 takes more registers: it is split where it is loaded)
+    constexpr int kParts = kFewThreads<T> / 256;
+    constexpr int kAhead = S::kPieces == 3 ? 4 / MB : MB == 4 ? 2 : 4;
+    __shared__ f32x4 s_acc[kParts][4][MB][64];
+    __shared__ __attribute__((aligned(16))) float s_z[16 * MB][68];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, q = lane >> 4;
+    const int32_t n = (int32_t)a.q.n, V = a.q.V, v0 = blockIdx.x * 64;
+    if (blockIdx.x == 0 && wave == kFewThreads<T> / 64 - 1) few_rows(a);
+    const int cols = wave & 3, part = wave >> 2;
+    const T *row = (const T *)a.table + min(v0 + cols * 16 + c, V - 1) * a.ld_table;
+    const T *mine[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) mine[i] = (const T *)a.h + min(i * 16 + c, n - 1) * a.ld_h;
+    f32x4 acc[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[i] = f32x4{0, 0, 0, 0};
+    for (int64_t k = part * S::kStep; k < a.D; k += kParts * kAhead * S::kStep) {
+        S w[kAhead], x[kAhead][MB];
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) {
+            const int64_t at = k + s * kParts * S::kStep + q * S::kLane;
+            w[s].load(row, at, a.D);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) x[s][i].load(mine[i], at, a.D);
+        }
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) {
+            bf16x8 fw[S::kFrags][S::kPieces];
+            w[s].frags(fw);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                bf16x8 fx[S::kFrags][S::kPieces];
+                x[s][i].frags(fx);
+#pragma unroll
+                for (int j = 0; j < S::kFrags; ++j)
+                    products<S::kPieces, S::kPieces>([&](int px, int pw) {
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[j][pw], fx[j][px],
+                                                                         acc[i], 0, 0, 0);
+                    });
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i) s_acc[part][cols][i][lane] = acc[i];
+    __syncthreads();
+    for (int t = wave; t < 4 * MB; t += kFewThreads<T> / 64) {
+        const int i = t >> 2;
+        f32x4 z = s_acc[0][t & 3][i][lane];
+#pragma unroll
+        for (int p = 1; p < kParts; ++p) z += s_acc[p][t & 3][i][lane];
+        *reinterpret_cast<f32x4 *>(&s_z[i * 16 + c][(t & 3) * 16 + q * 4]) = z * a.scale;
+    }
+    __syncthreads();
+    for (int32_t r = wave; r < n; r += kFewThreads<T> / 64)
+        a.out.row(r, blockIdx.x, V, a.q.labels[r], s_z[r][lane]);
+}
+
+// (four of the table's gradient)
+template <typename T>
+__device__ __forceinline__ void add_quad(T *to, f32x4 v, int64_t left, bool add) {
+    Raw<T, 4> x;
+    if (add) {
+        x.load_upto(to, left);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += x.template get<float>(e);
+    }
+    const float y[4] = {v[0], v[1], v[2], v[3]};
+    x.set_all(y);
+    x.store_upto(to, left);
+}
+
+// Workgroups of the gradients, about: what the CUs' LDS holds at a time.
+constexpr int few_blocks(int np, int pt) { return np == 3 ? 256 : pt == 3 ? 512 : 1024; }
+struct FewGrad {
+    const void *h, *table;
+    int64_t ld_h, ld_table;
+    int32_t n, V;
+    int64_t D;
+    const float *z;
+    int64_t ld_z;
+    RowArgs r;
+    float *dh;            // [splits][64][ld_dh], NULL: none
+    int64_t ld_dh;
+    void *dtable;         // NULL: none
+    int64_t ld_dtable;
+    int32_t type, add;
+    int32_t blocks_d, per;   // blocks along D; tiles of 64 columns of a split
+};
+constexpr int kFewPitch = 72;   // of a row of 64 in LDS: 16-byte accesses
+
+// Pieces of 8 values in LDS: rows `to` + 0 .. 7, a column.
+__device__ __forceinline__ void put_column(uint16_t *to, const float (&v)[8], int which,
+                                           bool split) {
+    Raw<bf16_t, 8> x;
+    set_piece(x, v, which, split);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[e * kFewPitch] = (uint16_t)(x.w[e / 2] >> (e & 1) * 16);
+}
+
+// Gradients, 64 elements along D for a split of the vocabulary's tiles: the
+// tile's softmax - [label] (FEW: of rows whose tiles are joined here) and the
+// table's elements lie in LDS in the orders that the two products want, dh's
+// sums stay in registers.  The next tile is under way meanwhile.
+template <typename T, int PT, bool FEW>
+__global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a) {
+    constexpr int NP = std::is_same_v<T, float> ? 3 : 1, kSize = kTile * kFewPitch;
+    __shared__ __attribute__((aligned(16))) uint16_t s_dz[NP][kSize], s_dzt[PT][kSize],
+        s_h[NP][kSize], s_e[NP][kSize];
+    const RowArgs &q = a.r;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, k8 = lane >> 4;
+    const int r = threadIdx.x >> 2, c16 = (threadIdx.x & 3) * 16;
+    // (an XCD's blocks are neighbours: rows' ends share lines of its L2)
+    const int32_t b = xcd_block(blockIdx.x, gridDim.x);
+    const int64_t d0 = (int64_t)(b % a.blocks_d) * kTile, left = a.D - d0 - c16;
+    const int32_t split = b / a.blocks_d;
+    const int32_t t0 = split * a.per, t1 = min(q.tiles, t0 + a.per);
+    const int32_t y = q.rows.label[r];
+    const bool held = y >= 0;
+    const float inside = q.rows.inside[r];
+    float most = 0.0f, soft = 0.0f;
+    if constexpr (FEW) {
+        float sum = 1.0f;
+        if (held) join_tiles(q.stats + (int64_t)r * q.tiles, q.tiles, threadIdx.x & 3, 4, most, sum);
+        soft = 1.0f / sum;
+        if (held && b == 0 && c16 == 0)
+            q.loss[r] = q.rows.weight[r] * ((most - q.picked[r]) + logf(sum));
+    } else if (held) {
+        most = q.out.most[r];
+        soft = q.out.soft[r];
+    }
+    const bool none = !__syncthreads_or(held);
+    if (a.dtable) {
+        Raw<T, 8> x[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x[i].load_upto((const T *)a.h + (held ? r * a.ld_h + d0 + c16 + i * 8 : 0),
+                           held ? left - i * 8 : 0);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[i].template get<float>(e);
+            for (int p = 0; p < NP; ++p)
+                put_column(s_h[p] + (c16 + i * 8) * kFewPitch + r, v, p, NP > 1);
+        }
+    }
+    Raw<float, 8> z[2];
+    Raw<T, 8> w[2];
+    auto fetch = [&](int32_t t) {
+        const int64_t v = (int64_t)t * kTile + r;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            z[i].load_upto(a.z + (held ? r * a.ld_z + t * kTile + c16 + i * 8 : 0), held ? 8 : 0);
+            const bool in = a.dh && v < a.V;
+            w[i].load_upto((const T *)a.table + (in ? v * a.ld_table + d0 + c16 + i * 8 : 0),
+                           in ? left - i * 8 : 0);
+        }
+    };
+    auto frag = [&](const uint16_t *s, int row, int kk) {
+        return *reinterpret_cast<const bf16x8 *>(s + row * kFewPitch + kk * 32 + k8 * 8);
+    };
+    const float by = *q.rows.outside;
+    f32x4 dh[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) dh[j] = f32x4{0, 0, 0, 0};
+    fetch(t0);
+    for (int32_t t = t0; t < t1; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float v[8], u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int32_t j = t * kTile + c16 + i * 8 + e;
+                float p = exp_fast(z[i].get<float>(e) - most) * soft;
+                if (j == y) p -= 1.0f;
+                v[e] = held && j < a.V ? p : 0.0f;
+                u[e] = v[e] * inside;
+            }
+            const int at = c16 + i * 8;
+            for (int p = 0; p < NP; ++p) {
+                Raw<bf16_t, 8> x;
+                set_piece(x, v, p, NP > 1);
+                *reinterpret_cast<Raw<bf16_t, 8> *>(s_dz[p] + r * kFewPitch + at) = x;
+            }
+            if (a.dtable)
+                for (int p = 0; p < PT; ++p)
+                    put_column(s_dzt[p] + at * kFewPitch + r, u, p, PT > 1);
+            if (a.dh) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = w[i].template get<float>(e);
+                for (int p = 0; p < NP; ++p)
+                    put_column(s_e[p] + at * kFewPitch + r, v, p, NP > 1);
+            }
+        }
+        if (t + 1 < t1) fetch(t + 1);
+        __syncthreads();
+        if (a.dh && wave * 16 < a.n) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    products<NP, NP>([&](int pz, int pw) {
+                        dh[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            frag(s_e[pw], j * 16 + c, kk), frag(s_dz[pz], wave * 16 + c, kk),
+                            dh[j], 0, 0, 0);
+                    });
+        }
+        if (a.dtable && !(a.add && none)) {
+            f32x4 de[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) de[j] = f32x4{0, 0, 0, 0};
+            for (int kk = 0; kk * 32 < a.n; ++kk)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    products<PT, NP>([&](int pz, int ph) {
+                        de[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            frag(s_h[ph], j * 16 + c, kk), frag(s_dzt[pz], wave * 16 + c, kk),
+                            de[j], 0, 0, 0);
+                    });
+            const int32_t v = t * kTile + wave * 16 + c;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t d = d0 + j * 16 + k8 * 4;
+                if (v >= a.V || d >= a.D) continue;
+                if (a.type == ECC_F32) 
+                    add_quad((float *)a.dtable + v * a.ld_dtable + d, de[j] * by, a.D - d, a.add);
+                else
+                    add_quad((bf16_t *)a.dtable + v * a.ld_dtable + d, de[j] * by, a.D - d, a.add);
+            }
+        }
+        __syncthreads();
+    }
+    if (!a.dh) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4 *>(a.dh + ((int64_t)split * kTile + wave * 16 + c) * a.ld_dh + d0 +
+                                   j * 16 + k8 * 4) = dh[j];
+}
+
+// dh from its splits: 16 threads per four elements, each of every sixteenth
+// split, and then of their sums in order; zeros for the rows that do not count.
+template <typename T>
+__global__ __launch_bounds__(256) void k_ce_few_join(const float *parts, int64_t ld, int32_t splits,
+                                                     Rows rows, int64_t D, T *dh, int64_t ld_dh) {
+    __shared__ f32x4 s_sum[16][16];
+    const int64_t r = blockIdx.y, d = (blockIdx.x * (int64_t)16 + (threadIdx.x & 15)) * 4;
+    const int part = threadIdx.x >> 4;
+    f32x4 sum = {0, 0, 0, 0};
+    if (rows.map[r] >= 0 && d < D)
+        for (int32_t s = part; s < splits; s += 16)
+            sum += *reinterpret_cast<const f32x4 *>(parts + ((int64_t)s * kTile + r) * ld + d);
+    s_sum[part][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (part || d >= D) return;
+    for (int p = 1; p < min(16, splits); ++p) sum += s_sum[p][threadIdx.x];
+    sum *= rows.factor[r];
+    const float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    Raw<T, 4> x;
+    x.set_all(v);
+    x.store_upto(dh + r * ld_dh + d, D - d);
+}
+
+// ---------------------------------------------------------------------------
 // sizes and work memory
 // ---------------------------------------------------------------------------
 
@@ -436,11 +757,32 @@ struct Plan {
     int np;                      // pieces of the operands
     int pz, pzt;                 // of dz for dh, for dE
     bool pack_table;
+    bool few;                    // one worker, up to kFewRows rows
+    bool tiles_z, pack_h;        // few rows: logits by tiles, of packed rows
+    int32_t blocks_d, splits, per;
     GemmShape shape_z, shape_h, shape_e;
     // offsets into the work buffer
     int64_t map, label, weight, factor, inside, live, ranges, counts, outside, table, table_t, h, h_t,
         z, dz, dzt, stats, picked, terms, sums, parts[2], parts_z, bytes;
 };
+
+// Do few rows' logits take gemm.h's tiles?  By the times that both take, in us:
+// k_ce_few takes so much per round of 256 workgroups and element of D for its
+// one, two or four blocks of 16 rows, which it reads again for every 64 columns;
+// tiles read the table at 5 bytes a ns, once they are under way, but pack it
+// first if its rows are fp32 or no multiple of 64.  bf16, 64 rows, D 4,096, V
+// 128,000: 590 us and 223 us; 1 row, D 1,024, V 1,000: 13 us and 20 us, with the
+// loss.  fp32, 64 rows: D 4,096, V 1,000: 155 us and 40 us; D 2,048, V 32,000: 171
+// us and 283 us.
+bool few_by_tiles(const ecc_cross_entropy_t *a) {
+    const bool f32 = a->type == ECC_F32;
+    static constexpr double kTimes[2][3] = {{0.0075, 0.0115, 0.0165}, {0.013, 0.022, 0.036}};
+    const double each = kTimes[f32][a->n <= 16 ? 0 : a->n <= 32 ? 1 : 2];
+    const double few = 8.0 + (double)((a->V + 64 * 256 - 1) / (64 * 256)) * a->D * each;
+    const double table = (double)a->V * a->D * 1e-6;
+    const double tiles = f32 || a->D % 64 ? 24.0 + table * (f32 ? 3.6 : 1.4) : 19.0 + table * 0.4;
+    return tiles < few;
+}
 
 Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     Plan p{};
@@ -454,6 +796,7 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.np = f32 ? 3 : 1;
     p.pz = f32 ? 3 : 1;
     p.pzt = a->grad_type == ECC_F32 ? 3 : 1;
+    p.few = a->P == 1 && a->n <= kFewRows;
     p.pack_table = !as_it_lies(a->d_table, a->ld_table, a->D, a->type);
     const int64_t row = p.np * 2 * p.Dp * (gradient ? 2 : 1) + p.tiles * 8 + 16 +
                         (gradient ? 4 * p.Vp + 2 * p.pz * p.Vp + 2 * p.pzt * p.Vp : 0);
@@ -479,6 +822,29 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.ranges = take(8 * (int64_t)a->P);
     p.counts = take(4 * (int64_t)a->P);
     p.outside = take(4 * (int64_t)a->P);
+    if (p.few) {
+        p.tiles_z = few_by_tiles(a);
+        if (p.tiles_z) {
+            p.pack_h = !as_it_lies(a->d_h, a->ld_h, a->D, a->type);
+            p.h = take(p.pack_h ? p.np * 2 * p.R * p.Dp : 0);
+            p.table = take(p.pack_table ? p.np * 2 * p.Vp * p.Dp : 0);
+            p.shape_z = gemm_shape(a->n, a->V, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+            p.parts_z = take(split_bytes(a->n, a->V, p.shape_z.splits, 1));
+        }
+        p.stats = take(8 * p.R * p.tiles);
+        p.picked = take(4 * p.R);
+        if (gradient) {
+            p.z = take(4 * p.R * p.Vp);
+            p.terms = take(8 * p.R);
+            p.blocks_d = (int32_t)(p.Dp / kTile);
+            p.splits = std::min(p.tiles, std::max(1, few_blocks(p.np, p.pzt) / p.blocks_d));
+            p.per = (p.tiles + p.splits - 1) / p.splits;
+            p.splits = (p.tiles + p.per - 1) / p.per;
+            p.parts[0] = take(4 * p.splits * p.R * p.Dp);
+        }
+        p.bytes = at;
+        return p;
+    }
     p.table = take(p.pack_table ? p.np * 2 * p.Vp * p.Dp : 0);
     p.h = take(p.np * 2 * p.R * p.Dp);
     p.stats = take(8 * p.R * p.tiles);
@@ -529,6 +895,81 @@ ecc_status_t check(const ecc_cross_entropy_t *a) {
                 (uintptr_t)a->d_labels % 4 == 0 && (uintptr_t)a->d_weight % 4 == 0,
             "an array is not aligned");
     return ECC_OK;
+}
+
+// The logits' product, in one go or in parts along D.
+void launch_logits(GemmArgs g, const Plan &p, char *w, const LogitsOut &out, const int32_t *live,
+                   hipStream_t s) {
+    if (p.shape_z.splits == 1) {
+        launch_gemm(g, out, s);
+        return;
+    }
+    float *parts = (float *)(w + p.parts_z);
+    g.splits = p.shape_z.splits;
+    launch_tiles({Product{g, parts_alone(parts)}, {}}, 1, {p.shape_z, {}}, s);
+    const int64_t waves = (int64_t)g.M * p.tiles;
+    hipLaunchKernelGGL(k_ce_logits, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, out, parts,
+                       g.splits, g.M, g.N, live, g.m_lo);
+}
+
+template <typename T>
+void launch_few(const FewArgs &f, const Plan &p, char *w, const FewGrad &g, bool gradient, void *dh,
+                int64_t ld_dh, hipStream_t s) {
+    const int32_t tiles = p.tiles, splits = p.splits;
+    if (p.tiles_z) {
+        hipLaunchKernelGGL(k_ce_few_rows, dim3(1), dim3(64), 0, s, f);
+        GemmArgs z{};
+        z.a = GemmOperand{(const bf16_t *)f.h, f.ld_h, 0};
+        z.b = GemmOperand{(const bf16_t *)f.table, f.ld_table, 0};
+        Packing packing;
+        auto pack = [&](const void *src, int64_t ld, int64_t rows, int64_t to) {
+            PackArgs k{};
+            k.src = src;
+            k.ld = ld;
+            k.cols = f.D;
+            k.n = k.total = rows;
+            k.rows_packed = k.n_pad = pad64(rows);
+            k.pieces = p.np;
+            k.rows = (bf16_t *)(w + to);
+            k.ld_rows = p.Dp;
+            k.plane_rows = k.rows_packed * p.Dp;
+            packing.add(k);
+            return GemmOperand{k.rows, p.Dp, k.plane_rows};
+        };
+        if (p.pack_h) z.a = pack(f.h, f.ld_h, g.n, p.h);
+        if (p.pack_table) z.b = pack(f.table, f.ld_table, g.V, p.table);
+        packing.launch(std::is_same_v<T, float> ? ECC_F32 : ECC_BF16, s);
+        z.M = g.n;
+        z.N = g.V;
+        z.K = (int32_t)p.Dp;
+        z.batches = 1;
+        set_products(z, p.np, p.np);
+        launch_logits(z, p, w, f.out, f.rows.live, s);
+    } else {
+        auto logits = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(kFewThreads<T>), 0, s, f);
+        };
+        if (g.n <= 16) logits(k_ce_few<T, 1>);
+        else if (g.n <= 32) logits(k_ce_few<T, 2>);
+        else logits(k_ce_few<T, 4>);
+    }
+    const bool few = gradient && tiles <= kFewTiles;
+    if (!few) hipLaunchKernelGGL(k_ce_rows, dim3(kTile / 4), dim3(256), 0, s, g.r);
+    if (!gradient) return;
+    auto gradients = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(g.blocks_d * splits)), dim3(256), 0, s, g);
+    };
+    auto of_pieces = [&](auto pieces) {
+        constexpr int PT = decltype(pieces)::value;
+        if (few) gradients(k_ce_few_grad<T, PT, true>);
+        else gradients(k_ce_few_grad<T, PT, false>);
+    };
+    if constexpr (std::is_same_v<T, float>) of_pieces(std::integral_constant<int, 3>{});
+    else if (g.type == ECC_F32) of_pieces(std::integral_constant<int, 3>{});
+    else of_pieces(std::integral_constant<int, 1>{});
+    if (!dh) return;
+    hipLaunchKernelGGL(k_ce_few_join<T>, dim3((unsigned)((g.D + 63) / 64), (unsigned)g.n), dim3(256),
+                       0, s, g.dh, g.ld_dh, splits, g.r.rows, g.D, (T *)dh, ld_dh);
 }
 
 // The gradient of a table without rows to learn from.
@@ -614,6 +1055,28 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
                     (float *)(w + p.factor), (float *)(w + p.inside), (int32_t *)(w + p.live),
                     (int2 *)(w + p.ranges), (int32_t *)(w + p.counts), (float *)(w + p.outside)};
     const Positions q{a->d_labels, a->d_weight, a->n, (int32_t)V};
+    if (p.few) {
+        const LogitsOut logits{gradient ? (float *)(w + p.z) : nullptr, p.Vp, (float)a->scale,
+                               (float2 *)(w + p.stats), p.tiles, a->d_labels, (float *)(w + p.picked)};
+        const FewArgs f{a->d_h, a->d_table, a->ld_h, a->ld_table, q, D, logits, rows,
+                        (float *)d_loss, (float)a->scale};
+        RowArgs row{};
+        row.M = kTile;
+        row.tiles = p.tiles;
+        row.stats = logits.stats;
+        row.picked = logits.picked;
+        row.rows = rows;
+        row.loss = (float *)d_loss;
+        float *terms = gradient ? (float *)(w + p.terms) : nullptr;
+        row.out = RowTerms{terms, gradient ? terms + kTile : nullptr};
+        const FewGrad g{a->d_h, a->d_table, a->ld_h, a->ld_table, (int32_t)N, (int32_t)V, D,
+                        logits.z, p.Vp, row, d_dh ? (float *)(w + p.parts[0]) : nullptr, p.Dp,
+                        d_dtable, ld_dtable, a->grad_type, accumulate, p.blocks_d, p.per};
+        if (a->type == ECC_F32) launch_few<float>(f, p, w, g, gradient, d_dh, ld_dh, s);
+        else launch_few<bf16_t>(f, p, w, g, gradient, d_dh, ld_dh, s);
+        ECC_LAUNCH_CHECK();
+        return ECC_OK;
+    }
     if (P > 1)
         hipLaunchKernelGGL(k_ce_count, dim3((unsigned)P), dim3(kMapThreads), 0, s, q, rows);
     hipLaunchKernelGGL(k_ce_map, dim3((unsigned)P), dim3(kMapThreads), 0, s, q, rows, P, p.rows,
@@ -669,15 +1132,7 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         const LogitsOut logits{gradient ? (float *)(w + p.z) : nullptr, p.Vp, (float)a->scale,
                                (float2 *)(w + p.stats), p.tiles, rows.label + r0,
                                (float *)(w + p.picked)};
-        if (p.shape_z.splits > 1) {
-            float *parts = (float *)(w + p.parts_z);
-            g.splits = p.shape_z.splits;
-            launch_tiles({Product{g, parts_alone(parts)}, {}}, 1, {p.shape_z, {}}, s);
-            hipLaunchKernelGGL(k_ce_logits, dim3((unsigned)((R * p.tiles + 3) / 4)), dim3(256), 0,
-                               s, logits, parts, g.splits, g.M, g.N, rows.live, g.m_lo);
-        } else {
-            launch_gemm(g, logits, s);
-        }
+        launch_logits(g, p, w, logits, rows.live, s);
         RowArgs row{};
         row.first = (int32_t)r0;
         row.M = (int32_t)R;

@@ -10,7 +10,6 @@
 // gradients one product with both stacked.  dg and du are rounded to bf16
 // where the gradient is bf16 itself, and kept as three pieces (gemm.h) where
 // it is fp32.
-#include "gemm.h"
 #include "pack.h"
 
 namespace ecc {
@@ -209,44 +208,7 @@ __global__ __launch_bounds__(256) void k_ffn_grad_join(FfnParts p, FfnGradOut<T,
 // eight waves share the elements along D in turn, kAhead loads of each wave
 // under way at once, and add up in LDS in their order.  Operands need no
 // alignment and fp32 is split where it is loaded, so that nothing is packed.
-constexpr int kFewRows = 64;
 constexpr int kFewWaves = 8;
-
-// 16 bytes of a lane's share of a step: 8 bf16, or 4 fp32.
-template <typename T>
-struct FewStep;
-template <>
-struct FewStep<bf16_t> {
-    static constexpr int kStep = 64, kLane = 16, kFrags = 2, kPieces = 1;
-    Raw<bf16_t, 8> raw[2];
-    __device__ __forceinline__ void load(const bf16_t *row, int64_t k, int64_t D) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) raw[j].load_upto(row + k + j * 8, D - k - j * 8);
-    }
-    __device__ __forceinline__ void frags(bf16x8 (&f)[2][1]) const {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) f[j][0] = __builtin_bit_cast(bf16x8, raw[j]);
-    }
-};
-template <>
-struct FewStep<float> {
-    static constexpr int kStep = 32, kLane = 8, kFrags = 1, kPieces = 3;
-    Raw<float, 8> raw;
-    __device__ __forceinline__ void load(const float *row, int64_t k, int64_t D) {
-        raw.load_upto(row + k, D - k);
-    }
-    __device__ __forceinline__ void frags(bf16x8 (&f)[1][3]) const {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = raw.get<float>(e);
-#pragma unroll
-        for (int which = 0; which < 3; ++which) {
-            Raw<bf16_t, 8> x;
-            set_piece(x, v, which, true);
-            f[0][which] = __builtin_bit_cast(bf16x8, x);
-        }
-    }
-};
 
 template <typename T, int ACT, int MB>
 __global__ __launch_bounds__(64 * kFewWaves) void k_ffn_few(const T *x, int64_t ld_x,
@@ -289,18 +251,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_ffn_few(const T *x, int64_t 
                 for (int g = 0; g < 2; ++g)
 #pragma unroll
                     for (int j = 0; j < S::kFrags; ++j) {
-                        auto add = [&](int pw, int pa) {
+                        products<S::kPieces, S::kPieces>([&](int pw, int pa) {
                             acc[g][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                                 fw[g][j][pw], fa[j][pa], acc[g][i], 0, 0, 0);
-                        };
-                        if constexpr (S::kPieces == 3) {
-                            add(1, 1);
-                            add(0, 2);
-                            add(2, 0);
-                            add(0, 1);
-                            add(1, 0);
-                        }
-                        add(0, 0);
+                        });
                     }
             }
         }

@@ -83,6 +83,17 @@ inline void set_products(GemmArgs &g, int na, int nb) {
     }
 }
 
+// The same for pieces in registers: f(piece of A, piece of B).
+template <int NA, int NB, class F>
+__device__ __forceinline__ void products(F &&f) {
+    if constexpr (NA > 1 && NB > 1) f(1, 1);
+    if constexpr (NB > 2) f(0, 2);
+    if constexpr (NA > 2) f(2, 0);
+    if constexpr (NB > 1) f(0, 1);
+    if constexpr (NA > 1) f(1, 0);
+    f(0, 0);
+}
+
 // Where a lane's sums lie: acc[i][j][e] is row m + 16 i, column n + 16 j + e
 // of the tile's matrix (of pairs: acc[i][j] and acc[i][j + NI / 2] are the
 // first's and the second's column n + 16 j + e).
@@ -159,6 +170,13 @@ __device__ __forceinline__ void phase_end() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// Blocks go round the XCDs: each takes a contiguous share.
+__device__ __forceinline__ int xcd_block(int block, int blocks) {
+    const int per = (blocks + 7) >> 3, more = blocks - ((per - 1) << 3);
+    const int xcd = block & 7, at = block >> 3;
+    return xcd * per + at - max(0, xcd - more);
+}
+
 template <int BM, int BN, int WM, int WN, int STAGES, class Epi>
 __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int block,
                                           int blocks) {
@@ -177,10 +195,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs &g, const Epi &epi, int
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
-    // the tile: blocks go round the XCDs, each takes a contiguous share
-    const int per = (blocks + 7) >> 3, more = blocks - ((per - 1) << 3);
-    const int xcd = block & 7, at = block >> 3;
-    int t = xcd * per + at - max(0, xcd - more);  // (uniform: from scalars alone)
+    int t = xcd_block(block, blocks);  // (uniform: from scalars alone)
     const int tiles = g.tiles_m * g.tiles_n;
     const int part = t / tiles;
     t -= part * tiles;

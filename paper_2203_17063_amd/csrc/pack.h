@@ -3,7 +3,7 @@
 // in the matrix's own order or transposed.
 #pragma once
 
-#include "lm_common.h"
+#include "gemm.h"
 
 namespace ecc {
 
@@ -165,6 +165,46 @@ struct Packing {
         if (type == ECC_F32)
             hipLaunchKernelGGL(k_pack<float>, dim3((unsigned)blocks), dim3(256), 0, s, l);
         else hipLaunchKernelGGL(k_pack<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, s, l);
+    }
+};
+
+// Up to this many rows need nothing packed: operands go straight into the matrix
+// cores' registers, at any alignment, fp32 split where it is loaded.
+constexpr int kFewRows = 64;
+
+// A lane's share of a step along k: 16 bf16, or 8 fp32.
+template <typename T>
+struct FewStep;
+template <>
+struct FewStep<bf16_t> {
+    static constexpr int kStep = 64, kLane = 16, kFrags = 2, kPieces = 1;
+    Raw<bf16_t, 8> raw[2];
+    __device__ __forceinline__ void load(const bf16_t *row, int64_t k, int64_t D) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) raw[j].load_upto(row + k + j * 8, D - k - j * 8);
+    }
+    __device__ __forceinline__ void frags(bf16x8 (&f)[2][1]) const {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[j][0] = __builtin_bit_cast(bf16x8, raw[j]);
+    }
+};
+template <>
+struct FewStep<float> {
+    static constexpr int kStep = 32, kLane = 8, kFrags = 1, kPieces = 3;
+    Raw<float, 8> raw;
+    __device__ __forceinline__ void load(const float *row, int64_t k, int64_t D) {
+        raw.load_upto(row + k, D - k);
+    }
+    __device__ __forceinline__ void frags(bf16x8 (&f)[1][3]) const {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = raw.get<float>(e);
+#pragma unroll
+        for (int which = 0; which < 3; ++which) {
+            Raw<bf16_t, 8> x;
+            set_piece(x, v, which, true);
+            f[0][which] = __builtin_bit_cast(bf16x8, x);
+        }
     }
 };
 

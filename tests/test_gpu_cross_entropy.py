@@ -265,6 +265,41 @@ def test_no_rows():
             assert (one == 1).all()
 
 
+@pytest.mark.parametrize("dtype,grad", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("n,D,V", [
+    (1, 2, 1), (2, 64, 63), (15, 63, 64), (16, 65, 65), (17, 200, 2048), (31, 130, 2049),
+    (32, 257, 1000), (33, 31, 640), (48, 1001, 90), (63, 128, 4001), (64, 96, 2113),
+    (40, 2112, 700), (40, 2050, 2100)])
+def test_few_rows(dtype, grad, n, D, V):
+    """Up to 64 rows of one worker, whose operands are taken as they lie: blocks
+    of 16 rows, 64 columns and 64 elements, tiles joined in one launch and in
+    two, at any alignment; long rows of small vocabularies by tiles of a split
+    product, packed and as they lie, with the same bits."""
+    announce("cross entropy, few rows", dtype, grad, n, D, V)
+    h, table, y, w = _inputs(n, D, V, dtype, 11)
+    y[0], w[0] = V - 1, 0.7      # (a row that counts)
+    want = _check(h, table, y, w, scale=-0.6, dtype=grad)
+    for alike in (None, torch.full_like(w, 0.25)):
+        _check(h, table, y, alike, dtype=grad)
+    # rows with gaps, at any element; NaN in rows that do not count
+    dead = (w == 0) | (y < 0) | (y >= V)
+
+    def wide(t, rows):
+        buf = torch.full((t.shape[0], D + 3), 7.0, dtype=t.dtype, device="cuda")
+        buf[:, 1:1 + D] = t
+        if rows is not None:
+            buf[rows] = math.nan
+        return buf, buf[:, 1:1 + D]
+    outs = [wide(torch.zeros_like(t), None) for t in (h, want[2][0])]
+    got = _lm().cross_entropy(wide(h, dead)[1], wide(table, None)[1], y, w, scale=-0.6,
+                              dh=outs[0][1], dtable=outs[1][1][None], accumulate=True)
+    # (added to zeros)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for buf, view in outs:
+        view.fill_(7.0)
+        assert (buf == 7.0).all()
+
+
 def test_gradient_against_differences():
     """Central differences of the loss along random directions, in fp32."""
     lm = _lm()
