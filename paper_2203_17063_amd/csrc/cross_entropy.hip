@@ -21,7 +21,7 @@
 //
 // Up to 64 rows of one worker take kernels of their own, which need no packed
 // and no transposed table (its two passes are most of such a call): 61 rows,
-// D 96, V 1,003, fp32: 23 us against 47 us, in three launches instead of seven;
+// D 96, V 1,003, fp32: 20 us against 47 us, in three launches instead of seven;
 // 8 rows, D 4,096, V 128,000, bf16: 0.93 ms against 1.28 ms.
 #include "pack.h"
 
@@ -576,30 +576,46 @@ struct FewGrad {
 };
 constexpr int kFewPitch = 72;   // of a row of 64 in LDS: 16-byte accesses
 
-// Pieces of 8 values in LDS: rows `to` + 0 .. 7, a column.
-__device__ __forceinline__ void put_column(uint16_t *to, const float (&v)[8], int which,
-                                           bool split) {
-    Raw<bf16_t, 8> x;
+// Where a block's element lies in LDS, turned round: the four threads that write
+// a row's elements reach different banks (39 rows, D 3,473, V 43,897, fp32: the
+// call takes 1.00 ms, and 1.19 ms where they meet in one).
+__device__ __forceinline__ int turned(int col, int row) {
+    return col * kFewPitch + (row ^ (col & 48));
+}
+// A piece of N neighbouring columns of a row.
+template <int N>
+__device__ __forceinline__ void put_columns(uint16_t *s, int col, int row, const float (&v)[N],
+                                            int which, bool split) {
+    Raw<bf16_t, N> x;
     set_piece(x, v, which, split);
+    uint16_t *to = s + turned(col, row);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) to[e * kFewPitch] = (uint16_t)(x.w[e / 2] >> (e & 1) * 16);
+    for (int e = 0; e < N; ++e) to[e * kFewPitch] = (uint16_t)(x.w[e / 2] >> (e & 1) * 16);
 }
 
 // Gradients, 64 elements along D for a split of the vocabulary's tiles: the
 // tile's softmax - [label] (FEW: of rows whose tiles are joined here) and the
 // table's elements lie in LDS in the orders that the two products want, dh's
 // sums stay in registers.  The next tile is under way meanwhile.
+// fp32's pieces fill a CU's LDS with one workgroup, which then has 16 waves (8:
+// 1.01 ms for the case above; bf16 with pieces of dE, 4 waves: 182 us, 8: 217 us
+// for 32 rows, D 2,048, V 32,000).
+template <typename T>
+constexpr int kFewWaves = std::is_same_v<T, float> ? 16 : 4;
 template <typename T, int PT, bool FEW>
-__global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a) {
+__global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad a) {
+    constexpr int W = kFewWaves<T>, CN = kTile / W, N = CN < 8 ? CN : 8, J = 16 / W;
     constexpr int NP = std::is_same_v<T, float> ? 3 : 1, kSize = kTile * kFewPitch;
     __shared__ __attribute__((aligned(16))) uint16_t s_dz[NP][kSize], s_dzt[PT][kSize],
         s_h[NP][kSize], s_e[NP][kSize];
     const RowArgs &q = a.r;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, k8 = lane >> 4;
-    const int r = threadIdx.x >> 2, c16 = (threadIdx.x & 3) * 16;
+    // a thread's columns of a row of a tile; a wave's rows and columns of sums
+    const int r = threadIdx.x / W, c0 = threadIdx.x % W * CN;
+    const int lane = threadIdx.x & 63, c = lane & 15, k8 = lane >> 4;
+    const int wave = threadIdx.x >> 6 & 3, j0 = (threadIdx.x >> 8) * J;
     // (an XCD's blocks are neighbours: rows' ends share lines of its L2)
     const int32_t b = xcd_block(blockIdx.x, gridDim.x);
-    const int64_t d0 = (int64_t)(b % a.blocks_d) * kTile, left = a.D - d0 - c16;
+    const int64_t d0 = (int64_t)(b % a.blocks_d) * kTile, left = a.D - d0 - c0;
     const int32_t split = b / a.blocks_d;
     const int32_t t0 = split * a.per, t1 = min(q.tiles, t0 + a.per);
     const int32_t y = q.rows.label[r];
@@ -608,9 +624,9 @@ __global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a)
     float most = 0.0f, soft = 0.0f;
     if constexpr (FEW) {
         float sum = 1.0f;
-        if (held) join_tiles(q.stats + (int64_t)r * q.tiles, q.tiles, threadIdx.x & 3, 4, most, sum);
+        if (held) join_tiles(q.stats + (int64_t)r * q.tiles, q.tiles, threadIdx.x % W, W, most, sum);
         soft = 1.0f / sum;
-        if (held && b == 0 && c16 == 0)
+        if (held && b == 0 && c0 == 0)
             q.loss[r] = q.rows.weight[r] * ((most - q.picked[r]) + logf(sum));
     } else if (held) {
         most = q.out.most[r];
@@ -618,64 +634,67 @@ __global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a)
     }
     const bool none = !__syncthreads_or(held);
     if (a.dtable) {
-        Raw<T, 8> x[2];
+        Raw<T, N> x[CN / N];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            x[i].load_upto((const T *)a.h + (held ? r * a.ld_h + d0 + c16 + i * 8 : 0),
-                           held ? left - i * 8 : 0);
-            float v[8];
+        for (int i = 0; i < CN / N; ++i) {
+            x[i].load_upto((const T *)a.h + (held ? r * a.ld_h + d0 + c0 + i * N : 0),
+                           held ? left - i * N : 0);
+            float v[N];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = x[i].template get<float>(e);
+            for (int e = 0; e < N; ++e) v[e] = x[i].template get<float>(e);
             for (int p = 0; p < NP; ++p)
-                put_column(s_h[p] + (c16 + i * 8) * kFewPitch + r, v, p, NP > 1);
+                put_columns(s_h[p], c0 + i * N, r, v, p, NP > 1);
         }
     }
-    Raw<float, 8> z[2];
-    Raw<T, 8> w[2];
+    Raw<float, N> z[CN / N];
+    Raw<T, N> w[CN / N];
     auto fetch = [&](int32_t t) {
         const int64_t v = (int64_t)t * kTile + r;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            z[i].load_upto(a.z + (held ? r * a.ld_z + t * kTile + c16 + i * 8 : 0), held ? 8 : 0);
+        for (int i = 0; i < CN / N; ++i) {
+            z[i].load_upto(a.z + (held ? r * a.ld_z + t * kTile + c0 + i * N : 0), held ? N : 0);
             const bool in = a.dh && v < a.V;
-            w[i].load_upto((const T *)a.table + (in ? v * a.ld_table + d0 + c16 + i * 8 : 0),
-                           in ? left - i * 8 : 0);
+            w[i].load_upto((const T *)a.table + (in ? v * a.ld_table + d0 + c0 + i * N : 0),
+                           in ? left - i * N : 0);
         }
     };
     auto frag = [&](const uint16_t *s, int row, int kk) {
         return *reinterpret_cast<const bf16x8 *>(s + row * kFewPitch + kk * 32 + k8 * 8);
     };
+    auto frag_t = [&](const uint16_t *s, int col, int kk) {
+        return *reinterpret_cast<const bf16x8 *>(s + turned(col, kk * 32 + k8 * 8));
+    };
     const float by = *q.rows.outside;
-    f32x4 dh[4];
+    f32x4 dh[J];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dh[j] = f32x4{0, 0, 0, 0};
+    for (int j = 0; j < J; ++j) dh[j] = f32x4{0, 0, 0, 0};
     fetch(t0);
     for (int32_t t = t0; t < t1; ++t) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float v[8], u[8];
+        for (int i = 0; i < CN / N; ++i) {
+            float v[N], u[N];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int32_t j = t * kTile + c16 + i * 8 + e;
-                float p = exp_fast(z[i].get<float>(e) - most) * soft;
+            for (int e = 0; e < N; ++e) {
+                const int32_t j = t * kTile + c0 + i * N + e;
+                float p = exp_fast(z[i].template get<float>(e) - most) * soft;
                 if (j == y) p -= 1.0f;
                 v[e] = held && j < a.V ? p : 0.0f;
                 u[e] = v[e] * inside;
             }
-            const int at = c16 + i * 8;
+            const int at = c0 + i * N;
             for (int p = 0; p < NP; ++p) {
-                Raw<bf16_t, 8> x;
+                Raw<bf16_t, N> x;
                 set_piece(x, v, p, NP > 1);
-                *reinterpret_cast<Raw<bf16_t, 8> *>(s_dz[p] + r * kFewPitch + at) = x;
+                *reinterpret_cast<Raw<bf16_t, N> *>(s_dz[p] + r * kFewPitch + at) = x;
             }
             if (a.dtable)
                 for (int p = 0; p < PT; ++p)
-                    put_column(s_dzt[p] + at * kFewPitch + r, u, p, PT > 1);
+                    put_columns(s_dzt[p], at, r, u, p, PT > 1);
             if (a.dh) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = w[i].template get<float>(e);
+                for (int e = 0; e < N; ++e) v[e] = w[i].template get<float>(e);
                 for (int p = 0; p < NP; ++p)
-                    put_column(s_e[p] + at * kFewPitch + r, v, p, NP > 1);
+                    put_columns(s_e[p], at, r, v, p, NP > 1);
             }
         }
         if (t + 1 < t1) fetch(t + 1);
@@ -684,29 +703,29 @@ __global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a)
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < J; ++j)
                     products<NP, NP>([&](int pz, int pw) {
                         dh[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            frag(s_e[pw], j * 16 + c, kk), frag(s_dz[pz], wave * 16 + c, kk),
+                            frag_t(s_e[pw], (j0 + j) * 16 + c, kk), frag(s_dz[pz], wave * 16 + c, kk),
                             dh[j], 0, 0, 0);
                     });
         }
         if (a.dtable && !(a.add && none)) {
-            f32x4 de[4];
+            f32x4 de[J];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) de[j] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < J; ++j) de[j] = f32x4{0, 0, 0, 0};
             for (int kk = 0; kk * 32 < a.n; ++kk)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < J; ++j)
                     products<PT, NP>([&](int pz, int ph) {
                         de[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            frag(s_h[ph], j * 16 + c, kk), frag(s_dzt[pz], wave * 16 + c, kk),
+                            frag_t(s_h[ph], (j0 + j) * 16 + c, kk), frag_t(s_dzt[pz], wave * 16 + c, kk),
                             de[j], 0, 0, 0);
                     });
             const int32_t v = t * kTile + wave * 16 + c;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t d = d0 + j * 16 + k8 * 4;
+            for (int j = 0; j < J; ++j) {
+                const int64_t d = d0 + (j0 + j) * 16 + k8 * 4;
                 if (v >= a.V || d >= a.D) continue;
                 if (a.type == ECC_F32) 
                     add_quad((float *)a.dtable + v * a.ld_dtable + d, de[j] * by, a.D - d, a.add);
@@ -718,9 +737,9 @@ __global__ __launch_bounds__(256, PT == 1 ? 4 : 2) void k_ce_few_grad(FewGrad a)
     }
     if (!a.dh) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < J; ++j)
         *reinterpret_cast<f32x4 *>(a.dh + ((int64_t)split * kTile + wave * 16 + c) * a.ld_dh + d0 +
-                                   j * 16 + k8 * 4) = dh[j];
+                                   (j0 + j) * 16 + k8 * 4) = dh[j];
 }
 
 // dh from its splits: 16 threads per four elements, each of every sixteenth
@@ -956,13 +975,14 @@ void launch_few(const FewArgs &f, const Plan &p, char *w, const FewGrad &g, bool
     const bool few = gradient && tiles <= kFewTiles;
     if (!few) hipLaunchKernelGGL(k_ce_rows, dim3(kTile / 4), dim3(256), 0, s, g.r);
     if (!gradient) return;
-    auto gradients = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(g.blocks_d * splits)), dim3(256), 0, s, g);
+    auto gradients = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(g.blocks_d * splits)), dim3(waves * 64), 0,
+                           s, g);
     };
     auto of_pieces = [&](auto pieces) {
         constexpr int PT = decltype(pieces)::value;
-        if (few) gradients(k_ce_few_grad<T, PT, true>);
-        else gradients(k_ce_few_grad<T, PT, false>);
+        if (few) gradients(k_ce_few_grad<T, PT, true>, kFewWaves<T>);
+        else gradients(k_ce_few_grad<T, PT, false>, kFewWaves<T>);
     };
     if constexpr (std::is_same_v<T, float>) of_pieces(std::integral_constant<int, 3>{});
     else if (g.type == ECC_F32) of_pieces(std::integral_constant<int, 3>{});
