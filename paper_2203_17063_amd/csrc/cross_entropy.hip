@@ -270,7 +270,7 @@ struct LogitsOut {
         if (z) z[m * ld + n] = in ? v : 0.0f;
         const float most = wave_all(in ? v : -__builtin_inff(), OpMax());
         const float from = most == -__builtin_inff() ? 0.0f : most;
-        const float sum = wave_all(in ? exp_fast(v - from) : 0.0f, OpSum());
+        const float sum = wave_all(in ? exp_short(v - from) : 0.0f, OpSum());
         if ((threadIdx.x & 63) == 0) stats[(int64_t)m * tiles + tile] = make_float2(most, sum);
     }
     template <int NI, bool WHOLE>
@@ -288,7 +288,7 @@ struct LogitsOut {
         for (int j = 0; j < NI; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (WHOLE || n + 16 * j + e < N) sum += exp_fast(v[j][e] - from);
+                if (WHOLE || n + 16 * j + e < N) sum += exp_short(v[j][e] - from);
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
     }
@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int32_t j = col0 + c8 + e;
-            float v = exp_fast(x[p].get<float>(e) - most) * soft;
+            float v = exp_short(x[p].get<float>(e) - most) * soft;
             if (j == y) v -= 1.0f;
             mine[p][e] = y >= 0 && j < a.V ? v : 0.0f;
         }
@@ -676,7 +676,7 @@ __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad 
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const int32_t j = t * kTile + c0 + i * N + e;
-                float p = exp_fast(z[i].template get<float>(e) - most) * soft;
+                float p = exp_short(z[i].template get<float>(e) - most) * soft;
                 if (j == y) p -= 1.0f;
                 v[e] = held && j < a.V ? p : 0.0f;
                 u[e] = v[e] * inside;

@@ -19,15 +19,21 @@ namespace {
 // 7.1.26 (Hastings), within 1.5e-7 of it: half of 1 - erf(|x|) is a polynomial
 // in 1 / (1 + p |x|) times exp(-x^2), at x = g / sqrt 2 the exponential that the
 // derivative needs too.  For negative g that half is the factor itself, so that
-// small values keep their digits.
-template <int ACT>
+// small values keep their digits.  Exponentials of fp32 rows within 2 ulp, of
+// bf16 rows the short ones: 8,192 rows, D 256, F 2,501: 40 us against 45 us.
+template <typename T>
+__device__ __forceinline__ float exp_of(float x) {
+    if constexpr (std::is_same_v<T, float>) return exp_fast(x);
+    else return exp_short(x);
+}
+template <int ACT, typename T>
 __device__ __forceinline__ void activation(float g, float &a, float &da) {
     if constexpr (ACT == ECC_ACT_SILU) {
-        const float q = recip_fast(1.0f + exp_fast(-g));
+        const float q = recip_fast(1.0f + exp_of<T>(-g));
         a = g * q;
         da = q * (1.0f + g * (1.0f - q));
     } else {
-        const float e = exp_fast(-0.5f * g * g);
+        const float e = exp_of<T>(-0.5f * g * g);
         const float t = recip_fast(__builtin_fmaf(__builtin_fabsf(g), 0.3275911f * 0.70710678f, 1.0f));
         float h = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
         h = __builtin_fmaf(t, h, 1.421413741f);
@@ -57,7 +63,7 @@ struct FfnOut {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, da;
-                    activation<ACT>(acc[i][j][e], a, da);
+                    activation<ACT, T>(acc[i][j][e], a, da);
                     v[j][e] = a * acc[i][j + NI / 2][e];
                 }
             turn<NI / 2>(t.lds, v, [&](int row, int col, f32x4 u) {
@@ -107,7 +113,7 @@ struct FfnGradOut {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float a, da;
-                        activation<ACT>(acc[i0 + i][j][e], a, da);
+                        activation<ACT, T>(acc[i0 + i][j][e], a, da);
                         const float v = x[i][j].template get<float>(e);
                         // (columns behind the last are zeros: what was summed
                         // for them is the last one's again)
@@ -163,7 +169,7 @@ __global__ __launch_bounds__(256) void k_ffn_join(FfnParts p, FfnOut<T, ACT> out
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float a, da;
-        activation<ACT>(g[e], a, da);
+        activation<ACT, T>(g[e], a, da);
         v[e] = a * u[e];
     }
     Raw<T, 4> x;
@@ -188,7 +194,7 @@ __global__ __launch_bounds__(256) void k_ffn_grad_join(FfnParts p, FfnGradOut<T,
         for (int e = 0; e < 4; ++e) {
             if (n + e >= p.N) continue;
             float a, da;
-            activation<ACT>(g[e], a, da);
+            activation<ACT, T>(g[e], a, da);
             const float v = x.template get<float>(e);
             dg[e] = v * u[e] * da;
             du[e] = v * a;
@@ -278,7 +284,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_ffn_few(const T *x, int64_t 
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float b, db;
-        activation<ACT>(g[e], b, db);
+        activation<ACT, T>(g[e], b, db);
         v[e] = b * u[e];
     }
     Raw<T, 4> out;

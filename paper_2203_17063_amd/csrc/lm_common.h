@@ -259,6 +259,12 @@ __device__ __forceinline__ float exp_fast(float x) {
     const float e = __builtin_amdgcn_exp2f(t);
     return __builtin_fmaf(e * kLn2, r, e);
 }
+// exp(x) off by (1.2 |x| + 1) 2^-24 of it, in five issue slots instead of
+// thirteen: for terms of a sum beside exp(0) (2,048 rows of 2,048 against 32,003:
+// 241 us against 251 us), and for rows of bf16.
+__device__ __forceinline__ float exp_short(float x) {
+    return __builtin_amdgcn_exp2f(x * 1.44269502f);
+}
 // 1 / x within 1 ulp, 0 beyond 2^126
 __device__ __forceinline__ float recip_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 

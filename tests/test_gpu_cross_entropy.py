@@ -3,11 +3,12 @@ gradients, against the definition in 64 bits.
 
 Tolerances (u = 2^-24; products as in product_bounds.py).  With a row's logits
 off by up to e = max e_j + 2 u max |z_j| (the scale's product) and spread over X,
-its exponentials are off by (X + 4) u more, and their sum by 2 e + (2 X + 64 +
-V / 64) u relative in all (the additions of 64 columns, their joins in a wave of
-64).  So the loss is within w (3 e + k u (1 + |lse - z_y| + |z|)), k = 2 X + 64
-+ V / 64, and a softmax value within p (4 e + 2 k u).  dz is off by scale * w
-times that and 4 u of both its terms, and is stored with half a step of bf16
+its exponentials are off by (2.2 X + 2) u more (X + 1.2 X of the difference and
+the exponent; beyond X = 104 they are 0), and their sum by 2 e + (2 X + 64 + V /
+64) u relative in all (the rest of X, the additions of 64 columns in 18 steps,
+their joins in a wave of 64).  So the loss is within w (3 e + k u (1 + |lse -
+z_y| + |z|)), k = 2 X + 64 + V / 64, and a softmax value within p (4 e + 2 k u).
+dz is off by scale * w times that and 4 u of both its terms, and is stored with half a step of bf16
 where a gradient is bf16, or as three pieces (none)."""
 import math
 

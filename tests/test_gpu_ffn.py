@@ -4,8 +4,9 @@ backward, against the definition in 64 bits.
 Tolerances (u = 2^-24; products as in product_bounds.py).  With g and u_ off by
 eg and eu, act(g) is off by at most 1.13 eg (the largest slope of either
 activation) and its own arithmetic, 16 u (|g| + 1) (an exponential or error
-function within 4 u, and some operations; the functions are at most |g|); its
-slope by 1.2 eg (the largest second derivative is below 1.2) and 24 u.  A product
+function within 4 u, and some operations; the functions are at most |g|; bf16's
+exponential of x within (1.2 |x| + 1) u, which g q (1 - q) and g^3 exp(-g^2 / 2)
+make less than 4 u of); its slope by 1.2 eg (the largest second derivative is below 1.2) and 24 u.  A product
 of three such factors adds 4 u.  dg and du are stored with half a step of bf16
 where a gradient is bf16, or as three pieces (none)."""
 import math
