@@ -301,6 +301,56 @@ def test_few_rows(dtype, grad, n, D, V):
         assert (buf == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype,grad,n,D,V", [
+    (BF16, BF16, 50, 130, 700), (BF16, F32, 9, 520, 2500), (F32, F32, 33, 70, 400),
+    (BF16, BF16, 60, 2048, 500), (F32, F32, 40, 2050, 300)])
+def test_few_rows_calls(dtype, grad, n, D, V):
+    """Either gradient alone, a work buffer full of NaN of which nothing behind
+    its size is touched, and replayed graphs, down to no row that counts."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    announce("cross entropy, few rows' calls", dtype, grad, n, D, V)
+    h, table, y, w = _inputs(n, D, V, dtype, 17)
+    want = lm.cross_entropy(h, table, y, w, dtype=grad)
+    kinds = {BF16: E.ECC_BF16, F32: E.ECC_F32}
+    a = E.ecc_cross_entropy_t(n, V, D, 1, kinds[dtype], kinds[grad], 0, h.data_ptr(), D,
+                              table.data_ptr(), D, y.data_ptr(), w.data_ptr(), 1.0)
+    stream = torch.cuda.current_stream().cuda_stream
+    for which in (0, 1, 2, 3):
+        size = E.ecc_cross_entropy_work_size(a, 1 if which else 0)
+        work = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+        loss = torch.full_like(want[0], math.nan)
+        dh = torch.full_like(want[1], math.nan) if which & 1 else None
+        dt = torch.full_like(want[2], math.nan) if which & 2 else None
+        E.ecc_cross_entropy(a, loss, dh, D, dt, D, V * D, 0, work, stream)
+        if which:
+            for got, all_of_it in ((loss, want[0]), (dh, want[1]), (dt, want[2])):
+                assert got is None or torch.equal(got, all_of_it)
+        else:
+            # (tiles are joined by 64 lanes where there is the loss alone, by four
+            # where there are gradients and up to 32 tiles)
+            within(loss, *_reference(h, table, y, w, 1.0, 1, grad)[0], "loss alone")
+        assert (work[size:] == 255).all()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = lm.cross_entropy(h, table, y, w, dtype=grad)
+    for k in range(4):
+        h2, _, y2, w2 = _inputs(n, D, V, dtype, 18 + k)
+        h.copy_(h2)
+        y.copy_(y2 if k < 3 else torch.full_like(y2, -1))
+        w.copy_(w2)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = lm.cross_entropy(h, table, y, w, dtype=grad)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        if k == 3:
+            assert all((t == 0).all() for t in got)
+            old = torch.full_like(want[2], -0.0)
+            lm.cross_entropy(h, table, y, w, dtable=old, accumulate=True)
+            assert torch.signbit(old).all()      # (left alone)
+
+
 def test_gradient_against_differences():
     """Central differences of the loss along random directions, in fp32."""
     lm = _lm()
