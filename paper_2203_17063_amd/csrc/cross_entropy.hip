@@ -19,10 +19,11 @@
 // label's term is near the weight in most rows of a model that learns, and
 // would be off by one and the same half step everywhere (0.0037 of dE).
 //
-// Up to 64 rows of one worker take kernels of their own, which need no packed
+// Up to 64 rows in all take kernels of their own, which need no packed
 // and no transposed table (its two passes are most of such a call): 61 rows,
 // D 96, V 1,003, fp32: 20 us against 47 us, in three launches instead of seven;
-// 8 rows, D 4,096, V 128,000, bf16: 0.93 ms against 1.28 ms.
+// 8 rows, D 4,096, V 128,000, bf16: 0.93 ms against 1.28 ms; 64 workers' rows, D
+// 256, V 32,000, bf16: 0.29 ms against 0.92 ms.
 #include "pack.h"
 
 namespace ecc {
@@ -437,17 +438,18 @@ __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// few rows of one worker
+// few rows
 // ---------------------------------------------------------------------------
 
-// The rows stay where they are (those that do not count have label -1), and
+// Up to kFewRows rows of all workers, which stay where they are (those that do not count have label -1), and
 // nothing is packed: the table is read once for the logits and once for dh, by
 // kernels that are bound by that and by their latency (1 row, D 3,268, V 49,125,
 // bf16: 92 us for 321 MB of logits' operands; gradients 233 us for 642 MB).
 struct FewArgs {
     const void *h, *table;
     int64_t ld_h, ld_table;
-    Positions q;
+    Positions q;         // n: of all workers
+    int32_t of_worker;
     int64_t D;
     LogitsOut out;
     Rows rows;
@@ -455,14 +457,28 @@ struct FewArgs {
     float scale;
 };
 
-// What k_ce_map leaves, by a wave.
+// What k_ce_map leaves, by a wave, a row per lane.
 __device__ __forceinline__ void few_rows(const FewArgs &a) {
-    const int32_t r = threadIdx.x & 63, n = (int32_t)a.q.n;
+    const int32_t r = threadIdx.x & 63, n = (int32_t)a.q.n, first = r - r % a.of_worker;
     const bool held = r < n && a.q.counts(r);
     const float w = held ? (a.q.weight ? a.q.weight[r] : 1.0f) : 0.0f;
-    const float least = -wave_all(held ? -w : -__builtin_inff(), OpMax());
-    const float most = wave_all(held ? w : -__builtin_inff(), OpMax());
-    const bool alike = least == most && !__any(w != w);
+    // (its worker's rows)
+    float least = held ? w : __builtin_inff(), most = held ? w : -__builtin_inff();
+    bool odd = w != w;
+    if (a.of_worker == n) {
+        least = -wave_all(-least, OpMax());
+        most = wave_all(most, OpMax());
+        odd = __any(odd);
+    } else {
+        const float low = least, high = most;
+        const uint64_t all_odd = __ballot(odd);
+        for (int32_t i = 0; i < a.of_worker; ++i) {
+            least = fminf(least, __shfl(low, first + i, 64));
+            most = fmaxf(most, __shfl(high, first + i, 64));
+            odd = odd || (all_odd >> (first + i & 63) & 1);
+        }
+    }
+    const bool alike = least == most && !odd;
     const float factor = w * a.scale;
     a.rows.map[r] = held ? r : -1;
     a.rows.label[r] = held ? a.q.labels[r] : -1;
@@ -470,10 +486,8 @@ __device__ __forceinline__ void few_rows(const FewArgs &a) {
     a.rows.factor[r] = factor;
     a.rows.inside[r] = alike ? 1.0f : factor;
     if (r < n && !held) a.loss[r] = 0.0f;
-    if (r == 0) {
-        *a.rows.live = kTile;
-        *a.rows.outside = alike ? least * a.scale : 1.0f;
-    }
+    if (r < n && r == first) a.rows.outside[r / a.of_worker] = alike ? least * a.scale : 1.0f;
+    if (r == 0) *a.rows.live = kTile;
 }
 
 __global__ __launch_bounds__(64) void k_ce_few_rows(FewArgs a) { few_rows(a); }
@@ -562,7 +576,7 @@ constexpr int few_blocks(int np, int pt) { return np == 3 ? 256 : pt == 3 ? 512 
 struct FewGrad {
     const void *h, *table;
     int64_t ld_h, ld_table;
-    int32_t n, V;
+    int32_t n, of_worker, V;   // rows of all workers, of one
     int64_t D;
     const float *z;
     int64_t ld_z;
@@ -570,10 +584,11 @@ struct FewGrad {
     float *dh;            // [splits][64][ld_dh], NULL: none
     int64_t ld_dh;
     void *dtable;         // NULL: none
-    int64_t ld_dtable;
+    int64_t ld_dtable, worker_stride;
     int32_t type, add;
     int32_t blocks_d, per;   // blocks along D; tiles of 64 columns of a split
 };
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kFewPitch = 72;   // of a row of 64 in LDS: 16-byte accesses
 
 // Where a block's element lies in LDS, turned round: the four threads that write
@@ -596,13 +611,14 @@ __device__ __forceinline__ void put_columns(uint16_t *s, int col, int row, const
 // Gradients, 64 elements along D for a split of the vocabulary's tiles: the
 // tile's softmax - [label] (FEW: of rows whose tiles are joined here) and the
 // table's elements lie in LDS in the orders that the two products want, dh's
-// sums stay in registers.  The next tile is under way meanwhile.
+// sums stay in registers.  The next tile is under way meanwhile.  dE is formed
+// once for each worker (WORKERS: several), of all rows with the others' masked.
 // fp32's pieces fill a CU's LDS with one workgroup, which then has 16 waves (8:
 // 1.01 ms for the case above; bf16 with pieces of dE, 4 waves: 182 us, 8: 217 us
 // for 32 rows, D 2,048, V 32,000).
 template <typename T>
 constexpr int kFewWaves = std::is_same_v<T, float> ? 16 : 4;
-template <typename T, int PT, bool FEW>
+template <typename T, int PT, bool FEW, bool WORKERS>
 __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad a) {
     constexpr int W = kFewWaves<T>, CN = kTile / W, N = CN < 8 ? CN : 8, J = 16 / W;
     constexpr int NP = std::is_same_v<T, float> ? 3 : 1, kSize = kTile * kFewPitch;
@@ -632,7 +648,9 @@ __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad 
         most = q.out.most[r];
         soft = q.out.soft[r];
     }
-    const bool none = !__syncthreads_or(held);
+    const uint64_t live = __ballot(q.rows.label[lane] >= 0);
+    const int32_t workers = WORKERS ? a.n / a.of_worker : 1;
+    const float outside = q.rows.outside[WORKERS ? min(lane, workers - 1) : 0];
     if (a.dtable) {
         Raw<T, N> x[CN / N];
 #pragma unroll
@@ -664,7 +682,6 @@ __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad 
     auto frag_t = [&](const uint16_t *s, int col, int kk) {
         return *reinterpret_cast<const bf16x8 *>(s + turned(col, kk * 32 + k8 * 8));
     };
-    const float by = *q.rows.outside;
     f32x4 dh[J];
 #pragma unroll
     for (int j = 0; j < J; ++j) dh[j] = f32x4{0, 0, 0, 0};
@@ -710,27 +727,51 @@ __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad 
                             dh[j], 0, 0, 0);
                     });
         }
-        if (a.dtable && !(a.add && none)) {
+        for (int32_t p = 0; a.dtable && p < workers; ++p) {
+            const int32_t lo = WORKERS ? p * a.of_worker : 0, hi = lo + a.of_worker;
+            if (a.add && !(live >> lo & (~uint64_t(0) >> (64 - a.of_worker)))) continue;
             f32x4 de[J];
 #pragma unroll
             for (int j = 0; j < J; ++j) de[j] = f32x4{0, 0, 0, 0};
-            for (int kk = 0; kk * 32 < a.n; ++kk)
+            for (int kk = lo / 32; kk * 32 < hi; ++kk) {
+                // one worker's rows, of both operands: another's may be NaN
+                u32x4 keep;
 #pragma unroll
-                for (int j = 0; j < J; ++j)
+                for (int e = 0; e < 4; ++e) {
+                    const int32_t row = kk * 32 + k8 * 8 + 2 * e;
+                    keep[e] = (row >= lo && row < hi ? 0xffffu : 0u) |
+                              (row + 1 >= lo && row + 1 < hi ? 0xffff0000u : 0u);
+                }
+                auto kept = [&](bf16x8 v) {
+                    if (!WORKERS) return v;
+                    return __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, v) & keep);
+                };
+                bf16x8 dz[PT];
+#pragma unroll
+                for (int i = 0; i < PT; ++i) dz[i] = kept(frag_t(s_dzt[i], wave * 16 + c, kk));
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    bf16x8 h[NP];
+#pragma unroll
+                    for (int i = 0; i < NP; ++i)
+                        h[i] = kept(frag_t(s_h[i], (j0 + j) * 16 + c, kk));
                     products<PT, NP>([&](int pz, int ph) {
-                        de[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            frag_t(s_h[ph], (j0 + j) * 16 + c, kk), frag_t(s_dzt[pz], wave * 16 + c, kk),
-                            de[j], 0, 0, 0);
+                        de[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[ph], dz[pz], de[j], 0, 0,
+                                                                       0);
                     });
+                }
+            }
+            const float by = WORKERS ? __shfl(outside, p, 64) : outside;
             const int32_t v = t * kTile + wave * 16 + c;
+            const int64_t at = p * a.worker_stride + v * a.ld_dtable;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const int64_t d = d0 + (j0 + j) * 16 + k8 * 4;
                 if (v >= a.V || d >= a.D) continue;
-                if (a.type == ECC_F32) 
-                    add_quad((float *)a.dtable + v * a.ld_dtable + d, de[j] * by, a.D - d, a.add);
+                if (a.type == ECC_F32)
+                    add_quad((float *)a.dtable + at + d, de[j] * by, a.D - d, a.add);
                 else
-                    add_quad((bf16_t *)a.dtable + v * a.ld_dtable + d, de[j] * by, a.D - d, a.add);
+                    add_quad((bf16_t *)a.dtable + at + d, de[j] * by, a.D - d, a.add);
             }
         }
         __syncthreads();
@@ -776,7 +817,7 @@ struct Plan {
     int np;                      // pieces of the operands
     int pz, pzt;                 // of dz for dh, for dE
     bool pack_table;
-    bool few;                    // one worker, up to kFewRows rows
+    bool few;                    // up to kFewRows rows in all
     bool tiles_z, pack_h;        // few rows: logits by tiles, of packed rows
     int32_t blocks_d, splits, per;
     GemmShape shape_z, shape_h, shape_e;
@@ -796,7 +837,8 @@ struct Plan {
 bool few_by_tiles(const ecc_cross_entropy_t *a) {
     const bool f32 = a->type == ECC_F32;
     static constexpr double kTimes[2][3] = {{0.0075, 0.0115, 0.0165}, {0.013, 0.022, 0.036}};
-    const double each = kTimes[f32][a->n <= 16 ? 0 : a->n <= 32 ? 1 : 2];
+    const int64_t N = a->P * a->n;
+    const double each = kTimes[f32][N <= 16 ? 0 : N <= 32 ? 1 : 2];
     const double few = 8.0 + (double)((a->V + 64 * 256 - 1) / (64 * 256)) * a->D * each;
     const double table = (double)a->V * a->D * 1e-6;
     const double tiles = f32 || a->D % 64 ? 24.0 + table * (f32 ? 3.6 : 1.4) : 19.0 + table * 0.4;
@@ -807,7 +849,8 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     Plan p{};
     p.N = a->P * a->n;
     p.n_pad = pad64(a->n);
-    p.rows = a->P * p.n_pad;
+    p.few = p.N <= kFewRows;
+    p.rows = p.few ? kFewRows : a->P * p.n_pad;
     p.Dp = pad64(a->D);
     p.Vp = pad64(a->V);
     p.tiles = (int32_t)(p.Vp / 64);
@@ -815,7 +858,6 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.np = f32 ? 3 : 1;
     p.pz = f32 ? 3 : 1;
     p.pzt = a->grad_type == ECC_F32 ? 3 : 1;
-    p.few = a->P == 1 && a->n <= kFewRows;
     p.pack_table = !as_it_lies(a->d_table, a->ld_table, a->D, a->type);
     const int64_t row = p.np * 2 * p.Dp * (gradient ? 2 : 1) + p.tiles * 8 + 16 +
                         (gradient ? 4 * p.Vp + 2 * p.pz * p.Vp + 2 * p.pzt * p.Vp : 0);
@@ -847,8 +889,8 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
             p.pack_h = !as_it_lies(a->d_h, a->ld_h, a->D, a->type);
             p.h = take(p.pack_h ? p.np * 2 * p.R * p.Dp : 0);
             p.table = take(p.pack_table ? p.np * 2 * p.Vp * p.Dp : 0);
-            p.shape_z = gemm_shape(a->n, a->V, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
-            p.parts_z = take(split_bytes(a->n, a->V, p.shape_z.splits, 1));
+            p.shape_z = gemm_shape(p.N, a->V, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 1, true);
+            p.parts_z = take(split_bytes(p.N, a->V, p.shape_z.splits, 1));
         }
         p.stats = take(8 * p.R * p.tiles);
         p.picked = take(4 * p.R);
@@ -981,8 +1023,13 @@ void launch_few(const FewArgs &f, const Plan &p, char *w, const FewGrad &g, bool
     };
     auto of_pieces = [&](auto pieces) {
         constexpr int PT = decltype(pieces)::value;
-        if (few) gradients(k_ce_few_grad<T, PT, true>, kFewWaves<T>);
-        else gradients(k_ce_few_grad<T, PT, false>, kFewWaves<T>);
+        auto of = [&](auto workers) {
+            constexpr bool WORKERS = decltype(workers)::value;
+            if (few) gradients(k_ce_few_grad<T, PT, true, WORKERS>, kFewWaves<T>);
+            else gradients(k_ce_few_grad<T, PT, false, WORKERS>, kFewWaves<T>);
+        };
+        if (g.of_worker < g.n) of(std::true_type{});
+        else of(std::false_type{});
     };
     if constexpr (std::is_same_v<T, float>) of_pieces(std::integral_constant<int, 3>{});
     else if (g.type == ECC_F32) of_pieces(std::integral_constant<int, 3>{});
@@ -1078,7 +1125,8 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
     if (p.few) {
         const LogitsOut logits{gradient ? (float *)(w + p.z) : nullptr, p.Vp, (float)a->scale,
                                (float2 *)(w + p.stats), p.tiles, a->d_labels, (float *)(w + p.picked)};
-        const FewArgs f{a->d_h, a->d_table, a->ld_h, a->ld_table, q, D, logits, rows,
+        const FewArgs f{a->d_h, a->d_table, a->ld_h, a->ld_table,
+                        {a->d_labels, a->d_weight, N, (int32_t)V}, (int32_t)a->n, D, logits, rows,
                         (float *)d_loss, (float)a->scale};
         RowArgs row{};
         row.M = kTile;
@@ -1089,9 +1137,10 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         row.loss = (float *)d_loss;
         float *terms = gradient ? (float *)(w + p.terms) : nullptr;
         row.out = RowTerms{terms, gradient ? terms + kTile : nullptr};
-        const FewGrad g{a->d_h, a->d_table, a->ld_h, a->ld_table, (int32_t)N, (int32_t)V, D,
-                        logits.z, p.Vp, row, d_dh ? (float *)(w + p.parts[0]) : nullptr, p.Dp,
-                        d_dtable, ld_dtable, a->grad_type, accumulate, p.blocks_d, p.per};
+        const FewGrad g{a->d_h, a->d_table, a->ld_h, a->ld_table, (int32_t)N, (int32_t)a->n,
+                        (int32_t)V, D, logits.z, p.Vp, row,
+                        d_dh ? (float *)(w + p.parts[0]) : nullptr, p.Dp, d_dtable, ld_dtable,
+                        worker_stride, a->grad_type, accumulate, p.blocks_d, p.per};
         if (a->type == ECC_F32) launch_few<float>(f, p, w, g, gradient, d_dh, ld_dh, s);
         else launch_few<bf16_t>(f, p, w, g, gradient, d_dh, ld_dh, s);
         ECC_LAUNCH_CHECK();

@@ -301,6 +301,39 @@ def test_few_rows(dtype, grad, n, D, V):
         assert (buf == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype,grad", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("P,n,D,V", [
+    (2, 32, 64, 100), (64, 1, 70, 130), (3, 21, 33, 2100), (9, 7, 129, 63), (2, 3, 640, 2500),
+    (6, 10, 2112, 300)])
+def test_few_rows_of_workers(dtype, grad, P, n, D, V):
+    """Up to 64 rows of several workers: each one's table gradient from its rows
+    alone, alike or different weights, one whose rows do not count, added to what
+    is there, and NaN and infinities in another worker's rows."""
+    lm = _lm()
+    announce("cross entropy, few rows of workers", dtype, grad, P, n, D, V)
+    h, table, y, w = _inputs(P * n, D, V, dtype, 23)
+    y[:n] = -1
+    y[n], w[n] = V - 1, 0.6
+    want = _check(h, table, y, w, P=P, dtype=grad)
+    assert (want[2][0] == 0).all()
+    own = torch.arange(1, P + 1, device="cuda").repeat_interleave(n) / (2.0 * P)
+    _check(h, table, y, own.float(), scale=-1.5, P=P, dtype=grad)
+    gap = torch.full((P, V + 2, D + 3), 7.0, dtype=grad, device="cuda")
+    dt = gap[:, 1:V + 1, 2:D + 2]
+    dt.zero_()
+    dt[0] = -0.0
+    got = lm.cross_entropy(h, table, y, w, P=P, dtable=dt, accumulate=True)
+    assert torch.equal(got[2], want[2]) and torch.signbit(dt[0]).all()
+    dt.fill_(7.0)
+    assert (gap == 7.0).all()
+    bad = h.clone()
+    bad[n, 0], bad[2 * n - 1, D - 1] = math.inf, math.nan
+    got = lm.cross_entropy(bad, table, y, w, P=P, dtype=grad)
+    keep = torch.arange(P, device="cuda") != 1
+    assert torch.equal(got[2][keep], want[2][keep])
+    assert torch.equal(got[1].view(P, n, D)[keep], want[1].view(P, n, D)[keep])
+
+
 @pytest.mark.parametrize("dtype,grad,n,D,V", [
     (BF16, BF16, 50, 130, 700), (BF16, F32, 9, 520, 2500), (F32, F32, 33, 70, 400),
     (BF16, BF16, 60, 2048, 500), (F32, F32, 40, 2050, 300)])
