@@ -308,11 +308,32 @@ void launch_few(const ecc_ffn_t *a, void *d_y, int64_t ld_y, hipStream_t s) {
 struct Plan {
     int64_t N, n_pad, rows, Dp, Fp;
     int np, pd;                   // pieces of the operands, of dg and du
+    bool few;                     // forward by k_ffn_few
     bool pack_x, pack_gate, pack_up;
     GemmShape shape_f, shape_x, shape_w;
     int64_t parts_f[2];
     int64_t x, gate, up, x_t, w_t, d, d_t, parts[2], bytes;
 };
+
+// Do few rows go by k_ffn_few?  By the times that it and the tiles take, in us per
+// MB of bf16 weights: one, two or four blocks of 16 rows, each read again for
+// every 16 columns, of rows that begin at 16 bytes or not; and how long one
+// workgroup takes for its share of D.  Tiles pack weights whose rows are no
+// multiple of 64.  D 4,096, F 12,288: 8 rows 37 us and 34 us, 64 rows 69 us and 34
+// us; D 4,096, F 1,000: 8 rows 13 us and 19 us, 64 rows 24 us and 20 us; D 2,001,
+// F 5,003: 8 rows 32 us and 36 us, 64 rows 64 us and 36 us.  fp32 weights, 64 rows,
+// D 4,096, F 12,288: 178 us and 400 us; D 2,001, F 5,003: 61 us and 82 us.
+bool takes_few(const ecc_ffn_t *a) {
+    const int64_t N = a->P * a->n;
+    if (N > kFewRows) return false;
+    if (a->type == ECC_F32) return true;
+    static constexpr double kTimes[2][3] = {{0.138, 0.19, 0.29}, {0.54, 0.83, 1.34}};
+    static constexpr double kLong[3] = {0.0007, 0.0016, 0.0034};
+    const int rows = N <= 16 ? 0 : N <= 32 ? 1 : 2;
+    const double mb = 4e-6 * (double)a->D * a->F;
+    const double few = 10.0 + std::max(mb * kTimes[a->D % 8 != 0][rows], a->D * kLong[rows]);
+    return few <= 14.0 + mb * (a->D % 64 ? 0.52 : 0.1);
+}
 
 Plan make_plan(const ecc_ffn_t *a, bool gradient) {
     Plan p{};
@@ -323,6 +344,11 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
     p.Fp = pad64(a->F);
     p.np = a->type == ECC_F32 ? 3 : 1;
     p.pd = a->type == ECC_F32 || a->grad_type == ECC_F32 ? 3 : 1;
+    p.few = !gradient && takes_few(a);
+    if (p.few) {
+        p.bytes = 16;
+        return p;
+    }
     p.pack_x = !as_it_lies(a->d_x, a->ld_x, a->D, a->type);
     p.pack_gate = !as_it_lies(a->d_w_gate, a->ld_gate, a->D, a->type);
     p.pack_up = !as_it_lies(a->d_w_up, a->ld_up, a->D, a->type);
@@ -338,7 +364,6 @@ Plan make_plan(const ecc_ffn_t *a, bool gradient) {
     p.gate = take(p.pack_gate ? p.np * 2 * p.Fp * p.Dp : 0);
     p.up = take(p.pack_up ? p.np * 2 * p.Fp * p.Dp : 0);
     p.shape_f = gemm_shape(p.N, a->F, p.Dp / kGemmK * (p.np == 3 ? 6 : 1), 2, true);
-    if (!gradient && p.N <= kFewRows) p.shape_f.splits = 1;
     for (int64_t &at_f : p.parts_f) at_f = take(split_bytes(p.N, a->F, p.shape_f.splits, 1));
     if (gradient) {
         p.x_t = take(p.np * 2 * a->D * p.rows);
@@ -483,7 +508,7 @@ ecc_status_t ecc_ffn_forward(const ecc_ffn_t *a, void *d_y, int64_t ld_y, void *
         for (const Span &i : in) ECC_ARG(!spans_meet(o, i), "an output overlaps an input");
     ECC_ARG(!spans_meet(out[0], out[1]), "an output and the work buffer overlap");
     hipStream_t s = (hipStream_t)hip_stream;
-    if (p.N <= kFewRows) {
+    if (p.few) {
         with_kind(a, [&](auto t, auto act) {
             launch_few<decltype(t), decltype(act)::value>(a, d_y, ld_y, s);
         });

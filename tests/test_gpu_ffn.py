@@ -130,6 +130,33 @@ def test_larger(dtype, P, n, D, F):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,D,F", [
+    (1, 4096, 6700), (16, 4096, 6400), (32, 4096, 300), (33, 4096, 300), (64, 4097, 260),
+    (20, 2001, 3000), (40, 1000, 5100), (64, 136, 100)])
+def test_few_rows(dtype, n, D, F):
+    """Up to 64 rows on either side of where tiles take over, with the same bits
+    at any alignment, in and out."""
+    lm = _lm()
+    announce("ffn, few rows", dtype, n, D, F)
+    x, wg, wu, _ = _inputs(n, D, F, dtype, 21)
+    for act in ("silu", "gelu"):
+        y = lm.gated_ffn(x, wg, wu, act=act)
+        within(y, *_forward(x, wg, wu, act), "y")
+
+    def wide(t, gap, at):
+        buf = torch.full((t.shape[0], t.shape[1] + gap), 7.0, dtype=dtype, device="cuda")
+        buf[:, at:at + t.shape[1]] = t
+        return buf, buf[:, at:at + t.shape[1]]
+    sx, sg, su = (wide(t, 5, 3)[1] for t in (x, wg, wu))
+    obuf, out = wide(torch.zeros_like(y), 3, 1)
+    for args in ((sx, wg, wu), (x, sg, su), (sx, wg, su)):
+        lm.gated_ffn(*args, act=act, out=out)
+        assert torch.equal(out, y)
+        out.fill_(7.0)
+        assert (obuf == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_strides_and_alignments(dtype):
     """Rows with gaps, arrays at any element, outputs in wide buffers whose gaps
     stay, more leading dimensions; the same bits as dense operands give."""
