@@ -828,18 +828,21 @@ struct Plan {
 
 // Do few rows' logits take gemm.h's tiles?  By the times that both take, in us:
 // k_ce_few takes so much per round of 256 workgroups and element of D for its
-// one, two or four blocks of 16 rows, which it reads again for every 64 columns;
-// tiles read the table at 5 bytes a ns, once they are under way, but pack it
-// first if its rows are fp32 or no multiple of 64.  bf16, 64 rows, D 4,096, V
-// 128,000: 590 us and 223 us; 1 row, D 1,024, V 1,000: 13 us and 20 us, with the
-// loss.  fp32, 64 rows: D 4,096, V 1,000: 155 us and 40 us; D 2,048, V 32,000: 171
-// us and 283 us.
+// one, two or four blocks of 16 rows, which it reads again for every 64 columns
+// (twice as much for rows of bf16 that do not begin at 4 bytes); tiles read the
+// table at 5 bytes a ns, once they are under way, but pack it first if its rows
+// are fp32 or no multiple of 64.  The loss alone, bf16: 64 rows, D 4,096, V
+// 128,000: 590 us and 223 us; 1 row, D 1,024, V 1,000: 13 us and 20 us; 32 rows, D
+// 2,001, V 5,003: 65 us and 30 us; 64 rows, D 3,268, V 49,125: 194 us and 237 us.
+// fp32, 64 rows: D 4,096, V 1,000: 155 us and 40 us; D 2,048, V 32,000: 171 us and
+// 283 us.
 bool few_by_tiles(const ecc_cross_entropy_t *a) {
     const bool f32 = a->type == ECC_F32;
     static constexpr double kTimes[2][3] = {{0.0075, 0.0115, 0.0165}, {0.013, 0.022, 0.036}};
     const int64_t N = a->P * a->n;
     const double each = kTimes[f32][N <= 16 ? 0 : N <= 32 ? 1 : 2];
-    const double few = 8.0 + (double)((a->V + 64 * 256 - 1) / (64 * 256)) * a->D * each;
+    const double odd = f32 || a->D % 2 == 0 ? 1.0 : 2.0;
+    const double few = 8.0 + (double)((a->V + 64 * 256 - 1) / (64 * 256)) * a->D * each * odd;
     const double table = (double)a->V * a->D * 1e-6;
     const double tiles = f32 || a->D % 64 ? 24.0 + table * (f32 ? 3.6 : 1.4) : 19.0 + table * 0.4;
     return tiles < few;

@@ -317,7 +317,7 @@ struct Plan {
 
 // Do few rows go by k_ffn_few?  By the times that it and the tiles take, in us per
 // MB of bf16 weights: one, two or four blocks of 16 rows, each read again for
-// every 16 columns, of rows that begin at 16 bytes or not; and how long one
+// every 16 columns, of rows that begin at 4 bytes or not; and how long one
 // workgroup takes for its share of D.  Tiles pack weights whose rows are no
 // multiple of 64.  D 4,096, F 12,288: 8 rows 37 us and 34 us, 64 rows 69 us and 34
 // us; D 4,096, F 1,000: 8 rows 13 us and 19 us, 64 rows 24 us and 20 us; D 2,001,
@@ -331,7 +331,7 @@ bool takes_few(const ecc_ffn_t *a) {
     static constexpr double kLong[3] = {0.0007, 0.0016, 0.0034};
     const int rows = N <= 16 ? 0 : N <= 32 ? 1 : 2;
     const double mb = 4e-6 * (double)a->D * a->F;
-    const double few = 10.0 + std::max(mb * kTimes[a->D % 8 != 0][rows], a->D * kLong[rows]);
+    const double few = 10.0 + std::max(mb * kTimes[a->D % 2 != 0][rows], a->D * kLong[rows]);
     return few <= 14.0 + mb * (a->D % 64 ? 0.52 : 0.1);
 }
 
