@@ -316,23 +316,24 @@ struct Plan {
 };
 
 // Do few rows go by k_ffn_few?  By the times that it and the tiles take, in us per
-// MB of bf16 weights: one, two or four blocks of 16 rows, each read again for
-// every 16 columns, of rows that begin at 4 bytes or not; and how long one
-// workgroup takes for its share of D.  Tiles pack weights whose rows are no
-// multiple of 64.  D 4,096, F 12,288: 8 rows 37 us and 34 us, 64 rows 69 us and 34
-// us; D 4,096, F 1,000: 8 rows 13 us and 19 us, 64 rows 24 us and 20 us; D 2,001,
-// F 5,003: 8 rows 32 us and 36 us, 64 rows 64 us and 36 us.  fp32 weights, 64 rows,
-// D 4,096, F 12,288: 178 us and 400 us; D 2,001, F 5,003: 61 us and 82 us.
+// MB of bf16 weights out of memory: one, two or four blocks of 16 rows, each read
+// again for every 16 columns, of rows that begin at 4 bytes or not; and how long
+// one workgroup takes for its share of D.  Tiles pack weights whose rows are no
+// multiple of 64.  D 4,096, F 12,288: 8 rows 39 us and 48 us, 64 rows 74 us and 50
+// us; D 4,096, F 1,000: 8 rows 13 us and 17 us, 64 rows 25 us and 21 us; D 2,001, F
+// 5,003: 8 rows 29 us and 35 us, 64 rows 64 us and 37 us; D 1,000, F 8,000: 64 rows
+// 16 us and 30 us.  (Weights that the last cache holds come out in 34 us instead of
+// 48, a loop over one layer's.)  fp32, 64 rows, D 4,096, F 4,096: 63 us and 138 us.
 bool takes_few(const ecc_ffn_t *a) {
     const int64_t N = a->P * a->n;
     if (N > kFewRows) return false;
     if (a->type == ECC_F32) return true;
-    static constexpr double kTimes[2][3] = {{0.138, 0.19, 0.29}, {0.54, 0.83, 1.34}};
-    static constexpr double kLong[3] = {0.0007, 0.0016, 0.0034};
+    static constexpr double kTimes[2][3] = {{0.165, 0.225, 0.325}, {0.57, 0.87, 1.38}};
+    static constexpr double kLong[3] = {0.0013, 0.0021, 0.0039};
     const int rows = N <= 16 ? 0 : N <= 32 ? 1 : 2;
     const double mb = 4e-6 * (double)a->D * a->F;
-    const double few = 10.0 + std::max(mb * kTimes[a->D % 2 != 0][rows], a->D * kLong[rows]);
-    return few <= 14.0 + mb * (a->D % 64 ? 0.52 : 0.1);
+    const double few = 9.0 + std::max(mb * kTimes[a->D % 2][rows], a->D * kLong[rows]);
+    return few <= (a->D % 64 ? 12.0 + mb * 0.57 : std::max(17.0, 10.0 + mb * 0.19));
 }
 
 Plan make_plan(const ecc_ffn_t *a, bool gradient) {
