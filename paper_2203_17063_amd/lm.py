@@ -631,8 +631,7 @@ def _tensors(grads, out, P):
             if out_kind is None:
                 _type(o, "an output")
             pack(data, at, g.data_ptr(), o.data_ptr(), n, stride,
-                 stride if o.is_contiguous() else _worker_parts(o, P, "an output")[1], kind,
-                 out_kind)
+                 n if o.is_contiguous() else _worker_parts(o, P, "an output")[1], kind, out_kind)
         at += size
     return (E.ecc_tensor_t * count).from_buffer(data), grads[0]
 

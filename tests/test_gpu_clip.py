@@ -191,6 +191,41 @@ def test_into_contributions():
     assert ((grads[1].double() - keep.double() * by[:, None]).abs() <= 1e-6 * keep.abs()).all()
 
 
+@pytest.mark.parametrize("wide_out", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_out_of_contributions(dtype, wide_out):
+    """Gradients within one buffer of all workers', as the feed-forward block and
+    cross entropy write them, clipped into dense tensors and into places of
+    another pitch; what lies around the outputs stays."""
+    lm = _lm()
+    announce("clip, out of contributions", dtype, wide_out)
+    P, shapes = 3, [(31, 7), (1,), (5000,), (2, 10)]
+    sizes = [math.prod(s) for s in shapes]
+    wide = torch.zeros((P, 2 * sum(sizes)), dtype=dtype, device="cuda")
+    grads, at = [], 5
+    for dense, s, n in zip(_grads(shapes, [dtype] * 4, P, 11), shapes, sizes):
+        grads.append(wide[:, at:at + n].unflatten(1, s))
+        grads[-1].copy_(dense)
+        at += n + 3
+    want = _norms(grads, P)
+    for out_type in (F32, F64):
+        # (room for a worker's elements at any of the gradients' distances)
+        room = P * wide.shape[1] + 64
+        bufs, out = [], []
+        for s, n in zip(shapes, sizes):
+            bufs.append(torch.full((room,), 7.0, dtype=out_type, device="cuda"))
+            pitch = n + 11 if wide_out else n
+            out.append(bufs[-1][16:16 + P * pitch].view(P, pitch)[:, :n].unflatten(1, s))
+            assert out[-1].is_contiguous() != wide_out
+        _near(lm.clip_grads(grads, 1.0, P=P, out=out), want, sum(sizes))
+        for g, o, buf in zip(grads, out, bufs):
+            exact = g.double() * (1.0 / want).cuda().view((P,) + (1,) * (g.dim() - 1))
+            tol = ULP[out_type] * exact.abs() + 1e-12 * exact.abs()
+            assert ((o.double() - exact).abs() <= tol).all()
+            o.fill_(7.0)
+            assert (buf == 7.0).all()
+
+
 def test_alignments():
     """Tensors at every element of 16 bytes, of every length around the vectors'."""
     lm = _lm()

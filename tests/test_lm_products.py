@@ -222,3 +222,37 @@ def test_clip_refused():
     with pytest.raises(E.EccError) as e:
         E.ecc_grad_norm(1, 1, _tensors({}), 1 << 20, 9 << 20)
     assert e.value.status == E.ECC_ERR_ARG
+
+
+@pytest.mark.parametrize("wide_grad", [False, True])
+@pytest.mark.parametrize("wide_out", [False, True])
+@pytest.mark.parametrize("P", [None, 1, 3])
+def test_workers_of_gradients_and_outputs(wide_grad, wide_out, P, monkeypatch):
+    """What the library is told of dense gradients and of gradients within wider
+    buffers, beside dense outputs and outputs within wider ones: a worker's
+    elements, and each tensor's own distance from one worker to the next."""
+    torch = pytest.importorskip("torch")
+    from paper_2203_17063_amd import lm
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0, raising=False)
+    lead = () if P is None else (P,)
+
+    def tensors(wide, pitch, dtype):
+        if P is None or not wide:
+            return [torch.zeros(lead + s, dtype=dtype) for s in ((2, 5), (7,))]
+        flat = torch.zeros((P, pitch), dtype=dtype)
+        return [flat[:, 3:13].unflatten(1, (2, 5)), flat[:, 20:27]]
+    grads, outs = tensors(wide_grad, 100, torch.float32), tensors(wide_out, 60, torch.float64)
+    a, first = lm._tensors(grads, outs, P)
+    assert first is grads[0] and len(a) == 2
+    for t, g, o, n in zip(a, grads, outs, (10, 7)):
+        assert (t.d_grad, t.d_out, t.n) == (g.data_ptr(), o.data_ptr(), n)
+        assert (t.type, t.out_type) == (E.ECC_F32, E.ECC_F64)
+        if P == 3:    # (of one worker there is no distance)
+            assert t.stride == (100 if wide_grad else n)
+            assert t.out_stride == (60 if wide_out else n)
+    # the last worker's elements lie within the tensors that were given
+    for t, g, o in zip(a, grads, outs):
+        for at, stride, held in ((t.d_grad, t.stride, g), (t.d_out, t.out_stride, o)):
+            memory = held.untyped_storage()
+            end = at + (((P or 1) - 1) * stride + t.n) * held.element_size()
+            assert end <= memory.data_ptr() + memory.nbytes()
