@@ -140,14 +140,16 @@ struct PackList {
     PackArgs a[8];
     int32_t count;
     int32_t first[8];   // their first blocks
+    int32_t at;         // the launch's first block
 };
 
 template <typename T>
 static __global__ __launch_bounds__(256) void k_pack(PackList l) {
+    const int32_t block = (int32_t)blockIdx.x + l.at;
     int i = 0;
     for (int k = 1; k < l.count; ++k)
-        if ((int32_t)blockIdx.x >= l.first[k]) i = k;
-    pack_block<T>(l.a[i], (int32_t)blockIdx.x - l.first[i]);
+        if (block >= l.first[k]) i = k;
+    pack_block<T>(l.a[i], block - l.first[i]);
 }
 
 // Matrices of one type to pack.
@@ -161,10 +163,14 @@ struct Packing {
         blocks += a.rows_packed / kTile * a.col_blocks;
     }
     void launch(int32_t type, hipStream_t s) {
-        if (blocks == 0) return;
-        if (type == ECC_F32)
-            hipLaunchKernelGGL(k_pack<float>, dim3((unsigned)blocks), dim3(256), 0, s, l);
-        else hipLaunchKernelGGL(k_pack<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, s, l);
+        // (a launch has fewer than 2^32 threads)
+        constexpr int64_t kMost = int64_t(1) << 23;
+        for (int64_t at = 0; at < blocks; at += kMost) {
+            l.at = (int32_t)at;
+            const dim3 grid((unsigned)std::min(kMost, blocks - at));
+            if (type == ECC_F32) hipLaunchKernelGGL(k_pack<float>, grid, dim3(256), 0, s, l);
+            else hipLaunchKernelGGL(k_pack<bf16_t>, grid, dim3(256), 0, s, l);
+        }
     }
 };
 

@@ -16,7 +16,8 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from gpu_common import announce                                        # noqa: E402
-from product_bounds import BF16, F32, F64, U, ULP, product, within     # noqa: E402
+from product_bounds import (BF16, F32, F64, U, ULP, product, product_error,     # noqa: E402
+                            within)
 
 pytestmark = pytest.mark.gpu
 
@@ -226,6 +227,31 @@ def test_no_rows(dtype):
         one = [torch.ones((P, 5, 7), dtype=dtype, device="cuda") for _ in range(2)]
         lm.gated_ffn_grad(x, wg, wg, dy, P=P, dw_gate=one[0], dw_up=one[1], accumulate=True)
         assert all((t == 1).all() for t in one)
+
+
+def test_many_workers():
+    """Workers of one row each, padded to 64: dg and du in their other order, in
+    three pieces, take more workgroups than one launch has."""
+    lm = _lm()
+    P, F = 44500, 4032
+    announce("ffn, many workers", P, F)
+    assert 6 * P * (F // 64) * 256 >= 2 ** 32
+    if torch.cuda.mem_get_info()[0] < (170 << 30):
+        pytest.skip("not enough memory")
+    x, wg, wu, dy = _inputs(P, 1, F, BF16, 22)
+    got = lm.gated_ffn_grad(x, wg, wu, dy, P=P, dtype=F32)
+    # _backward's formulas, for products of one term
+    a, ea, da, eda, u, eu = _projections(x, wg, wu, "silu")
+    x, dy = x.double(), dy.double()
+    dg, du = dy * u * da, dy * a
+    edg = dy.abs() * (eu * (da.abs() + eda) + u.abs() * eda) + 4 * U * dg.abs()
+    edu = dy.abs() * ea + 4 * U * du.abs()
+    for name, d, e in (("dw_gate", dg, edg), ("dw_up", du, edu)):
+        error = (product_error(1, F32) * (d.abs() + e) + e) * x.abs()
+        bad = (got[name][:, :, 0].double() - d * x).abs() > error + ULP[F32] * (d * x).abs() + 2.0 ** -120
+        assert not bad.any(), (name, int(bad.sum()))
+    del got
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
