@@ -864,14 +864,12 @@ Plan make_plan(const ecc_cross_entropy_t *a, bool gradient) {
     p.pack_table = !as_it_lies(a->d_table, a->ld_table, a->D, a->type);
     const int64_t row = p.np * 2 * p.Dp * (gradient ? 2 : 1) + p.tiles * 8 + 16 +
                         (gradient ? 4 * p.Vp + 2 * p.pz * p.Vp + 2 * p.pzt * p.Vp : 0);
-    // (large tiles' rows at a time; of vocabularies beyond 1.3e6, whose 256 rows may
-    // not fit, blocks of 64, which always do: 16 bytes for each of 64 x 2^22 logits)
-    const int64_t fit = kPieceBytes / row, unit = fit < 256 ? 64 : 256;
-    p.R = std::max<int64_t>(64, std::min(fit & -unit, p.rows));
+    p.R = std::max<int64_t>(256, kPieceBytes / row & ~int64_t(255));
+    p.R = std::max<int64_t>(64, std::min(p.R, p.rows));
     p.pieces_of_rows = (p.rows + p.R - 1) / p.R;
     // (pieces of equal length)
     if (p.pieces_of_rows > 1)
-        p.R = (p.rows / p.pieces_of_rows + unit - 1 + (p.rows % p.pieces_of_rows > 0)) & -unit;
+        p.R = (p.rows / p.pieces_of_rows + 255 + (p.rows % p.pieces_of_rows > 0)) & ~int64_t(255);
     p.pieces_of_rows = (p.rows + p.R - 1) / p.R;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
