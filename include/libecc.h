@@ -828,7 +828,9 @@ ecc_status_t ecc_distill(const ecc_distill_t *a, void *d_loss, void *d_dz, int64
  *   dh_r = sum_j dz_r[j] E_j,   dE_p[j] = sum over worker p's rows of dz_r[j] h_r
  * A row whose label y_r lies outside [0, V), or whose weight is 0, is not
  * read: its loss and gradient are 0 (d_weight NULL: all 1).  The logits exist
- * for a piece of rows at a time, 5 GiB of them and their gradients at most.
+ * for a piece of rows at a time: 5 GiB of them and their gradients at most, or
+ * 256 rows where those take more (V from 1.3e6 on; 16 GiB for the largest
+ * vocabulary in fp32).
  *   d_h        P * n rows of `type`, ECC_F32 or ECC_BF16; d_table V rows of it
  *   d_labels   int32 [P * n];  d_weight  fp32 [P * n] or NULL
  *   d_loss     fp32 [P * n]

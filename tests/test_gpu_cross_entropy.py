@@ -251,6 +251,33 @@ def test_several_pieces_of_rows(dtype, grad, P):
     within(new, value, 13 * size + 2 * U * (value.abs() + size), "dtable, added to")
 
 
+@pytest.mark.parametrize("dtype,grad", [(BF16, BF16), (BF16, F32), (F32, F32)])
+def test_largest_vocabulary(dtype, grad):
+    """As many tokens as are taken, of which 256 rows are a piece."""
+    from paper_2203_17063_amd import capi as E
+    lm = _lm()
+    N, D, V = 300, 3, E.ECC_CROSS_ENTROPY_MAX_VOCAB
+    announce("cross entropy, largest vocabulary", dtype, grad)
+    if torch.cuda.mem_get_info()[0] < (64 << 30):
+        pytest.skip("not enough memory")
+    h, table, y, w = _inputs(N, D, V, dtype, 24)
+    y[7] = V - 1
+    loss, dh, dtable = lm.cross_entropy(h, table, y, w, dtype=grad)
+    total = torch.zeros((1, V, D), dtype=F64, device="cuda")
+    error = torch.zeros_like(total)
+    step = 30
+    for r in range(0, N, step):
+        rows = slice(r, r + step)
+        want = _reference(h[rows], table, y[rows], w[rows], 1.0, 1, grad)
+        within(loss[rows], *want[0], "loss")
+        within(dh[rows], *want[1], "dh")
+        total += want[2][0]
+        error += want[2][1]
+    # (the sum over all rows is one chain, and pieces are added in fp32)
+    size = error + 2 * U * 10 * (total.abs() + error)
+    within(dtable, total, 11 * size, "dtable")
+
+
 def test_no_rows():
     lm = _lm()
     announce("cross entropy, no rows")

@@ -256,3 +256,20 @@ def test_workers_of_gradients_and_outputs(wide_grad, wide_out, P, monkeypatch):
             memory = held.untyped_storage()
             end = at + (((P or 1) - 1) * stride + t.n) * held.element_size()
             assert end <= memory.data_ptr() + memory.nbytes()
+
+
+@pytest.mark.parametrize("V", [1 << 20, 2000001, E.ECC_CROSS_ENTROPY_MAX_VOCAB])
+@pytest.mark.parametrize("kinds", [(E.ECC_F32, E.ECC_F32), (E.ECC_BF16, E.ECC_F32),
+                                   (E.ECC_BF16, E.ECC_BF16)])
+def test_cross_entropy_pieces_of_large_vocabularies(V, kinds):
+    """A piece's logits and gradients stay within 5 GiB, or 256 rows of them,
+    however many rows there are."""
+    operands, grads = (3 if kind == E.ECC_F32 else 1 for kind in kinds)
+    # a logit in fp32, its gradient's pieces in both orders, 8 bytes for 64 of them
+    row = (V + 63) // 64 * (64 * (4 + 2 * operands + 2 * grads) + 8)
+    for P, n in ((1, 4096), (3, 100), (1, 1 << 20)):
+        a = _ce(n=n, V=V, P=P, d_table=1 << 33, type=kinds[0], grad_type=kinds[1])
+        # beside it: the table's pieces in both orders, sums of a bf16 gradient over
+        # pieces of rows, and what is kept per row and worker
+        rest = (2 * operands * 2 * 64 + 4 * P * 64) * (V + 64) + 64 * n * P + (1 << 26)
+        assert E.ecc_cross_entropy_work_size(a, 1) < max(5 << 30, 256 * row) + rest
