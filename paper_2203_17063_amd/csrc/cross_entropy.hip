@@ -385,8 +385,9 @@ constexpr int32_t kFewTiles = 32;
 
 // softmax - [label] in both orders, blocks of 64 x 64.  Bound by memory: 4 bytes
 // read and 2 written for each order and piece.  FEW: the blocks join the tiles
-// of their rows by themselves, and zero the positions that do not count.
-template <bool FEW>
+// of their rows by themselves, and zero the positions that do not count.  Rows of
+// fp32 take exponentials within 2 ulp, so that small probabilities keep their digits.
+template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
     __shared__ PackTile s;
     __shared__ float s_most[kTile], s_soft[kTile];
@@ -430,7 +431,7 @@ __global__ __launch_bounds__(256) void k_ce_dz(DzArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int32_t j = col0 + c8 + e;
-            float v = exp_short(x[p].get<float>(e) - most) * soft;
+            float v = exp_of<T>(x[p].get<float>(e) - most) * soft;
             if (j == y) v -= 1.0f;
             mine[p][e] = y >= 0 && j < a.V ? v : 0.0f;
         }
@@ -695,7 +696,7 @@ __global__ __launch_bounds__((64 * kFewWaves<T>), 4) void k_ce_few_grad(FewGrad 
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const int32_t j = t * kTile + c0 + i * N + e;
-                float p = exp_short(z[i].template get<float>(e) - most) * soft;
+                float p = exp_of<T>(z[i].template get<float>(e) - most) * soft;
                 if (j == y) p -= 1.0f;
                 v[e] = held && j < a.V ? p : 0.0f;
                 u[e] = v[e] * inside;
@@ -1240,10 +1241,12 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
         z.pieces_t = p.pzt;
         z.col_blocks = p.tiles;
         z.blocks = (int32_t)(R / kTile * p.tiles);
-        if (few)
-            hipLaunchKernelGGL(k_ce_dz<true>, dim3((unsigned)(z.blocks + (unread + 3) / 4)),
-                               dim3(256), 0, s, z);
-        else hipLaunchKernelGGL(k_ce_dz<false>, dim3((unsigned)z.blocks), dim3(256), 0, s, z);
+        const dim3 dz_grid((unsigned)(z.blocks + (few ? (unread + 3) / 4 : 0)));
+        auto softmax = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dz_grid, dim3(256), 0, s, z);
+        };
+        if (a->type == ECC_F32) softmax(few ? k_ce_dz<float, true> : k_ce_dz<float, false>);
+        else softmax(few ? k_ce_dz<bf16_t, true> : k_ce_dz<bf16_t, false>);
         Product products[2];
         GemmShape shapes[2];
         float *parts[2];

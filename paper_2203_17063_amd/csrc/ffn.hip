@@ -21,11 +21,6 @@ namespace {
 // derivative needs too.  For negative g that half is the factor itself, so that
 // small values keep their digits.  Exponentials of fp32 rows within 2 ulp, of
 // bf16 rows the short ones: 8,192 rows, D 256, F 2,501: 40 us against 45 us.
-template <typename T>
-__device__ __forceinline__ float exp_of(float x) {
-    if constexpr (std::is_same_v<T, float>) return exp_fast(x);
-    else return exp_short(x);
-}
 template <int ACT, typename T>
 __device__ __forceinline__ void activation(float g, float &a, float &da) {
     if constexpr (ACT == ECC_ACT_SILU) {

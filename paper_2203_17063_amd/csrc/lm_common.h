@@ -260,10 +260,17 @@ __device__ __forceinline__ float exp_fast(float x) {
     return __builtin_fmaf(e * kLn2, r, e);
 }
 // exp(x) off by (1.2 |x| + 1) 2^-24 of it, in five issue slots instead of
-// thirteen: for terms of a sum beside exp(0) (2,048 rows of 2,048 against 32,003:
-// 241 us against 251 us), and for rows of bf16.
+// thirteen: for rows of bf16, and for the sum over 64 columns beside exp(0) of any
+// rows (2,048 rows of 2,048 against 32,003: 241 us against 251 us), which it
+// leaves within 3.5 2^-24 (63 terms of x = -3.1; others count for less).
 __device__ __forceinline__ float exp_short(float x) {
     return __builtin_amdgcn_exp2f(x * 1.44269502f);
+}
+// exp(x) for rows of T.
+template <typename T>
+__device__ __forceinline__ float exp_of(float x) {
+    if constexpr (std::is_same_v<T, float>) return exp_fast(x);
+    else return exp_short(x);
 }
 // 1 / x within 1 ulp, 0 beyond 2^126
 __device__ __forceinline__ float recip_fast(float x) { return __builtin_amdgcn_rcpf(x); }

@@ -154,6 +154,30 @@ def test_large_logits(dtype):
     assert (loss[known & (w > 0)] >= 0).all()
 
 
+@pytest.mark.parametrize("P,n,V", [(1, 70, 300), (1, 70, 2500), (1, 40, 300), (1, 40, 2500),
+                                   (2, 9, 2500), (2, 100, 500)])
+def test_small_probabilities(P, n, V):
+    """fp32 probabilities down to e^-66, each to fp32's precision.  One row counts,
+    whose logits are the table's column itself: its gradient in the table is
+    softmax - [label], where the exponential is off by 4 u (2 ulp), the sum by 2
+    u (the other terms are below 1e-8 in all), its inverse by 2 u, their product
+    and the stored sum of three pieces by u each."""
+    announce("cross entropy, small probabilities", P, n, V)
+    table = -torch.linspace(24.0, 66.0, V, dtype=F64).to(F32).cuda()[:, None]
+    table[0] = 0.0
+    y = torch.full((P * n,), -1, dtype=torch.int32, device="cuda")
+    y[-1] = 0
+    h = torch.ones((P * n, 1), device="cuda")
+    _, _, got = _lm().cross_entropy(h, table, y, P=P)
+    # (on the CPU: the GPU's softmax in 64 bits is off by 3e-6 of its small values)
+    want = torch.exp(table[:, 0].cpu().double())
+    want /= want.sum()
+    got = got[-1, :, 0].cpu().double()
+    assert (got[1:] - want[1:]).abs().le(12 * U * want[1:]).all(), \
+        float((got[1:] / want[1:] - 1).abs().max() / U)
+    assert abs(float(got[0] - (want[0] - 1))) <= 8 * U
+
+
 def test_rows_of_infinities():
     """A row whose hidden state is not finite spoils its own loss and gradient
     only, and the table's."""
