@@ -875,7 +875,8 @@ ecc_status_t ecc_cross_entropy(const ecc_cross_entropy_t *a, void *d_loss, void 
  * elements and two matrices of F rows of D:
  *   g = x Wg^T,  u = x Wu^T,  y = act(g) u
  * (act(g) = g / (1 + exp(-g)), or g (1 + erf(g / sqrt 2)) / 2 with erf within
- * 1.5e-7), and its gradients for a given dy:
+ * 1.5e-7: act is within 7.5e-8 |g|, so that its small values for g below -3 have
+ * few digits), and its gradients for a given dy:
  *   dg = dy u act'(g),  du = dy act(g)
  *   dx = dg Wg + du Wu,  dWg_p = dg_p^T x_p,  dWu_p = du_p^T x_p
  * (g and u are formed again).  x, Wg, Wu, y, dy and dx are of `type`, ECC_F32

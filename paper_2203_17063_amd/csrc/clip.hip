@@ -27,7 +27,7 @@ namespace ecc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTableEntries = 56;     // 3.6 KiB of a launch's 4 KiB of arguments
+constexpr int kTableEntries = 56;     // 3.1 KiB of a launch's 4 KiB of arguments
 constexpr int64_t kChunkMin = 4096;   // elements
 constexpr int64_t kChunks = 32768;    // of all workers, about
 constexpr int64_t kFewChunks = 1024;  // of a worker, whose sums the scaling adds

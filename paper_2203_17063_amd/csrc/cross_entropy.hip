@@ -19,9 +19,11 @@
 // label's term is near the weight in most rows of a model that learns, and
 // would be off by one and the same half step everywhere (0.0037 of dE).
 //
-// Up to 64 rows in all take kernels of their own, which need no packed
-// and no transposed table (its two passes are most of such a call): 61 rows,
-// D 96, V 1,003, fp32: 20 us against 47 us, in three launches instead of seven;
+// Up to 64 rows in all take kernels of their own, which need no transposed table,
+// and a packed one only where tiles form the logits sooner all the same
+// (few_by_tiles): the table's two passes are most of such a call.  61 rows, D 96,
+// V 1,003, fp32: 20 us against 47 us, in three launches instead of seven (four for
+// V above 2,048);
 // 8 rows, D 4,096, V 128,000, bf16: 0.93 ms against 1.28 ms; 64 workers' rows, D
 // 256, V 32,000, bf16: 0.29 ms against 0.92 ms.
 #include "pack.h"

@@ -18,9 +18,11 @@ namespace {
 // act(g) and its derivative.  The error function is Abramowitz and Stegun's
 // 7.1.26 (Hastings), within 1.5e-7 of it: half of 1 - erf(|x|) is a polynomial
 // in 1 / (1 + p |x|) times exp(-x^2), at x = g / sqrt 2 the exponential that the
-// derivative needs too.  For negative g that half is the factor itself, so that
-// small values keep their digits.  Exponentials of fp32 rows within 2 ulp, of
-// bf16 rows the short ones: 8,192 rows, D 256, F 2,501: 40 us against 45 us.
+// derivative needs too.  For negative g that half is the factor itself, within
+// 7.5e-8; the bound is an absolute one, so that small factors have fewer digits
+// (off by 5e-5 of themselves at g = -3, 5e-4 at -4, 1.6e-3 at -5, 1e-2 at -8, where
+// 1 + erf in fp32 has none left from -5.5 on).  Exponentials of fp32 rows within 2
+// ulp, of bf16 rows the short ones: 8,192 rows, D 256, F 2,501: 40 us against 45 us.
 template <int ACT, typename T>
 __device__ __forceinline__ void activation(float g, float &a, float &da) {
     if constexpr (ACT == ECC_ACT_SILU) {
@@ -315,7 +317,9 @@ struct Plan {
 // MB of bf16 weights out of memory: one, two or four blocks of 16 rows, each read
 // again for every 16 columns, of rows that begin at 4 bytes or not; and how long
 // one workgroup takes for its share of D.  Tiles pack weights whose rows are no
-// multiple of 64.  D 4,096, F 12,288: 8 rows 39 us and 48 us, 64 rows 74 us and 50
+// multiple of 64.  Rows are taken to lie one behind the other: the choice goes by
+// the sizes alone, so that operands at another place or pitch give the same bits.
+// D 4,096, F 12,288: 8 rows 39 us and 48 us, 64 rows 74 us and 50
 // us; D 4,096, F 1,000: 8 rows 13 us and 17 us, 64 rows 25 us and 21 us; D 2,001, F
 // 5,003: 8 rows 29 us and 35 us, 64 rows 64 us and 37 us; D 1,000, F 8,000: 64 rows
 // 16 us and 30 us.  (Weights that the last cache holds come out in 34 us instead of

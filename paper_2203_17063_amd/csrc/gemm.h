@@ -43,7 +43,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGemmK = 64;        // elements along k of one step
 constexpr int kGemmGroup = 4;     // tile rows of a band
-// Row pitch of an operand: 32-bit offsets reach the rows of a tile.
+// Row pitch of an operand, below this: 32-bit offsets reach the rows of a tile.
 constexpr int64_t kGemmMaxLd = int64_t(1) << 23;
 
 // Rows of `ld` elements (a multiple of 8, 16-byte aligned), pieces `plane`
@@ -429,8 +429,9 @@ void launch_short_tiles(const GemmArgs &g, const Epi &epi, hipStream_t s) {
 // parts are joined by k_gemm_join): what takes the least by the times that a
 // round of 256 tiles takes, in us: 1.5 a step and 8 before and after them for
 // large tiles, 0.6 and 4 for small ones, and the join at 4 TB/s.  (M x N and
-// `steps` of all products, per batch.)  4,136 x 1,001 of 516 steps: 3 parts of
-// large tiles, 0.25 ms, against 0.65 ms for small tiles in one.
+// `steps` of all products, per batch.)  4,136 x 1,001 of 516 steps: 7 parts of
+// large tiles, 0.32 ms with their join (the call that holds it 593 us; 590 us by 3
+// parts, 619 by 6, 687 by 2, 719 by 4, 994 in one; small tiles 835 us in one).
 // Products of one or two steps take short tiles instead: small ones of 64 KiB of
 // LDS, two to a CU, so that one's results are written while the other begins.
 // 5,000 rows x 2 x 2,178 columns of two steps: 18 us against 25 us; gradients of

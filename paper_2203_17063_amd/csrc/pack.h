@@ -217,7 +217,7 @@ struct FewStep<float> {
 // Can a product take a bf16 matrix as it lies?
 inline bool as_it_lies(const void *p, int64_t ld, int64_t cols, int32_t type) {
     return type == ECC_BF16 && (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 64 == 0 &&
-           ld < (int64_t(1) << 23);
+           ld < kGemmMaxLd;
 }
 
 }  // namespace ecc

@@ -12,7 +12,8 @@ stride.  Operands, outputs and work buffers of a call lie on one GPU, which
 need not be the current one.  Sums over rows and tokens are held in fp32, or
 fp64 where an operand or the result is fp64; a row's own sums (norms, softmax
 statistics) in fp32, or fp64 for rows of fp64; norms of whole gradients in fp64.
-cross_entropy and gated_ffn are products of fp32 or bf16 operands, not fp64.
+cross_entropy and gated_ffn are products of fp32 or bf16 operands, not fp64;
+fp32 ones must be finite (an infinite element makes its sums NaN).
 """
 from __future__ import annotations
 
@@ -425,10 +426,11 @@ def _product_type(t, what):
 
 def cross_entropy(h, table, labels, weight=None, scale=1.0, P=1, grad=True, dtype=None, loss=None,
                   dh=None, dtable=None, accumulate=False, work=None):
-    """(loss, dh, dtable) of the logits scale * h table^T, which are never held
-    as a whole: per row of h (..., D) weight (log sum exp of its logits - the
-    logit of its label), and the gradients of the losses' sum in h and, per
-    worker (P, V, D), in the table.
+    """(loss, dh, dtable) of the logits scale * h table^T, which exist for a piece
+    of rows at a time (with their gradients 5 GiB of the work buffer at most, or
+    256 rows of a vocabulary for which those are more): per row of h (..., D)
+    weight (log sum exp of its logits - the logit of its label), and the gradients
+    of the losses' sum in h and, per worker (P, V, D), in the table.
 
     labels: int32, outside [0, V) for none; weight: fp32.  grad: None for the
     loss only.  dtype: of dtable, float32 or the table's (which it is by
@@ -519,7 +521,7 @@ def _ffn(x, w_gate, w_up, act, P, dtype):
 
 def gated_ffn(x, w_gate, w_up, act="silu", out=None, work=None):
     """act(x w_gate^T) * (x w_up^T), of shape (..., F), for weights (F, D).
-    act: "silu" or "gelu" (by erf)."""
+    act: "silu" or "gelu" (by erf, within 7.5e-8 |x w_gate^T|)."""
     a, _, F = _ffn(x, w_gate, w_up, act, 1, x.dtype)
     out = _out(out, x.shape[:-1] + (F,), x.dtype, x, "out")
     _, ld = _rows(out, "out")
